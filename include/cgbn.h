@@ -78,7 +78,9 @@ enum {
     CGBN_ERR_TUNING = 9,     /* unknown tuning key or value out of range */
     CGBN_ERR_MOMENTUM = 10,  /* momentum outside [0, 1] */
     CGBN_ERR_ALIAS = 11,     /* two outputs that must differ are the same buffer */
-    CGBN_ERR_SCRATCH = 12    /* cgbn_forward_static: the problem needs more than CGBN_STATIC_SCRATCH_BYTES */
+    CGBN_ERR_SCRATCH = 12,   /* cgbn_forward_static: the problem needs more than CGBN_STATIC_SCRATCH_BYTES */
+    CGBN_ERR_ACTIVATION = 13, /* an activation or rotation that is not in its list */
+    CGBN_ERR_STRIDE = 14     /* rows of a strided tensor overlap */
 };
 
 typedef int cgbn_layout;
@@ -251,6 +253,82 @@ cgbn_status cgbn_frozen_backward(const void* dy, int N, int C, int H, int W, cgb
 cgbn_status cgbn_update_running_stats(const float* mean, const float* mean_lo, const float* invstd,
                                       float eps, long long M, int C, float momentum, int unbiased,
                                       float* running_mean, float* running_var, void* stream);
+
+/* ---- The layers beside the normalization: matrix product with bias, residual and activation; the gated feed-forward
+ * block; the per-head norm of queries and keys with the rotation by position.  Rows are tokens, pixels or crops: a
+ * channels-last map [N][H][W][C] is M = N*H*W rows of C values, and a 1x1 convolution of it is cgbn_linear_forward
+ * (a fixed-statistics layer folds into its weights and bias, the shortcut and the ReLU are its residual and activation).
+ *   - Tensors are dense row by row (but for the strides of cgbn_head_norm_*), their element type `dtype` (weights too), base
+ *     addresses 16-byte aligned; widths may be odd.  Bias vectors, norm weights and their gradients are float.
+ *   - Sums are held in 32 bits and results rounded once, to nearest even; what a backward pass hands from one of its kernels
+ *     to the next (dz, dg, du below) is rounded to `dtype`.  Float products run on the float matrix instructions.
+ *   - M (or T) may be 0: forward calls do nothing, backward calls write zero weight gradients.
+ *   - Outputs and inputs are different buffers unless said otherwise (equal pointers where that is wrong are answered with
+ *     CGBN_ERR_ALIAS; partial overlaps are undefined).  The workspace may be NULL where the size below is not more than 256.
+ *   - Nothing waits for a sibling workgroup: calls on different streams may overlap, each with its own workspace.
+ *   - NaN and infinities are not errors; they reach the results whose sums they enter, and no others. ---- */
+
+typedef int cgbn_activation; /* of z: z; max(0, z); z * Phi(z) with the normal distribution's Phi; z / (1 + exp(-z)) */
+enum { CGBN_ACT_NONE = 0, CGBN_ACT_RELU = 1, CGBN_ACT_GELU = 2, CGBN_ACT_SILU = 3 };
+
+/* Bytes of workspace for M rows of K values in, N out (backward: 0 or 1).  0 if the arguments are invalid. */
+size_t cgbn_linear_workspace_bytes(long long M, int N, int K, cgbn_dtype dtype, int backward);
+
+/* z = x w^T + bias + residual, y = act(z).  In: x[M][K], w[N][K], bias[N] or NULL, residual[M][N] or NULL.  Out: y[M][N],
+ * and z[M][N] if not NULL (what the backward of GELU and SiLU starts from).  y may be exactly residual. */
+cgbn_status cgbn_linear_forward(const void* x, const void* w, const float* bias, const void* residual, long long M, int N,
+                                int K, cgbn_activation act, void* y, void* z, cgbn_dtype dtype,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/* Its backward: dz = dy * act'(z), dx = dz w, dw = dz^T x, dbias = sum over rows of dz, dresidual = dz.  `saved` is the
+ * stored y for ReLU (gradient passes where y > 0), the stored z for GELU and SiLU, and not read without an activation.
+ * Outputs may be NULL where they are not wanted.  dresidual may be exactly dy. */
+cgbn_status cgbn_linear_backward(const void* dy, const void* x, const void* w, const void* saved, long long M, int N, int K,
+                                 cgbn_activation act, void* dx, void* dw, float* dbias, void* dresidual, cgbn_dtype dtype,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+size_t cgbn_gated_workspace_bytes(long long M, int F, int K, cgbn_dtype dtype, int backward);
+
+/* g = x w_gate^T, u = x w_up^T, h = act(g) * u, one kernel.  In: x[M][K], w_gate[F][K], w_up[F][K].  Out: h[M][F], and
+ * gate[M][F] = g, up[M][F] = u if not NULL (both or neither), which the backward starts from. */
+cgbn_status cgbn_gated_forward(const void* x, const void* w_gate, const void* w_up, long long M, int F, int K,
+                               cgbn_activation act, void* h, void* gate, void* up, cgbn_dtype dtype,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* Its backward: dg = dh * u * act'(g), du = dh * act(g), dx = dg w_gate + du w_up, dw_gate = dg^T x, dw_up = du^T x.
+ * dx may be NULL, and so may dw_gate and dw_up (both or neither). */
+cgbn_status cgbn_gated_backward(const void* dh, const void* x, const void* w_gate, const void* w_up, const void* gate,
+                                const void* up, long long M, int F, int K, cgbn_activation act, void* dx, void* dw_gate,
+                                void* dw_up, cgbn_dtype dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Which values of a head are turned together: i and i + R/2, or 2i and 2i + 1, for i in [0, R/2). */
+typedef int cgbn_rotation;
+enum { CGBN_ROTATE_HALVES = 0, CGBN_ROTATE_PAIRS = 1 };
+
+/* Every row x[D] (one head of one token): n = weight * x / sqrt(mean(x^2) + eps), then its first R values are rotated by the
+ * token's position: (a, b) -> (a c - b s, b c + a s) with c = cos[p][i], s = sin[p][i], p = positions[token] (the token's
+ * own index if positions is NULL).  R = 0: no rotation, positions, cos and sin are not read.
+ *   q: Hq heads of D values side by side in each of T rows, row to row `ldq` elements (q and k may be slices of a joint
+ *   projection's rows); k: Hk heads, `ldk`; Hk may be 0, k, wk and yk are then not read.  wq[D], wk[D]; cos, sin
+ *   [table_rows][R/2]; outputs with strides of their own; yq may be exactly q (with its stride), yk exactly k.
+ *   1 <= D <= 1024, R even.  A position outside [0, table_rows) reads nothing and makes the R rotated values of its rows NaN. */
+cgbn_status cgbn_head_norm_forward(const void* q, long long ldq, const void* k, long long ldk, long long T, int Hq, int Hk,
+                                   int D, int R, cgbn_rotation style, const int* positions, const float* cos,
+                                   const float* sin, int table_rows, const float* wq, const float* wk, float eps,
+                                   void* yq, long long ldyq, void* yk, long long ldyk, cgbn_dtype dtype, void* stream);
+
+/* Bytes of workspace of its backward. */
+size_t cgbn_head_norm_workspace_bytes(long long T, int Hq, int Hk, int D, cgbn_dtype dtype);
+
+/* Its backward, from the layer's inputs q and k: dq, dk, and the weights' gradients dwq[D], dwk[D] summed over all tokens and
+ * heads.  dq may be exactly dyq (with its stride), dk exactly dyk.  A position outside the table makes its rows' gradients
+ * NaN, and with them dwq and dwk. */
+cgbn_status cgbn_head_norm_backward(const void* dyq, long long lddyq, const void* dyk, long long lddyk, const void* q,
+                                    long long ldq, const void* k, long long ldk, long long T, int Hq, int Hk, int D, int R,
+                                    cgbn_rotation style, const int* positions, const float* cos, const float* sin,
+                                    int table_rows, const float* wq, const float* wk, float eps, void* dq, long long lddq,
+                                    void* dk, long long lddk, float* dwq, float* dwk, cgbn_dtype dtype,
+                                    void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- housekeeping ---- */
 

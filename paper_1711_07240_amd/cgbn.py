@@ -26,6 +26,8 @@ CGBN_OK = 0
 
 LAYOUTS = {"NCHW": CGBN_NCHW, "NHWC": CGBN_NHWC}
 DTYPES = {"f32": CGBN_F32, "bf16": CGBN_BF16}
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+ROTATIONS = {"halves": 0, "interleaved": 1}
 
 _c_int, _c_ll, _c_f, _c_sz, _c_p = (ctypes.c_int, ctypes.c_longlong, ctypes.c_float,
                                      ctypes.c_size_t, ctypes.c_void_p)
@@ -59,6 +61,17 @@ SIGNATURES = {
     "cgbn_frozen_forward": (_c_int, [_c_p] + [_c_int] * 4 + [_c_int, _c_int] + [_c_p] * 4 + [_c_f, _c_p, _c_p]),
     "cgbn_frozen_backward": (_c_int, [_c_p] + [_c_int] * 4 + [_c_int, _c_int] + [_c_p] * 2 + [_c_f, _c_p, _c_p]),
     "cgbn_update_running_stats": (_c_int, [_c_p, _c_p, _c_p, _c_f, _c_ll, _c_int, _c_f, _c_int, _c_p, _c_p, _c_p]),
+    "cgbn_linear_workspace_bytes": (_c_sz, [_c_ll, _c_int, _c_int, _c_int, _c_int]),
+    "cgbn_linear_forward": (_c_int, [_c_p] * 4 + [_c_ll, _c_int, _c_int, _c_int, _c_p, _c_p, _c_int, _c_p, _c_sz, _c_p]),
+    "cgbn_linear_backward": (_c_int, [_c_p] * 4 + [_c_ll, _c_int, _c_int, _c_int] + [_c_p] * 4 + [_c_int, _c_p, _c_sz, _c_p]),
+    "cgbn_gated_workspace_bytes": (_c_sz, [_c_ll, _c_int, _c_int, _c_int, _c_int]),
+    "cgbn_gated_forward": (_c_int, [_c_p] * 3 + [_c_ll, _c_int, _c_int, _c_int] + [_c_p] * 3 + [_c_int, _c_p, _c_sz, _c_p]),
+    "cgbn_gated_backward": (_c_int, [_c_p] * 6 + [_c_ll, _c_int, _c_int, _c_int] + [_c_p] * 3 + [_c_int, _c_p, _c_sz, _c_p]),
+    "cgbn_head_norm_forward": (_c_int, [_c_p, _c_ll] * 2 + [_c_ll] + [_c_int] * 5 + [_c_p] * 3 + [_c_int, _c_p, _c_p, _c_f]
+                               + [_c_p, _c_ll] * 2 + [_c_int, _c_p]),
+    "cgbn_head_norm_workspace_bytes": (_c_sz, [_c_ll, _c_int, _c_int, _c_int, _c_int]),
+    "cgbn_head_norm_backward": (_c_int, [_c_p, _c_ll] * 4 + [_c_ll] + [_c_int] * 5 + [_c_p] * 3 + [_c_int, _c_p, _c_p, _c_f]
+                                + [_c_p, _c_ll] * 2 + [_c_p, _c_p, _c_int, _c_p, _c_sz, _c_p]),
     "cgbn_calibration_copy": (_c_int, [_c_p, _c_p, _c_sz, _c_p]),
     "cgbn_status_string": (ctypes.c_char_p, [_c_int]),
     "cgbn_set_tuning": (_c_int, [ctypes.c_char_p, _c_ll]),
@@ -313,6 +326,68 @@ def cgbn_update_running_stats(mean, mean_lo, invstd, eps, M, C, momentum, unbias
     _check(lib().cgbn_update_running_stats(_ptr(mean), _ptr(mean_lo), _ptr(invstd), float(eps), int(M), int(C),
                                            float(momentum), int(bool(unbiased)), _ptr(running_mean),
                                            _ptr(running_var), _stream(stream)), "cgbn_update_running_stats")
+
+
+def _room(workspace, workspace_bytes) -> int:
+    return _nbytes(workspace) if workspace_bytes is None and workspace is not None else (workspace_bytes or 0)
+
+
+def cgbn_linear_workspace_bytes(M, N, K, dtype, backward) -> int:
+    return int(lib().cgbn_linear_workspace_bytes(M, N, K, _enum(DTYPES, dtype), int(bool(backward))))
+
+
+def cgbn_linear_forward(x, w, bias, residual, M, N, K, act, y, z=None, dtype="f32", workspace=None, workspace_bytes=None,
+                        stream=None) -> None:
+    _check(lib().cgbn_linear_forward(_ptr(x), _ptr(w), _ptr(bias), _ptr(residual), M, N, K, _enum(ACTIVATIONS, act), _ptr(y),
+                                     _ptr(z), _enum(DTYPES, dtype), _ptr(workspace), _room(workspace, workspace_bytes),
+                                     _stream(stream)), "cgbn_linear_forward")
+
+
+def cgbn_linear_backward(dy, x, w, saved, M, N, K, act, dx, dw, dbias=None, dresidual=None, dtype="f32", workspace=None,
+                         workspace_bytes=None, stream=None) -> None:
+    _check(lib().cgbn_linear_backward(_ptr(dy), _ptr(x), _ptr(w), _ptr(saved), M, N, K, _enum(ACTIVATIONS, act), _ptr(dx),
+                                      _ptr(dw), _ptr(dbias), _ptr(dresidual), _enum(DTYPES, dtype), _ptr(workspace),
+                                      _room(workspace, workspace_bytes), _stream(stream)), "cgbn_linear_backward")
+
+
+def cgbn_gated_workspace_bytes(M, F, K, dtype, backward) -> int:
+    return int(lib().cgbn_gated_workspace_bytes(M, F, K, _enum(DTYPES, dtype), int(bool(backward))))
+
+
+def cgbn_gated_forward(x, w_gate, w_up, M, F, K, act, h, gate=None, up=None, dtype="f32", workspace=None,
+                       workspace_bytes=None, stream=None) -> None:
+    _check(lib().cgbn_gated_forward(_ptr(x), _ptr(w_gate), _ptr(w_up), M, F, K, _enum(ACTIVATIONS, act), _ptr(h), _ptr(gate),
+                                    _ptr(up), _enum(DTYPES, dtype), _ptr(workspace), _room(workspace, workspace_bytes),
+                                    _stream(stream)), "cgbn_gated_forward")
+
+
+def cgbn_gated_backward(dh, x, w_gate, w_up, gate, up, M, F, K, act, dx, dw_gate, dw_up, dtype="f32", workspace=None,
+                        workspace_bytes=None, stream=None) -> None:
+    _check(lib().cgbn_gated_backward(_ptr(dh), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(gate), _ptr(up), M, F, K,
+                                     _enum(ACTIVATIONS, act), _ptr(dx), _ptr(dw_gate), _ptr(dw_up), _enum(DTYPES, dtype),
+                                     _ptr(workspace), _room(workspace, workspace_bytes), _stream(stream)),
+           "cgbn_gated_backward")
+
+
+def cgbn_head_norm_forward(q, ldq, k, ldk, T, Hq, Hk, D, R, style, positions, cos, sin, table_rows, wq, wk, eps, yq, ldyq, yk,
+                           ldyk, dtype="f32", stream=None) -> None:
+    _check(lib().cgbn_head_norm_forward(_ptr(q), ldq, _ptr(k), ldk, T, Hq, Hk, D, R, _enum(ROTATIONS, style), _ptr(positions),
+                                        _ptr(cos), _ptr(sin), table_rows, _ptr(wq), _ptr(wk), float(eps), _ptr(yq), ldyq,
+                                        _ptr(yk), ldyk, _enum(DTYPES, dtype), _stream(stream)), "cgbn_head_norm_forward")
+
+
+def cgbn_head_norm_workspace_bytes(T, Hq, Hk, D, dtype) -> int:
+    return int(lib().cgbn_head_norm_workspace_bytes(T, Hq, Hk, D, _enum(DTYPES, dtype)))
+
+
+def cgbn_head_norm_backward(dyq, lddyq, dyk, lddyk, q, ldq, k, ldk, T, Hq, Hk, D, R, style, positions, cos, sin, table_rows,
+                            wq, wk, eps, dq, lddq, dk, lddk, dwq, dwk, dtype="f32", workspace=None, workspace_bytes=None,
+                            stream=None) -> None:
+    _check(lib().cgbn_head_norm_backward(_ptr(dyq), lddyq, _ptr(dyk), lddyk, _ptr(q), ldq, _ptr(k), ldk, T, Hq, Hk, D, R,
+                                         _enum(ROTATIONS, style), _ptr(positions), _ptr(cos), _ptr(sin), table_rows, _ptr(wq),
+                                         _ptr(wk), float(eps), _ptr(dq), lddq, _ptr(dk), lddk, _ptr(dwq), _ptr(dwk),
+                                         _enum(DTYPES, dtype), _ptr(workspace), _room(workspace, workspace_bytes),
+                                         _stream(stream)), "cgbn_head_norm_backward")
 
 
 def cgbn_calibration_copy(src, dst, nbytes, stream=None) -> None:

@@ -2129,6 +2129,8 @@ const char* cgbn_status_string(cgbn_status status)
     case CGBN_ERR_MOMENTUM: return "momentum outside [0, 1]";
     case CGBN_ERR_ALIAS: return "two outputs that must differ are the same buffer";
     case CGBN_ERR_SCRATCH: return "the problem needs more scratch than the library's static array holds";
+    case CGBN_ERR_ACTIVATION: return "activation or rotation out of range";
+    case CGBN_ERR_STRIDE: return "rows of a strided tensor overlap";
     }
     return "unknown status";
 }

@@ -1,0 +1,112 @@
+// The matrix product of a layer for few rows (one token ... a few dozen): y = act(x W^T + ...), the gated pair likewise.
+//
+// What such a call has to do is read W once; its products are nothing.  A workgroup takes 16 rows of W (of both matrices of a
+// gated pair) and its wavefronts share the reduction, 128 bytes of every row at a time in turn, so the workgroup walks 16 (32)
+// streams of whole lines.  W goes from memory straight to the registers that the matrix instruction reads: lane l holds 32 bytes of
+// row l % 16 (which r a lane holds is free as long as both operands agree), several steps in flight.  x is small and comes
+// from the caches.  The wavefronts' sums meet in LDS and are added in wavefront order.
+#pragma once
+
+#include "cgbn_gemm.h"
+
+namespace cgbn {
+
+// 16 bytes of an operand's row, zero beyond `left` elements; WHOLE: rows start on 16 bytes and hold whole chunks
+template <typename T, bool WHOLE> __device__ __forceinline__ u32x4 row_chunk(const T* p, int left)
+{
+    constexpr int E = 16 / (int)sizeof(T);
+    if constexpr (WHOLE) {
+        return left > 0 ? *reinterpret_cast<const u32x4*>(p) : u32x4{0, 0, 0, 0};
+    } else {
+        u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if (e < left) {
+                if constexpr (sizeof(T) == 2) v[e / 2] |= (uint32_t)p[e].bits << (16 * (e & 1));
+                else v[e] = __float_as_uint(p[e]);
+            }
+        }
+        return v;
+    }
+}
+
+// FM: 16-row blocks of x; NW: wavefronts
+template <typename T, bool GATED, bool WHOLE, int FM, int NW>
+__global__ __launch_bounds__(NW * kWave) void gemm_rows(const GemmArgs G)
+{
+    constexpr int E = 16 / (int)sizeof(T), STEP = 8 * E, P = GATED ? 2 : 1, U = FM == 1 ? 4 : 2;
+    __shared__ f32x4 sums[NW][FM * P][kWave];
+    const int l = (int)threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), t = l & 15, q = l >> 4;
+    const int j0 = (int)blockIdx.x * 16, i0 = (int)blockIdx.y * 16 * FM;
+    const T *pw[P], *px[FM];
+#pragma unroll
+    for (int p = 0; p < P; ++p) pw[p] = static_cast<const T*>(G.B[p]) + (long long)min(j0 + t, G.J - 1) * G.ldb + q * 2 * E;
+#pragma unroll
+    for (int m = 0; m < FM; ++m) px[m] = static_cast<const T*>(G.A[0]) + (long long)min(i0 + m * 16 + t, G.I - 1) * G.lda + q * 2 * E;
+
+    f32x4 acc[P][FM];
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int m = 0; m < FM; ++m) acc[p][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int steps = (G.R + STEP - 1) / STEP, full = G.R / STEP;
+    int s = wave;
+    for (; s + (U - 1) * NW < full; s += U * NW) {
+        u32x4 w[U][P][2], x[U][FM][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = (s + u * NW) * STEP + h * E;
+#pragma unroll
+                for (int p = 0; p < P; ++p) w[u][p][h] = row_chunk<T, WHOLE>(pw[p] + r, E);
+#pragma unroll
+                for (int m = 0; m < FM; ++m) x[u][m][h] = row_chunk<T, WHOLE>(px[m] + r, E);
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int m = 0; m < FM; ++m) acc[p][m] = multiply<T>(w[u][p][h], x[u][m][h], acc[p][m]);
+    }
+    for (; s < steps; s += NW) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = s * STEP + h * E, left = G.R - r - q * 2 * E;
+            u32x4 x[FM];
+#pragma unroll
+            for (int m = 0; m < FM; ++m) x[m] = row_chunk<T, WHOLE>(px[m] + r, left);
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const u32x4 w = row_chunk<T, WHOLE>(pw[p] + r, left);
+#pragma unroll
+                for (int m = 0; m < FM; ++m) acc[p][m] = multiply<T>(w, x[m], acc[p][m]);
+            }
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int m = 0; m < FM; ++m) sums[wave][p * FM + m][l] = acc[p][m];
+    __syncthreads();
+    if (wave >= FM) return;
+    const int m = wave, i = i0 + m * 16 + t, j = j0 + q * 4;
+    if (i >= G.I || j >= G.J) return;
+    const bool whole = j + 4 <= G.J && G.J % 4 == 0;
+    float v[P][4];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        f32x4 a = sums[0][p * FM + m][l];
+#pragma unroll
+        for (int k = 1; k < NW; ++k) a += sums[k][p * FM + m][l];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[p][k] = a[k];
+    }
+    if constexpr (GATED) finish_gated<T, 4>(G, v[0], v[1], i, j, whole);
+    else finish_linear<T, 4>(G, v[0], i, j, whole);
+}
+
+}  // namespace cgbn

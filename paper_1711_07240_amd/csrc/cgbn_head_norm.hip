@@ -1,0 +1,545 @@
+// The norm of queries and keys, head by head, with the rotation by position in the same pass, and its backward.
+//
+//   forward   r = 1 / sqrt(mean(x^2) + eps);  n = w x r;  y = rotation(n)
+//   backward  e = inverse rotation(dy);  dw = sum over rows of e x r;  t = e w;  dx = r (t - x r mean(t x r))
+//
+// Bound by memory: forward one read and one write of q and k, backward two reads and one write (r comes from x again: reading
+// a stored r would save nothing, x is read anyway).  A row of D values is held by a group of lanes, two 16-byte chunks a
+// lane, chosen so that the values that are turned together are in the same lane: with halves, chunk c and the one R/2 values
+// on; with pairs any two.  So nothing but the row's sums crosses lanes.  A wavefront takes heads of ONE token: cosines and sines,
+// which in float are twice the bytes of a bfloat16 row, and the weights are fetched once for all of them.
+// Rows whose length, strides or addresses do not go in whole chunks, or whose halves do not, take the kernels with one value
+// a lane (`_any`): a wavefront a row, partners read again from the cache.
+//
+// Sums are float: a row's over at most 16 values a lane, then a fixed tree; the weights' gradients per lane over the rows a wavefront
+// walks, then over wavefronts in order, then over workgroups in double precision.  No atomics.
+#include "cgbn.h"
+#include "cgbn_column_sums.h"
+
+#include <cmath>
+#include <cstring>
+
+namespace cgbn {
+namespace {
+
+struct HeadArgs {
+    const void *x[2], *dy[2];          // q, k
+    void* out[2];                      // yq, yk or dq, dk
+    long long ldx[2], lddy[2], ldo[2];
+    const float *w[2], *cos, *sin;
+    const int* positions;
+    float* part;                       // backward: [workgroups][2][D]
+    long long T;
+    int H[2], D, R, table;
+    int style;                         // CGBN_ROTATE_*
+    float eps, inv_D;
+    int pairs, lead, far, rest;        // chunk pairs of a row; those turned together as halves, chunks between them; see chunks_of()
+    int parts;                         // wavefronts that share a token's heads
+};
+
+// The sum over the L lanes of a group (a power of two, groups aligned): every lane gets it, whatever its place, in the same order.
+template <int L> __device__ __forceinline__ float group_sum(float v)
+{
+#define CGBN_DPP_ADD(ctrl_) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl_, 0xf, 0xf, true))
+    if constexpr (L >= 2) CGBN_DPP_ADD(0xB1);      // lane ^ 1
+    if constexpr (L >= 4) CGBN_DPP_ADD(0x4E);      // lane ^ 2
+    if constexpr (L >= 8) CGBN_DPP_ADD(0x141);     // the other half of 8
+    if constexpr (L >= 16) CGBN_DPP_ADD(0x140);    // the other half of 16
+#undef CGBN_DPP_ADD
+    if constexpr (L >= 32) v += __shfl_xor(v, 16);
+    if constexpr (L >= 64) v += __shfl_xor(v, 32);
+    return v;
+}
+
+// The first elements of a lane's two chunks (-1: none).  As halves: `lead` pairs of chunks `far` apart, then the `rest` chunks
+// that are not turned, first half with second half.
+template <int E> __device__ __forceinline__ void chunks_of(const HeadArgs& A, int p, int* c0, int* c1)
+{
+    *c0 = *c1 = -1;
+    if (p >= A.pairs) return;
+    if (p < A.lead) {
+        *c0 = p * E;
+        *c1 = (p + A.far) * E;
+    } else {
+        const int k = p - A.lead, first = 2 * A.lead, half = (A.rest + 1) / 2;
+        *c0 = (first + k) * E;
+        if (k + half < A.rest) *c1 = (first + k + half) * E;
+    }
+}
+
+// cosines and sines of a lane's chunks.  Halves: of value e of both chunks; pairs: of values 2e, 2e + 1 of chunk 0 in the first
+// half, of chunk 1 in the second.  Not turned: 1 and 0.
+template <int E> struct Turn {
+    float c[E], s[E];
+    __device__ __forceinline__ void load(const HeadArgs& A, long long token, int p, int c0, int c1)
+    {
+#pragma unroll
+        for (int e = 0; e < E; ++e) { c[e] = 1.f; s[e] = 0.f; }
+        if (A.R == 0) return;
+        const long long pos = A.positions ? (long long)A.positions[token] : token;
+        const bool in = pos >= 0 && pos < A.table;
+        const long long row = in ? pos * (A.R / 2) : 0;
+        const float bad = __int_as_float(0x7fc00000);
+        if (A.style == CGBN_ROTATE_HALVES) {
+            if (c0 < 0 || p >= A.lead) return;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                c[e] = in ? A.cos[row + c0 + e] : bad;
+                s[e] = in ? A.sin[row + c0 + e] : bad;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const int first = e < E / 2 ? c0 : c1, v = first + 2 * (e % (E / 2));
+                if (first >= 0 && v < A.R) {
+                    c[e] = in ? A.cos[row + v / 2] : bad;
+                    s[e] = in ? A.sin[row + v / 2] : bad;
+                }
+            }
+        }
+    }
+    // sign 1: turn; -1: turn back
+    template <int SIGN> __device__ __forceinline__ void apply(int style, float (&a)[E], float (&b)[E]) const
+    {
+        if (style == CGBN_ROTATE_HALVES) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float u = a[e], v = b[e], t = SIGN * s[e];
+                a[e] = u * c[e] - v * t;
+                b[e] = v * c[e] + u * t;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < E / 2; ++e) {
+                const float t = SIGN * s[e], u = a[2 * e], v = a[2 * e + 1];
+                a[2 * e] = u * c[e] - v * t;
+                a[2 * e + 1] = v * c[e] + u * t;
+                const float t2 = SIGN * s[E / 2 + e], u2 = b[2 * e], v2 = b[2 * e + 1];
+                b[2 * e] = u2 * c[E / 2 + e] - v2 * t2;
+                b[2 * e + 1] = v2 * c[E / 2 + e] + u2 * t2;
+            }
+        }
+    }
+};
+
+template <typename T, int E> __device__ __forceinline__ void load_chunk(const T* row, int c, float (&v)[E])
+{
+    if (c >= 0) Elem<T>::loadv(row + c, v);
+    else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = 0.f;
+    }
+}
+
+// L: lanes of a row
+template <typename T, int L> __global__ __launch_bounds__(kThreads) void head_forward(const HeadArgs A)
+{
+    constexpr int E = Elem<T>::VEC, G = kWave / L;
+    const int lane = (int)threadIdx.x % kWave, p = lane % L, g = lane / L;
+    const long long wave = (long long)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
+    const long long token = wave / A.parts;
+    const int part = (int)(wave - token * A.parts);
+    if (token >= A.T) return;
+    int c0, c1;
+    chunks_of<E>(A, p, &c0, &c1);
+    Turn<E> turn;
+    turn.load(A, token, p, c0, c1);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        if (part * G >= A.H[t]) continue;
+        float w0[E], w1[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) { w0[e] = c0 >= 0 ? A.w[t][c0 + e] : 0.f; w1[e] = c1 >= 0 ? A.w[t][c1 + e] : 0.f; }
+        for (int h = part * G + g; h < A.H[t]; h += A.parts * G) {
+            const T* x = static_cast<const T*>(A.x[t]) + token * A.ldx[t] + (long long)h * A.D;
+            T* y = static_cast<T*>(A.out[t]) + token * A.ldo[t] + (long long)h * A.D;
+            float a[E], b[E], s = 0.f;
+            load_chunk<T, E>(x, c0, a);
+            load_chunk<T, E>(x, c1, b);
+#pragma unroll
+            for (int e = 0; e < E; ++e) s += a[e] * a[e] + b[e] * b[e];
+            const float r = 1.f / sqrtf(group_sum<L>(s) * A.inv_D + A.eps);
+#pragma unroll
+            for (int e = 0; e < E; ++e) { a[e] *= r * w0[e]; b[e] *= r * w1[e]; }
+            turn.template apply<1>(A.style, a, b);
+            if (c0 >= 0) Elem<T>::storev(y + c0, a, 0);
+            if (c1 >= 0) Elem<T>::storev(y + c1, b, 0);
+        }
+    }
+}
+
+// A workgroup's sums of dw, from the wavefronts' (LDS, [4][D]) to its row of `part`
+__device__ __forceinline__ void store_dw(const HeadArgs& A, const float* red, int t)
+{
+    __syncthreads();
+    for (int d = (int)threadIdx.x; d < A.D; d += kThreads)
+        A.part[((long long)blockIdx.x * 2 + t) * A.D + d] = ((red[d] + red[A.D + d]) + red[2 * A.D + d]) + red[3 * A.D + d];
+    __syncthreads();
+}
+
+template <typename T, int L> __global__ __launch_bounds__(kThreads) void head_backward(const HeadArgs A)
+{
+    constexpr int E = Elem<T>::VEC, G = kWave / L;
+    extern __shared__ float red[];                    // [4][D]
+    const int lane = (int)threadIdx.x % kWave, p = lane % L, g = lane / L, wave = (int)threadIdx.x / kWave;
+    int c0, c1;
+    chunks_of<E>(A, p, &c0, &c1);
+    for (int t = 0; t < 2; ++t) {
+        float w0[E], w1[E], dw0[E], dw1[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            w0[e] = A.H[t] && c0 >= 0 ? A.w[t][c0 + e] : 0.f;
+            w1[e] = A.H[t] && c1 >= 0 ? A.w[t][c1 + e] : 0.f;
+            dw0[e] = dw1[e] = 0.f;
+        }
+        const long long waves = (long long)gridDim.x * (kThreads / kWave);
+        for (long long u = (long long)blockIdx.x * (kThreads / kWave) + wave; u < A.T * A.parts; u += waves) {
+            const long long token = u / A.parts;
+            const int part = (int)(u - token * A.parts);
+            if (part * G >= A.H[t]) continue;
+            Turn<E> turn;
+            turn.load(A, token, p, c0, c1);
+            for (int h = part * G + g; h < A.H[t]; h += A.parts * G) {
+                const T* x = static_cast<const T*>(A.x[t]) + token * A.ldx[t] + (long long)h * A.D;
+                const T* dy = static_cast<const T*>(A.dy[t]) + token * A.lddy[t] + (long long)h * A.D;
+                T* dx = static_cast<T*>(A.out[t]) + token * A.ldo[t] + (long long)h * A.D;
+                float a[E], b[E], ea[E], eb[E], s = 0.f, m = 0.f;
+                load_chunk<T, E>(x, c0, a);
+                load_chunk<T, E>(x, c1, b);
+                load_chunk<T, E>(dy, c0, ea);
+                load_chunk<T, E>(dy, c1, eb);
+                turn.template apply<-1>(A.style, ea, eb);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    s += a[e] * a[e] + b[e] * b[e];
+                    m += ea[e] * w0[e] * a[e] + eb[e] * w1[e] * b[e];
+                }
+                const float r = 1.f / sqrtf(group_sum<L>(s) * A.inv_D + A.eps);
+                const float k = group_sum<L>(m) * r * r * A.inv_D;          // mean(t x r) r
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    dw0[e] += ea[e] * (a[e] * r);
+                    dw1[e] += eb[e] * (b[e] * r);
+                    a[e] = r * (ea[e] * w0[e] - a[e] * k);
+                    b[e] = r * (eb[e] * w1[e] - b[e] * k);
+                }
+                if (c0 >= 0) Elem<T>::storev(dx + c0, a, 0);
+                if (c1 >= 0) Elem<T>::storev(dx + c1, b, 0);
+            }
+        }
+        // over the groups of the wavefront (fixed order), then over wavefronts
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+#pragma unroll
+            for (int o = L; o < kWave; o *= 2) { dw0[e] += __shfl_xor(dw0[e], o); dw1[e] += __shfl_xor(dw1[e], o); }
+            if (g == 0 && c0 >= 0) red[wave * A.D + c0 + e] = dw0[e];
+            if (g == 0 && c1 >= 0) red[wave * A.D + c1 + e] = dw1[e];
+        }
+        store_dw(A, red, t);
+    }
+}
+
+// ---- one value a lane and step: any length, stride and alignment ----
+
+constexpr int kMaxD = 1024, kSlots = kMaxD / kWave;
+
+// the value turned together with value d (R > d), whether d is the first of the two, and the angle's index
+__device__ __forceinline__ int partner_of(const HeadArgs& A, int d, bool* is_first, int* angle)
+{
+    if (A.style == CGBN_ROTATE_HALVES) {
+        const int half = A.R / 2;
+        *is_first = d < half;
+        *angle = d < half ? d : d - half;
+        return d < half ? d + half : d - half;
+    }
+    *is_first = (d & 1) == 0;
+    *angle = d / 2;
+    return d ^ 1;
+}
+
+struct Angles {
+    long long row;
+    bool in;
+    __device__ __forceinline__ Angles(const HeadArgs& A, long long token)
+    {
+        const long long pos = A.positions && A.R ? (long long)A.positions[token] : token;
+        in = pos >= 0 && pos < A.table;
+        row = in ? pos * (A.R / 2) : 0;
+    }
+    __device__ __forceinline__ float cos(const HeadArgs& A, int k) const { return in ? A.cos[row + k] : __int_as_float(0x7fc00000); }
+    __device__ __forceinline__ float sin(const HeadArgs& A, int k) const { return in ? A.sin[row + k] : __int_as_float(0x7fc00000); }
+};
+
+// in place (out == x) every value is read, partners too, before the row's first is written
+template <typename T> __global__ __launch_bounds__(kThreads) void head_forward_any(const HeadArgs A)
+{
+    const int lane = (int)threadIdx.x % kWave, heads = A.H[0] + A.H[1];
+    const long long row = (long long)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
+    if (row >= A.T * heads) return;
+    const long long token = row / heads;
+    int h = (int)(row - token * heads);
+    const int t = h >= A.H[0];
+    if (t) h -= A.H[0];
+    const T* x = static_cast<const T*>(A.x[t]) + token * A.ldx[t] + (long long)h * A.D;
+    T* y = static_cast<T*>(A.out[t]) + token * A.ldo[t] + (long long)h * A.D;
+    const Angles ang(A, token);
+    float v[kSlots], s = 0.f;
+#pragma unroll
+    for (int k = 0; k < kSlots; ++k) {
+        const int d = k * kWave + lane;
+        v[k] = d < A.D ? Elem<T>::load1(x + d) : 0.f;
+        s += v[k] * v[k];
+    }
+    const float r = 1.f / sqrtf(group_sum<kWave>(s) * A.inv_D + A.eps);
+#pragma unroll
+    for (int k = 0; k < kSlots; ++k) {
+        const int d = k * kWave + lane;
+        if (d >= A.D) continue;
+        v[k] *= r * A.w[t][d];
+        if (d < A.R) {
+            bool first;
+            int angle;
+            const int o = partner_of(A, d, &first, &angle);
+            const float other = Elem<T>::load1(x + o) * (r * A.w[t][o]), sn = ang.sin(A, angle);
+            v[k] = v[k] * ang.cos(A, angle) + (first ? -other * sn : other * sn);
+        }
+    }
+    // partners' values are in registers by now: the loads above feed the values that are stored, but those of other lanes
+    // may still be on their way while this lane stores, so all of them are waited for
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < kSlots; ++k) {
+        const int d = k * kWave + lane;
+        if (d < A.D) Elem<T>::store1(y + d, v[k]);
+    }
+}
+
+template <typename T> __global__ __launch_bounds__(kThreads) void head_backward_any(const HeadArgs A)
+{
+    extern __shared__ float red[];                    // [4][D]
+    const int lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
+    const long long waves = (long long)gridDim.x * (kThreads / kWave);
+    for (int t = 0; t < 2; ++t) {
+        float dw[kSlots];
+#pragma unroll
+        for (int k = 0; k < kSlots; ++k) dw[k] = 0.f;
+        for (long long row = (long long)blockIdx.x * (kThreads / kWave) + wave; row < A.T * A.H[t]; row += waves) {
+            const long long token = row / A.H[t];
+            const int h = (int)(row - token * A.H[t]);
+            const T* x = static_cast<const T*>(A.x[t]) + token * A.ldx[t] + (long long)h * A.D;
+            const T* dy = static_cast<const T*>(A.dy[t]) + token * A.lddy[t] + (long long)h * A.D;
+            T* dx = static_cast<T*>(A.out[t]) + token * A.ldo[t] + (long long)h * A.D;
+            const Angles ang(A, token);
+            float v[kSlots], e[kSlots], s = 0.f, m = 0.f;
+#pragma unroll
+            for (int k = 0; k < kSlots; ++k) {
+                const int d = k * kWave + lane;
+                v[k] = e[k] = 0.f;
+                if (d >= A.D) continue;
+                v[k] = Elem<T>::load1(x + d);
+                e[k] = Elem<T>::load1(dy + d);
+                if (d < A.R) {
+                    bool first;
+                    int angle;
+                    const int o = partner_of(A, d, &first, &angle);
+                    const float other = Elem<T>::load1(dy + o), sn = ang.sin(A, angle);
+                    e[k] = e[k] * ang.cos(A, angle) + (first ? other * sn : -other * sn);
+                }
+                s += v[k] * v[k];
+                m += e[k] * A.w[t][d] * v[k];
+            }
+            const float r = 1.f / sqrtf(group_sum<kWave>(s) * A.inv_D + A.eps);
+            const float f = group_sum<kWave>(m) * r * r * A.inv_D;
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // as above: dx may be dy
+#pragma unroll
+            for (int k = 0; k < kSlots; ++k) {
+                const int d = k * kWave + lane;
+                if (d >= A.D) continue;
+                dw[k] += e[k] * (v[k] * r);
+                Elem<T>::store1(dx + d, r * (e[k] * A.w[t][d] - v[k] * f));
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kSlots; ++k)
+            if (k * kWave + lane < A.D) red[wave * A.D + k * kWave + lane] = dw[k];
+        store_dw(A, red, t);
+    }
+}
+
+// ---- host ----
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+cgbn_status launched() { return hipGetLastError() == hipSuccess ? CGBN_OK : CGBN_ERR_HIP; }
+
+constexpr long long kMaxTokens = 1ll << 30, kMaxStride = 1ll << 32;
+constexpr int kMaxHeads = 1 << 14;
+constexpr int kBackwardGroups = 1024;         // four workgroups a compute unit
+
+cgbn_status check_sizes(long long T, int Hq, int Hk, int D, int dtype)
+{
+    if (dtype != CGBN_F32 && dtype != CGBN_BF16) return CGBN_ERR_ENUM;
+    if (T < 0 || T > kMaxTokens || Hq < 1 || Hq > kMaxHeads || Hk < 0 || Hk > kMaxHeads || D < 1 || D > kMaxD) return CGBN_ERR_SHAPE;
+    if (T * (Hq + Hk) > (1ll << 33)) return CGBN_ERR_SHAPE;            // grids stay within 31 bits
+    return CGBN_OK;
+}
+
+// workgroups of a backward call
+int backward_groups(long long T, int Hq, int Hk)
+{
+    const long long rows = T * (Hq + Hk), groups = (rows + 15) / 16;   // (at least four rows a wavefront, but for the last)
+    return (int)(groups < kBackwardGroups ? (groups < 1 ? 1 : groups) : kBackwardGroups);
+}
+
+template <typename T> bool plan_chunks(HeadArgs* A, bool backward)
+{
+    constexpr int E = 16 / (int)sizeof(T);
+    if (A->D % E != 0) return false;
+    for (int t = 0; t < (A->H[1] ? 2 : 1); ++t) {
+        if (!aligned16(A->x[t]) || !aligned16(A->out[t]) || A->ldx[t] % E != 0 || A->ldo[t] % E != 0) return false;
+        if (backward && (!aligned16(A->dy[t]) || A->lddy[t] % E != 0)) return false;
+    }
+    const int chunks = A->D / E;
+    A->lead = A->far = 0;
+    if (A->style == CGBN_ROTATE_HALVES && A->R) {
+        if ((A->R / 2) % E != 0) return false;
+        A->lead = A->far = A->R / 2 / E;
+    }
+    A->rest = chunks - 2 * A->lead;
+    A->pairs = A->lead + (A->rest + 1) / 2;
+    return A->pairs <= kWave;
+}
+
+int lanes_of(int pairs)
+{
+    int l = 1;
+    while (l < pairs) l *= 2;
+    return l;
+}
+
+#define CGBN_LANES(X_) X_(1) X_(2) X_(4) X_(8) X_(16) X_(32) X_(64)
+
+template <typename T> cgbn_status run_forward(HeadArgs& A, hipStream_t st)
+{
+    if (!plan_chunks<T>(&A, false)) {
+        const long long rows = A.T * (A.H[0] + A.H[1]);
+        hipLaunchKernelGGL(head_forward_any<T>, dim3((unsigned)((rows + 3) / 4)), dim3(kThreads), 0, st, A);
+        return launched();
+    }
+    const int L = lanes_of(A.pairs), G = kWave / L, most = ((A.H[0] > A.H[1] ? A.H[0] : A.H[1]) + G - 1) / G;
+    // a wavefront takes all heads of its token unless there are too few tokens to fill the device with
+    A.parts = 1;
+    while (A.parts < most && A.T * A.parts < 4096) A.parts *= 2;
+    if (A.parts > most) A.parts = most;
+    const dim3 grid((unsigned)((A.T * A.parts + 3) / 4));
+#define CGBN_CASE(L_) \
+    case L_: hipLaunchKernelGGL((head_forward<T, L_>), grid, dim3(kThreads), 0, st, A); break;
+    switch (L) { CGBN_LANES(CGBN_CASE) }
+#undef CGBN_CASE
+    return launched();
+}
+
+template <typename T> cgbn_status run_backward(HeadArgs& A, float* dwq, float* dwk, hipStream_t st)
+{
+    const int groups = backward_groups(A.T, A.H[0], A.H[1]);
+    const size_t lds = (size_t)4 * A.D * sizeof(float);
+    if (!plan_chunks<T>(&A, true)) {
+        hipLaunchKernelGGL(head_backward_any<T>, dim3((unsigned)groups), dim3(kThreads), lds, st, A);
+    } else {
+        const int L = lanes_of(A.pairs), G = kWave / L, most = ((A.H[0] > A.H[1] ? A.H[0] : A.H[1]) + G - 1) / G;
+        A.parts = 1;
+        while (A.parts < most && A.T * A.parts < 4096) A.parts *= 2;
+        if (A.parts > most) A.parts = most;
+#define CGBN_CASE(L_) \
+        case L_: hipLaunchKernelGGL((head_backward<T, L_>), dim3((unsigned)groups), dim3(kThreads), lds, st, A); break;
+        switch (L) { CGBN_LANES(CGBN_CASE) }
+#undef CGBN_CASE
+    }
+    if (launched() != CGBN_OK) return CGBN_ERR_HIP;
+    const int n = A.H[1] ? 2 * A.D : A.D;
+    // (a workgroup's row of partial sums has both weights' side by side; without keys the second half is zero and stays unread)
+    hipLaunchKernelGGL(column_sums, dim3((unsigned)((n + 15) / 16)), dim3(kThreads), 0, st, A.part, groups, 2 * A.D, n, dwq, A.D, dwk);
+    return launched();
+}
+
+cgbn_status check_call(const HeadArgs& A, cgbn_dtype dtype, cgbn_rotation style, bool backward)
+{
+    const cgbn_status s = check_sizes(A.T, A.H[0], A.H[1], A.D, dtype);
+    if (s != CGBN_OK) return s;
+    if (style != CGBN_ROTATE_HALVES && style != CGBN_ROTATE_PAIRS) return CGBN_ERR_ACTIVATION;
+    if (A.R < 0 || A.R > A.D || A.R % 2 != 0 || (A.R && A.table < 1)) return CGBN_ERR_SHAPE;
+    if (!(A.eps > 0.f) || std::isinf(A.eps)) return CGBN_ERR_EPS;
+    if (A.R && A.T && (!A.cos || !A.sin)) return CGBN_ERR_NULL;
+    const size_t elem = dtype == CGBN_F32 ? 4 : 2;
+    for (int t = 0; t < (A.H[1] ? 2 : 1); ++t) {
+        if (!A.w[t] || (A.T && (!A.x[t] || !A.out[t] || (backward && !A.dy[t])))) return CGBN_ERR_NULL;
+        const long long width = (long long)A.H[t] * A.D;
+        if (A.ldx[t] > kMaxStride || A.ldo[t] > kMaxStride || (backward && A.lddy[t] > kMaxStride)) return CGBN_ERR_SHAPE;
+        if (A.T > 1 && (A.ldx[t] < width || A.ldo[t] < width || (backward && A.lddy[t] < width))) return CGBN_ERR_STRIDE;
+        if (reinterpret_cast<uintptr_t>(A.x[t]) % elem || reinterpret_cast<uintptr_t>(A.out[t]) % elem ||
+            (backward && reinterpret_cast<uintptr_t>(A.dy[t]) % elem))
+            return CGBN_ERR_ALIGN;
+        // in place: row for row
+        const void* in = backward ? A.dy[t] : A.x[t];
+        const long long ld = backward ? A.lddy[t] : A.ldx[t];
+        if (A.T && A.out[t] == in && A.T > 1 && A.ldo[t] != ld) return CGBN_ERR_ALIAS;
+        if (A.T && backward && A.out[t] == A.x[t] && A.T > 1 && A.ldo[t] != A.ldx[t]) return CGBN_ERR_ALIAS;
+    }
+    if (A.T && A.H[1] && A.out[0] == A.out[1]) return CGBN_ERR_ALIAS;
+    return CGBN_OK;
+}
+
+}  // namespace
+}  // namespace cgbn
+
+using namespace cgbn;
+
+extern "C" {
+
+cgbn_status cgbn_head_norm_forward(const void* q, long long ldq, const void* k, long long ldk, long long T, int Hq, int Hk, int D, int R,
+                                   cgbn_rotation style, const int* positions, const float* cos, const float* sin, int table_rows, const float* wq,
+                                   const float* wk, float eps, void* yq, long long ldyq, void* yk, long long ldyk, cgbn_dtype dtype, void* stream)
+{
+    HeadArgs A;
+    std::memset(&A, 0, sizeof(A));
+    A.x[0] = q; A.x[1] = k; A.out[0] = yq; A.out[1] = yk;
+    A.ldx[0] = ldq; A.ldx[1] = ldk; A.ldo[0] = ldyq; A.ldo[1] = ldyk;
+    A.w[0] = wq; A.w[1] = wk; A.cos = cos; A.sin = sin; A.positions = positions;
+    A.T = T; A.H[0] = Hq; A.H[1] = Hk; A.D = D; A.R = R; A.table = table_rows; A.style = style; A.eps = eps;
+    const cgbn_status s = check_call(A, dtype, style, false);
+    if (s != CGBN_OK || T == 0) return s;
+    A.inv_D = 1.f / (float)D;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return dtype == CGBN_F32 ? run_forward<float>(A, st) : run_forward<bf16_t>(A, st);
+}
+
+size_t cgbn_head_norm_workspace_bytes(long long T, int Hq, int Hk, int D, cgbn_dtype dtype)
+{
+    if (check_sizes(T, Hq, Hk, D, dtype) != CGBN_OK) return 0;
+    return ((size_t)backward_groups(T, Hq, Hk) * 2 * D * sizeof(float) + 255) / 256 * 256;
+}
+
+cgbn_status cgbn_head_norm_backward(const void* dyq, long long lddyq, const void* dyk, long long lddyk, const void* q, long long ldq, const void* k,
+                                    long long ldk, long long T, int Hq, int Hk, int D, int R, cgbn_rotation style, const int* positions,
+                                    const float* cos, const float* sin, int table_rows, const float* wq, const float* wk, float eps, void* dq,
+                                    long long lddq, void* dk, long long lddk, float* dwq, float* dwk, cgbn_dtype dtype, void* workspace,
+                                    size_t workspace_bytes, void* stream)
+{
+    HeadArgs A;
+    std::memset(&A, 0, sizeof(A));
+    A.x[0] = q; A.x[1] = k; A.dy[0] = dyq; A.dy[1] = dyk; A.out[0] = dq; A.out[1] = dk;
+    A.ldx[0] = ldq; A.ldx[1] = ldk; A.lddy[0] = lddyq; A.lddy[1] = lddyk; A.ldo[0] = lddq; A.ldo[1] = lddk;
+    A.w[0] = wq; A.w[1] = wk; A.cos = cos; A.sin = sin; A.positions = positions;
+    A.T = T; A.H[0] = Hq; A.H[1] = Hk; A.D = D; A.R = R; A.table = table_rows; A.style = style; A.eps = eps;
+    const cgbn_status s = check_call(A, dtype, style, true);
+    if (s != CGBN_OK) return s;
+    if (!dwq || (Hk && !dwk)) return CGBN_ERR_NULL;
+    if (dwq == dwk) return CGBN_ERR_ALIAS;
+    const size_t need = cgbn_head_norm_workspace_bytes(T, Hq, Hk, D, dtype);
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need) return CGBN_ERR_WORKSPACE;
+    A.part = static_cast<float*>(workspace);
+    A.inv_D = 1.f / (float)D;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return dtype == CGBN_F32 ? run_backward<float>(A, dwq, dwk, st) : run_backward<bf16_t>(A, dwq, dwk, st);
+}
+
+}  // extern "C"

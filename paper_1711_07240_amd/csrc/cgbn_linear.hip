@@ -1,0 +1,521 @@
+// The layers beside the normalization: matrix product with bias, residual and activation, and the gated feed-forward block,
+// forward and backward.  Argument checks, workspace layout, launches; the products themselves are in cgbn_gemm.h (tiles) and
+// cgbn_gemm_rows.h (few rows).
+#include "cgbn.h"
+#include "cgbn_gemm_plan.h"
+#include "cgbn_gemm_rows.h"
+#include "cgbn_column_sums.h"
+
+#include <cstring>
+
+namespace cgbn {
+namespace {
+
+// ---- small kernels around the products ----
+
+// rows of n elements to rows of np, the filling zero: operands whose rows do not start on 16 bytes
+template <typename T> __global__ __launch_bounds__(kThreads) void pad_rows(const T* src, T* dst, long long rows, int n, int np)
+{
+    constexpr int E = 16 / (int)sizeof(T);
+    const int chunks = np / E;
+    const long long id = (long long)blockIdx.x * kThreads + threadIdx.x;
+    if (id >= rows * chunks) return;
+    const long long r = id / chunks;
+    const int c = (int)(id - r * chunks) * E;
+    float v[E];
+    load_run<T, E>(src + r * n + c, v, n - c, false);
+    store_run<T, E>(dst + r * np + c, v, E, true);
+}
+
+struct DzArgs {
+    const void *dy, *saved;        // [M][N]; saved null: act none
+    void *dz, *dresidual;          // [M][ld], [M][N]; either may be null
+    float* part;                   // [row blocks][N] column sums, or null
+    long long M;
+    int N, ld, act;
+    int tw, rows;                  // vectors of a row that a workgroup covers (a power of two, at most 64); rows of a block
+};
+
+// dz = dy * act'(saved), and its column sums.  Memory bound: one read of dy and saved, one write of dz.  A thread stays in
+// one column vector and walks rows; its sums are of at most rows * tw / 256 values, in float.
+template <typename T, bool WHOLE> __global__ __launch_bounds__(kThreads) void linear_dz(const DzArgs A)
+{
+    constexpr int E = 16 / (int)sizeof(T);
+    __shared__ float red[kThreads * E];
+    const int tw = A.tw, c = ((int)blockIdx.x * tw + (int)threadIdx.x % tw) * E, first = (int)threadIdx.x / tw, stride = kThreads / tw;
+    const bool in = c < A.ld;
+    const int valid = A.N - c;
+    float sum[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[e] = 0.f;
+    const long long r0 = (long long)blockIdx.y * A.rows, r1 = min(r0 + A.rows, A.M);
+    if (in) {
+        for (long long r = r0 + first; r < r1; r += stride) {
+            float g[E];
+            load_run<T, E>(static_cast<const T*>(A.dy) + r * A.N + c, g, valid, WHOLE);
+            if (A.saved) {
+                float z[E];
+                load_run<T, E>(static_cast<const T*>(A.saved) + r * A.N + c, z, valid, WHOLE);
+                // (where ReLU passes nothing dz is zero, not dy * 0: an infinity there does not become NaN)
+#pragma unroll
+                for (int e = 0; e < E; ++e) g[e] = A.act == ACT_RELU ? (z[e] > 0.f ? g[e] : 0.f) : g[e] * act_slope(z[e], A.act);
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[e] += g[e];
+            if (A.dz) {
+                if constexpr (!WHOLE) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) g[e] = e < valid ? g[e] : 0.f;
+                }
+                store_run<T, E>(static_cast<T*>(A.dz) + r * A.ld + c, g, E, true);
+            }
+            if (A.dresidual) store_run<T, E>(static_cast<T*>(A.dresidual) + r * A.N + c, g, valid, WHOLE);
+        }
+    }
+    if (!A.part) return;
+#pragma unroll
+    for (int e = 0; e < E; ++e) red[threadIdx.x * E + e] = sum[e];
+    __syncthreads();
+    for (int v = (int)threadIdx.x; v < tw * E; v += kThreads) {
+        float s = 0.f;
+        for (int k = 0; k < stride; ++k) s += red[k * tw * E + v];
+        const int n = (int)blockIdx.x * tw * E + v;
+        if (n < A.N) A.part[(long long)blockIdx.y * A.N + n] = s;
+    }
+}
+
+struct GateArgs {
+    const void *dh, *gate, *up;    // [M][F]
+    void *dg, *du;                 // [M][ld]
+    long long M;
+    int F, ld, act;
+};
+
+// dg = dh * up * act'(gate), du = dh * act(gate), rounded to the operands' type for the products that follow (as they would be
+// had they been tensors of the layer): memory bound, three reads and two writes.
+template <typename T, bool WHOLE> __global__ __launch_bounds__(kThreads) void gated_dz(const GateArgs A)
+{
+    constexpr int E = 16 / (int)sizeof(T);
+    const int chunks = A.ld / E;
+    const long long total = A.M * chunks;
+    for (long long id = (long long)blockIdx.x * kThreads + threadIdx.x; id < total; id += (long long)gridDim.x * kThreads) {
+        const long long r = id / chunks;
+        const int c = (int)(id - r * chunks) * E, valid = A.F - c;
+        const long long o = r * A.F + c;
+        float h[E], g[E], u[E];
+        load_run<T, E>(static_cast<const T*>(A.dh) + o, h, valid, WHOLE);
+        load_run<T, E>(static_cast<const T*>(A.gate) + o, g, valid, WHOLE);
+        load_run<T, E>(static_cast<const T*>(A.up) + o, u, valid, WHOLE);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float slope = act_slope(g[e], A.act), a = act_apply(g[e], A.act);
+            g[e] = A.act == ACT_RELU && !(g[e] > 0.f) ? 0.f : h[e] * u[e] * slope;
+            u[e] = h[e] * a;
+            if (!WHOLE && e >= valid) g[e] = u[e] = 0.f;
+        }
+        store_run<T, E>(static_cast<T*>(A.dg) + r * A.ld + c, g, E, true);
+        store_run<T, E>(static_cast<T*>(A.du) + r * A.ld + c, u, E, true);
+    }
+}
+
+template <typename T> __global__ __launch_bounds__(kThreads) void fill_zero(T* p, long long n)
+{
+    const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
+    if (i < n) p[i] = T{};
+}
+
+// ---- host ----
+
+#define CGBN_TRY(call_)                                  \
+    do {                                                 \
+        const cgbn_status s_ = (call_);                  \
+        if (s_ != CGBN_OK) return s_;                    \
+    } while (0)
+#define CGBN_HIP(call_)                                  \
+    do {                                                 \
+        if ((call_) != hipSuccess) return CGBN_ERR_HIP;  \
+    } while (0)
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
+constexpr int kMaxWidth = 1 << 20;                  // of N, K, F: a tile's byte offsets stay within 32 bits
+constexpr long long kMaxRows = 1ll << 30;
+constexpr long long kMaxElements = 1ll << 38;       // of a matrix: grids stay within 31 bits
+constexpr int kFewRows = 32;                        // up to here a forward product takes gemm_rows
+
+cgbn_status check_sizes(long long M, int N, int K, int dtype)
+{
+    if (dtype != CGBN_F32 && dtype != CGBN_BF16) return CGBN_ERR_ENUM;
+    if (M < 0 || M > kMaxRows || N < 1 || N > kMaxWidth || K < 1 || K > kMaxWidth) return CGBN_ERR_SHAPE;
+    if (M * N > kMaxElements || M * K > kMaxElements || (long long)N * K > kMaxElements) return CGBN_ERR_SHAPE;
+    return CGBN_OK;
+}
+
+// How a call uses its workspace: byte offsets of its parts, 0 bytes for those it needs not.
+struct Layout {
+    size_t at = 0;
+    size_t take(size_t bytes)
+    {
+        const size_t o = at;
+        at += round256(bytes);
+        return o;
+    }
+};
+
+struct Widths {
+    int elem, E;
+    explicit Widths(int dtype) : elem(dtype == CGBN_F32 ? 4 : 2), E(16 / elem) {}
+    int padded(int n) const { return (n + E - 1) / E * E; }
+    bool odd(int n) const { return n % E != 0; }
+};
+
+struct ForwardPlan {
+    bool rows;                  // gemm_rows
+    GemmPlan g;
+    size_t x, w, part, bytes;   // padded copies of x and of the weights; partial sums
+};
+
+ForwardPlan plan_forward(long long M, int N, int K, int dtype, bool gated)
+{
+    const Widths W(dtype);
+    ForwardPlan p;
+    std::memset(&p, 0, sizeof(p));
+    p.rows = M <= kFewRows;
+    if (p.rows) return p;
+    p.g = plan_gemm(W.elem, gated, M, N, K, 1, 1);
+    Layout l;
+    if (W.odd(K)) {
+        p.x = l.take((size_t)M * W.padded(K) * W.elem);
+        p.w = l.take((size_t)N * W.padded(K) * W.elem * (gated ? 2 : 1));
+    }
+    p.part = l.take(p.g.part_bytes);
+    p.bytes = l.at;
+    return p;
+}
+
+struct BackwardPlan {
+    GemmPlan dx, dw;
+    size_t dz, x, w, part, sums, bytes;
+    int sum_blocks, sum_rows, tw;
+};
+
+BackwardPlan plan_backward(long long M, int N, int K, int dtype, bool gated)
+{
+    const Widths W(dtype);
+    BackwardPlan p;
+    std::memset(&p, 0, sizeof(p));
+    p.dx = plan_gemm(W.elem, false, M, K, N, gated ? 2 : 1, 1);
+    p.dw = plan_gemm(W.elem, false, N, K, M, 1, gated ? 2 : 1);
+    Layout l;
+    p.dz = l.take((size_t)M * W.padded(N) * W.elem * (gated ? 2 : 1));
+    if (W.odd(K)) {
+        p.x = l.take((size_t)M * W.padded(K) * W.elem);
+        p.w = l.take((size_t)N * W.padded(K) * W.elem * (gated ? 2 : 1));
+    }
+    p.part = l.take(p.dx.part_bytes > p.dw.part_bytes ? p.dx.part_bytes : p.dw.part_bytes);
+    // column sums: enough blocks of rows to fill the device, no block of fewer rows than a workgroup walks in eight passes
+    const int vecs = W.padded(N) / W.E;
+    p.tw = 1;
+    while (p.tw < 64 && p.tw < vecs) p.tw *= 2;
+    const long long across = (vecs + p.tw - 1) / p.tw, least = 8ll * (kThreads / p.tw);
+    long long blocks = 2048 / across > 1 ? 2048 / across : 1;
+    if (blocks > (M + least - 1) / least) blocks = (M + least - 1) / least;
+    if (blocks < 1) blocks = 1;
+    p.sum_rows = (int)((M + blocks - 1) / blocks);
+    p.sum_blocks = p.sum_rows ? (int)((M + p.sum_rows - 1) / p.sum_rows) : 0;
+    if (!gated) p.sums = l.take((size_t)p.sum_blocks * N * sizeof(float));
+    p.bytes = l.at;
+    return p;
+}
+
+cgbn_status check_workspace(size_t need, const void* workspace, size_t have)
+{
+    if (need == 0) return CGBN_OK;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || have < need) return CGBN_ERR_WORKSPACE;
+    return CGBN_OK;
+}
+
+template <typename T> hipError_t pad(const void* src, void* dst, long long rows, int n, int np, hipStream_t st)
+{
+    const long long ids = rows * (np / (16 / (int)sizeof(T)));
+    hipLaunchKernelGGL(pad_rows<T>, dim3((unsigned)((ids + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, static_cast<const T*>(src),
+                       static_cast<T*>(dst), rows, n, np);
+    return hipGetLastError();
+}
+
+template <typename T, bool GATED, bool WHOLE> hipError_t launch_rows(const GemmArgs& G, hipStream_t st)
+{
+    const dim3 grid((unsigned)((G.J + 15) / 16));
+    if (G.I <= 16) hipLaunchKernelGGL((gemm_rows<T, GATED, WHOLE, 1, 8>), grid, dim3(8 * kWave), 0, st, G);
+    else hipLaunchKernelGGL((gemm_rows<T, GATED, WHOLE, 2, 8>), grid, dim3(8 * kWave), 0, st, G);
+    return hipGetLastError();
+}
+
+template <typename T, bool GATED>
+cgbn_status forward(GemmArgs G, const ForwardPlan& p, char* ws, hipStream_t st)
+{
+    const int K = G.R;
+    const Widths W(sizeof(T) == 4 ? CGBN_F32 : CGBN_BF16);
+    G.segs = G.batch = 1;
+    G.lda = G.ldb = K;
+    G.ldc = G.J;
+    if (p.rows) {
+        CGBN_HIP((W.odd(K) ? launch_rows<T, GATED, false>(G, st) : launch_rows<T, GATED, true>(G, st)));
+        return CGBN_OK;
+    }
+    if (W.odd(K)) {
+        const int kp = W.padded(K);
+        CGBN_HIP(pad<T>(G.A[0], ws + p.x, G.I, K, kp, st));
+        G.A[0] = ws + p.x;
+        for (int k = 0; k < (GATED ? 2 : 1); ++k) {
+            char* to = ws + p.w + (size_t)k * G.J * kp * sizeof(T);
+            CGBN_HIP(pad<T>(G.B[k], to, G.J, K, kp, st));
+            G.B[k] = to;
+        }
+        G.lda = G.ldb = kp;
+    }
+    G.part = reinterpret_cast<float*>(ws + p.part);
+    CGBN_HIP((launch_gemm<T, FORM_NT, GATED>(p.g, G, st)));
+    return CGBN_OK;
+}
+
+// dx = dz W (two pairs: summed) and dW = dz^T x (two: side by side), dz rows of `ldz` elements
+template <typename T>
+cgbn_status products(const void* const dz[2], int ldz, int pairs, const void* x, const void* const w[2], long long M, int N, int K, void* dx,
+                     void* const dw[2], const BackwardPlan& p, char* ws, hipStream_t st)
+{
+    const Widths W(sizeof(T) == 4 ? CGBN_F32 : CGBN_BF16);
+    const int kp = W.padded(K);
+    GemmArgs G;
+    std::memset(&G, 0, sizeof(G));
+    G.part = reinterpret_cast<float*>(ws + p.part);
+    G.J = K;
+    G.ldb = kp;
+    G.ldc = K;
+    G.lda = ldz;
+    if (dx) {
+        for (int k = 0; k < pairs; ++k) {
+            G.A[k] = dz[k];
+            G.B[k] = w[k];
+            if (W.odd(K)) {
+                char* to = ws + p.w + (size_t)k * N * kp * sizeof(T);
+                CGBN_HIP(pad<T>(w[k], to, N, K, kp, st));
+                G.B[k] = to;
+            }
+        }
+        G.C[0] = dx;
+        G.I = (int)M;
+        G.R = N;
+        G.segs = pairs;
+        G.batch = 1;
+        CGBN_HIP((launch_gemm<T, FORM_NN, false>(p.dx, G, st)));
+    }
+    if (dw[0]) {
+        if (W.odd(K)) {
+            CGBN_HIP(pad<T>(x, ws + p.x, M, K, kp, st));
+            x = ws + p.x;
+        }
+        for (int k = 0; k < pairs; ++k) {
+            G.A[k] = dz[k];
+            G.B[k] = x;
+            G.C[k] = dw[k];
+        }
+        G.I = N;
+        G.R = (int)M;
+        G.segs = 1;
+        G.batch = pairs;
+        CGBN_HIP((launch_gemm<T, FORM_TN, false>(p.dw, G, st)));
+    }
+    return CGBN_OK;
+}
+
+template <typename T> hipError_t zero(void* p, long long n, hipStream_t st)
+{
+    if (!p || n == 0) return hipSuccess;
+    hipLaunchKernelGGL(fill_zero<T>, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, static_cast<T*>(p), n);
+    return hipGetLastError();
+}
+
+template <typename T>
+cgbn_status linear_backward(const void* dy, const void* x, const void* w, const void* saved, long long M, int N, int K, int act, void* dx, void* dw,
+                            float* dbias, void* dresidual, char* ws, hipStream_t st)
+{
+    if (M == 0) {
+        CGBN_HIP(zero<T>(dw, (long long)N * K, st));
+        CGBN_HIP(zero<float>(dbias, N, st));
+        return CGBN_OK;
+    }
+    const Widths W(sizeof(T) == 4 ? CGBN_F32 : CGBN_BF16);
+    const int dtype = sizeof(T) == 4 ? CGBN_F32 : CGBN_BF16;
+    const BackwardPlan p = plan_backward(M, N, K, dtype, false);
+    const int np = W.padded(N);
+    const void* dz = dy;
+    const bool products_follow = dx || dw, changes = act != ACT_NONE || W.odd(N);
+    DzArgs A;
+    std::memset(&A, 0, sizeof(A));
+    if (dresidual && dresidual != dy && !W.odd(N)) {
+        A.dz = dresidual;                         // dz is what the residual's gradient is: one buffer serves both
+        dz = dresidual;
+    } else {
+        if (products_follow && changes) {
+            A.dz = ws + p.dz;
+            dz = ws + p.dz;
+        }
+        // (in place: an element is read before the same thread writes it)
+        if (dresidual && (dresidual != dy || act != ACT_NONE)) A.dresidual = dresidual;
+    }
+    if (A.dz || A.dresidual || dbias) {
+        A.dy = dy;
+        A.saved = act == ACT_NONE ? nullptr : saved;
+        A.part = dbias ? reinterpret_cast<float*>(ws + p.sums) : nullptr;
+        A.M = M; A.N = N; A.ld = np; A.act = act;
+        A.tw = p.tw; A.rows = p.sum_rows;
+        const int vecs = np / W.E;
+        const dim3 grid((unsigned)((vecs + p.tw - 1) / p.tw), (unsigned)p.sum_blocks);
+        if (W.odd(N)) hipLaunchKernelGGL((linear_dz<T, false>), grid, dim3(kThreads), 0, st, A);
+        else hipLaunchKernelGGL((linear_dz<T, true>), grid, dim3(kThreads), 0, st, A);
+        CGBN_HIP(hipGetLastError());
+        if (dbias) {
+            hipLaunchKernelGGL(column_sums, dim3((unsigned)((N + 15) / 16)), dim3(kThreads), 0, st, A.part, p.sum_blocks, N, N, dbias, N, nullptr);
+            CGBN_HIP(hipGetLastError());
+        }
+    }
+    const void *dzs[2] = {dz, nullptr}, *ws_[2] = {w, nullptr};
+    void* dws[2] = {dw, nullptr};
+    return products<T>(dzs, np, 1, x, ws_, M, N, K, dx, dws, p, ws, st);
+}
+
+template <typename T>
+cgbn_status gated_backward(const void* dh, const void* x, const void* wg, const void* wu, const void* gate, const void* up, long long M, int F, int K,
+                           int act, void* dx, void* dwg, void* dwu, char* ws, hipStream_t st)
+{
+    if (M == 0) {
+        CGBN_HIP(zero<T>(dwg, (long long)F * K, st));
+        CGBN_HIP(zero<T>(dwu, (long long)F * K, st));
+        return CGBN_OK;
+    }
+    const Widths W(sizeof(T) == 4 ? CGBN_F32 : CGBN_BF16);
+    const BackwardPlan p = plan_backward(M, F, K, sizeof(T) == 4 ? CGBN_F32 : CGBN_BF16, true);
+    const int fp = W.padded(F);
+    char* dg = ws + p.dz;
+    char* du = dg + (size_t)M * fp * sizeof(T);
+    const GateArgs A = {dh, gate, up, dg, du, M, F, fp, act};
+    const long long ids = M * (fp / W.E), groups = (ids + kThreads - 1) / kThreads;
+    const dim3 grid((unsigned)(groups < 8192 ? groups : 8192));
+    if (W.odd(F)) hipLaunchKernelGGL((gated_dz<T, false>), grid, dim3(kThreads), 0, st, A);
+    else hipLaunchKernelGGL((gated_dz<T, true>), grid, dim3(kThreads), 0, st, A);
+    CGBN_HIP(hipGetLastError());
+    const void *dzs[2] = {dg, du}, *ws_[2] = {wg, wu};
+    void* dws[2] = {dwg, dwu};
+    return products<T>(dzs, fp, 2, x, ws_, M, F, K, dx, dws, p, ws, st);
+}
+
+}  // namespace
+}  // namespace cgbn
+
+using namespace cgbn;
+
+extern "C" {
+
+size_t cgbn_linear_workspace_bytes(long long M, int N, int K, cgbn_dtype dtype, int backward)
+{
+    if (check_sizes(M, N, K, dtype) != CGBN_OK) return 0;
+    if (M == 0) return 256;
+    const size_t b = backward ? plan_backward(M, N, K, dtype, false).bytes : plan_forward(M, N, K, dtype, false).bytes;
+    return b ? b : 256;
+}
+
+cgbn_status cgbn_linear_forward(const void* x, const void* w, const float* bias, const void* residual, long long M, int N, int K, cgbn_activation act,
+                                void* y, void* z, cgbn_dtype dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!w || (M != 0 && (!x || !y))) return CGBN_ERR_NULL;          // (no rows, no tensors)
+    CGBN_TRY(check_sizes(M, N, K, dtype));
+    if (act < CGBN_ACT_NONE || act > CGBN_ACT_SILU) return CGBN_ERR_ACTIVATION;
+    if (M == 0) return CGBN_OK;
+    if (!aligned16(x) || !aligned16(w) || !aligned16(y) || !aligned16(residual) || !aligned16(z)) return CGBN_ERR_ALIGN;
+    if (y == z || y == x || z == x || y == w || z == w) return CGBN_ERR_ALIAS;
+    const ForwardPlan p = plan_forward(M, N, K, dtype, false);
+    CGBN_TRY(check_workspace(p.bytes, workspace, workspace_bytes));
+    GemmArgs G;
+    std::memset(&G, 0, sizeof(G));
+    G.A[0] = x; G.B[0] = w; G.C[0] = y; G.Z[0] = z; G.bias = bias; G.residual = residual;
+    G.I = (int)M; G.J = N; G.R = K; G.act = act;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    char* ws = static_cast<char*>(workspace);
+    return dtype == CGBN_F32 ? forward<float, false>(G, p, ws, st) : forward<bf16_t, false>(G, p, ws, st);
+}
+
+cgbn_status cgbn_linear_backward(const void* dy, const void* x, const void* w, const void* saved, long long M, int N, int K, cgbn_activation act,
+                                 void* dx, void* dw, float* dbias, void* dresidual, cgbn_dtype dtype, void* workspace, size_t workspace_bytes,
+                                 void* stream)
+{
+    if (!w || (M != 0 && (!dy || !x))) return CGBN_ERR_NULL;
+    CGBN_TRY(check_sizes(M, N, K, dtype));
+    if (act < CGBN_ACT_NONE || act > CGBN_ACT_SILU) return CGBN_ERR_ACTIVATION;
+    if (act != CGBN_ACT_NONE && M != 0 && !saved) return CGBN_ERR_NULL;
+    if (!aligned16(dy) || !aligned16(x) || !aligned16(w) || !aligned16(saved) || !aligned16(dx) || !aligned16(dw) || !aligned16(dresidual))
+        return CGBN_ERR_ALIGN;
+    if (M != 0 && dx && (dx == dw || dx == dresidual || dx == dy || dx == x || dx == w)) return CGBN_ERR_ALIAS;
+    if (M != 0 && dw && (dw == dresidual || dw == dy || dw == x || dw == w)) return CGBN_ERR_ALIAS;
+    if (M != 0 && dresidual && (dresidual == x || dresidual == w)) return CGBN_ERR_ALIAS;
+    if (M > 0) CGBN_TRY(check_workspace(plan_backward(M, N, K, dtype, false).bytes, workspace, workspace_bytes));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    char* ws = static_cast<char*>(workspace);
+    return dtype == CGBN_F32 ? linear_backward<float>(dy, x, w, saved, M, N, K, act, dx, dw, dbias, dresidual, ws, st)
+                             : linear_backward<bf16_t>(dy, x, w, saved, M, N, K, act, dx, dw, dbias, dresidual, ws, st);
+}
+
+size_t cgbn_gated_workspace_bytes(long long M, int F, int K, cgbn_dtype dtype, int backward)
+{
+    if (check_sizes(M, F, K, dtype) != CGBN_OK) return 0;
+    if (M == 0) return 256;
+    const size_t b = backward ? plan_backward(M, F, K, dtype, true).bytes : plan_forward(M, F, K, dtype, true).bytes;
+    return b ? b : 256;
+}
+
+cgbn_status cgbn_gated_forward(const void* x, const void* w_gate, const void* w_up, long long M, int F, int K, cgbn_activation act, void* h,
+                               void* gate, void* up, cgbn_dtype dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!w_gate || !w_up || (M != 0 && (!x || !h || !gate != !up))) return CGBN_ERR_NULL;
+    CGBN_TRY(check_sizes(M, F, K, dtype));
+    if (act < CGBN_ACT_NONE || act > CGBN_ACT_SILU) return CGBN_ERR_ACTIVATION;
+    if (M == 0) return CGBN_OK;
+    if (!aligned16(x) || !aligned16(w_gate) || !aligned16(w_up) || !aligned16(h) || !aligned16(gate) || !aligned16(up)) return CGBN_ERR_ALIGN;
+    const void* const outs[3] = {h, gate, up};
+    for (int k = 0; k < 3; ++k)
+        if (outs[k] && (outs[k] == x || outs[k] == w_gate || outs[k] == w_up || outs[k] == outs[(k + 1) % 3])) return CGBN_ERR_ALIAS;
+    const ForwardPlan p = plan_forward(M, F, K, dtype, true);
+    CGBN_TRY(check_workspace(p.bytes, workspace, workspace_bytes));
+    GemmArgs G;
+    std::memset(&G, 0, sizeof(G));
+    G.A[0] = x; G.B[0] = w_gate; G.B[1] = w_up; G.C[0] = h; G.Z[0] = gate; G.Z[1] = up;
+    G.I = (int)M; G.J = F; G.R = K; G.act = act;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    char* ws = static_cast<char*>(workspace);
+    return dtype == CGBN_F32 ? forward<float, true>(G, p, ws, st) : forward<bf16_t, true>(G, p, ws, st);
+}
+
+cgbn_status cgbn_gated_backward(const void* dh, const void* x, const void* w_gate, const void* w_up, const void* gate, const void* up, long long M,
+                                int F, int K, cgbn_activation act, void* dx, void* dw_gate, void* dw_up, cgbn_dtype dtype, void* workspace,
+                                size_t workspace_bytes, void* stream)
+{
+    if (!w_gate || !w_up || !dw_gate != !dw_up || (M != 0 && (!dh || !x || !gate || !up))) return CGBN_ERR_NULL;
+    CGBN_TRY(check_sizes(M, F, K, dtype));
+    if (act < CGBN_ACT_NONE || act > CGBN_ACT_SILU) return CGBN_ERR_ACTIVATION;
+    if (!aligned16(dh) || !aligned16(x) || !aligned16(w_gate) || !aligned16(w_up) || !aligned16(gate) || !aligned16(up) || !aligned16(dx) ||
+        !aligned16(dw_gate) || !aligned16(dw_up))
+        return CGBN_ERR_ALIGN;
+    const void* const outs[3] = {dx, dw_gate, dw_up};
+    for (int k = 0; k < 3; ++k)
+        if (outs[k] && (outs[k] == x || outs[k] == w_gate || outs[k] == w_up || outs[k] == dh || outs[k] == gate || outs[k] == up ||
+                        outs[k] == outs[(k + 1) % 3]))
+            return CGBN_ERR_ALIAS;
+    if (M > 0) CGBN_TRY(check_workspace(plan_backward(M, F, K, dtype, true).bytes, workspace, workspace_bytes));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    char* ws = static_cast<char*>(workspace);
+    return dtype == CGBN_F32 ? gated_backward<float>(dh, x, w_gate, w_up, gate, up, M, F, K, act, dx, dw_gate, dw_up, ws, st)
+                             : gated_backward<bf16_t>(dh, x, w_gate, w_up, gate, up, M, F, K, act, dx, dw_gate, dw_up, ws, st);
+}
+
+}  // extern "C"
