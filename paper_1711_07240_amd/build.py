@@ -45,9 +45,9 @@ def _units(obj_dir):
     OBJ = obj_dir
     units = [(os.path.join(OBJ, name + ".o"), os.path.join(CSRC, name + ".hip"), []) for name in ("cgbn", "cgbn_linear", "cgbn_head_norm")]
     for tname, t in (("f32", "float"), ("bf16", "bf16_t")):
-        for form, gated in ((0, "false"), (0, "true"), (1, "false"), (2, "false")):
-            units.append((os.path.join(OBJ, f"gemm_{tname}_{form}{'_gated' if gated == 'true' else ''}.o"), os.path.join(CSRC, "cgbn_gemm_inst.hip"),
-                          [f"-DCGBN_INST_T={t}", f"-DCGBN_INST_FORM={form}", f"-DCGBN_INST_GATED={gated}"]))
+        for form, fname in enumerate(("forward", "gated", "backward")):
+            units.append((os.path.join(OBJ, f"gemm_{tname}_{fname}.o"), os.path.join(CSRC, "cgbn_gemm_inst.hip"),
+                          [f"-DCGBN_INST_T={t}", f"-DCGBN_INST_FORM={form}"]))
     for tname, t in (("f32", "float"), ("bf16", "bf16_t")):
         for fwd in (1, 0):
             for act in ((0, 1, 2) if fwd else (0, 1)):       # forward: plain, ReLU, shortcut + ReLU

@@ -15,14 +15,15 @@
 // bfloat16 by the LDS reads that transpose 4 x 16 blocks, so no operand is ever transposed in memory.
 //
 // The product is formed as C^T (B is the matrix instruction's first operand), so that a lane's four accumulators are
-// neighbours in a row of C.  Where B is in rows, which of its rows feed which row of which fragment is free: they are dealt so that a
-// lane ends up with 16 neighbours (8 + 8 of a gated pair), which makes the epilogue's loads and stores 16 bytes wide.
+// neighbours in a row of C.
 //
 // Sums are held in 32 bits throughout.  Where tiles are too few for 256 compute units the reduction is split and the partial
 // sums, float, are joined by gemm_join in split order: results never depend on the order in which workgroups end.
 #pragma once
 
 #include "cgbn_kernels.h"
+
+#include <type_traits>
 
 namespace cgbn {
 
@@ -46,11 +47,23 @@ struct GemmArgs {
 
 // ---- activations, on 32-bit values ----
 
+// exp(-x): the hardware's 2^y
+__device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2f(x * -1.4426950408889634f); }
+
+// Phi(-|z|), e being exp(-z^2 / 2): the rational approximation of the complementary error function that Abramowitz and Stegun give as
+// 7.1.26 (after Hastings), off by at most 7.5e-8 here; a fifth of the instructions of the library's erff, which at 128 values a lane
+// took longer than a step of the product.
+__device__ __forceinline__ float normal_tail(float z, float e)
+{
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.23164189f, fabsf(z), 1.f));         // 0.3275911 / sqrt(2)
+    return e * (t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5307027145f, -0.7265760135f), 0.7107068705f), -0.142248368f), 0.127414796f));
+}
+
 __device__ __forceinline__ float act_apply(float z, int act)
 {
     if (act == ACT_RELU) return z > 0.f ? z : (z != z ? z : 0.f);
-    if (act == ACT_GELU) return z * (0.5f + 0.5f * erff(z * 0.70710678118654752f));
-    if (act == ACT_SILU) return z / (1.f + expf(-z));
+    if (act == ACT_GELU) return fmaf(-fabsf(z), normal_tail(z, exp_neg(0.5f * z * z)), z > 0.f ? z : 0.f);      // z Phi(z), z - z Phi(-z)
+    if (act == ACT_SILU) return z * __builtin_amdgcn_rcpf(1.f + exp_neg(z));
     return z;
 }
 
@@ -58,9 +71,13 @@ __device__ __forceinline__ float act_apply(float z, int act)
 __device__ __forceinline__ float act_slope(float z, int act)
 {
     if (act == ACT_RELU) return z > 0.f ? 1.f : 0.f;
-    if (act == ACT_GELU) return 0.5f + 0.5f * erff(z * 0.70710678118654752f) + z * 0.39894228040143268f * expf(-0.5f * z * z);
+    if (act == ACT_GELU) {
+        const float e = exp_neg(0.5f * z * z);
+        const float p = normal_tail(z, e);
+        return (z < 0.f ? p : 1.f - p) + z * 0.39894228040143268f * e;
+    }
     if (act == ACT_SILU) {
-        const float s = 1.f / (1.f + expf(-z));
+        const float s = __builtin_amdgcn_rcpf(1.f + exp_neg(z));
         return s + z * s * (1.f - s);
     }
     return 1.f;
@@ -119,15 +136,11 @@ template <typename T, int N> __device__ __forceinline__ void store_run(T* p, con
 
 // 16 bytes a lane from base + off to LDS at `lds` + 16 * lane.  Written out because the compiler, which cannot tell the two
 // halves of the buffer apart, would have every LDS read wait for the loads in flight into the other half.  No register is
-// written (but m0, in which the compiler keeps nothing); dma_wait_and_meet() below makes the bytes visible.  The wait states
-// are those that m0, and an address in scalar registers that the vector unit may have written, need before the load.
+// written (but m0, in which the compiler keeps nothing); dma_wait_and_meet() below makes the bytes visible.  The wait state is what m0
+// needs before the load.
 __device__ __forceinline__ void dma16(uint32_t lds, const char* base, uint32_t off)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
-}
-__device__ __forceinline__ void dma16(uint32_t lds, const char* p)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
 }
 // every load of this wavefront has landed, every LDS read of it has returned; then the workgroup meets
 __device__ __forceinline__ void dma_wait_and_meet()
@@ -135,22 +148,12 @@ __device__ __forceinline__ void dma_wait_and_meet()
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-__device__ __attribute__((aligned(16))) const uint32_t gemm_zeros[4] = {0, 0, 0, 0};
-
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8_hw __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) char lds_char;
 
-// How the rows of B (operand in rows) are dealt to fragments: lane t of a fragment's 16 rows, fragment f of 4.
-enum { DEAL_PLAIN = 0, DEAL_16 = 1, DEAL_GATED = 2 };
-
-// xor key of a row of an operand in rows (8 chunks of 16 bytes a row): the 16 rows that a fragment read touches at once spread over all banks
-template <int DEAL> __device__ __forceinline__ int row_key(int row)
-{
-    if constexpr (DEAL == DEAL_16) return (row & 3) | ((row >> 4) & 1) << 2;
-    if constexpr (DEAL == DEAL_GATED) return (row & 3) | ((row >> 3) & 1) << 2;
-    return row & 7;
-}
+// xor key of a row of an operand in rows (8 chunks of 16 bytes a row): the rows that a fragment read touches at once spread over all banks
+__device__ __forceinline__ int row_key(int row) { return row & 7; }
 
 // xor key, in 16-byte chunks, of a row of an operand in columns with CR chunks a row
 template <typename T, int CR> __device__ __forceinline__ int col_key(int row)
@@ -162,7 +165,7 @@ template <typename T, int CR> __device__ __forceinline__ int col_key(int row)
 }
 
 // One operand's share of a step: ROWS (of i or j) x 128 bytes of r, staged by NT threads.
-template <typename T, bool COLS, int ROWS, int NT, int DEAL> struct Operand {
+template <typename T, bool COLS, int ROWS, int NT, bool PAIR> struct Operand {
     static constexpr int E = 16 / (int)sizeof(T);           // elements of a chunk
     static constexpr int STEP = 128 / (int)sizeof(T);       // r of a step
     static constexpr int CR = COLS ? ROWS / E : 8;          // chunks of a row of the tile in LDS
@@ -170,7 +173,7 @@ template <typename T, bool COLS, int ROWS, int NT, int DEAL> struct Operand {
     static constexpr int IT = BYTES / 16 / NT;
     static constexpr int HALF = ROWS / 2;
     static_assert(BYTES % (16 * NT) == 0, "whole passes");
-    static_assert(DEAL != DEAL_GATED || HALF % (NT / 8) == 0, "a pass stays within one of the two matrices");
+    static_assert(!PAIR || HALF % (NT / 8) == 0, "a pass stays within one of the two matrices");
 
     uint32_t off[IT];
 
@@ -180,7 +183,7 @@ template <typename T, bool COLS, int ROWS, int NT, int DEAL> struct Operand {
     {
         const int slot = (it * NT + (int)threadIdx.x) % CR;
         if constexpr (COLS) return slot ^ col_key<T, CR>(row_of(it));
-        else return slot ^ row_key<DEAL>(row_of(it));
+        else return slot ^ row_key(row_of(it));
     }
     // first: the tile's first i; n: how many there are (rows and chunks beyond are read at the last one: results unused)
     __device__ __forceinline__ void init(int first, int n, long long ld)
@@ -191,7 +194,7 @@ template <typename T, bool COLS, int ROWS, int NT, int DEAL> struct Operand {
                 const int c = min(first / E + chunk_of(it), (n + E - 1) / E - 1) - first / E;
                 off[it] = (uint32_t)(row_of(it) * ld * (int)sizeof(T)) + c * 16;
             } else {
-                const int r = DEAL == DEAL_GATED ? row_of(it) % HALF : row_of(it);
+                const int r = PAIR ? row_of(it) % HALF : row_of(it);
                 off[it] = (uint32_t)((min(first + r, n - 1) - first) * ld * (int)sizeof(T)) + chunk_of(it) * 16;
             }
         }
@@ -200,40 +203,32 @@ template <typename T, bool COLS, int ROWS, int NT, int DEAL> struct Operand {
     {
         return static_cast<const char*>(p) + (COLS ? (long long)step * STEP * ld + first : (long long)first * ld + (long long)step * STEP) * (int)sizeof(T);
     }
-    // p1: the second matrix of a gated pair.  lds: where the tile goes.  left: r that remain from this step on
-    __device__ __forceinline__ void stage(uint32_t lds, const void* p0, const void* p1, int first, int step, long long ld, int left) const
+    // bytes from one step to the next
+    static __device__ __forceinline__ long long advance(long long ld) { return COLS ? STEP * ld * (int)sizeof(T) : 128; }
+    // Pass `it` of a step whose data starts at b0 (gated: of the second matrix at b1); lds: where the wavefront's share of the tile goes.
+    __device__ __forceinline__ void pass(int it, uint32_t lds, const char* b0, const char* b1) const
     {
-        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-        const char* b0 = at(p0, first, step, ld);
-        const char* b1 = DEAL == DEAL_GATED ? at(p1, first, step, ld) : b0;
-        if (left >= STEP) {
-#pragma unroll
-            for (int it = 0; it < IT; ++it)
-                dma16(lds + (it * NT + wave * kWave) * 16, DEAL == DEAL_GATED && it * (NT / 8) >= HALF ? b1 : b0, off[it]);
-        } else {
-#pragma unroll
-            for (int it = 0; it < IT; ++it) {
-                const bool in = (COLS ? row_of(it) : chunk_of(it) * E) < left;
-                const char* b = DEAL == DEAL_GATED && it * (NT / 8) >= HALF ? b1 : b0;
-                dma16(lds + (it * NT + wave * kWave) * 16, in ? b + off[it] : reinterpret_cast<const char*>(gemm_zeros));
-            }
-        }
+        dma16(lds + it * NT * 16, PAIR && it * (NT / 8) >= HALF ? b1 : b0, off[it]);
+    }
+    // ... with only `left` r of the operand remaining: zeros for what lies beyond (a lane that is switched off leaves its 16
+    // bytes of LDS alone)
+    __device__ __forceinline__ void last_pass(int it, uint32_t lds, lds_char* tile, const char* b0, const char* b1, int left) const
+    {
+        if ((COLS ? row_of(it) : chunk_of(it) * E) < left) pass(it, lds, b0, b1);
+        else *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(tile + (it * NT + (int)threadIdx.x) * 16) = u32x4{0, 0, 0, 0};
     }
 };
 
 // A fragment: 16 rows of i x 16 bytes of r a lane, that is lane l holds row l % 16 and chunk 4 * ks + l / 16 of the step.
 // (bfloat16: what one matrix instruction takes; float: four of them, r being dealt to them in the same way on both sides.)
-// first: the fragment's first row within the tile (a multiple of 16), or its column group where rows are dealt.
-template <typename T, bool COLS, int ROWS, int DEAL>
+// base: the first of the rows that are walked, within the tile; f: which of their fragments.
+template <typename T, bool COLS, int ROWS>
 __device__ __forceinline__ u32x4 fragment(const lds_char* tile, int base, int f, int ks)
 {
     const int l = (int)threadIdx.x % kWave, t = l & 15, q = l >> 4;
     if constexpr (!COLS) {
-        int row;
-        if constexpr (DEAL == DEAL_16) row = base + (t >> 2) * 16 + f * 4 + (t & 3);
-        else if constexpr (DEAL == DEAL_GATED) row = (f >> 1) * (ROWS / 2) + base + (t >> 2) * 8 + (f & 1) * 4 + (t & 3);
-        else row = base + f * 16 + t;
-        return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(tile + row * 128 + (((ks * 4 + q) ^ row_key<DEAL>(row)) << 4));
+        const int row = base + f * 16 + t;
+        return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(tile + row * 128 + (((ks * 4 + q) ^ row_key(row)) << 4));
     } else {
         constexpr int RB = ROWS * (int)sizeof(T), CR = RB / 16;
         if constexpr (sizeof(T) == 2) {
@@ -270,9 +265,9 @@ template <typename T> __device__ __forceinline__ f32x4 multiply(const u32x4& a, 
 // work of its own; within it tiles go in blocks of 8 rows of tiles, column by column, so that the ones in flight at a time share operands in
 // the die's L2.
 struct TileId { int i, j, split, z; };
-__device__ __forceinline__ TileId tile_of(const GemmArgs& G)
+__device__ __forceinline__ TileId tile_of(const GemmArgs& G, int id, int n)
 {
-    const int n = (int)gridDim.x, id = (int)blockIdx.x, die = id & 7, q = n >> 3, r = n & 7;
+    const int die = id & 7, q = n >> 3, r = n & 7;
     int w = (die < r ? die * (q + 1) : r * (q + 1) + (die - r) * q) + (id >> 3);
     TileId t;
     const int tiles = G.ti * G.tj;
@@ -289,52 +284,55 @@ __device__ __forceinline__ TileId tile_of(const GemmArgs& G)
 
 // ---- epilogues: a run of N neighbours of a row ----
 
-template <typename T, int N> __device__ __forceinline__ void finish_linear(const GemmArgs& G, float (&v)[N], int i, int j, bool whole)
+template <int N> __device__ __forceinline__ void activate(float (&v)[N], int act)
 {
-    const int valid = G.J - j;
-    const long long o = (long long)i * G.ldc + j;
-    if (G.bias) {
-#pragma unroll
-        for (int k = 0; k < N; ++k) v[k] += k < valid ? G.bias[j + k] : 0.f;
+#define CGBN_ACTIVATE(act_)                                   \
+    if (act == act_) {                                        \
+        _Pragma("unroll") for (int k = 0; k < N; ++k) v[k] = act_apply(v[k], act_); \
     }
-    if (G.residual) {
-        float r[N];
-        load_run<T, N>(static_cast<const T*>(G.residual) + o, r, valid, whole);
+    CGBN_ACTIVATE(ACT_RELU)
+    CGBN_ACTIVATE(ACT_GELU)
+    CGBN_ACTIVATE(ACT_SILU)
+#undef CGBN_ACTIVATE
+}
+
+// v: the products; r: bias and residual.  o: the run's first element in the outputs; whole: it lies within the row and on 16 bytes
+template <typename T, int N>
+__device__ __forceinline__ void finish_linear(const GemmArgs& G, float (&v)[N], const float (&r)[N], long long o, int valid, bool whole)
+{
 #pragma unroll
-        for (int k = 0; k < N; ++k) v[k] += r[k];
-    }
+    for (int k = 0; k < N; ++k) v[k] += r[k];
     if (G.Z[0]) store_run<T, N>(static_cast<T*>(G.Z[0]) + o, v, valid, whole);
-    if (G.act == ACT_RELU) {
-#pragma unroll
-        for (int k = 0; k < N; ++k) v[k] = act_apply(v[k], ACT_RELU);
-    } else if (G.act == ACT_GELU) {
-#pragma unroll
-        for (int k = 0; k < N; ++k) v[k] = act_apply(v[k], ACT_GELU);
-    } else if (G.act == ACT_SILU) {
-#pragma unroll
-        for (int k = 0; k < N; ++k) v[k] = act_apply(v[k], ACT_SILU);
-    }
+    activate(v, G.act);
     store_run<T, N>(static_cast<T*>(G.C[0]) + o, v, valid, whole);
 }
 
-template <typename T, int N> __device__ __forceinline__ void finish_gated(const GemmArgs& G, float (&g)[N], const float (&u)[N], int i, int j, bool whole)
+// what finish_linear adds
+template <int N> __device__ __forceinline__ void load_bias(const GemmArgs& G, float (&b)[N], int j, int valid)
 {
-    const int valid = G.J - j;
-    const long long o = (long long)i * G.ldc + j;
+#pragma unroll
+    for (int k = 0; k < N; ++k) b[k] = G.bias && k < valid ? G.bias[j + k] : 0.f;
+}
+template <typename T, int N> __device__ __forceinline__ void load_extras(const GemmArgs& G, float (&r)[N], const float (&b)[N], long long o, int valid, bool whole)
+{
+    if (G.residual) {
+        load_run<T, N>(static_cast<const T*>(G.residual) + o, r, valid, whole);
+#pragma unroll
+        for (int k = 0; k < N; ++k) r[k] += b[k];
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) r[k] = b[k];
+    }
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void finish_gated(const GemmArgs& G, float (&g)[N], const float (&u)[N], long long o, int valid, bool whole)
+{
     if (G.Z[0]) {
         store_run<T, N>(static_cast<T*>(G.Z[0]) + o, g, valid, whole);
         store_run<T, N>(static_cast<T*>(G.Z[1]) + o, u, valid, whole);
     }
-    if (G.act == ACT_RELU) {
-#pragma unroll
-        for (int k = 0; k < N; ++k) g[k] = act_apply(g[k], ACT_RELU);
-    } else if (G.act == ACT_GELU) {
-#pragma unroll
-        for (int k = 0; k < N; ++k) g[k] = act_apply(g[k], ACT_GELU);
-    } else if (G.act == ACT_SILU) {
-#pragma unroll
-        for (int k = 0; k < N; ++k) g[k] = act_apply(g[k], ACT_SILU);
-    }
+    activate(g, G.act);
 #pragma unroll
     for (int k = 0; k < N; ++k) g[k] *= u[k];
     store_run<T, N>(static_cast<T*>(G.C[0]) + o, g, valid, whole);
@@ -342,21 +340,22 @@ template <typename T, int N> __device__ __forceinline__ void finish_gated(const 
 
 // ---- the product ----
 
-template <typename T, int FORM, bool GATED, bool PART, int BI, int BJ, int WI, int WJ>
-__global__ __launch_bounds__(WI * WJ * kWave) void gemm_tile(const GemmArgs G)
+constexpr int tile_lds(int bi, int bj) { return 2 * (bi + bj) * 128; }
+
+// One workgroup's share, number `id` of `n`.
+template <typename T, int FORM, bool GATED, int BI, int BJ, int WI, int WJ>
+__device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int id, int n)
 {
-    constexpr int NT = WI * WJ * kWave, TI = BI / WI, FI = TI / 16, FJ = 4;
-    static_assert(BJ / WJ == 64 && TI % 16 == 0, "a wavefront's share is 64 columns wide");
+    constexpr int NT = WI * WJ * kWave, TI = BI / WI, FI = TI / 16, TJ = BJ / WJ, FJ = TJ / 16;
     constexpr bool ACOLS = FORM == FORM_TN, BCOLS = FORM != FORM_NT;
-    constexpr int DEAL = BCOLS ? DEAL_PLAIN : (GATED ? DEAL_GATED : DEAL_16);
-    typedef Operand<T, ACOLS, BI, NT, DEAL_PLAIN> OA;
-    typedef Operand<T, BCOLS, BJ, NT, DEAL> OB;
+    typedef Operand<T, ACOLS, BI, NT, false> OA;
+    typedef Operand<T, BCOLS, BJ, NT, GATED> OB;
     constexpr int STAGE = OA::BYTES + OB::BYTES;
-    __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
+    static_assert(2 * STAGE == tile_lds(BI, BJ), "two steps");
     lds_char* const tile = (lds_char*)lds;
     const uint32_t lds0 = (uint32_t)(uintptr_t)tile;
 
-    const TileId w = tile_of(G);
+    const TileId w = tile_of(G, id, n);
     const int i0 = w.i * BI, j0 = w.j * (GATED ? BJ / 2 : BJ);
     OA a;
     OB b;
@@ -365,83 +364,203 @@ __global__ __launch_bounds__(WI * WJ * kWave) void gemm_tile(const GemmArgs G)
     const int seg_steps = (G.R + OA::STEP - 1) / OA::STEP;
     const int first = w.split * G.per, last = min(first + G.per, seg_steps * G.segs);
 
-    auto stage = [&](int s, int buf) {
-        const int seg = s >= seg_steps, step = s - seg * seg_steps, which = seg + w.z, left = G.R - step * OA::STEP;
-        const uint32_t to = lds0 + buf * STAGE;
-        a.stage(to, G.A[which], nullptr, i0, step, G.lda, left);
-        b.stage(to + OA::BYTES, GATED ? G.B[0] : G.B[which], G.B[1], j0, step, G.ldb, left);
+    // The next step to be staged: where its data starts, and the r that remain in its segment.
+    int seg = first >= seg_steps, left = G.R - (first - seg * seg_steps) * OA::STEP;
+    const char *pa = OA::at(G.A[seg + w.z], i0, first - seg * seg_steps, G.lda), *pb = OB::at(GATED ? G.B[0] : G.B[seg + w.z], j0, first - seg * seg_steps, G.ldb),
+               *pb2 = GATED ? OB::at(G.B[1], j0, first, G.ldb) : pb;
+    const char *const next_a = OA::at(G.A[1], i0, 0, G.lda), *const next_b = OB::at(G.B[1], j0, 0, G.ldb);
+    const long long da = OA::advance(G.lda), db = OB::advance(G.ldb);
+    auto staged = [&] {
+        pa += da; pb += db; pb2 += db;
+        left -= OA::STEP;
+        if (!GATED && left <= 0) { pa = next_a; pb = next_b; left = G.R; }          // (a second segment, or nothing more to stage)
+    };
+    constexpr int PASSES = OA::IT + OB::IT;
+    const uint32_t lds_wave = lds0 + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave) * (kWave * 16);
+    // (an address must not be read by a load within five wait states of the vector unit's writing it; from here on only the scalar
+    // unit touches these)
+    asm volatile("s_nop 4" : "+s"(pa), "+s"(pb), "+s"(pb2));
+    auto pass = [&](int buf, int p, bool whole) {
+        const uint32_t to = buf * STAGE + (p < OA::IT ? 0 : OA::BYTES);
+        if (p < OA::IT) {
+            if (whole) a.pass(p, lds_wave + to, pa, nullptr);
+            else a.last_pass(p, lds_wave + to, tile + to, pa, nullptr, left);
+        } else {
+            if (whole) b.pass(p - OA::IT, lds_wave + to, pb, pb2);
+            else b.last_pass(p - OA::IT, lds_wave + to, tile + to, pb, pb2, left);
+        }
+    };
+    auto stage = [&](int buf) {
+        const bool whole = left >= OA::STEP;
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) pass(buf, p, whole);
+        staged();
     };
 
     const int wave = (int)threadIdx.x / kWave, wi = wave / WJ, wj = wave % WJ;
-    const int abase = wi * TI, bbase = wj * (GATED ? 32 : 64);
+    const int abase = wi * TI, bbase = wj * (GATED ? TJ / 2 : TJ);
     f32x4 acc[FI][FJ];
 #pragma unroll
     for (int x = 0; x < FI; ++x)
 #pragma unroll
         for (int y = 0; y < FJ; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    if (first < last) stage(first, 0);
-    for (int s = first; s < last; ++s) {
+    // A step is multiplied in two halves (ks), row of fragments by row.  What a half needs is read from LDS during the half before:
+    // B's fragments into a second set of registers, A's into the row just multiplied.  Where the step's own reads end, one or two
+    // rows into the second half, the workgroup meets; the loads of the step after next are issued between the rows that
+    // follow, and have a whole step to arrive.
+    constexpr int LAG = FI >= 4 ? 2 : 1;
+    u32x4 fa[FI], fb[2][FJ];
+    auto read_a = [&](int buf, int ks, int x) { fa[x] = fragment<T, ACOLS, BI>(tile + buf * STAGE, abase, x, ks); };
+    auto read_b = [&](int buf, int ks) {
+#pragma unroll
+        for (int y = 0; y < FJ; ++y) fb[ks][y] = fragment<T, BCOLS, BJ>(tile + buf * STAGE + OA::BYTES, bbase + (GATED && y >= FJ / 2 ? BJ / 2 : 0), GATED ? y % (FJ / 2) : y, ks);
+    };
+    auto multiply_row = [&](int ks, int x) {
+#pragma unroll
+        for (int y = 0; y < FJ; ++y) acc[x][y] = multiply<T>(fb[ks][y], fa[x], acc[x][y]);
+    };
+    if (first < last) {
+        stage(0);
         dma_wait_and_meet();
-        const int buf = (s - first) & 1;
-        if (s + 1 < last) stage(s + 1, buf ^ 1);
-        const lds_char* ta = tile + buf * STAGE;
-        const lds_char* tb = ta + OA::BYTES;
+        if (first + 1 < last) stage(1);
+        read_b(0, 0);
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            u32x4 fb[FJ], fa[FI];
+        for (int x = 0; x < FI; ++x) read_a(0, 0, x);
+    }
+    // NEXT: another step follows; MORE: and yet another, whose loads start here; WHOLE: it is a whole one
+    auto step = [&](int buf, auto NEXT, auto MORE, auto WHOLE) {
+        read_b(buf, 1);
 #pragma unroll
-            for (int y = 0; y < FJ; ++y) fb[y] = fragment<T, BCOLS, BJ, DEAL>(tb, bbase, y, ks);
+        for (int x = 0; x < FI; ++x) {
+            multiply_row(0, x);
+            read_a(buf, 1, x);
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
-            for (int x = 0; x < FI; ++x) fa[x] = fragment<T, ACOLS, BI, DEAL_PLAIN>(ta, abase, x, ks);
+        for (int x = 0; x < LAG; ++x) multiply_row(1, x);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (NEXT()) {
+            dma_wait_and_meet();                // the next step is in LDS, and everyone has read this one
+            read_b(buf ^ 1, 0);
 #pragma unroll
-            for (int x = 0; x < FI; ++x)
+            for (int x = 0; x < LAG; ++x) read_a(buf ^ 1, 0, x);
+        }
 #pragma unroll
-                for (int y = 0; y < FJ; ++y) acc[x][y] = multiply<T>(fb[y], fa[x], acc[x][y]);
+        for (int x = LAG; x < FI; ++x) {
+            if constexpr (MORE()) {
+#pragma unroll
+                for (int p = (x - LAG) * PASSES / (FI - LAG); p < (x - LAG + 1) * PASSES / (FI - LAG); ++p) pass(buf, p, WHOLE());
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            multiply_row(1, x);
+            if constexpr (NEXT()) read_a(buf ^ 1, 0, x);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (MORE()) staged();
+    };
+    typedef std::integral_constant<bool, true> yes;
+    typedef std::integral_constant<bool, false> no;
+    int buf = 0, s = first;
+    while (s + 2 < last) {
+        for (; s + 2 < last && left >= OA::STEP; ++s, buf ^= 1) step(buf, yes(), yes(), yes());
+        if (s + 2 < last) {                     // the end of a segment
+            step(buf, yes(), yes(), no());
+            ++s, buf ^= 1;
         }
     }
+    if (s + 1 < last) {
+        step(buf, yes(), no(), no());
+        buf ^= 1;
+    }
+    if (first < last) step(buf, no(), no(), no());
 
+    // The accumulators go to memory through LDS, each wavefront through its own part of it, in as many rounds as that takes: a lane
+    // holds 4 columns of one row of each fragment, and would fetch and store 16 rows of 32 bytes; from LDS it takes a run
+    // of N columns, 16 bytes of the output, beside its neighbours'.
+    constexpr int WIDE = GATED ? TJ / 2 : TJ, ROOM = 2 * STAGE / (WI * WJ) / (TJ * 4) / 16;
+    constexpr int FX = ROOM >= FI ? FI : ROOM >= FI / 2 ? FI / 2 : FI / 4;                  // rows of fragments in a round
+    static_assert(FX >= 1 && FX <= ROOM, "a round fits");
     const int l = (int)threadIdx.x % kWave, t = l & 15, q = l >> 4;
+    lds_char* const mine = tile + wave * (FX * 16 * TJ * 4);
+    typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+    auto store_round = [&](int i_first, auto PART) {
+        constexpr int N = PART() ? 4 : Elem<T>::VEC, LANES = WIDE / N, ROWS = kWave / LANES, U = FX * 16 / ROWS < 4 ? FX * 16 / ROWS : 4;
+        static_assert(FX * 16 % (ROWS * U) == 0, "whole rounds");
+        constexpr bool EXTRAS = FORM == FORM_NT && !PART() && !GATED;
+        const int j = j0 + wj * WIDE + (l % LANES) * N, valid = G.J - j;
+        const bool whole = valid >= N && G.J % N == 0;
+        float bias[N];
+        if constexpr (EXTRAS) load_bias<N>(G, bias, j, valid);
+        for (int r0 = l / LANES; r0 < FX * 16; r0 += ROWS * U) {
+            float extra[U][N];
+            if constexpr (EXTRAS) {
 #pragma unroll
-    for (int x = 0; x < FI; ++x) {
-        const int i = i0 + wi * TI + x * 16 + t;
-        if (i >= G.I) continue;
-        if constexpr (GATED) {
-            const int j = j0 + wj * 32 + q * 8;
-            if (j >= G.J) continue;
-            float g[8], u[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) { g[k] = acc[x][k >> 2][k & 3]; u[k] = acc[x][2 + (k >> 2)][k & 3]; }
-            if constexpr (PART) {
-                const bool whole = j + 8 <= G.J && G.J % 4 == 0;
-                float* p = G.part + ((long long)w.split * 2 * G.I + i) * G.J + j;
-                store_run<float, 8>(p, g, G.J - j, whole);
-                store_run<float, 8>(p + (long long)G.I * G.J, u, G.J - j, whole);
-            } else {
-                finish_gated<T, 8>(G, g, u, i, j, j + 8 <= G.J && G.J % 8 == 0);
+                for (int u = 0; u < U; ++u) {
+                    const int i = i_first + r0 + u * ROWS;
+                    if (i < G.I && valid > 0) load_extras<T, N>(G, extra[u], bias, (long long)i * G.ldc + j, valid, whole);
+                }
             }
-        } else if constexpr (FORM == FORM_NT) {
-            const int j = j0 + wj * 64 + q * 16;
-            if (j >= G.J) continue;
-            float v[16];
 #pragma unroll
-            for (int k = 0; k < 16; ++k) v[k] = acc[x][k >> 2][k & 3];
-            if constexpr (PART) store_run<float, 16>(G.part + ((long long)w.split * G.I + i) * G.J + j, v, G.J - j, j + 16 <= G.J && G.J % 4 == 0);
-            else finish_linear<T, 16>(G, v, i, j, j + 16 <= G.J && G.J % 8 == 0);
-        } else {
+            for (int u = 0; u < U; ++u) {
+                const int r = r0 + u * ROWS, i = i_first + r;
+                if (i >= G.I || valid <= 0) continue;
+                float v[N], up[N];
 #pragma unroll
-            for (int y = 0; y < FJ; ++y) {
-                const int j = j0 + wj * 64 + y * 16 + q * 4;
-                if (j >= G.J) continue;
-                float v[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = acc[x][y][k];
-                const bool whole = j + 4 <= G.J && G.J % 4 == 0;
-                if constexpr (PART) store_run<float, 4>(G.part + ((long long)(w.split * G.batch + w.z) * G.I + i) * G.J + j, v, G.J - j, whole);
-                else store_run<T, 4>(static_cast<T*>(G.C[w.z]) + (long long)i * G.ldc + j, v, G.J - j, whole);
+                for (int k = 0; k < N; k += 4) {
+                    const int c = ((l % LANES) * N + k) / 4;
+                    const f32x4 a4 = *(lds_f32x4*)(mine + r * (TJ * 4) + ((c ^ (r & 7)) << 4));
+                    v[k] = a4.x; v[k + 1] = a4.y; v[k + 2] = a4.z; v[k + 3] = a4.w;
+                    if constexpr (GATED) {
+                        const f32x4 u4 = *(lds_f32x4*)(mine + r * (TJ * 4) + (((c + WIDE / 4) ^ (r & 7)) << 4));
+                        up[k] = u4.x; up[k + 1] = u4.y; up[k + 2] = u4.z; up[k + 3] = u4.w;
+                    }
+                }
+                const long long o = (long long)i * G.ldc + j;
+                if constexpr (PART()) {
+                    float* p = G.part + ((long long)(GATED ? 2 * w.split : w.split * G.batch + w.z) * G.I + i) * G.J + j;
+                    store_run<float, N>(p, v, valid, whole);
+                    if constexpr (GATED) store_run<float, N>(p + (long long)G.I * G.J, up, valid, whole);
+                } else if constexpr (GATED) {
+                    finish_gated<T, N>(G, v, up, o, valid, whole);
+                } else if constexpr (FORM == FORM_NT) {
+                    finish_linear<T, N>(G, v, extra[u], o, valid, whole);
+                } else {
+                    store_run<T, N>(static_cast<T*>(G.C[w.z]) + o, v, valid, whole);
+                }
             }
         }
+    };
+    dma_wait_and_meet();                            // everyone has read the last step
+#pragma unroll
+    for (int x0 = 0; x0 < FI; x0 += FX) {
+        // (16-byte chunk c of a row lies at c ^ (row & 7): rows are a multiple of all banks long)
+#pragma unroll
+        for (int x = 0; x < FX; ++x)
+#pragma unroll
+            for (int y = 0; y < FJ; ++y) *(lds_f32x4*)(mine + (x * 16 + t) * (TJ * 4) + (((y * 4 + q) ^ (t & 7)) << 4)) = acc[x0 + x][y];
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // (the lanes of a wavefront read each other's)
+        if (G.splits > 1) store_round(i0 + wi * TI + x0 * 16, yes());
+        else store_round(i0 + wi * TI + x0 * 16, no());
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
+}
+
+template <typename T, int FORM, bool GATED, int BI, int BJ, int WI, int WJ>
+__global__ __launch_bounds__(WI * WJ * kWave) void gemm_tile(const GemmArgs G)
+{
+    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(BI, BJ)];
+    tile_product<T, FORM, GATED, BI, BJ, WI, WJ>(G, lds, (int)blockIdx.x, (int)gridDim.x);
+}
+
+// dx = dz W and dW = dz^T x in one launch: neither needs the other, and the second's workgroups fill the compute units that
+// the first's last round leaves idle.
+template <typename T, int BI, int BJ, int WI, int WJ>
+__global__ __launch_bounds__(WI * WJ * kWave) void gemm_two(const GemmArgs X, const GemmArgs W, int nx)
+{
+    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(BI, BJ)];
+    if ((int)blockIdx.x < nx) tile_product<T, FORM_NN, false, BI, BJ, WI, WJ>(X, lds, (int)blockIdx.x, nx);
+    else tile_product<T, FORM_TN, false, BI, BJ, WI, WJ>(W, lds, (int)blockIdx.x - nx, (int)gridDim.x - nx);
 }
 
 // Partial sums of a split reduction, added in split order, then the epilogue.  N values a thread (4 where J allows whole vectors).
@@ -467,11 +586,17 @@ __global__ __launch_bounds__(kThreads) void gemm_join(const GemmArgs G)
             for (int k = 0; k < N; ++k) u[k] += t[k];
         }
     }
-    const long long z = GATED ? 0 : e / plane, o = e - z * plane;
-    const int i = (int)(o / G.J), j = (int)(o - (long long)i * G.J);
-    if constexpr (GATED) finish_gated<T, N>(G, v, u, i, j, N == 4);
-    else if constexpr (FORM == FORM_NT) finish_linear<T, N>(G, v, i, j, N == 4);
-    else store_run<T, N>(static_cast<T*>(G.C[z]) + (long long)i * G.ldc + j, v, N, N == 4);
+    const long long z = GATED ? 0 : e / plane, o = e - z * plane;        // (outputs are dense)
+    if constexpr (GATED) {
+        finish_gated<T, N>(G, v, u, o, N, N == 4);
+    } else if constexpr (FORM == FORM_NT) {
+        float bias[N];
+        load_bias<N>(G, bias, (int)(o % G.J), N);
+        load_extras<T, N>(G, u, bias, o, N, N == 4);
+        finish_linear<T, N>(G, v, u, o, N, N == 4);
+    } else {
+        store_run<T, N>(static_cast<T*>(G.C[z]) + o, v, N, N == 4);
+    }
 }
 
 }  // namespace cgbn

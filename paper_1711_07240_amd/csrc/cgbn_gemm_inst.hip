@@ -1,34 +1,62 @@
-// The matrix-product kernels of one element type and form (CGBN_INST_T, CGBN_INST_FORM, CGBN_INST_GATED): see cgbn_gemm.h.
+// The matrix-product kernels of one element type and form: see cgbn_gemm.h.  The build passes CGBN_INST_T and CGBN_INST_FORM; 0: the
+// forward product, 1: the gated pair, 2: the two of a backward pass, together and each by itself.
 #include "cgbn_gemm.h"
 #include "cgbn_gemm_plan.h"
 
 namespace cgbn {
+namespace {
 
-template <> hipError_t launch_gemm<CGBN_INST_T, CGBN_INST_FORM, CGBN_INST_GATED>(const GemmPlan& p, GemmArgs G, hipStream_t st)
+void take(const GemmPlan& p, GemmArgs* G)
 {
-    G.ti = p.ti; G.tj = p.tj; G.splits = p.splits; G.per = p.per;
-    const dim3 grid((unsigned)((long long)p.ti * p.tj * p.splits * G.batch));
-#define CGBN_TILE_CASE(n_, BI_, BJ_, WI_, WJ_)                                                                                   \
-    case n_:                                                                                                                     \
-        if (p.splits > 1)                                                                                                        \
-            hipLaunchKernelGGL((gemm_tile<CGBN_INST_T, CGBN_INST_FORM, CGBN_INST_GATED, true, BI_, BJ_, WI_, WJ_>), grid,        \
-                               dim3(WI_ * WJ_ * kWave), 0, st, G);                                                               \
-        else                                                                                                                     \
-            hipLaunchKernelGGL((gemm_tile<CGBN_INST_T, CGBN_INST_FORM, CGBN_INST_GATED, false, BI_, BJ_, WI_, WJ_>), grid,       \
-                               dim3(WI_ * WJ_ * kWave), 0, st, G);                                                               \
-        break;
-    switch (p.shape) { CGBN_TILE_SHAPES(CGBN_TILE_CASE) }
-#undef CGBN_TILE_CASE
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.splits == 1) return e;
-    const long long values = (long long)G.I * G.J * (CGBN_INST_GATED ? 1 : G.batch);
+    G->ti = p.ti; G->tj = p.tj; G->splits = p.splits; G->per = p.per;
+}
+
+unsigned groups_of(const GemmArgs& G) { return (unsigned)((long long)G.ti * G.tj * G.splits * G.batch); }
+
+template <typename T, int FORM, bool GATED> hipError_t join(const GemmArgs& G, hipStream_t st)
+{
+    if (G.splits == 1) return hipSuccess;
+    const long long values = (long long)G.I * G.J * (GATED ? 1 : G.batch);
     if (G.J % 4 == 0)
-        hipLaunchKernelGGL((gemm_join<CGBN_INST_T, CGBN_INST_FORM, CGBN_INST_GATED, 4>), dim3((unsigned)((values / 4 + kThreads - 1) / kThreads)),
-                           dim3(kThreads), 0, st, G);
+        hipLaunchKernelGGL((gemm_join<T, FORM, GATED, 4>), dim3((unsigned)((values / 4 + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, G);
     else
-        hipLaunchKernelGGL((gemm_join<CGBN_INST_T, CGBN_INST_FORM, CGBN_INST_GATED, 1>), dim3((unsigned)((values + kThreads - 1) / kThreads)),
-                           dim3(kThreads), 0, st, G);
+        hipLaunchKernelGGL((gemm_join<T, FORM, GATED, 1>), dim3((unsigned)((values + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, G);
     return hipGetLastError();
 }
+
+template <typename T, int FORM, bool GATED> hipError_t launch_one(const GemmPlan& p, GemmArgs G, hipStream_t st)
+{
+    take(p, &G);
+#define CGBN_CASE(n_, BI_, BJ_, WI_, WJ_) \
+    case n_: hipLaunchKernelGGL((gemm_tile<T, FORM, GATED, BI_, BJ_, WI_, WJ_>), dim3(groups_of(G)), dim3(WI_ * WJ_ * kWave), 0, st, G); break;
+    switch (p.shape) { CGBN_TILE_SHAPES(CGBN_CASE) }
+#undef CGBN_CASE
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess ? e : join<T, FORM, GATED>(G, st);
+}
+
+}  // namespace
+
+#if CGBN_INST_FORM == 0
+template <> hipError_t launch_gemm<CGBN_INST_T, FORM_NT, false>(const GemmPlan& p, GemmArgs G, hipStream_t st) { return launch_one<CGBN_INST_T, FORM_NT, false>(p, G, st); }
+#elif CGBN_INST_FORM == 1
+template <> hipError_t launch_gemm<CGBN_INST_T, FORM_NT, true>(const GemmPlan& p, GemmArgs G, hipStream_t st) { return launch_one<CGBN_INST_T, FORM_NT, true>(p, G, st); }
+#else
+template <> hipError_t launch_gemm<CGBN_INST_T, FORM_NN, false>(const GemmPlan& p, GemmArgs G, hipStream_t st) { return launch_one<CGBN_INST_T, FORM_NN, false>(p, G, st); }
+template <> hipError_t launch_gemm<CGBN_INST_T, FORM_TN, false>(const GemmPlan& p, GemmArgs G, hipStream_t st) { return launch_one<CGBN_INST_T, FORM_TN, false>(p, G, st); }
+template <> hipError_t launch_two<CGBN_INST_T>(const GemmPlan& px, GemmArgs X, const GemmPlan& pw, GemmArgs W, hipStream_t st)
+{
+    take(px, &X);
+    take(pw, &W);
+    const unsigned nx = groups_of(X), nw = groups_of(W);
+#define CGBN_CASE(n_, BI_, BJ_, WI_, WJ_) \
+    case n_: hipLaunchKernelGGL((gemm_two<CGBN_INST_T, BI_, BJ_, WI_, WJ_>), dim3(nx + nw), dim3(WI_ * WJ_ * kWave), 0, st, X, W, (int)nx); break;
+    switch (px.shape) { CGBN_TILE_SHAPES(CGBN_CASE) }
+#undef CGBN_CASE
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess) e = join<CGBN_INST_T, FORM_NN, false>(X, st);
+    return e != hipSuccess ? e : join<CGBN_INST_T, FORM_TN, false>(W, st);
+}
+#endif
 
 }  // namespace cgbn

@@ -1,5 +1,5 @@
-// Which kernel, tile shape and number of splits a matrix product takes.  Host code; no device is asked for anything, so that
-// a workspace can be sized where there is none: the kernels are for one device, of 256 compute units.
+// Which tile shape and how many splits of the reduction a matrix product takes.  Host code; no device is asked for anything, so
+// that a workspace can be sized where there is none: the kernels are for one device, of 256 compute units.
 #pragma once
 
 #include "cgbn_gemm.h"
@@ -8,48 +8,112 @@ namespace cgbn {
 
 // number, rows and columns of the tile, wavefronts along each
 #define CGBN_TILE_SHAPES(X_) \
-    X_(0, 256, 256, 2, 4)    \
-    X_(1, 256, 128, 4, 2)    \
-    X_(2, 128, 128, 2, 2)    \
-    X_(3, 128, 64, 4, 1)     \
-    X_(4, 64, 64, 2, 1)
+    X_(0, 256, 256, 2, 2)    \
+    X_(1, 128, 128, 2, 2)    \
+    X_(2, 128, 64, 4, 1)     \
+    X_(3, 64, 64, 2, 1)
 
 struct GemmPlan {
     int shape, ti, tj, splits, per;
     size_t part_bytes;          // of workspace, 0 where the reduction is not split
+    double groups, cost;        // workgroups; seconds that a compute unit spends on one of them
+    double join;                // seconds for joining the splits
 };
 
+// The shapes' rates, in operations a second of the whole device with the compute units full: bfloat16 as measured on
+// 8192 x 8192 x 8192; float runs at the matrix instructions' rate with any of them.  Where a compute unit holds few wavefronts,
+// their waits show: the fraction of the rate with one and with two workgroups a unit.
+struct TileShape {
+    int bi, bj, waves;
+    double rate, one, two;
+};
+inline const TileShape& tile_shape(int s)
+{
+    static const TileShape shapes[] = {
+        {256, 256, 4, 1450e12, 1., 1.}, {128, 128, 4, 1170e12, 0.65, 1.}, {128, 64, 4, 900e12, 0.5, 0.8}, {64, 64, 2, 690e12, 0.3, 0.55}};
+    return shapes[s];
+}
+constexpr int kTileShapes = 4;
+
+// the plan with one shape and one number of splits; false: more than can be
+inline bool plan_with(int shape, long long want, int elem, bool gated, long long I, long long J, long long R, int segs, int batch, GemmPlan* p)
+{
+    const TileShape& t = tile_shape(shape);
+    const int step = 128 / elem, bj = gated ? t.bj / 2 : t.bj;
+    const long long steps = (R + step - 1) / step * segs, per = (steps + want - 1) / want, splits = (steps + per - 1) / per;
+    const double part = splits > 1 ? (double)splits * batch * (gated ? 2 : 1) * I * J * 4 : 0;
+    const long long ti = (I + t.bi - 1) / t.bi, tj = (J + bj - 1) / bj;
+    if (part > 1e9 || (double)ti * tj * splits * batch > 1e9) return false;
+    *p = GemmPlan{shape, (int)ti, (int)tj, (int)splits, (int)per, (size_t)part, (double)ti * tj * splits * batch, 0, 0};
+    const double in_a_unit = p->groups / 256;
+    double rate = elem == 2 ? t.rate * (in_a_unit <= 1 ? t.one : in_a_unit <= 2 ? t.two : 1.) : 139e12 * (in_a_unit <= 1 ? t.waves / 4. : 1.);
+    // (a workgroup's first loads and last stores: a microsecond, and 16384 values of the tile in half of one)
+    p->cost = per * 2. * t.bi * t.bj * step / (rate / 256) + 1e-6 + 0.5e-6 * t.bi * t.bj / 16384;
+    p->join = splits > 1 ? 4e-6 + part * 2 / 4e12 : 0;
+    return true;
+}
+
+template <typename F> inline void each_split(long long steps, F f)
+{
+    // (a split of fewer than four steps is all prologue)
+    for (long long want = 1; want == 1 || (want <= 256 && steps / want >= 4); want = want < 4 ? want + 1 : want + want / 4)
+        if (!f(want)) break;
+}
+
+// the seconds of a product by itself: rounds of workgroups
+inline double time_alone(const GemmPlan& p) { return (double)(long long)((p.groups + 255) / 256) * p.cost + p.join; }
+
+inline GemmPlan plan_shape(int shape, int elem, bool gated, long long I, long long J, long long R, int segs, int batch)
+{
+    const int step = 128 / elem;
+    GemmPlan best{}, p;
+    each_split((R + step - 1) / step * segs, [&](long long want) {
+        if (!plan_with(shape, want, elem, gated, I, J, R, segs, batch, &p)) return false;
+        if (best.ti == 0 || time_alone(p) < time_alone(best)) best = p;
+        return true;
+    });
+    return best;
+}
 
 inline GemmPlan plan_gemm(int elem, bool gated, long long I, long long J, long long R, int segs, int batch)
 {
-    static const struct { int bi, bj; double rate; } shapes[] = {
-        {256, 256, 0.50}, {256, 128, 0.42}, {128, 128, 0.36}, {128, 64, 0.26}, {64, 64, 0.18}};
-    const double unit_peak = (elem == 2 ? 2.5e15 : 157e12) / 256;       // operations a second of one compute unit
-    const int step = 128 / elem;
-    const long long steps = (R + step - 1) / step * segs;
     GemmPlan best{};
-    double best_t = 1e30;
-    for (int s = 0; s < 5; ++s) {
-        const int bj = gated ? shapes[s].bj / 2 : shapes[s].bj;
-        const long long ti = (I + shapes[s].bi - 1) / shapes[s].bi, tj = (J + bj - 1) / bj;
-        const double t_step = 2.0 * shapes[s].bi * shapes[s].bj * step / (unit_peak * (elem == 2 ? shapes[s].rate : 0.8));
-        for (long long want = 1; want <= 256; want = want < 4 ? want + 1 : want + want / 4) {
-            if (want > 1 && steps / want < 4) break;
-            const long long per = (steps + want - 1) / want, splits = (steps + per - 1) / per;
-            const double part = splits > 1 ? (double)splits * batch * (gated ? 2 : 1) * I * J * 4 : 0;
-            if (part > 1e9) break;
-            const long long groups = ti * tj * batch * splits;
-            const double rounds = (double)((groups + 255) / 256);
-            const double t = rounds * (per * t_step + 1.5e-6) + (splits > 1 ? 4e-6 + part * 2 / 4e12 : 0);
-            if (t < best_t) {
-                best_t = t;
-                best = GemmPlan{s, (int)ti, (int)tj, (int)splits, (int)per, splits > 1 ? (size_t)part : 0};
-            }
-        }
+    for (int s = 0; s < kTileShapes; ++s) {
+        const GemmPlan p = plan_shape(s, elem, gated, I, J, R, segs, batch);
+        if (p.ti && (best.ti == 0 || time_alone(p) < time_alone(best))) best = p;
     }
     return best;
 }
 
+// dx [M][K] = dz [M][N] W and dW [N][K] = dz^T x, `pairs` of them: with one shape, each split as it would be alone or not at all
+inline void plan_two(int elem, long long M, int N, int K, int pairs, GemmPlan* dx, GemmPlan* dw)
+{
+    double best = 0;
+    dx->ti = 0;
+    for (int s = 0; s < kTileShapes; ++s) {
+        GemmPlan x[2], w[2];
+        x[0] = plan_shape(s, elem, false, M, K, N, pairs, 1);
+        w[0] = plan_shape(s, elem, false, N, K, M, 1, pairs);
+        if (!x[0].ti || !w[0].ti || !plan_with(s, 1, elem, false, M, K, N, pairs, 1, &x[1]) || !plan_with(s, 1, elem, false, N, K, M, 1, pairs, &w[1])) continue;
+        for (int a = 0; a < 2; ++a)
+            for (int b = 0; b < 2; ++b) {
+                // a unit takes the next workgroup when it is done with one: the last to be started end half of one's time
+                // after the average, and no sooner than they take
+                const double work = (x[a].groups * x[a].cost + w[b].groups * w[b].cost) / 256;
+                double t = work + 0.5 * w[b].cost;
+                if (t < x[a].cost) t = x[a].cost;
+                t += x[a].join + w[b].join;
+                if (dx->ti == 0 || t < best) {
+                    best = t;
+                    *dx = x[a];
+                    *dw = w[b];
+                }
+            }
+    }
+}
+
 template <typename T, int FORM, bool GATED> hipError_t launch_gemm(const GemmPlan& p, GemmArgs G, hipStream_t st);
+// both products of a backward pass in one launch
+template <typename T> hipError_t launch_two(const GemmPlan& px, GemmArgs X, const GemmPlan& pw, GemmArgs W, hipStream_t st);
 
 }  // namespace cgbn

@@ -96,6 +96,13 @@ __global__ __launch_bounds__(NW * kWave) void gemm_rows(const GemmArgs G)
     const int m = wave, i = i0 + m * 16 + t, j = j0 + q * 4;
     if (i >= G.I || j >= G.J) return;
     const bool whole = j + 4 <= G.J && G.J % 4 == 0;
+    const long long o = (long long)i * G.ldc + j;
+    float extra[4];
+    if constexpr (!GATED) {
+        float bias[4];
+        load_bias<4>(G, bias, j, G.J - j);
+        load_extras<T, 4>(G, extra, bias, o, G.J - j, whole);
+    }
     float v[P][4];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -105,8 +112,8 @@ __global__ __launch_bounds__(NW * kWave) void gemm_rows(const GemmArgs G)
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[p][k] = a[k];
     }
-    if constexpr (GATED) finish_gated<T, 4>(G, v[0], v[1], i, j, whole);
-    else finish_linear<T, 4>(G, v[0], i, j, whole);
+    if constexpr (GATED) finish_gated<T, 4>(G, v[0], v[1], o, G.J - j, whole);
+    else finish_linear<T, 4>(G, v[0], extra, o, G.J - j, whole);
 }
 
 }  // namespace cgbn

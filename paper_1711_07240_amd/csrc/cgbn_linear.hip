@@ -179,8 +179,7 @@ struct ForwardPlan {
 ForwardPlan plan_forward(long long M, int N, int K, int dtype, bool gated)
 {
     const Widths W(dtype);
-    ForwardPlan p;
-    std::memset(&p, 0, sizeof(p));
+    ForwardPlan p{};
     p.rows = M <= kFewRows;
     if (p.rows) return p;
     p.g = plan_gemm(W.elem, gated, M, N, K, 1, 1);
@@ -196,24 +195,24 @@ ForwardPlan plan_forward(long long M, int N, int K, int dtype, bool gated)
 
 struct BackwardPlan {
     GemmPlan dx, dw;
-    size_t dz, x, w, part, sums, bytes;
+    size_t dz, x, w, part_x, part_w, sums, bytes;
     int sum_blocks, sum_rows, tw;
 };
 
+// (one plan whichever of dx and dW a call wants: it is what the workspace is sized by)
 BackwardPlan plan_backward(long long M, int N, int K, int dtype, bool gated)
 {
     const Widths W(dtype);
-    BackwardPlan p;
-    std::memset(&p, 0, sizeof(p));
-    p.dx = plan_gemm(W.elem, false, M, K, N, gated ? 2 : 1, 1);
-    p.dw = plan_gemm(W.elem, false, N, K, M, 1, gated ? 2 : 1);
+    BackwardPlan p{};
+    plan_two(W.elem, M, N, K, gated ? 2 : 1, &p.dx, &p.dw);
     Layout l;
     p.dz = l.take((size_t)M * W.padded(N) * W.elem * (gated ? 2 : 1));
     if (W.odd(K)) {
         p.x = l.take((size_t)M * W.padded(K) * W.elem);
         p.w = l.take((size_t)N * W.padded(K) * W.elem * (gated ? 2 : 1));
     }
-    p.part = l.take(p.dx.part_bytes > p.dw.part_bytes ? p.dx.part_bytes : p.dw.part_bytes);
+    p.part_x = l.take(p.dx.part_bytes);
+    p.part_w = l.take(p.dw.part_bytes);
     // column sums: enough blocks of rows to fill the device, no block of fewer rows than a workgroup walks in eight passes
     const int vecs = W.padded(N) / W.E;
     p.tw = 1;
@@ -287,29 +286,29 @@ cgbn_status products(const void* const dz[2], int ldz, int pairs, const void* x,
 {
     const Widths W(sizeof(T) == 4 ? CGBN_F32 : CGBN_BF16);
     const int kp = W.padded(K);
-    GemmArgs G;
-    std::memset(&G, 0, sizeof(G));
-    G.part = reinterpret_cast<float*>(ws + p.part);
-    G.J = K;
-    G.ldb = kp;
-    G.ldc = K;
-    G.lda = ldz;
+    GemmArgs X, G;              // dx, dW
+    std::memset(&X, 0, sizeof(X));
+    X.J = K;
+    X.lda = ldz;
+    X.ldb = kp;
+    X.ldc = K;
+    G = X;
+    for (int k = 0; k < pairs; ++k) X.A[k] = G.A[k] = dz[k];
     if (dx) {
         for (int k = 0; k < pairs; ++k) {
-            G.A[k] = dz[k];
-            G.B[k] = w[k];
+            X.B[k] = w[k];
             if (W.odd(K)) {
                 char* to = ws + p.w + (size_t)k * N * kp * sizeof(T);
                 CGBN_HIP(pad<T>(w[k], to, N, K, kp, st));
-                G.B[k] = to;
+                X.B[k] = to;
             }
         }
-        G.C[0] = dx;
-        G.I = (int)M;
-        G.R = N;
-        G.segs = pairs;
-        G.batch = 1;
-        CGBN_HIP((launch_gemm<T, FORM_NN, false>(p.dx, G, st)));
+        X.C[0] = dx;
+        X.I = (int)M;
+        X.R = N;
+        X.segs = pairs;
+        X.batch = 1;
+        X.part = reinterpret_cast<float*>(ws + p.part_x);
     }
     if (dw[0]) {
         if (W.odd(K)) {
@@ -317,7 +316,6 @@ cgbn_status products(const void* const dz[2], int ldz, int pairs, const void* x,
             x = ws + p.x;
         }
         for (int k = 0; k < pairs; ++k) {
-            G.A[k] = dz[k];
             G.B[k] = x;
             G.C[k] = dw[k];
         }
@@ -325,8 +323,11 @@ cgbn_status products(const void* const dz[2], int ldz, int pairs, const void* x,
         G.R = (int)M;
         G.segs = 1;
         G.batch = pairs;
-        CGBN_HIP((launch_gemm<T, FORM_TN, false>(p.dw, G, st)));
+        G.part = reinterpret_cast<float*>(ws + p.part_w);
     }
+    if (dx && dw[0]) CGBN_HIP(launch_two<T>(p.dx, X, p.dw, G, st));
+    else if (dx) CGBN_HIP((launch_gemm<T, FORM_NN, false>(p.dx, X, st)));
+    else if (dw[0]) CGBN_HIP((launch_gemm<T, FORM_TN, false>(p.dw, G, st)));
     return CGBN_OK;
 }
 
