@@ -108,6 +108,13 @@ template <typename T, int N> __device__ __forceinline__ void load_run(const T* p
     }
 }
 
+// a whole 16 bytes
+template <typename T> __device__ __forceinline__ void unpack_run(const u32x4& w, float (&v)[16 / sizeof(T)])
+{
+    if constexpr (sizeof(T) == 2) Elem<T>::unpack(w, v);
+    else Elem<T>::unpack(__builtin_bit_cast(f32x4, w), v);
+}
+
 template <typename T, int N> __device__ __forceinline__ void store_run(T* p, const float (&v)[N], int valid, bool whole)
 {
     constexpr int V = Elem<T>::VEC < N ? Elem<T>::VEC : N;
@@ -398,6 +405,21 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
     };
 
     const int wave = (int)threadIdx.x / kWave, wi = wave / WJ, wj = wave % WJ;
+    // A tile's residual is asked for before anything else where registers are left for it: with few steps there is nothing to hide
+    // its way behind at the end.  (Laid out as store_round below takes it.)
+    constexpr bool EARLY = FORM == FORM_NT && !GATED && TI * TJ * (int)sizeof(T) / kWave <= 128;
+    constexpr int EV = Elem<T>::VEC, ELANES = TJ / EV, EROWS = kWave / ELANES, EARLY_N = EARLY ? TI / EROWS : 1;
+    u32x4 early[EARLY_N];
+    if constexpr (EARLY) {
+        const int j = j0 + wj * TJ + ((int)threadIdx.x % ELANES) * EV;
+        if (G.residual && G.splits == 1 && G.J % EV == 0) {
+#pragma unroll
+            for (int k = 0; k < EARLY_N; ++k) {
+                const int i = i0 + wi * TI + k * EROWS + (int)threadIdx.x % kWave / ELANES;
+                if (i < G.I && j < G.J) early[k] = *reinterpret_cast<const u32x4*>(static_cast<const T*>(G.residual) + (long long)i * G.ldc + j);
+            }
+        }
+    }
     const int abase = wi * TI, bbase = wj * (GATED ? TJ / 2 : TJ);
     f32x4 acc[FI][FJ];
 #pragma unroll
@@ -484,7 +506,8 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
     const int l = (int)threadIdx.x % kWave, t = l & 15, q = l >> 4;
     lds_char* const mine = tile + wave * (FX * 16 * TJ * 4);
     typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
-    auto store_round = [&](int i_first, auto PART) {
+    auto store_round = [&](int x0, auto PART) {
+        const int i_first = i0 + wi * TI + x0 * 16;
         constexpr int N = PART() ? 4 : Elem<T>::VEC, LANES = WIDE / N, ROWS = kWave / LANES, U = FX * 16 / ROWS < 4 ? FX * 16 / ROWS : 4;
         static_assert(FX * 16 % (ROWS * U) == 0, "whole rounds");
         constexpr bool EXTRAS = FORM == FORM_NT && !PART() && !GATED;
@@ -492,13 +515,22 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
         const bool whole = valid >= N && G.J % N == 0;
         float bias[N];
         if constexpr (EXTRAS) load_bias<N>(G, bias, j, valid);
-        for (int r0 = l / LANES; r0 < FX * 16; r0 += ROWS * U) {
+        constexpr int BATCHES = FX * 16 / (ROWS * U);
+        auto batch = [&](int b0) {
+            const int r0 = b0 + l / LANES;
             float extra[U][N];
             if constexpr (EXTRAS) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int i = i_first + r0 + u * ROWS;
-                    if (i < G.I && valid > 0) load_extras<T, N>(G, extra[u], bias, (long long)i * G.ldc + j, valid, whole);
+                    if (i >= G.I || valid <= 0) continue;
+                    if (EARLY && G.residual && G.J % EV == 0) {
+                        if constexpr (EARLY) unpack_run<T>(early[(x0 * 16 + b0) / ROWS + u], extra[u]);
+#pragma unroll
+                        for (int k = 0; k < N; ++k) extra[u][k] += bias[k];
+                    } else {
+                        load_extras<T, N>(G, extra[u], bias, (long long)i * G.ldc + j, valid, whole);
+                    }
                 }
             }
 #pragma unroll
@@ -529,6 +561,12 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
                     store_run<T, N>(static_cast<T*>(G.C[w.z]) + o, v, valid, whole);
                 }
             }
+        };
+        if constexpr (EARLY && EXTRAS) {            // (registers cannot be indexed in a loop)
+#pragma unroll
+            for (int k = 0; k < BATCHES; ++k) batch(k * ROWS * U);
+        } else {
+            for (int k = 0; k < BATCHES; ++k) batch(k * ROWS * U);
         }
     };
     dma_wait_and_meet();                            // everyone has read the last step
@@ -540,8 +578,8 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
 #pragma unroll
             for (int y = 0; y < FJ; ++y) *(lds_f32x4*)(mine + (x * 16 + t) * (TJ * 4) + (((y * 4 + q) ^ (t & 7)) << 4)) = acc[x0 + x][y];
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // (the lanes of a wavefront read each other's)
-        if (G.splits > 1) store_round(i0 + wi * TI + x0 * 16, yes());
-        else store_round(i0 + wi * TI + x0 * 16, no());
+        if (G.splits > 1) store_round(x0, yes());
+        else store_round(x0, no());
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 }

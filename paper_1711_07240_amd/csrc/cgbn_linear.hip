@@ -378,7 +378,7 @@ cgbn_status linear_backward(const void* dy, const void* x, const void* w, const 
         else hipLaunchKernelGGL((linear_dz<T, true>), grid, dim3(kThreads), 0, st, A);
         CGBN_HIP(hipGetLastError());
         if (dbias) {
-            hipLaunchKernelGGL(column_sums, dim3((unsigned)((N + 15) / 16)), dim3(kThreads), 0, st, A.part, p.sum_blocks, N, N, dbias, N, nullptr);
+            hipLaunchKernelGGL(column_sums, dim3((unsigned)((N + 15) / 16)), dim3(kSumThreads), 0, st, A.part, p.sum_blocks, N, N, dbias, N, nullptr);
             CGBN_HIP(hipGetLastError());
         }
     }
