@@ -86,6 +86,7 @@ _call = None        # the extension, bound to the library's functions
 class _ByCtypes:
     """In the place of the extension where it is not built for this Python: every call goes through ctypes."""
     forward = forward_relu = backward = backward_relu = frozen_forward = frozen_backward = staticmethod(lambda *_: NotImplemented)
+    linear_forward = linear_backward = gated_forward = gated_backward = head_norm_forward = head_norm_backward = forward
 
 
 class CgbnError(RuntimeError):
@@ -117,9 +118,13 @@ def _load_extension(handle):
     loader = importlib.machinery.ExtensionFileLoader("_cgbn_call", CALL_PATH)
     call = importlib.util.module_from_spec(importlib.util.spec_from_loader("_cgbn_call", loader))
     loader.exec_module(call)
-    call.bind(tuple(ctypes.cast(getattr(handle, "cgbn_" + n), ctypes.c_void_p).value for n in
-                    ("forward", "forward_relu", "backward", "backward_relu", "frozen_forward", "frozen_backward")),
-              LAYOUTS, DTYPES, _stream)
+    def addresses(*names):
+        return tuple(ctypes.cast(getattr(handle, "cgbn_" + n), ctypes.c_void_p).value for n in names)
+
+    call.bind(addresses("forward", "forward_relu", "backward", "backward_relu", "frozen_forward", "frozen_backward"), LAYOUTS, DTYPES,
+              _stream)
+    call.bind_layers(addresses("linear_forward", "linear_backward", "gated_forward", "gated_backward", "head_norm_forward",
+                               "head_norm_backward"), ACTIVATIONS, ROTATIONS)
     return call
 
 
@@ -338,16 +343,26 @@ def cgbn_linear_workspace_bytes(M, N, K, dtype, backward) -> int:
 
 def cgbn_linear_forward(x, w, bias, residual, M, N, K, act, y, z=None, dtype="f32", workspace=None, workspace_bytes=None,
                         stream=None) -> None:
-    _check(lib().cgbn_linear_forward(_ptr(x), _ptr(w), _ptr(bias), _ptr(residual), M, N, K, _enum(ACTIVATIONS, act), _ptr(y),
-                                     _ptr(z), _enum(DTYPES, dtype), _ptr(workspace), _room(workspace, workspace_bytes),
-                                     _stream(stream)), "cgbn_linear_forward")
+    code = (_call or _calls()).linear_forward(x, w, bias, residual, M, N, K, act, y, z, dtype, workspace, workspace_bytes,
+                                              stream)
+    if code is NotImplemented:
+        code = lib().cgbn_linear_forward(_ptr(x), _ptr(w), _ptr(bias), _ptr(residual), M, N, K, _enum(ACTIVATIONS, act), _ptr(y),
+            _ptr(z), _enum(DTYPES, dtype), _ptr(workspace), _room(workspace, workspace_bytes),
+            _stream(stream))
+    if code:
+        _check(code, "cgbn_linear_forward")
 
 
 def cgbn_linear_backward(dy, x, w, saved, M, N, K, act, dx, dw, dbias=None, dresidual=None, dtype="f32", workspace=None,
                          workspace_bytes=None, stream=None) -> None:
-    _check(lib().cgbn_linear_backward(_ptr(dy), _ptr(x), _ptr(w), _ptr(saved), M, N, K, _enum(ACTIVATIONS, act), _ptr(dx),
-                                      _ptr(dw), _ptr(dbias), _ptr(dresidual), _enum(DTYPES, dtype), _ptr(workspace),
-                                      _room(workspace, workspace_bytes), _stream(stream)), "cgbn_linear_backward")
+    code = (_call or _calls()).linear_backward(dy, x, w, saved, M, N, K, act, dx, dw, dbias, dresidual, dtype, workspace,
+                                               workspace_bytes, stream)
+    if code is NotImplemented:
+        code = lib().cgbn_linear_backward(_ptr(dy), _ptr(x), _ptr(w), _ptr(saved), M, N, K, _enum(ACTIVATIONS, act), _ptr(dx),
+            _ptr(dw), _ptr(dbias), _ptr(dresidual), _enum(DTYPES, dtype), _ptr(workspace),
+            _room(workspace, workspace_bytes), _stream(stream))
+    if code:
+        _check(code, "cgbn_linear_backward")
 
 
 def cgbn_gated_workspace_bytes(M, F, K, dtype, backward) -> int:
@@ -356,24 +371,38 @@ def cgbn_gated_workspace_bytes(M, F, K, dtype, backward) -> int:
 
 def cgbn_gated_forward(x, w_gate, w_up, M, F, K, act, h, gate=None, up=None, dtype="f32", workspace=None,
                        workspace_bytes=None, stream=None) -> None:
-    _check(lib().cgbn_gated_forward(_ptr(x), _ptr(w_gate), _ptr(w_up), M, F, K, _enum(ACTIVATIONS, act), _ptr(h), _ptr(gate),
-                                    _ptr(up), _enum(DTYPES, dtype), _ptr(workspace), _room(workspace, workspace_bytes),
-                                    _stream(stream)), "cgbn_gated_forward")
+    code = (_call or _calls()).gated_forward(x, w_gate, w_up, M, F, K, act, h, gate, up, dtype, workspace, workspace_bytes,
+                                             stream)
+    if code is NotImplemented:
+        code = lib().cgbn_gated_forward(_ptr(x), _ptr(w_gate), _ptr(w_up), M, F, K, _enum(ACTIVATIONS, act), _ptr(h), _ptr(gate),
+            _ptr(up), _enum(DTYPES, dtype), _ptr(workspace), _room(workspace, workspace_bytes),
+            _stream(stream))
+    if code:
+        _check(code, "cgbn_gated_forward")
 
 
 def cgbn_gated_backward(dh, x, w_gate, w_up, gate, up, M, F, K, act, dx, dw_gate, dw_up, dtype="f32", workspace=None,
                         workspace_bytes=None, stream=None) -> None:
-    _check(lib().cgbn_gated_backward(_ptr(dh), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(gate), _ptr(up), M, F, K,
-                                     _enum(ACTIVATIONS, act), _ptr(dx), _ptr(dw_gate), _ptr(dw_up), _enum(DTYPES, dtype),
-                                     _ptr(workspace), _room(workspace, workspace_bytes), _stream(stream)),
-           "cgbn_gated_backward")
+    code = (_call or _calls()).gated_backward(dh, x, w_gate, w_up, gate, up, M, F, K, act, dx, dw_gate, dw_up, dtype,
+                                              workspace, workspace_bytes, stream)
+    if code is NotImplemented:
+        code = lib().cgbn_gated_backward(_ptr(dh), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(gate), _ptr(up), M, F, K,
+            _enum(ACTIVATIONS, act), _ptr(dx), _ptr(dw_gate), _ptr(dw_up), _enum(DTYPES, dtype),
+            _ptr(workspace), _room(workspace, workspace_bytes), _stream(stream))
+    if code:
+        _check(code, "cgbn_gated_backward")
 
 
 def cgbn_head_norm_forward(q, ldq, k, ldk, T, Hq, Hk, D, R, style, positions, cos, sin, table_rows, wq, wk, eps, yq, ldyq, yk,
                            ldyk, dtype="f32", stream=None) -> None:
-    _check(lib().cgbn_head_norm_forward(_ptr(q), ldq, _ptr(k), ldk, T, Hq, Hk, D, R, _enum(ROTATIONS, style), _ptr(positions),
-                                        _ptr(cos), _ptr(sin), table_rows, _ptr(wq), _ptr(wk), float(eps), _ptr(yq), ldyq,
-                                        _ptr(yk), ldyk, _enum(DTYPES, dtype), _stream(stream)), "cgbn_head_norm_forward")
+    code = (_call or _calls()).head_norm_forward(q, ldq, k, ldk, T, Hq, Hk, D, R, style, positions, cos, sin, table_rows,
+                                                 wq, wk, eps, yq, ldyq, yk, ldyk, dtype, stream)
+    if code is NotImplemented:
+        code = lib().cgbn_head_norm_forward(_ptr(q), ldq, _ptr(k), ldk, T, Hq, Hk, D, R, _enum(ROTATIONS, style), _ptr(positions),
+            _ptr(cos), _ptr(sin), table_rows, _ptr(wq), _ptr(wk), float(eps), _ptr(yq), ldyq,
+            _ptr(yk), ldyk, _enum(DTYPES, dtype), _stream(stream))
+    if code:
+        _check(code, "cgbn_head_norm_forward")
 
 
 def cgbn_head_norm_workspace_bytes(T, Hq, Hk, D, dtype) -> int:
@@ -383,11 +412,17 @@ def cgbn_head_norm_workspace_bytes(T, Hq, Hk, D, dtype) -> int:
 def cgbn_head_norm_backward(dyq, lddyq, dyk, lddyk, q, ldq, k, ldk, T, Hq, Hk, D, R, style, positions, cos, sin, table_rows,
                             wq, wk, eps, dq, lddq, dk, lddk, dwq, dwk, dtype="f32", workspace=None, workspace_bytes=None,
                             stream=None) -> None:
-    _check(lib().cgbn_head_norm_backward(_ptr(dyq), lddyq, _ptr(dyk), lddyk, _ptr(q), ldq, _ptr(k), ldk, T, Hq, Hk, D, R,
-                                         _enum(ROTATIONS, style), _ptr(positions), _ptr(cos), _ptr(sin), table_rows, _ptr(wq),
-                                         _ptr(wk), float(eps), _ptr(dq), lddq, _ptr(dk), lddk, _ptr(dwq), _ptr(dwk),
-                                         _enum(DTYPES, dtype), _ptr(workspace), _room(workspace, workspace_bytes),
-                                         _stream(stream)), "cgbn_head_norm_backward")
+    code = (_call or _calls()).head_norm_backward(dyq, lddyq, dyk, lddyk, q, ldq, k, ldk, T, Hq, Hk, D, R, style, positions,
+                                                  cos, sin, table_rows, wq, wk, eps, dq, lddq, dk, lddk, dwq, dwk, dtype,
+                                                  workspace, workspace_bytes, stream)
+    if code is NotImplemented:
+        code = lib().cgbn_head_norm_backward(_ptr(dyq), lddyq, _ptr(dyk), lddyk, _ptr(q), ldq, _ptr(k), ldk, T, Hq, Hk, D, R,
+            _enum(ROTATIONS, style), _ptr(positions), _ptr(cos), _ptr(sin), table_rows, _ptr(wq),
+            _ptr(wk), float(eps), _ptr(dq), lddq, _ptr(dk), lddk, _ptr(dwq), _ptr(dwk),
+            _enum(DTYPES, dtype), _ptr(workspace), _room(workspace, workspace_bytes),
+            _stream(stream))
+    if code:
+        _check(code, "cgbn_head_norm_backward")
 
 
 def cgbn_calibration_copy(src, dst, nbytes, stream=None) -> None:
