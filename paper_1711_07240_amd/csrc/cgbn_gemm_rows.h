@@ -2,8 +2,8 @@
 //
 // What such a call has to do is read W once; its products are nothing.  A workgroup takes 16 rows of W (of both matrices of a
 // gated pair) and its wavefronts share the reduction, 128 bytes of every row at a time in turn, so the workgroup walks 16 (32)
-// streams of whole lines.  W goes from memory straight to the registers that the matrix instruction reads: lane l holds 32 bytes of
-// row l % 16 (which r a lane holds is free as long as both operands agree), several steps in flight.  x is small and comes
+// streams of whole lines.  W goes from memory straight to the registers that the matrix instruction reads: lane l holds 16 bytes of
+// row l % 16, the four lanes of a row 64 neighbouring ones, several steps in flight.  x is small and comes
 // from the caches.  The wavefronts' sums meet in LDS and are added in wavefront order.
 #pragma once
 
@@ -34,15 +34,15 @@ template <typename T, bool WHOLE> __device__ __forceinline__ u32x4 row_chunk(con
 template <typename T, bool GATED, bool WHOLE, int FM, int NW>
 __global__ __launch_bounds__(NW * kWave) void gemm_rows(const GemmArgs G)
 {
-    constexpr int E = 16 / (int)sizeof(T), STEP = 8 * E, P = GATED ? 2 : 1, U = FM == 1 ? 4 : 2;
+    constexpr int E = 16 / (int)sizeof(T), STEP = 8 * E, P = GATED ? 2 : 1, U = FM == 1 && !GATED ? 4 : 2;
     __shared__ f32x4 sums[NW][FM * P][kWave];
     const int l = (int)threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), t = l & 15, q = l >> 4;
     const int j0 = (int)blockIdx.x * 16, i0 = (int)blockIdx.y * 16 * FM;
     const T *pw[P], *px[FM];
 #pragma unroll
-    for (int p = 0; p < P; ++p) pw[p] = static_cast<const T*>(G.B[p]) + (long long)min(j0 + t, G.J - 1) * G.ldb + q * 2 * E;
+    for (int p = 0; p < P; ++p) pw[p] = static_cast<const T*>(G.B[p]) + (long long)min(j0 + t, G.J - 1) * G.ldb + q * E;
 #pragma unroll
-    for (int m = 0; m < FM; ++m) px[m] = static_cast<const T*>(G.A[0]) + (long long)min(i0 + m * 16 + t, G.I - 1) * G.lda + q * 2 * E;
+    for (int m = 0; m < FM; ++m) px[m] = static_cast<const T*>(G.A[0]) + (long long)min(i0 + m * 16 + t, G.I - 1) * G.lda + q * E;
 
     f32x4 acc[P][FM];
 #pragma unroll
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(NW * kWave) void gemm_rows(const GemmArgs G)
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int r = (s + u * NW) * STEP + h * E;
+                const int r = (s + u * NW) * STEP + h * 4 * E;
 #pragma unroll
                 for (int p = 0; p < P; ++p) w[u][p][h] = row_chunk<T, WHOLE>(pw[p] + r, E);
 #pragma unroll
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(NW * kWave) void gemm_rows(const GemmArgs G)
     for (; s < steps; s += NW) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int r = s * STEP + h * E, left = G.R - r - q * 2 * E;
+            const int r = s * STEP + h * 4 * E, left = G.R - r - q * E;
             u32x4 x[FM];
 #pragma unroll
             for (int m = 0; m < FM; ++m) x[m] = row_chunk<T, WHOLE>(px[m] + r, left);

@@ -142,7 +142,9 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 constexpr int kMaxWidth = 1 << 20;                  // of N, K, F: a tile's byte offsets stay within 32 bits
 constexpr long long kMaxRows = 1ll << 30;
 constexpr long long kMaxElements = 1ll << 38;       // of a matrix: grids stay within 31 bits
-constexpr int kFewRows = 32;                        // up to here a forward product takes gemm_rows
+// Up to here a forward product takes gemm_rows: 13.3 us against 14.8 with tiles (32 rows, 4096 x 4096), 48 rows 18.8 against 14.2; the
+// gated pair 38 against 49 us (4096 x 11264) with 16 rows, 61 against 49 with 32.
+constexpr int kFewRows = 32, kFewRowsGated = 16;
 
 cgbn_status check_sizes(long long M, int N, int K, int dtype)
 {
@@ -180,7 +182,7 @@ ForwardPlan plan_forward(long long M, int N, int K, int dtype, bool gated)
 {
     const Widths W(dtype);
     ForwardPlan p{};
-    p.rows = M <= kFewRows;
+    p.rows = M <= (gated ? kFewRowsGated : kFewRows);
     if (p.rows) return p;
     p.g = plan_gemm(W.elem, gated, M, N, K, 1, 1);
     Layout l;
@@ -246,8 +248,14 @@ template <typename T> hipError_t pad(const void* src, void* dst, long long rows,
 template <typename T, bool GATED, bool WHOLE> hipError_t launch_rows(const GemmArgs& G, hipStream_t st)
 {
     const dim3 grid((unsigned)((G.J + 15) / 16));
-    if (G.I <= 16) hipLaunchKernelGGL((gemm_rows<T, GATED, WHOLE, 1, 8>), grid, dim3(8 * kWave), 0, st, G);
-    else hipLaunchKernelGGL((gemm_rows<T, GATED, WHOLE, 2, 8>), grid, dim3(8 * kWave), 0, st, G);
+    // 16 wavefronts, each with all of its loads in flight at once or twice, where there are steps for them: 8.0 against 8.5 us with 8 of
+    // them (one row, 4096 x 4096); with few steps they only wait for each other: 3.3 with 4 against 3.6 us (1024 x 1024)
+    const bool many = (long long)G.R * (int)sizeof(T) >= 32 * 128;
+#define CGBN_ROWS(FM_, NW_) hipLaunchKernelGGL((gemm_rows<T, GATED, WHOLE, FM_, NW_>), grid, dim3(NW_ * kWave), 0, st, G)
+    if (G.I <= 16 && many) CGBN_ROWS(1, 16);
+    else if (G.I <= 16) CGBN_ROWS(1, 4);
+    else if constexpr (!GATED) CGBN_ROWS(2, 16);
+#undef CGBN_ROWS
     return hipGetLastError();
 }
 
