@@ -83,30 +83,11 @@ __device__ __forceinline__ float act_slope(float z, int act)
     return 1.f;
 }
 
-// ---- runs of neighbouring values ----
+// ---- runs of neighbouring values, of which `valid` lie within the row ----
 
-template <typename T, int N> __device__ __forceinline__ void load_run(const T* p, float (&v)[N], int valid, bool whole)
-{
-    constexpr int V = Elem<T>::VEC < N ? Elem<T>::VEC : N;
-    if (whole) {
-        if constexpr (V == Elem<T>::VEC) {
-#pragma unroll
-            for (int k = 0; k < N; k += V) {
-                float t[V];
-                Elem<T>::loadv(p + k, t);
-#pragma unroll
-                for (int e = 0; e < V; ++e) v[k + e] = t[e];
-            }
-        } else if constexpr (N == 4) {                 // 4 bfloat16
-            const uint2 w = *reinterpret_cast<const uint2*>(p);
-            v[0] = bf16_to_f32(w.x & 0xffffu); v[1] = bf16_to_f32(w.x >> 16);
-            v[2] = bf16_to_f32(w.y & 0xffffu); v[3] = bf16_to_f32(w.y >> 16);
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < N; ++k) v[k] = k < valid ? Elem<T>::load1(p + k) : 0.f;
-    }
-}
+// 16 and 8 bytes at any address that a value can have: rows of odd lengths start anywhere, and the memory instructions take that
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 
 // a whole 16 bytes
 template <typename T> __device__ __forceinline__ void unpack_run(const u32x4& w, float (&v)[16 / sizeof(T)])
@@ -115,22 +96,49 @@ template <typename T> __device__ __forceinline__ void unpack_run(const u32x4& w,
     else Elem<T>::unpack(__builtin_bit_cast(f32x4, w), v);
 }
 
-template <typename T, int N> __device__ __forceinline__ void store_run(T* p, const float (&v)[N], int valid, bool whole)
+template <typename T, int N> __device__ __forceinline__ void load_run(const T* p, float (&v)[N], int valid)
 {
-    constexpr int V = Elem<T>::VEC < N ? Elem<T>::VEC : N;
-    if (whole) {
-        if constexpr (V == Elem<T>::VEC) {
+    constexpr int V = Elem<T>::VEC;
+    if (valid >= N && N >= 4) {
+        if constexpr (N % V == 0) {
 #pragma unroll
             for (int k = 0; k < N; k += V) {
                 float t[V];
+                unpack_run<T>(*reinterpret_cast<const u32x4_any*>(p + k), t);
 #pragma unroll
-                for (int e = 0; e < V; ++e) t[e] = v[k + e];
-                Elem<T>::storev(p + k, t, 0);
+                for (int e = 0; e < V; ++e) v[k + e] = t[e];
+            }
+        } else if constexpr (N == 4) {                 // 4 bfloat16
+            const u32x2_any w = *reinterpret_cast<const u32x2_any*>(p);
+            v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xffff0000u);
+            v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = k < valid ? Elem<T>::load1(p + k) : 0.f;
+    }
+}
+
+template <typename T, int N> __device__ __forceinline__ void store_run(T* p, const float (&v)[N], int valid)
+{
+    constexpr int V = Elem<T>::VEC;
+    if (valid >= N && N >= 4) {
+        if constexpr (N % V == 0) {
+#pragma unroll
+            for (int k = 0; k < N; k += V) {
+                u32x4 w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (sizeof(T) == 2) w[e] = f32x2_to_bf16x2(v[k + 2 * e], v[k + 2 * e + 1]);
+                    else w[e] = __float_as_uint(v[k + e]);
+                }
+                *reinterpret_cast<u32x4_any*>(p + k) = w;
             }
         } else if constexpr (N == 4) {
-            uint2 w;
-            w.x = f32x2_to_bf16x2(v[0], v[1]); w.y = f32x2_to_bf16x2(v[2], v[3]);
-            *reinterpret_cast<uint2*>(p) = w;
+            u32x2_any w;
+            w.x = f32x2_to_bf16x2(v[0], v[1]);
+            w.y = f32x2_to_bf16x2(v[2], v[3]);
+            *reinterpret_cast<u32x2_any*>(p) = w;
         }
     } else {
 #pragma unroll
@@ -303,15 +311,15 @@ template <int N> __device__ __forceinline__ void activate(float (&v)[N], int act
 #undef CGBN_ACTIVATE
 }
 
-// v: the products; r: bias and residual.  o: the run's first element in the outputs; whole: it lies within the row and on 16 bytes
+// v: the products; r: bias and residual.  o: the run's first element in the outputs
 template <typename T, int N>
-__device__ __forceinline__ void finish_linear(const GemmArgs& G, float (&v)[N], const float (&r)[N], long long o, int valid, bool whole)
+__device__ __forceinline__ void finish_linear(const GemmArgs& G, float (&v)[N], const float (&r)[N], long long o, int valid)
 {
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] += r[k];
-    if (G.Z[0]) store_run<T, N>(static_cast<T*>(G.Z[0]) + o, v, valid, whole);
+    if (G.Z[0]) store_run<T, N>(static_cast<T*>(G.Z[0]) + o, v, valid);
     activate(v, G.act);
-    store_run<T, N>(static_cast<T*>(G.C[0]) + o, v, valid, whole);
+    store_run<T, N>(static_cast<T*>(G.C[0]) + o, v, valid);
 }
 
 // what finish_linear adds
@@ -320,10 +328,10 @@ template <int N> __device__ __forceinline__ void load_bias(const GemmArgs& G, fl
 #pragma unroll
     for (int k = 0; k < N; ++k) b[k] = G.bias && k < valid ? G.bias[j + k] : 0.f;
 }
-template <typename T, int N> __device__ __forceinline__ void load_extras(const GemmArgs& G, float (&r)[N], const float (&b)[N], long long o, int valid, bool whole)
+template <typename T, int N> __device__ __forceinline__ void load_extras(const GemmArgs& G, float (&r)[N], const float (&b)[N], long long o, int valid)
 {
     if (G.residual) {
-        load_run<T, N>(static_cast<const T*>(G.residual) + o, r, valid, whole);
+        load_run<T, N>(static_cast<const T*>(G.residual) + o, r, valid);
 #pragma unroll
         for (int k = 0; k < N; ++k) r[k] += b[k];
     } else {
@@ -332,17 +340,16 @@ template <typename T, int N> __device__ __forceinline__ void load_extras(const G
     }
 }
 
-template <typename T, int N>
-__device__ __forceinline__ void finish_gated(const GemmArgs& G, float (&g)[N], const float (&u)[N], long long o, int valid, bool whole)
+template <typename T, int N> __device__ __forceinline__ void finish_gated(const GemmArgs& G, float (&g)[N], const float (&u)[N], long long o, int valid)
 {
     if (G.Z[0]) {
-        store_run<T, N>(static_cast<T*>(G.Z[0]) + o, g, valid, whole);
-        store_run<T, N>(static_cast<T*>(G.Z[1]) + o, u, valid, whole);
+        store_run<T, N>(static_cast<T*>(G.Z[0]) + o, g, valid);
+        store_run<T, N>(static_cast<T*>(G.Z[1]) + o, u, valid);
     }
     activate(g, G.act);
 #pragma unroll
     for (int k = 0; k < N; ++k) g[k] *= u[k];
-    store_run<T, N>(static_cast<T*>(G.C[0]) + o, g, valid, whole);
+    store_run<T, N>(static_cast<T*>(G.C[0]) + o, g, valid);
 }
 
 // ---- the product ----
@@ -412,11 +419,11 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
     u32x4 early[EARLY_N];
     if constexpr (EARLY) {
         const int j = j0 + wj * TJ + ((int)threadIdx.x % ELANES) * EV;
-        if (G.residual && G.splits == 1 && G.J % EV == 0) {
+        if (G.residual && G.splits == 1) {
 #pragma unroll
             for (int k = 0; k < EARLY_N; ++k) {
                 const int i = i0 + wi * TI + k * EROWS + (int)threadIdx.x % kWave / ELANES;
-                if (i < G.I && j < G.J) early[k] = *reinterpret_cast<const u32x4*>(static_cast<const T*>(G.residual) + (long long)i * G.ldc + j);
+                if (i < G.I && j + EV <= G.J) early[k] = *reinterpret_cast<const u32x4_any*>(static_cast<const T*>(G.residual) + (long long)i * G.ldc + j);
             }
         }
     }
@@ -512,7 +519,6 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
         static_assert(FX * 16 % (ROWS * U) == 0, "whole rounds");
         constexpr bool EXTRAS = FORM == FORM_NT && !PART() && !GATED;
         const int j = j0 + wj * WIDE + (l % LANES) * N, valid = G.J - j;
-        const bool whole = valid >= N && G.J % N == 0;
         float bias[N];
         if constexpr (EXTRAS) load_bias<N>(G, bias, j, valid);
         constexpr int BATCHES = FX * 16 / (ROWS * U);
@@ -524,12 +530,12 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
                 for (int u = 0; u < U; ++u) {
                     const int i = i_first + r0 + u * ROWS;
                     if (i >= G.I || valid <= 0) continue;
-                    if (EARLY && G.residual && G.J % EV == 0) {
+                    if (EARLY && G.residual && valid >= N) {
                         if constexpr (EARLY) unpack_run<T>(early[(x0 * 16 + b0) / ROWS + u], extra[u]);
 #pragma unroll
                         for (int k = 0; k < N; ++k) extra[u][k] += bias[k];
                     } else {
-                        load_extras<T, N>(G, extra[u], bias, (long long)i * G.ldc + j, valid, whole);
+                        load_extras<T, N>(G, extra[u], bias, (long long)i * G.ldc + j, valid);
                     }
                 }
             }
@@ -551,14 +557,14 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
                 const long long o = (long long)i * G.ldc + j;
                 if constexpr (PART()) {
                     float* p = G.part + ((long long)(GATED ? 2 * w.split : w.split * G.batch + w.z) * G.I + i) * G.J + j;
-                    store_run<float, N>(p, v, valid, whole);
-                    if constexpr (GATED) store_run<float, N>(p + (long long)G.I * G.J, up, valid, whole);
+                    store_run<float, N>(p, v, valid);
+                    if constexpr (GATED) store_run<float, N>(p + (long long)G.I * G.J, up, valid);
                 } else if constexpr (GATED) {
-                    finish_gated<T, N>(G, v, up, o, valid, whole);
+                    finish_gated<T, N>(G, v, up, o, valid);
                 } else if constexpr (FORM == FORM_NT) {
-                    finish_linear<T, N>(G, v, extra[u], o, valid, whole);
+                    finish_linear<T, N>(G, v, extra[u], o, valid);
                 } else {
-                    store_run<T, N>(static_cast<T*>(G.C[w.z]) + o, v, valid, whole);
+                    store_run<T, N>(static_cast<T*>(G.C[w.z]) + o, v, valid);
                 }
             }
         };
@@ -601,39 +607,62 @@ __global__ __launch_bounds__(WI * WJ * kWave) void gemm_two(const GemmArgs X, co
     else tile_product<T, FORM_TN, false, BI, BJ, WI, WJ>(W, lds, (int)blockIdx.x - nx, (int)gridDim.x - nx);
 }
 
-// Partial sums of a split reduction, added in split order, then the epilogue.  N values a thread (4 where J allows whole vectors).
+// Partial sums of a split reduction, added in a fixed order, then the epilogue.  N values a thread (4 where J allows whole vectors).
+// Where there are few values and many splits, `lanes` threads (a power of two) share a value's splits: 128 x 512 values of 120
+// splits took 31 us with one thread each, 8 with sixteen.
 template <typename T, int FORM, bool GATED, int N>
-__global__ __launch_bounds__(kThreads) void gemm_join(const GemmArgs G)
+__global__ __launch_bounds__(kThreads) void gemm_join(const GemmArgs G, int lanes)
 {
-    const long long plane = (long long)G.I * G.J, planes = GATED ? 2 : G.batch;
-    const long long e = ((long long)blockIdx.x * kThreads + threadIdx.x) * N;
-    const long long total = GATED ? plane : plane * planes;
-    if (e >= total) return;
-    const float* p = G.part + e;
-    float v[N], u[N];
+    constexpr int P = GATED ? 2 : 1, U = 4;
+    __shared__ float red[kThreads * N * P];
+    const long long plane = (long long)G.I * G.J, planes = GATED ? 2 : G.batch, total = GATED ? plane : plane * planes;
+    const int across = kThreads / lanes, lane = (int)threadIdx.x / across, at = (int)threadIdx.x % across;
+    const long long e = ((long long)blockIdx.x * across + at) * N;
+    float v[P][N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = u[k] = 0.f;
-    for (int s = 0; s < G.splits; ++s, p += plane * planes) {
-        float t[N];
-        load_run<float, N>(p, t, N, N == 4);
+    for (int p = 0; p < P; ++p)
 #pragma unroll
-        for (int k = 0; k < N; ++k) v[k] += t[k];
-        if constexpr (GATED) {
-            load_run<float, N>(p + plane, t, N, N == 4);
+        for (int k = 0; k < N; ++k) v[p][k] = 0.f;
+    if (e < total) {
+        for (int s0 = lane; s0 < G.splits; s0 += U * lanes) {
+            float t[U][P][N];
 #pragma unroll
-            for (int k = 0; k < N; ++k) u[k] += t[k];
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+                    load_run<float, N>(G.part + e + (s0 + u * lanes) * plane * planes + p * plane, t[u][p], s0 + u * lanes < G.splits ? N : 0);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int k = 0; k < N; ++k) v[p][k] += t[u][p][k];
         }
     }
+    if (lanes > 1) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int k = 0; k < N; ++k) red[(p * N + k) * kThreads + threadIdx.x] = v[p][k];
+        __syncthreads();
+        if (lane != 0) return;
+        for (int o = 1; o < lanes; ++o)
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int k = 0; k < N; ++k) v[p][k] += red[(p * N + k) * kThreads + o * across + at];
+    }
+    if (e >= total) return;
     const long long z = GATED ? 0 : e / plane, o = e - z * plane;        // (outputs are dense)
     if constexpr (GATED) {
-        finish_gated<T, N>(G, v, u, o, N, N == 4);
+        finish_gated<T, N>(G, v[0], v[1], o, N);
     } else if constexpr (FORM == FORM_NT) {
-        float bias[N];
+        float bias[N], extra[N];
         load_bias<N>(G, bias, (int)(o % G.J), N);
-        load_extras<T, N>(G, u, bias, o, N, N == 4);
-        finish_linear<T, N>(G, v, u, o, N, N == 4);
+        load_extras<T, N>(G, extra, bias, o, N);
+        finish_linear<T, N>(G, v[0], extra, o, N);
     } else {
-        store_run<T, N>(static_cast<T*>(G.C[z]) + o, v, N, N == 4);
+        store_run<T, N>(static_cast<T*>(G.C[z]) + o, v[0], N);
     }
 }
 

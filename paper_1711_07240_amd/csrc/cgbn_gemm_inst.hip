@@ -16,11 +16,13 @@ unsigned groups_of(const GemmArgs& G) { return (unsigned)((long long)G.ti * G.tj
 template <typename T, int FORM, bool GATED> hipError_t join(const GemmArgs& G, hipStream_t st)
 {
     if (G.splits == 1) return hipSuccess;
-    const long long values = (long long)G.I * G.J * (GATED ? 1 : G.batch);
-    if (G.J % 4 == 0)
-        hipLaunchKernelGGL((gemm_join<T, FORM, GATED, 4>), dim3((unsigned)((values / 4 + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, G);
-    else
-        hipLaunchKernelGGL((gemm_join<T, FORM, GATED, 1>), dim3((unsigned)((values + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, G);
+    const int n = G.J % 4 == 0 ? 4 : 1;
+    const long long threads = (long long)G.I * G.J * (GATED ? 1 : G.batch) / n;
+    int lanes = 1;
+    while (lanes < 16 && lanes * 4 <= G.splits && threads * lanes < 256 * 1024) lanes *= 2;
+    const dim3 grid((unsigned)((threads * lanes + kThreads - 1) / kThreads));
+    if (n == 4) hipLaunchKernelGGL((gemm_join<T, FORM, GATED, 4>), grid, dim3(kThreads), 0, st, G, lanes);
+    else hipLaunchKernelGGL((gemm_join<T, FORM, GATED, 1>), grid, dim3(kThreads), 0, st, G, lanes);
     return hipGetLastError();
 }
 

@@ -21,8 +21,8 @@ struct GemmPlan {
 };
 
 // The shapes' rates, in operations a second of the whole device with the compute units full: bfloat16 as measured on
-// 8192 x 8192 x 8192; float runs at the matrix instructions' rate with any of them.  Where a compute unit holds few wavefronts,
-// their waits show: the fraction of the rate with one and with two workgroups a unit; `start`, their prologue's time.
+// 8192 x 8192 x 8192; float runs at the matrix instructions' rate with any of them.  Where a vector unit holds few wavefronts,
+// their waits show: the fraction of the rate with one and with two of them; `start`, their prologue's time.
 struct TileShape {
     int bi, bj, waves;
     double rate, one, two, start;
@@ -30,7 +30,7 @@ struct TileShape {
 inline const TileShape& tile_shape(int s)
 {
     static const TileShape shapes[] = {
-        {256, 256, 4, 1450e12, 1., 1., 2.5e-6}, {128, 128, 4, 1170e12, 0.65, 1., 0.8e-6}, {128, 64, 4, 900e12, 0.5, 0.8, 0.5e-6}, {64, 64, 2, 690e12, 0.3, 0.55, 0.3e-6}};
+        {256, 256, 4, 1450e12, 1., 1., 7e-6}, {128, 128, 4, 1170e12, 0.65, 1., 0.8e-6}, {128, 64, 4, 900e12, 0.5, 0.8, 0.5e-6}, {64, 64, 2, 690e12, 0.6, 0.8, 0.3e-6}};
     return shapes[s];
 }
 constexpr int kTileShapes = 4;
@@ -45,8 +45,10 @@ inline bool plan_with(int shape, long long want, int elem, bool gated, long long
     const long long ti = (I + t.bi - 1) / t.bi, tj = (J + bj - 1) / bj;
     if (part > 1e9 || (double)ti * tj * splits * batch > 1e9) return false;
     *p = GemmPlan{shape, (int)ti, (int)tj, (int)splits, (int)per, (size_t)part, (double)ti * tj * splits * batch, 0, 0};
-    const double in_a_unit = p->groups / 256;
-    double rate = elem == 2 ? t.rate * (in_a_unit <= 1 ? t.one : in_a_unit <= 2 ? t.two : 1.) : 139e12 * (in_a_unit <= 1 ? t.waves / 4. : 1.);
+    // wavefronts of a compute unit's workgroups, dealt over its four vector units: the busiest has `deep` of them
+    const double waves = (double)((long long)((p->groups + 255) / 256)) * t.waves / 4, deep = (double)(long long)(waves + 0.75);
+    const double fill = waves / deep;
+    const double rate = elem == 2 ? t.rate * fill * (deep <= 1 ? t.one : deep <= 2 ? t.two : 1.) : 139e12 * fill * (deep <= 1 ? 0.86 : 1.);
     // (what a workgroup does besides: its first loads' way, and its rows of A, which it shares with the tiles beside it, and its
     // results, at the rate of memory)
     const double bytes = (double)t.bi * per * 128 / (double)(tj < 8 ? tj : 8) + (double)t.bi * bj * (gated ? 2 : 1) * (splits > 1 ? 4 : elem * 1.25);

@@ -11,27 +11,24 @@
 
 namespace cgbn {
 
-// 16 bytes of an operand's row, zero beyond `left` elements; WHOLE: rows start on 16 bytes and hold whole chunks
-template <typename T, bool WHOLE> __device__ __forceinline__ u32x4 row_chunk(const T* p, int left)
+// 16 bytes of an operand's row, zero beyond `left` elements
+template <typename T> __device__ __forceinline__ u32x4 row_chunk(const T* p, int left)
 {
     constexpr int E = 16 / (int)sizeof(T);
-    if constexpr (WHOLE) {
-        return left > 0 ? *reinterpret_cast<const u32x4*>(p) : u32x4{0, 0, 0, 0};
-    } else {
-        u32x4 v = {0, 0, 0, 0};
+    if (left >= E) return *reinterpret_cast<const u32x4_any*>(p);
+    u32x4 v = {0, 0, 0, 0};
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            if (e < left) {
-                if constexpr (sizeof(T) == 2) v[e / 2] |= (uint32_t)p[e].bits << (16 * (e & 1));
-                else v[e] = __float_as_uint(p[e]);
-            }
+    for (int e = 0; e < E; ++e) {
+        if (e < left) {
+            if constexpr (sizeof(T) == 2) v[e / 2] |= (uint32_t)p[e].bits << (16 * (e & 1));
+            else v[e] = __float_as_uint(p[e]);
         }
-        return v;
     }
+    return v;
 }
 
 // FM: 16-row blocks of x; NW: wavefronts
-template <typename T, bool GATED, bool WHOLE, int FM, int NW>
+template <typename T, bool GATED, int FM, int NW>
 __global__ __launch_bounds__(NW * kWave) void gemm_rows(const GemmArgs G)
 {
     constexpr int E = 16 / (int)sizeof(T), STEP = 8 * E, P = GATED ? 2 : 1, U = FM == 1 && !GATED ? 4 : 2;
@@ -59,9 +56,9 @@ __global__ __launch_bounds__(NW * kWave) void gemm_rows(const GemmArgs G)
             for (int h = 0; h < 2; ++h) {
                 const int r = (s + u * NW) * STEP + h * 4 * E;
 #pragma unroll
-                for (int p = 0; p < P; ++p) w[u][p][h] = row_chunk<T, WHOLE>(pw[p] + r, E);
+                for (int p = 0; p < P; ++p) w[u][p][h] = row_chunk<T>(pw[p] + r, E);
 #pragma unroll
-                for (int m = 0; m < FM; ++m) x[u][m][h] = row_chunk<T, WHOLE>(px[m] + r, E);
+                for (int m = 0; m < FM; ++m) x[u][m][h] = row_chunk<T>(px[m] + r, E);
             }
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -78,10 +75,10 @@ __global__ __launch_bounds__(NW * kWave) void gemm_rows(const GemmArgs G)
             const int r = s * STEP + h * 4 * E, left = G.R - r - q * E;
             u32x4 x[FM];
 #pragma unroll
-            for (int m = 0; m < FM; ++m) x[m] = row_chunk<T, WHOLE>(px[m] + r, left);
+            for (int m = 0; m < FM; ++m) x[m] = row_chunk<T>(px[m] + r, left);
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const u32x4 w = row_chunk<T, WHOLE>(pw[p] + r, left);
+                const u32x4 w = row_chunk<T>(pw[p] + r, left);
 #pragma unroll
                 for (int m = 0; m < FM; ++m) acc[p][m] = multiply<T>(w, x[m], acc[p][m]);
             }
@@ -95,13 +92,12 @@ __global__ __launch_bounds__(NW * kWave) void gemm_rows(const GemmArgs G)
     if (wave >= FM) return;
     const int m = wave, i = i0 + m * 16 + t, j = j0 + q * 4;
     if (i >= G.I || j >= G.J) return;
-    const bool whole = j + 4 <= G.J && G.J % 4 == 0;
     const long long o = (long long)i * G.ldc + j;
     float extra[4];
     if constexpr (!GATED) {
         float bias[4];
         load_bias<4>(G, bias, j, G.J - j);
-        load_extras<T, 4>(G, extra, bias, o, G.J - j, whole);
+        load_extras<T, 4>(G, extra, bias, o, G.J - j);
     }
     float v[P][4];
 #pragma unroll
@@ -112,8 +108,8 @@ __global__ __launch_bounds__(NW * kWave) void gemm_rows(const GemmArgs G)
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[p][k] = a[k];
     }
-    if constexpr (GATED) finish_gated<T, 4>(G, v[0], v[1], o, G.J - j, whole);
-    else finish_linear<T, 4>(G, v[0], extra, o, G.J - j, whole);
+    if constexpr (GATED) finish_gated<T, 4>(G, v[0], v[1], o, G.J - j);
+    else finish_linear<T, 4>(G, v[0], extra, o, G.J - j);
 }
 
 }  // namespace cgbn

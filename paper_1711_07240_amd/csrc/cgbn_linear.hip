@@ -23,8 +23,8 @@ template <typename T> __global__ __launch_bounds__(kThreads) void pad_rows(const
     const long long r = id / chunks;
     const int c = (int)(id - r * chunks) * E;
     float v[E];
-    load_run<T, E>(src + r * n + c, v, n - c, false);
-    store_run<T, E>(dst + r * np + c, v, E, true);
+    load_run<T, E>(src + r * n + c, v, n - c);
+    store_run<T, E>(dst + r * np + c, v, E);
 }
 
 struct DzArgs {
@@ -38,7 +38,7 @@ struct DzArgs {
 
 // dz = dy * act'(saved), and its column sums.  Memory bound: one read of dy and saved, one write of dz.  A thread stays in
 // one column vector and walks rows; its sums are of at most rows * tw / 256 values, in float.
-template <typename T, bool WHOLE> __global__ __launch_bounds__(kThreads) void linear_dz(const DzArgs A)
+template <typename T> __global__ __launch_bounds__(kThreads) void linear_dz(const DzArgs A)
 {
     constexpr int E = 16 / (int)sizeof(T);
     __shared__ float red[kThreads * E];
@@ -52,10 +52,10 @@ template <typename T, bool WHOLE> __global__ __launch_bounds__(kThreads) void li
     if (in) {
         for (long long r = r0 + first; r < r1; r += stride) {
             float g[E];
-            load_run<T, E>(static_cast<const T*>(A.dy) + r * A.N + c, g, valid, WHOLE);
+            load_run<T, E>(static_cast<const T*>(A.dy) + r * A.N + c, g, valid);
             if (A.saved) {
                 float z[E];
-                load_run<T, E>(static_cast<const T*>(A.saved) + r * A.N + c, z, valid, WHOLE);
+                load_run<T, E>(static_cast<const T*>(A.saved) + r * A.N + c, z, valid);
                 // (where ReLU passes nothing dz is zero, not dy * 0: an infinity there does not become NaN)
 #pragma unroll
                 for (int e = 0; e < E; ++e) g[e] = A.act == ACT_RELU ? (z[e] > 0.f ? g[e] : 0.f) : g[e] * act_slope(z[e], A.act);
@@ -63,13 +63,10 @@ template <typename T, bool WHOLE> __global__ __launch_bounds__(kThreads) void li
 #pragma unroll
             for (int e = 0; e < E; ++e) sum[e] += g[e];
             if (A.dz) {
-                if constexpr (!WHOLE) {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) g[e] = e < valid ? g[e] : 0.f;
-                }
-                store_run<T, E>(static_cast<T*>(A.dz) + r * A.ld + c, g, E, true);
+                // (beyond the row the filling is zero: what was loaded there is)
+                store_run<T, E>(static_cast<T*>(A.dz) + r * A.ld + c, g, E);
             }
-            if (A.dresidual) store_run<T, E>(static_cast<T*>(A.dresidual) + r * A.N + c, g, valid, WHOLE);
+            if (A.dresidual) store_run<T, E>(static_cast<T*>(A.dresidual) + r * A.N + c, g, valid);
         }
     }
     if (!A.part) return;
@@ -93,7 +90,7 @@ struct GateArgs {
 
 // dg = dh * up * act'(gate), du = dh * act(gate), rounded to the operands' type for the products that follow (as they would be
 // had they been tensors of the layer): memory bound, three reads and two writes.
-template <typename T, bool WHOLE> __global__ __launch_bounds__(kThreads) void gated_dz(const GateArgs A)
+template <typename T> __global__ __launch_bounds__(kThreads) void gated_dz(const GateArgs A)
 {
     constexpr int E = 16 / (int)sizeof(T);
     const int chunks = A.ld / E;
@@ -103,18 +100,17 @@ template <typename T, bool WHOLE> __global__ __launch_bounds__(kThreads) void ga
         const int c = (int)(id - r * chunks) * E, valid = A.F - c;
         const long long o = r * A.F + c;
         float h[E], g[E], u[E];
-        load_run<T, E>(static_cast<const T*>(A.dh) + o, h, valid, WHOLE);
-        load_run<T, E>(static_cast<const T*>(A.gate) + o, g, valid, WHOLE);
-        load_run<T, E>(static_cast<const T*>(A.up) + o, u, valid, WHOLE);
+        load_run<T, E>(static_cast<const T*>(A.dh) + o, h, valid);
+        load_run<T, E>(static_cast<const T*>(A.gate) + o, g, valid);
+        load_run<T, E>(static_cast<const T*>(A.up) + o, u, valid);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const float slope = act_slope(g[e], A.act), a = act_apply(g[e], A.act);
             g[e] = A.act == ACT_RELU && !(g[e] > 0.f) ? 0.f : h[e] * u[e] * slope;
             u[e] = h[e] * a;
-            if (!WHOLE && e >= valid) g[e] = u[e] = 0.f;
         }
-        store_run<T, E>(static_cast<T*>(A.dg) + r * A.ld + c, g, E, true);
-        store_run<T, E>(static_cast<T*>(A.du) + r * A.ld + c, u, E, true);
+        store_run<T, E>(static_cast<T*>(A.dg) + r * A.ld + c, g, E);
+        store_run<T, E>(static_cast<T*>(A.du) + r * A.ld + c, u, E);
     }
 }
 
@@ -220,7 +216,7 @@ BackwardPlan plan_backward(long long M, int N, int K, int dtype, bool gated)
     p.tw = 1;
     while (p.tw < 64 && p.tw < vecs) p.tw *= 2;
     const long long across = (vecs + p.tw - 1) / p.tw, least = 8ll * (kThreads / p.tw);
-    long long blocks = 2048 / across > 1 ? 2048 / across : 1;
+    long long blocks = 1024 / across > 1 ? 1024 / across : 1;
     if (blocks > (M + least - 1) / least) blocks = (M + least - 1) / least;
     if (blocks < 1) blocks = 1;
     p.sum_rows = (int)((M + blocks - 1) / blocks);
@@ -245,13 +241,13 @@ template <typename T> hipError_t pad(const void* src, void* dst, long long rows,
     return hipGetLastError();
 }
 
-template <typename T, bool GATED, bool WHOLE> hipError_t launch_rows(const GemmArgs& G, hipStream_t st)
+template <typename T, bool GATED> hipError_t launch_rows(const GemmArgs& G, hipStream_t st)
 {
     const dim3 grid((unsigned)((G.J + 15) / 16));
     // 16 wavefronts, each with all of its loads in flight at once or twice, where there are steps for them: 8.0 against 8.5 us with 8 of
     // them (one row, 4096 x 4096); with few steps they only wait for each other: 3.3 with 4 against 3.6 us (1024 x 1024)
     const bool many = (long long)G.R * (int)sizeof(T) >= 32 * 128;
-#define CGBN_ROWS(FM_, NW_) hipLaunchKernelGGL((gemm_rows<T, GATED, WHOLE, FM_, NW_>), grid, dim3(NW_ * kWave), 0, st, G)
+#define CGBN_ROWS(FM_, NW_) hipLaunchKernelGGL((gemm_rows<T, GATED, FM_, NW_>), grid, dim3(NW_ * kWave), 0, st, G)
     if (G.I <= 16 && many) CGBN_ROWS(1, 16);
     else if (G.I <= 16) CGBN_ROWS(1, 4);
     else if constexpr (!GATED) CGBN_ROWS(2, 16);
@@ -268,7 +264,7 @@ cgbn_status forward(GemmArgs G, const ForwardPlan& p, char* ws, hipStream_t st)
     G.lda = G.ldb = K;
     G.ldc = G.J;
     if (p.rows) {
-        CGBN_HIP((W.odd(K) ? launch_rows<T, GATED, false>(G, st) : launch_rows<T, GATED, true>(G, st)));
+        CGBN_HIP((launch_rows<T, GATED>(G, st)));
         return CGBN_OK;
     }
     if (W.odd(K)) {
@@ -382,8 +378,7 @@ cgbn_status linear_backward(const void* dy, const void* x, const void* w, const 
         A.tw = p.tw; A.rows = p.sum_rows;
         const int vecs = np / W.E;
         const dim3 grid((unsigned)((vecs + p.tw - 1) / p.tw), (unsigned)p.sum_blocks);
-        if (W.odd(N)) hipLaunchKernelGGL((linear_dz<T, false>), grid, dim3(kThreads), 0, st, A);
-        else hipLaunchKernelGGL((linear_dz<T, true>), grid, dim3(kThreads), 0, st, A);
+        hipLaunchKernelGGL(linear_dz<T>, grid, dim3(kThreads), 0, st, A);
         CGBN_HIP(hipGetLastError());
         if (dbias) {
             hipLaunchKernelGGL(column_sums, dim3((unsigned)((N + 15) / 16)), dim3(kSumThreads), 0, st, A.part, p.sum_blocks, N, N, dbias, N, nullptr);
@@ -412,8 +407,7 @@ cgbn_status gated_backward(const void* dh, const void* x, const void* wg, const 
     const GateArgs A = {dh, gate, up, dg, du, M, F, fp, act};
     const long long ids = M * (fp / W.E), groups = (ids + kThreads - 1) / kThreads;
     const dim3 grid((unsigned)(groups < 8192 ? groups : 8192));
-    if (W.odd(F)) hipLaunchKernelGGL((gated_dz<T, false>), grid, dim3(kThreads), 0, st, A);
-    else hipLaunchKernelGGL((gated_dz<T, true>), grid, dim3(kThreads), 0, st, A);
+    hipLaunchKernelGGL(gated_dz<T>, grid, dim3(kThreads), 0, st, A);
     CGBN_HIP(hipGetLastError());
     const void *dzs[2] = {dg, du}, *ws_[2] = {wg, wu};
     void* dws[2] = {dwg, dwu};
