@@ -276,6 +276,21 @@ template <typename T> __device__ __forceinline__ f32x4 multiply(const u32x4& a, 
     }
 }
 
+// Float values as sums of three bfloat16, which is exact: 24 bits are 8 and 8 and 8, each cut off and the rest, without rounding, kept.
+// (Parts below the smallest normal number are lost: values under 1e-33 have fewer than 24 bits.)  8 values of a lane, from two chunks.
+__device__ __forceinline__ void split_float(const u32x4& lo, const u32x4& hi, u32x4 (&part)[3])
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t x = k < 2 ? lo[2 * k] : hi[2 * k - 4], y = k < 2 ? lo[2 * k + 1] : hi[2 * k - 3];
+        const float xr = __uint_as_float(x) - __uint_as_float(x & 0xffff0000u), yr = __uint_as_float(y) - __uint_as_float(y & 0xffff0000u);
+        const float xs = xr - __uint_as_float(__float_as_uint(xr) & 0xffff0000u), ys = yr - __uint_as_float(__float_as_uint(yr) & 0xffff0000u);
+        part[0][k] = __builtin_amdgcn_perm(y, x, 0x07060302);                                            // the upper halves of both
+        part[1][k] = __builtin_amdgcn_perm(__float_as_uint(yr), __float_as_uint(xr), 0x07060302);
+        part[2][k] = __builtin_amdgcn_perm(__float_as_uint(ys), __float_as_uint(xs), 0x07060302);
+    }
+}
+
 // Which tile a workgroup takes.  Consecutive workgroups go to the 8 dies in turn, so each die is given a run of consecutive
 // work of its own; within it tiles go in blocks of 8 rows of tiles, column by column, so that the ones in flight at a time share operands in
 // the die's L2.
@@ -355,6 +370,8 @@ template <typename T, int N> __device__ __forceinline__ void finish_gated(const 
 // ---- the product ----
 
 constexpr int tile_lds(int bi, int bj) { return 2 * (bi + bj) * 128; }
+// wavefronts that a vector unit must have registers for, by the values that one accumulates
+constexpr int tile_waves(int values) { return values > 64 * 64 ? 1 : 2; }
 
 // One workgroup's share, number `id` of `n`.
 template <typename T, int FORM, bool GATED, int BI, int BJ, int WI, int WJ>
@@ -434,75 +451,119 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
 #pragma unroll
         for (int y = 0; y < FJ; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    // A step is multiplied in two halves (ks), row of fragments by row.  What a half needs is read from LDS during the half before:
-    // B's fragments into a second set of registers, A's into the row just multiplied.  Where the step's own reads end, one or two
-    // rows into the second half, the workgroup meets; the loads of the step after next are issued between the rows that
-    // follow, and have a whole step to arrive.
-    constexpr int LAG = FI >= 4 ? 2 : 1;
-    u32x4 fa[FI], fb[2][FJ];
-    auto read_a = [&](int buf, int ks, int x) { fa[x] = fragment<T, ACOLS, BI>(tile + buf * STAGE, abase, x, ks); };
-    auto read_b = [&](int buf, int ks) {
-#pragma unroll
-        for (int y = 0; y < FJ; ++y) fb[ks][y] = fragment<T, BCOLS, BJ>(tile + buf * STAGE + OA::BYTES, bbase + (GATED && y >= FJ / 2 ? BJ / 2 : 0), GATED ? y % (FJ / 2) : y, ks);
-    };
-    auto multiply_row = [&](int ks, int x) {
-#pragma unroll
-        for (int y = 0; y < FJ; ++y) acc[x][y] = multiply<T>(fb[ks][y], fa[x], acc[x][y]);
-    };
-    if (first < last) {
-        stage(0);
-        dma_wait_and_meet();
-        if (first + 1 < last) stage(1);
-        read_b(0, 0);
-#pragma unroll
-        for (int x = 0; x < FI; ++x) read_a(0, 0, x);
-    }
-    // NEXT: another step follows; MORE: and yet another, whose loads start here; WHOLE: it is a whole one
-    auto step = [&](int buf, auto NEXT, auto MORE, auto WHOLE) {
-        read_b(buf, 1);
-#pragma unroll
-        for (int x = 0; x < FI; ++x) {
-            multiply_row(0, x);
-            read_a(buf, 1, x);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-#pragma unroll
-        for (int x = 0; x < LAG; ++x) multiply_row(1, x);
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (NEXT()) {
-            dma_wait_and_meet();                // the next step is in LDS, and everyone has read this one
-            read_b(buf ^ 1, 0);
-#pragma unroll
-            for (int x = 0; x < LAG; ++x) read_a(buf ^ 1, 0, x);
-        }
-#pragma unroll
-        for (int x = LAG; x < FI; ++x) {
-            if constexpr (MORE()) {
-#pragma unroll
-                for (int p = (x - LAG) * PASSES / (FI - LAG); p < (x - LAG + 1) * PASSES / (FI - LAG); ++p) pass(buf, p, WHOLE());
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            multiply_row(1, x);
-            if constexpr (NEXT()) read_a(buf ^ 1, 0, x);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        if constexpr (MORE()) staged();
-    };
     typedef std::integral_constant<bool, true> yes;
     typedef std::integral_constant<bool, false> no;
-    int buf = 0, s = first;
-    while (s + 2 < last) {
-        for (; s + 2 < last && left >= OA::STEP; ++s, buf ^= 1) step(buf, yes(), yes(), yes());
-        if (s + 2 < last) {                     // the end of a segment
-            step(buf, yes(), yes(), no());
-            ++s, buf ^= 1;
+    if constexpr (sizeof(T) == 4) {
+        // Float: each value as three bfloat16 (split_float), of whose nine products the six that count run on the bfloat16
+        // instructions, 16 times the rate of those for float.  What is dropped is below 2^-23 of a product, less than its rounding.
+        // The leading products have accumulators of their own: where an infinity makes one of those infinite, the others, in which it may
+        // have met a zero, have no say.
+        f32x4 rest[FI][FJ];
+#pragma unroll
+        for (int x = 0; x < FI; ++x)
+#pragma unroll
+            for (int y = 0; y < FJ; ++y) rest[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (first < last) stage(0);
+        for (int s = first, buf = 0; s < last; ++s, buf ^= 1) {
+            dma_wait_and_meet();
+            if (s + 1 < last) stage(buf ^ 1);
+            const lds_char* const ta = tile + buf * STAGE;
+            u32x4 pb[FJ][3];
+#pragma unroll
+            for (int y = 0; y < FJ; ++y) {
+                const int at = bbase + (GATED && y >= FJ / 2 ? BJ / 2 : 0), f = GATED ? y % (FJ / 2) : y;
+                split_float(fragment<T, BCOLS, BJ>(ta + OA::BYTES, at, f, 0), fragment<T, BCOLS, BJ>(ta + OA::BYTES, at, f, 1), pb[y]);
+            }
+#pragma unroll
+            for (int x = 0; x < FI; ++x) {
+                u32x4 pa[3];
+                split_float(fragment<T, ACOLS, BI>(ta, abase, x, 0), fragment<T, ACOLS, BI>(ta, abase, x, 1), pa);
+#pragma unroll
+                for (int k = 0; k < 6; ++k) {
+                    constexpr int ka[6] = {0, 2, 1, 0, 1, 0}, kb[6] = {2, 0, 1, 1, 0, 0};          // small ones first
+#pragma unroll
+                    for (int y = 0; y < FJ; ++y) {
+                        f32x4& to = k == 5 ? acc[x][y] : rest[x][y];
+                        to = multiply<bf16_t>(pb[y][kb[k]], pa[ka[k]], to);
+                    }
+                }
+            }
         }
+#pragma unroll
+        for (int x = 0; x < FI; ++x)
+#pragma unroll
+            for (int y = 0; y < FJ; ++y)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc[x][y][k] = fabsf(acc[x][y][k]) < INFINITY ? acc[x][y][k] + rest[x][y][k] : acc[x][y][k];
+    } else {
+        // A step is multiplied in two halves (ks), row of fragments by row.  What a half needs is read from LDS during the half before:
+        // B's fragments into a second set of registers, A's into the row just multiplied.  Where the step's own reads end, one or two
+        // rows into the second half, the workgroup meets; the loads of the step after next are issued between the rows that
+        // follow, and have a whole step to arrive.
+        constexpr int LAG = FI >= 4 ? 2 : 1;
+        u32x4 fa[FI], fb[2][FJ];
+        auto read_a = [&](int buf, int ks, int x) { fa[x] = fragment<T, ACOLS, BI>(tile + buf * STAGE, abase, x, ks); };
+        auto read_b = [&](int buf, int ks) {
+#pragma unroll
+            for (int y = 0; y < FJ; ++y) fb[ks][y] = fragment<T, BCOLS, BJ>(tile + buf * STAGE + OA::BYTES, bbase + (GATED && y >= FJ / 2 ? BJ / 2 : 0), GATED ? y % (FJ / 2) : y, ks);
+        };
+        auto multiply_row = [&](int ks, int x) {
+#pragma unroll
+            for (int y = 0; y < FJ; ++y) acc[x][y] = multiply<T>(fb[ks][y], fa[x], acc[x][y]);
+        };
+        if (first < last) {
+            stage(0);
+            dma_wait_and_meet();
+            if (first + 1 < last) stage(1);
+            read_b(0, 0);
+#pragma unroll
+            for (int x = 0; x < FI; ++x) read_a(0, 0, x);
+        }
+        // NEXT: another step follows; MORE: and yet another, whose loads start here; WHOLE: it is a whole one
+        auto step = [&](int buf, auto NEXT, auto MORE, auto WHOLE) {
+            read_b(buf, 1);
+#pragma unroll
+            for (int x = 0; x < FI; ++x) {
+                multiply_row(0, x);
+                read_a(buf, 1, x);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int x = 0; x < LAG; ++x) multiply_row(1, x);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (NEXT()) {
+                dma_wait_and_meet();                // the next step is in LDS, and everyone has read this one
+                read_b(buf ^ 1, 0);
+#pragma unroll
+                for (int x = 0; x < LAG; ++x) read_a(buf ^ 1, 0, x);
+            }
+#pragma unroll
+            for (int x = LAG; x < FI; ++x) {
+                if constexpr (MORE()) {
+#pragma unroll
+                    for (int p = (x - LAG) * PASSES / (FI - LAG); p < (x - LAG + 1) * PASSES / (FI - LAG); ++p) pass(buf, p, WHOLE());
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                multiply_row(1, x);
+                if constexpr (NEXT()) read_a(buf ^ 1, 0, x);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if constexpr (MORE()) staged();
+        };
+        int buf = 0, s = first;
+        while (s + 2 < last) {
+            for (; s + 2 < last && left >= OA::STEP; ++s, buf ^= 1) step(buf, yes(), yes(), yes());
+            if (s + 2 < last) {                     // the end of a segment
+                step(buf, yes(), yes(), no());
+                ++s, buf ^= 1;
+            }
+        }
+        if (s + 1 < last) {
+            step(buf, yes(), no(), no());
+            buf ^= 1;
+        }
+        if (first < last) step(buf, no(), no(), no());
     }
-    if (s + 1 < last) {
-        step(buf, yes(), no(), no());
-        buf ^= 1;
-    }
-    if (first < last) step(buf, no(), no(), no());
 
     // The accumulators go to memory through LDS, each wavefront through its own part of it, in as many rounds as that takes: a lane
     // holds 4 columns of one row of each fragment, and would fetch and store 16 rows of 32 bytes; from LDS it takes a run
@@ -591,7 +652,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
 }
 
 template <typename T, int FORM, bool GATED, int BI, int BJ, int WI, int WJ>
-__global__ __launch_bounds__(WI * WJ * kWave) void gemm_tile(const GemmArgs G)
+__global__ __launch_bounds__(WI * WJ * kWave, tile_waves(BI * BJ / (WI * WJ))) void gemm_tile(const GemmArgs G)
 {
     __shared__ __attribute__((aligned(1024))) char lds[tile_lds(BI, BJ)];
     tile_product<T, FORM, GATED, BI, BJ, WI, WJ>(G, lds, (int)blockIdx.x, (int)gridDim.x);
@@ -600,7 +661,7 @@ __global__ __launch_bounds__(WI * WJ * kWave) void gemm_tile(const GemmArgs G)
 // dx = dz W and dW = dz^T x in one launch: neither needs the other, and the second's workgroups fill the compute units that
 // the first's last round leaves idle.
 template <typename T, int BI, int BJ, int WI, int WJ>
-__global__ __launch_bounds__(WI * WJ * kWave) void gemm_two(const GemmArgs X, const GemmArgs W, int nx)
+__global__ __launch_bounds__(WI * WJ * kWave, tile_waves(BI * BJ / (WI * WJ))) void gemm_two(const GemmArgs X, const GemmArgs W, int nx)
 {
     __shared__ __attribute__((aligned(1024))) char lds[tile_lds(BI, BJ)];
     if ((int)blockIdx.x < nx) tile_product<T, FORM_NN, false, BI, BJ, WI, WJ>(X, lds, (int)blockIdx.x, nx);

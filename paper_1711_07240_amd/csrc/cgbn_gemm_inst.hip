@@ -31,10 +31,20 @@ template <typename T, int FORM, bool GATED> hipError_t launch_one(const GemmPlan
     take(p, &G);
 #define CGBN_CASE(n_, BI_, BJ_, WI_, WJ_) \
     case n_: hipLaunchKernelGGL((gemm_tile<T, FORM, GATED, BI_, BJ_, WI_, WJ_>), dim3(groups_of(G)), dim3(WI_ * WJ_ * kWave), 0, st, G); break;
-    switch (p.shape) { CGBN_TILE_SHAPES(CGBN_CASE) }
+    if constexpr (sizeof(T) == 2) switch (p.shape) { CGBN_TILE_SHAPES(CGBN_CASE) }
+    else switch (p.shape) { CGBN_TILE_SHAPES_FLOAT(CGBN_CASE) }
 #undef CGBN_CASE
     const hipError_t e = hipGetLastError();
     return e != hipSuccess ? e : join<T, FORM, GATED>(G, st);
+}
+
+template <typename T> void two(int shape, const GemmArgs& X, const GemmArgs& W, int nx, unsigned n, hipStream_t st)
+{
+#define CGBN_CASE(n_, BI_, BJ_, WI_, WJ_) \
+    case n_: hipLaunchKernelGGL((gemm_two<T, BI_, BJ_, WI_, WJ_>), dim3(n), dim3(WI_ * WJ_ * kWave), 0, st, X, W, nx); break;
+    if constexpr (sizeof(T) == 2) switch (shape) { CGBN_TILE_SHAPES(CGBN_CASE) }
+    else switch (shape) { CGBN_TILE_SHAPES_FLOAT(CGBN_CASE) }
+#undef CGBN_CASE
 }
 
 }  // namespace
@@ -51,10 +61,7 @@ template <> hipError_t launch_two<CGBN_INST_T>(const GemmPlan& px, GemmArgs X, c
     take(px, &X);
     take(pw, &W);
     const unsigned nx = groups_of(X), nw = groups_of(W);
-#define CGBN_CASE(n_, BI_, BJ_, WI_, WJ_) \
-    case n_: hipLaunchKernelGGL((gemm_two<CGBN_INST_T, BI_, BJ_, WI_, WJ_>), dim3(nx + nw), dim3(WI_ * WJ_ * kWave), 0, st, X, W, (int)nx); break;
-    switch (px.shape) { CGBN_TILE_SHAPES(CGBN_CASE) }
-#undef CGBN_CASE
+    two<CGBN_INST_T>(px.shape, X, W, (int)nx, nx + nw, st);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess) e = join<CGBN_INST_T, FORM_NN, false>(X, st);
     return e != hipSuccess ? e : join<CGBN_INST_T, FORM_TN, false>(W, st);

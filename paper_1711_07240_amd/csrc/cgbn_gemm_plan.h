@@ -9,8 +9,11 @@ namespace cgbn {
 // number, rows and columns of the tile, wavefronts along each
 #define CGBN_TILE_SHAPES(X_) \
     X_(0, 256, 256, 2, 2)    \
-    X_(1, 128, 128, 2, 2)    \
-    X_(2, 128, 64, 4, 1)     \
+    CGBN_TILE_SHAPES_FLOAT(X_)
+// (float has two sets of accumulators)
+#define CGBN_TILE_SHAPES_FLOAT(X_) \
+    X_(1, 128, 128, 2, 2)          \
+    X_(2, 128, 64, 4, 1)           \
     X_(3, 64, 64, 2, 1)
 
 struct GemmPlan {
@@ -20,17 +23,19 @@ struct GemmPlan {
     double join;                // seconds for joining the splits
 };
 
-// The shapes' rates, in operations a second of the whole device with the compute units full: bfloat16 as measured on
-// 8192 x 8192 x 8192; float runs at the matrix instructions' rate with any of them.  Where a vector unit holds few wavefronts,
-// their waits show: the fraction of the rate with one and with two of them; `start`, their prologue's time.
+// The shapes' rates, in operations a second of the whole device with the compute units full: as measured on 8192 x 8192 x 8192
+// (float: 8192 x 8192 x 2048).  Where a vector unit holds few wavefronts, their waits show: the fraction of the rate with one and with two of
+// them; `start`, their prologue's time.
 struct TileShape {
     int bi, bj, waves;
-    double rate, one, two, start;
+    double rate, float_rate, one, two, start;
 };
 inline const TileShape& tile_shape(int s)
 {
-    static const TileShape shapes[] = {
-        {256, 256, 4, 1450e12, 1., 1., 7e-6}, {128, 128, 4, 1170e12, 0.65, 1., 0.8e-6}, {128, 64, 4, 900e12, 0.5, 0.8, 0.5e-6}, {64, 64, 2, 690e12, 0.6, 0.8, 0.3e-6}};
+    static const TileShape shapes[] = {{256, 256, 4, 1450e12, 0, 1., 1., 7e-6},
+                                       {128, 128, 4, 1170e12, 198e12, 0.65, 1., 0.8e-6},
+                                       {128, 64, 4, 900e12, 162e12, 0.5, 0.8, 0.5e-6},
+                                       {64, 64, 2, 690e12, 153e12, 0.6, 0.8, 0.3e-6}};
     return shapes[s];
 }
 constexpr int kTileShapes = 4;
@@ -39,6 +44,7 @@ constexpr int kTileShapes = 4;
 inline bool plan_with(int shape, long long want, int elem, bool gated, long long I, long long J, long long R, int segs, int batch, GemmPlan* p)
 {
     const TileShape& t = tile_shape(shape);
+    if (elem == 4 && t.float_rate == 0) return false;
     const int step = 128 / elem, bj = gated ? t.bj / 2 : t.bj;
     const long long steps = (R + step - 1) / step * segs, per = (steps + want - 1) / want, splits = (steps + per - 1) / per;
     const double part = splits > 1 ? (double)splits * batch * (gated ? 2 : 1) * I * J * 4 : 0;
@@ -48,7 +54,7 @@ inline bool plan_with(int shape, long long want, int elem, bool gated, long long
     // wavefronts of a compute unit's workgroups, dealt over its four vector units: the busiest has `deep` of them
     const double waves = (double)((long long)((p->groups + 255) / 256)) * t.waves / 4, deep = (double)(long long)(waves + 0.75);
     const double fill = waves / deep;
-    const double rate = elem == 2 ? t.rate * fill * (deep <= 1 ? t.one : deep <= 2 ? t.two : 1.) : 139e12 * fill * (deep <= 1 ? 0.86 : 1.);
+    const double rate = elem == 2 ? t.rate * fill * (deep <= 1 ? t.one : deep <= 2 ? t.two : 1.) : t.float_rate * fill * (deep <= 1 ? 0.75 : 1.);
     // (what a workgroup does besides: its first loads' way, and its rows of A, which it shares with the tiles beside it, and its
     // results, at the rate of memory)
     const double bytes = (double)t.bi * per * 128 / (double)(tj < 8 ? tj : 8) + (double)t.bi * bj * (gated ? 2 : 1) * (splits > 1 ? 4 : elem * 1.25);
