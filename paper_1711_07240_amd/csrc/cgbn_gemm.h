@@ -513,8 +513,8 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
         };
         if (first < last) {
             stage(0);
-            dma_wait_and_meet();
             if (first + 1 < last) stage(1);
+            dma_wait_and_meet();                // (both: with few steps it is the trips to memory one after another that take the time)
             read_b(0, 0);
 #pragma unroll
             for (int x = 0; x < FI; ++x) read_a(0, 0, x);
