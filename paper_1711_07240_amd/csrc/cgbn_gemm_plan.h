@@ -33,9 +33,9 @@ struct TileShape {
 inline const TileShape& tile_shape(int s)
 {
     static const TileShape shapes[] = {{256, 256, 4, 1450e12, 0, 1., 1., 7e-6},
-                                       {128, 128, 4, 1170e12, 198e12, 0.65, 1., 0.8e-6},
-                                       {128, 64, 4, 900e12, 162e12, 0.5, 0.8, 0.5e-6},
-                                       {64, 64, 2, 690e12, 153e12, 0.6, 0.8, 0.3e-6}};
+                                       {128, 128, 4, 1170e12, 198e12, 0.68, 1., 0.8e-6},
+                                       {128, 64, 4, 900e12, 162e12, 0.55, 0.85, 0.5e-6},
+                                       {64, 64, 2, 690e12, 153e12, 0.85, 0.95, 0.3e-6}};
     return shapes[s];
 }
 constexpr int kTileShapes = 4;
@@ -59,7 +59,7 @@ inline bool plan_with(int shape, long long want, int elem, bool gated, long long
     // results, at the rate of memory)
     const double bytes = (double)t.bi * per * 128 / (double)(tj < 8 ? tj : 8) + (double)t.bi * bj * (gated ? 2 : 1) * (splits > 1 ? 4 : elem * 1.25);
     p->cost = per * 2. * t.bi * t.bj * step / (rate / 256) + t.start + bytes / (5e12 / 256);
-    p->join = splits > 1 ? 4e-6 + part * 2 / 4e12 : 0;
+    p->join = splits > 1 ? 5e-6 + part * 2 / 4e12 : 0;
     return true;
 }
 

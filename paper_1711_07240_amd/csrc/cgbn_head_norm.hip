@@ -8,8 +8,9 @@
 // lane, chosen so that the values that are turned together are in the same lane: with halves, chunk c and the one R/2 values
 // on; with pairs any two.  So nothing but the row's sums crosses lanes.  A wavefront takes heads of ONE token: cosines and sines,
 // which in float are twice the bytes of a bfloat16 row, and the weights are fetched once for all of them.
-// Rows whose length, strides or addresses do not go in whole chunks, or whose halves do not, take the kernels with one value
-// a lane (`_any`): a wavefront a row, partners read again from the cache.
+// Chunks are 8 bytes where bfloat16 rows, strides, addresses or halves do not go in 16 (heads of 80 values, 40 of them turned: 348 us
+// value by value, 65 in chunks of 8 bytes; 5845 tokens of 144 heads); where they do not go in either, a wavefront takes a row, a value a lane
+// and step, and reads partners again from the cache (`_any`).
 //
 // Sums are float: a row's over at most 16 values a lane, then a fixed tree; the weights' gradients per lane over the rows a wavefront
 // walks, then over wavefronts in order, then over workgroups in double precision.  No atomics.
@@ -67,6 +68,24 @@ template <int E> __device__ __forceinline__ void chunks_of(const HeadArgs& A, in
     }
 }
 
+// N neighbouring floats at any float's address
+template <int N> __device__ __forceinline__ void load_floats(const float* p, float (&v)[N])
+{
+    typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int k = 0; k < N; k += 4) {
+            const f32x4_any t = *reinterpret_cast<const f32x4_any*>(p + k);
+            v[k] = t.x; v[k + 1] = t.y; v[k + 2] = t.z; v[k + 3] = t.w;
+        }
+    } else {
+        static_assert(N == 2, "");
+        typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
+        const f32x2_any t = *reinterpret_cast<const f32x2_any*>(p);
+        v[0] = t.x; v[1] = t.y;
+    }
+}
+
 // cosines and sines of a lane's chunks.  Halves: of value e of both chunks; pairs: of values 2e, 2e + 1 of chunk 0 in the first
 // half, of chunk 1 in the second.  Not turned: 1 and 0.
 template <int E> struct Turn {
@@ -82,19 +101,31 @@ template <int E> struct Turn {
         const float bad = __int_as_float(0x7fc00000);
         if (A.style == CGBN_ROTATE_HALVES) {
             if (c0 < 0 || p >= A.lead) return;
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                c[e] = in ? A.cos[row + c0 + e] : bad;
-                s[e] = in ? A.sin[row + c0 + e] : bad;
-            }
+            load_floats<E>(A.cos + row + c0, c);
+            load_floats<E>(A.sin + row + c0, s);
         } else {
+            // (chunks that are turned in part: the angles of those of their pairs that are)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int first = h ? c1 : c0, n = first < 0 ? 0 : (A.R - first) / 2;
+                if (n >= E / 2) {
+                    load_floats<E / 2>(A.cos + row + first / 2, *reinterpret_cast<float(*)[E / 2]>(c + h * (E / 2)));
+                    load_floats<E / 2>(A.sin + row + first / 2, *reinterpret_cast<float(*)[E / 2]>(s + h * (E / 2)));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E / 2; ++e) {
+                        if (e >= n) continue;
+                        c[h * (E / 2) + e] = A.cos[row + first / 2 + e];
+                        s[h * (E / 2) + e] = A.sin[row + first / 2 + e];
+                    }
+                }
+            }
+        }
+        if (!in) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const int first = e < E / 2 ? c0 : c1, v = first + 2 * (e % (E / 2));
-                if (first >= 0 && v < A.R) {
-                    c[e] = in ? A.cos[row + v / 2] : bad;
-                    s[e] = in ? A.sin[row + v / 2] : bad;
-                }
+                const bool turned = A.style == CGBN_ROTATE_HALVES || (e < E / 2 ? c0 >= 0 && c0 + 2 * e < A.R : c1 >= 0 && c1 + 2 * (e - E / 2) < A.R);
+                if (turned) c[e] = s[e] = bad;
             }
         }
     }
@@ -122,21 +153,51 @@ template <int E> struct Turn {
     }
 };
 
-template <typename T> __device__ __forceinline__ typename Elem<T>::Raw load_chunk(const T* row, int c)
+// E values as they are stored: 16 bytes, or 4 bfloat16 where rows or halves go in no whole 16 bytes
+template <typename T, int E> struct Chunk {
+    static_assert(E * sizeof(T) == 16, "");
+    typedef typename Elem<T>::Raw Raw;
+    static __device__ __forceinline__ Raw load(const T* p) { return Elem<T>::load_raw(p); }
+    static __device__ __forceinline__ void unpack(const Raw& v, float (&f)[E]) { Elem<T>::unpack(v, f); }
+    static __device__ __forceinline__ void store(T* p, const float (&f)[E]) { Elem<T>::storev(p, f, 0); }
+};
+template <> struct Chunk<bf16_t, 4> {
+    typedef uint2 Raw;
+    static __device__ __forceinline__ Raw load(const bf16_t* p) { return *reinterpret_cast<const uint2*>(p); }
+    static __device__ __forceinline__ void unpack(const Raw& v, float (&f)[4])
+    {
+        f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
+        f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
+    }
+    static __device__ __forceinline__ void store(bf16_t* p, const float (&f)[4])
+    {
+        *reinterpret_cast<uint2*>(p) = make_uint2(f32x2_to_bf16x2(f[0], f[1]), f32x2_to_bf16x2(f[2], f[3]));
+    }
+};
+
+template <typename T, int E> __device__ __forceinline__ typename Chunk<T, E>::Raw load_chunk(const T* row, int c)
 {
-    typename Elem<T>::Raw v{};
-    if (c >= 0) v = Elem<T>::load_raw(row + c);
+    typename Chunk<T, E>::Raw v{};
+    if (c >= 0) v = Chunk<T, E>::load(row + c);
     return v;
 }
 
+template <int E> __device__ __forceinline__ void load_weights(const float* w, int c0, int c1, float (&w0)[E], float (&w1)[E])
+{
+#pragma unroll
+    for (int e = 0; e < E; ++e) w0[e] = w1[e] = 0.f;
+    if (c0 >= 0) load_floats<E>(w + c0, w0);
+    if (c1 >= 0) load_floats<E>(w + c1, w1);
+}
+
 // Rows whose chunks are asked for before the first of them is used: with one at a time 4.4 TB/s forward and 2.6 backward, with
-// four 4.8 and 4.4 (bfloat16, 40 heads of 128 values; 32768 and 16384 tokens).
+// four, and angles and weights by vectors, 5.4 and 4.5 (bfloat16, 40 heads of 128 values; 32768 and 16384 tokens).
 constexpr int kAhead = 4;
 
 // L: lanes of a row
-template <typename T, int L> __global__ __launch_bounds__(kThreads) void head_forward(const HeadArgs A)
+template <typename T, int E, int L> __global__ __launch_bounds__(kThreads) void head_forward(const HeadArgs A)
 {
-    constexpr int E = Elem<T>::VEC, G = kWave / L;
+    constexpr int G = kWave / L;
     const int lane = (int)threadIdx.x % kWave, p = lane % L, g = lane / L;
     const long long wave = (long long)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
     const long long token = wave / A.parts;
@@ -150,35 +211,34 @@ template <typename T, int L> __global__ __launch_bounds__(kThreads) void head_fo
     for (int t = 0; t < 2; ++t) {
         if (part * G >= A.H[t]) continue;
         float w0[E], w1[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) { w0[e] = c0 >= 0 ? A.w[t][c0 + e] : 0.f; w1[e] = c1 >= 0 ? A.w[t][c1 + e] : 0.f; }
+        load_weights<E>(A.w[t], c0, c1, w0, w1);
         const T* const x = static_cast<const T*>(A.x[t]) + token * A.ldx[t];
         T* const y = static_cast<T*>(A.out[t]) + token * A.ldo[t];
         const int stride = A.parts * G;
         for (int h0 = part * G + g; h0 < A.H[t]; h0 += kAhead * stride) {
-            typename Elem<T>::Raw ra[kAhead], rb[kAhead];
+            typename Chunk<T, E>::Raw ra[kAhead], rb[kAhead];
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
                 const int h = h0 + k * stride;
                 if (h >= A.H[t]) continue;
-                ra[k] = load_chunk<T>(x + (long long)h * A.D, c0);
-                rb[k] = load_chunk<T>(x + (long long)h * A.D, c1);
+                ra[k] = load_chunk<T, E>(x + (long long)h * A.D, c0);
+                rb[k] = load_chunk<T, E>(x + (long long)h * A.D, c1);
             }
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
                 const int h = h0 + k * stride;
                 if (h >= A.H[t]) continue;
                 float a[E], b[E], s = 0.f;
-                Elem<T>::unpack(ra[k], a);
-                Elem<T>::unpack(rb[k], b);
+                Chunk<T, E>::unpack(ra[k], a);
+                Chunk<T, E>::unpack(rb[k], b);
 #pragma unroll
                 for (int e = 0; e < E; ++e) s += a[e] * a[e] + b[e] * b[e];
                 const float r = 1.f / sqrtf(group_sum<L>(s) * A.inv_D + A.eps);
 #pragma unroll
                 for (int e = 0; e < E; ++e) { a[e] *= r * w0[e]; b[e] *= r * w1[e]; }
                 turn.template apply<1>(A.style, a, b);
-                if (c0 >= 0) Elem<T>::storev(y + (long long)h * A.D + c0, a, 0);
-                if (c1 >= 0) Elem<T>::storev(y + (long long)h * A.D + c1, b, 0);
+                if (c0 >= 0) Chunk<T, E>::store(y + (long long)h * A.D + c0, a);
+                if (c1 >= 0) Chunk<T, E>::store(y + (long long)h * A.D + c1, b);
             }
         }
     }
@@ -193,21 +253,18 @@ __device__ __forceinline__ void store_dw(const HeadArgs& A, const float* red, in
     __syncthreads();
 }
 
-template <typename T, int L> __global__ __launch_bounds__(kThreads, 2) void head_backward(const HeadArgs A)
+template <typename T, int E, int L> __global__ __launch_bounds__(kThreads, 2) void head_backward(const HeadArgs A)
 {
-    constexpr int E = Elem<T>::VEC, G = kWave / L;
+    constexpr int G = kWave / L;
     extern __shared__ float red[];                    // [4][D]
     const int lane = (int)threadIdx.x % kWave, p = lane % L, g = lane / L, wave = (int)threadIdx.x / kWave;
     int c0, c1;
     chunks_of<E>(A, p, &c0, &c1);
     for (int t = 0; t < 2; ++t) {
         float w0[E], w1[E], dw0[E], dw1[E];
+        load_weights<E>(A.w[t], A.H[t] ? c0 : -1, A.H[t] ? c1 : -1, w0, w1);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            w0[e] = A.H[t] && c0 >= 0 ? A.w[t][c0 + e] : 0.f;
-            w1[e] = A.H[t] && c1 >= 0 ? A.w[t][c1 + e] : 0.f;
-            dw0[e] = dw1[e] = 0.f;
-        }
+        for (int e = 0; e < E; ++e) dw0[e] = dw1[e] = 0.f;
         const long long waves = (long long)gridDim.x * (kThreads / kWave);
         for (long long u = (long long)blockIdx.x * (kThreads / kWave) + wave; u < A.T * A.parts; u += waves) {
             const long long token = u / A.parts;
@@ -220,26 +277,26 @@ template <typename T, int L> __global__ __launch_bounds__(kThreads, 2) void head
             T* const dx = static_cast<T*>(A.out[t]) + token * A.ldo[t];
             const int stride = A.parts * G;
             for (int h0 = part * G + g; h0 < A.H[t]; h0 += kAhead * stride) {
-                typename Elem<T>::Raw ra[kAhead], rb[kAhead], rc[kAhead], rd[kAhead];
+                typename Chunk<T, E>::Raw ra[kAhead], rb[kAhead], rc[kAhead], rd[kAhead];
 #pragma unroll
                 for (int k = 0; k < kAhead; ++k) {
                     const int h = h0 + k * stride;
                     if (h >= A.H[t]) continue;
                     const long long o = (long long)h * A.D;
-                    ra[k] = load_chunk<T>(x + o, c0);
-                    rb[k] = load_chunk<T>(x + o, c1);
-                    rc[k] = load_chunk<T>(dy + o, c0);
-                    rd[k] = load_chunk<T>(dy + o, c1);
+                    ra[k] = load_chunk<T, E>(x + o, c0);
+                    rb[k] = load_chunk<T, E>(x + o, c1);
+                    rc[k] = load_chunk<T, E>(dy + o, c0);
+                    rd[k] = load_chunk<T, E>(dy + o, c1);
                 }
 #pragma unroll
                 for (int k = 0; k < kAhead; ++k) {
                     const int h = h0 + k * stride;
                     if (h >= A.H[t]) continue;
                     float a[E], b[E], ea[E], eb[E], s = 0.f, m = 0.f;
-                    Elem<T>::unpack(ra[k], a);
-                    Elem<T>::unpack(rb[k], b);
-                    Elem<T>::unpack(rc[k], ea);
-                    Elem<T>::unpack(rd[k], eb);
+                    Chunk<T, E>::unpack(ra[k], a);
+                    Chunk<T, E>::unpack(rb[k], b);
+                    Chunk<T, E>::unpack(rc[k], ea);
+                    Chunk<T, E>::unpack(rd[k], eb);
                     turn.template apply<-1>(A.style, ea, eb);
 #pragma unroll
                     for (int e = 0; e < E; ++e) {
@@ -255,8 +312,8 @@ template <typename T, int L> __global__ __launch_bounds__(kThreads, 2) void head
                         a[e] = r * (ea[e] * w0[e] - a[e] * f);
                         b[e] = r * (eb[e] * w1[e] - b[e] * f);
                     }
-                    if (c0 >= 0) Elem<T>::storev(dx + (long long)h * A.D + c0, a, 0);
-                    if (c1 >= 0) Elem<T>::storev(dx + (long long)h * A.D + c1, b, 0);
+                    if (c0 >= 0) Chunk<T, E>::store(dx + (long long)h * A.D + c0, a);
+                    if (c1 >= 0) Chunk<T, E>::store(dx + (long long)h * A.D + c1, b);
                 }
             }
         }
@@ -274,7 +331,7 @@ template <typename T, int L> __global__ __launch_bounds__(kThreads, 2) void head
 
 // ---- one value a lane and step: any length, stride and alignment ----
 
-constexpr int kMaxD = 1024, kSlots = kMaxD / kWave;
+constexpr int kMaxD = 1024;
 
 // the value turned together with value d (R > d), whether d is the first of the two, and the angle's index
 __device__ __forceinline__ int partner_of(const HeadArgs& A, int d, bool* is_first, int* angle)
@@ -303,8 +360,9 @@ struct Angles {
     __device__ __forceinline__ float sin(const HeadArgs& A, int k) const { return in ? A.sin[row + k] : __int_as_float(0x7fc00000); }
 };
 
+// kSlots: values a lane
 // in place (out == x) every value is read, partners too, before the row's first is written
-template <typename T> __global__ __launch_bounds__(kThreads) void head_forward_any(const HeadArgs A)
+template <typename T, int kSlots> __global__ __launch_bounds__(kThreads) void head_forward_any(const HeadArgs A)
 {
     const int lane = (int)threadIdx.x % kWave, heads = A.H[0] + A.H[1];
     const long long row = (long long)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
@@ -347,7 +405,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void head_forward_a
     }
 }
 
-template <typename T> __global__ __launch_bounds__(kThreads) void head_backward_any(const HeadArgs A)
+template <typename T, int kSlots> __global__ __launch_bounds__(kThreads) void head_backward_any(const HeadArgs A)
 {
     extern __shared__ float red[];                    // [4][D]
     const int lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
@@ -401,7 +459,6 @@ template <typename T> __global__ __launch_bounds__(kThreads) void head_backward_
 
 // ---- host ----
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 cgbn_status launched() { return hipGetLastError() == hipSuccess ? CGBN_OK : CGBN_ERR_HIP; }
 
 constexpr long long kMaxTokens = 1ll << 30, kMaxStride = 1ll << 32;
@@ -423,13 +480,15 @@ int backward_groups(long long T, int Hq, int Hk)
     return (int)(groups < kBackwardGroups ? (groups < 1 ? 1 : groups) : kBackwardGroups);
 }
 
-template <typename T> bool plan_chunks(HeadArgs* A, bool backward)
+// rows in chunks of E values
+template <typename T> bool plan_chunks(HeadArgs* A, int E, bool backward)
 {
-    constexpr int E = 16 / (int)sizeof(T);
+    const size_t bytes = E * sizeof(T);
     if (A->D % E != 0) return false;
     for (int t = 0; t < (A->H[1] ? 2 : 1); ++t) {
-        if (!aligned16(A->x[t]) || !aligned16(A->out[t]) || A->ldx[t] % E != 0 || A->ldo[t] % E != 0) return false;
-        if (backward && (!aligned16(A->dy[t]) || A->lddy[t] % E != 0)) return false;
+        if (reinterpret_cast<uintptr_t>(A->x[t]) % bytes || reinterpret_cast<uintptr_t>(A->out[t]) % bytes || A->ldx[t] % E != 0 || A->ldo[t] % E != 0)
+            return false;
+        if (backward && (reinterpret_cast<uintptr_t>(A->dy[t]) % bytes || A->lddy[t] % E != 0)) return false;
     }
     const int chunks = A->D / E;
     A->lead = A->far = 0;
@@ -451,42 +510,62 @@ int lanes_of(int pairs)
 
 #define CGBN_LANES(X_) X_(1) X_(2) X_(4) X_(8) X_(16) X_(32) X_(64)
 
-template <typename T> cgbn_status run_forward(HeadArgs& A, hipStream_t st)
+// a wavefront takes all heads of its token unless there are too few tokens to fill the device with
+void deal_heads(HeadArgs* A, int G)
 {
-    if (!plan_chunks<T>(&A, false)) {
-        const long long rows = A.T * (A.H[0] + A.H[1]);
-        hipLaunchKernelGGL(head_forward_any<T>, dim3((unsigned)((rows + 3) / 4)), dim3(kThreads), 0, st, A);
-        return launched();
-    }
-    const int L = lanes_of(A.pairs), G = kWave / L, most = ((A.H[0] > A.H[1] ? A.H[0] : A.H[1]) + G - 1) / G;
-    // a wavefront takes all heads of its token unless there are too few tokens to fill the device with
-    A.parts = 1;
-    while (A.parts < most && A.T * A.parts < 4096) A.parts *= 2;
-    if (A.parts > most) A.parts = most;
+    const int most = ((A->H[0] > A->H[1] ? A->H[0] : A->H[1]) + G - 1) / G;
+    A->parts = 1;
+    while (A->parts < most && A->T * A->parts < 4096) A->parts *= 2;
+    if (A->parts > most) A->parts = most;
+}
+
+template <typename T, int E> void launch_forward(HeadArgs& A, hipStream_t st)
+{
+    const int L = lanes_of(A.pairs);
+    deal_heads(&A, kWave / L);
     const dim3 grid((unsigned)((A.T * A.parts + 3) / 4));
 #define CGBN_CASE(L_) \
-    case L_: hipLaunchKernelGGL((head_forward<T, L_>), grid, dim3(kThreads), 0, st, A); break;
+    case L_: hipLaunchKernelGGL((head_forward<T, E, L_>), grid, dim3(kThreads), 0, st, A); break;
     switch (L) { CGBN_LANES(CGBN_CASE) }
 #undef CGBN_CASE
+}
+
+template <typename T, int E> void launch_backward(HeadArgs& A, int groups, size_t lds, hipStream_t st)
+{
+    const int L = lanes_of(A.pairs);
+    deal_heads(&A, kWave / L);
+#define CGBN_CASE(L_) \
+    case L_: hipLaunchKernelGGL((head_backward<T, E, L_>), dim3((unsigned)groups), dim3(kThreads), lds, st, A); break;
+    switch (L) { CGBN_LANES(CGBN_CASE) }
+#undef CGBN_CASE
+}
+
+#define CGBN_ANY(kernel_, grid_, lds_)                                                                                 \
+    do {                                                                                                               \
+        const dim3 g_((unsigned)(grid_));                                                                              \
+        if (A.D <= 64) hipLaunchKernelGGL((kernel_<T, 1>), g_, dim3(kThreads), lds_, st, A);                           \
+        else if (A.D <= 128) hipLaunchKernelGGL((kernel_<T, 2>), g_, dim3(kThreads), lds_, st, A);                     \
+        else if (A.D <= 256) hipLaunchKernelGGL((kernel_<T, 4>), g_, dim3(kThreads), lds_, st, A);                     \
+        else hipLaunchKernelGGL((kernel_<T, kMaxD / kWave>), g_, dim3(kThreads), lds_, st, A);                         \
+    } while (0)
+
+template <typename T> cgbn_status run_forward(HeadArgs& A, hipStream_t st)
+{
+    constexpr int E = 16 / (int)sizeof(T);
+    if (plan_chunks<T>(&A, E, false)) launch_forward<T, E>(A, st);
+    else if (sizeof(T) == 2 && plan_chunks<T>(&A, 4, false)) launch_forward<T, 4>(A, st);
+    else CGBN_ANY(head_forward_any, (A.T * (A.H[0] + A.H[1]) + 3) / 4, 0);
     return launched();
 }
 
 template <typename T> cgbn_status run_backward(HeadArgs& A, float* dwq, float* dwk, hipStream_t st)
 {
+    constexpr int E = 16 / (int)sizeof(T);
     const int groups = backward_groups(A.T, A.H[0], A.H[1]);
     const size_t lds = (size_t)4 * A.D * sizeof(float);
-    if (!plan_chunks<T>(&A, true)) {
-        hipLaunchKernelGGL(head_backward_any<T>, dim3((unsigned)groups), dim3(kThreads), lds, st, A);
-    } else {
-        const int L = lanes_of(A.pairs), G = kWave / L, most = ((A.H[0] > A.H[1] ? A.H[0] : A.H[1]) + G - 1) / G;
-        A.parts = 1;
-        while (A.parts < most && A.T * A.parts < 4096) A.parts *= 2;
-        if (A.parts > most) A.parts = most;
-#define CGBN_CASE(L_) \
-        case L_: hipLaunchKernelGGL((head_backward<T, L_>), dim3((unsigned)groups), dim3(kThreads), lds, st, A); break;
-        switch (L) { CGBN_LANES(CGBN_CASE) }
-#undef CGBN_CASE
-    }
+    if (plan_chunks<T>(&A, E, true)) launch_backward<T, E>(A, groups, lds, st);
+    else if (sizeof(T) == 2 && plan_chunks<T>(&A, 4, true)) launch_backward<T, 4>(A, groups, lds, st);
+    else CGBN_ANY(head_backward_any, groups, lds);
     if (launched() != CGBN_OK) return CGBN_ERR_HIP;
     const int n = A.H[1] ? 2 * A.D : A.D;
     // (a workgroup's row of partial sums has both weights' side by side; without keys the second half is zero and stays unread)
