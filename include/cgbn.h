@@ -261,7 +261,8 @@ cgbn_status cgbn_update_running_stats(const float* mean, const float* mean_lo, c
  *   - Tensors are dense row by row (but for the strides of cgbn_head_norm_*), their element type `dtype` (weights too), base
  *     addresses 16-byte aligned; widths may be odd.  Bias vectors, norm weights and their gradients are float.
  *   - Sums are held in 32 bits and results rounded once, to nearest even; what a backward pass hands from one of its kernels
- *     to the next (dz, dg, du below) is rounded to `dtype`.  Float products run on the float matrix instructions.
+ *     to the next (dz, dg, du below) is rounded to `dtype`.  Float products are formed from three bfloat16 parts a value, which are
+ *     exact, and are off by less than 2^-22 of themselves (values under 1e-33 have fewer bits); with few rows by float instructions.
  *   - M (or T) may be 0: forward calls do nothing, backward calls write zero weight gradients.
  *   - Outputs and inputs are different buffers unless said otherwise (equal pointers where that is wrong are answered with
  *     CGBN_ERR_ALIAS; partial overlaps are undefined).  The workspace may be NULL where the size below is not more than 256.

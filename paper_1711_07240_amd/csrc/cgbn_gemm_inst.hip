@@ -51,7 +51,9 @@ template <typename T> void two(int shape, const GemmArgs& X, const GemmArgs& W, 
 
 #if CGBN_INST_FORM == 0
 template <> hipError_t launch_gemm<CGBN_INST_T, FORM_NT, false>(const GemmPlan& p, GemmArgs G, hipStream_t st) { return launch_one<CGBN_INST_T, FORM_NT, false>(p, G, st); }
+template <> hipError_t launch_join<CGBN_INST_T, false>(const GemmArgs& G, hipStream_t st) { return join<CGBN_INST_T, FORM_NT, false>(G, st); }
 #elif CGBN_INST_FORM == 1
+template <> hipError_t launch_join<CGBN_INST_T, true>(const GemmArgs& G, hipStream_t st) { return join<CGBN_INST_T, FORM_NT, true>(G, st); }
 template <> hipError_t launch_gemm<CGBN_INST_T, FORM_NT, true>(const GemmPlan& p, GemmArgs G, hipStream_t st) { return launch_one<CGBN_INST_T, FORM_NT, true>(p, G, st); }
 #else
 template <> hipError_t launch_gemm<CGBN_INST_T, FORM_NN, false>(const GemmPlan& p, GemmArgs G, hipStream_t st) { return launch_one<CGBN_INST_T, FORM_NN, false>(p, G, st); }

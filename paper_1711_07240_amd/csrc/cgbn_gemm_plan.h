@@ -17,9 +17,10 @@ namespace cgbn {
     X_(3, 64, 64, 2, 1)
 
 struct GemmPlan {
-    int shape, ti, tj, splits, per;
+    int shape, elem, ti, tj, splits, per;
     size_t part_bytes;          // of workspace, 0 where the reduction is not split
-    double groups, cost;        // workgroups; seconds that a compute unit spends on one of them
+    double groups;              // workgroups
+    double work, besides;       // seconds that a full compute unit spends on one's products, and on its loads and stores
     double join;                // seconds for joining the splits
 };
 
@@ -28,14 +29,15 @@ struct GemmPlan {
 // them; `start`, their prologue's time.
 struct TileShape {
     int bi, bj, waves;
-    double rate, float_rate, one, two, start;
+    double start;
+    struct { double full, one, two; } rate[2];          // bfloat16, float
 };
 inline const TileShape& tile_shape(int s)
 {
-    static const TileShape shapes[] = {{256, 256, 4, 1450e12, 0, 1., 1., 7e-6},
-                                       {128, 128, 4, 1170e12, 198e12, 0.68, 1., 0.8e-6},
-                                       {128, 64, 4, 900e12, 162e12, 0.55, 0.85, 0.5e-6},
-                                       {64, 64, 2, 690e12, 153e12, 0.85, 0.95, 0.3e-6}};
+    static const TileShape shapes[] = {{256, 256, 4, 7e-6, {{1450e12, 1., 1.}, {0., 0., 0.}}},
+                                       {128, 128, 4, 0.8e-6, {{1170e12, 0.68, 1.}, {198e12, 0.72, 1.}}},
+                                       {128, 64, 4, 0.5e-6, {{900e12, 0.55, 0.85}, {162e12, 0.5, 0.7}}},
+                                       {64, 64, 2, 0.3e-6, {{690e12, 0.85, 0.95}, {153e12, 0.47, 0.75}}}};
     return shapes[s];
 }
 constexpr int kTileShapes = 4;
@@ -44,23 +46,30 @@ constexpr int kTileShapes = 4;
 inline bool plan_with(int shape, long long want, int elem, bool gated, long long I, long long J, long long R, int segs, int batch, GemmPlan* p)
 {
     const TileShape& t = tile_shape(shape);
-    if (elem == 4 && t.float_rate == 0) return false;
+    if (t.rate[elem == 4].full == 0.) return false;
     const int step = 128 / elem, bj = gated ? t.bj / 2 : t.bj;
     const long long steps = (R + step - 1) / step * segs, per = (steps + want - 1) / want, splits = (steps + per - 1) / per;
     const double part = splits > 1 ? (double)splits * batch * (gated ? 2 : 1) * I * J * 4 : 0;
     const long long ti = (I + t.bi - 1) / t.bi, tj = (J + bj - 1) / bj;
     if (part > 1e9 || (double)ti * tj * splits * batch > 1e9) return false;
-    *p = GemmPlan{shape, (int)ti, (int)tj, (int)splits, (int)per, (size_t)part, (double)ti * tj * splits * batch, 0, 0};
-    // wavefronts of a compute unit's workgroups, dealt over its four vector units: the busiest has `deep` of them
-    const double waves = (double)((long long)((p->groups + 255) / 256)) * t.waves / 4, deep = (double)(long long)(waves + 0.75);
-    const double fill = waves / deep;
-    const double rate = elem == 2 ? t.rate * fill * (deep <= 1 ? t.one : deep <= 2 ? t.two : 1.) : t.float_rate * fill * (deep <= 1 ? 0.75 : 1.);
+    *p = GemmPlan{shape, elem, (int)ti, (int)tj, (int)splits, (int)per, (size_t)part, (double)ti * tj * splits * batch, 0, 0, 0};
     // (what a workgroup does besides: its first loads' way, and its rows of A, which it shares with the tiles beside it, and its
     // results, at the rate of memory)
     const double bytes = (double)t.bi * per * 128 / (double)(tj < 8 ? tj : 8) + (double)t.bi * bj * (gated ? 2 : 1) * (splits > 1 ? 4 : elem * 1.25);
-    p->cost = per * 2. * t.bi * t.bj * step / (rate / 256) + t.start + bytes / (5e12 / 256);
+    p->besides = t.start + bytes / (5e12 / 256);
+    p->work = per * 2. * t.bi * t.bj * step / (t.rate[elem == 4].full / 256);
     p->join = splits > 1 ? 5e-6 + part * 2 / 4e12 : 0;
     return true;
+}
+
+// seconds that a compute unit spends on one workgroup of a launch of `groups` of them
+inline double cost_of(const GemmPlan& p, double groups)
+{
+    const TileShape& t = tile_shape(p.shape);
+    // wavefronts of a compute unit's workgroups, dealt over its four vector units: the busiest has `deep` of them
+    const double waves = (double)((long long)((groups + 255) / 256)) * t.waves / 4, deep = (double)(long long)(waves + 0.75);
+    const auto& rate = t.rate[p.elem == 4];
+    return p.work / (waves / deep * (deep <= 1 ? rate.one : deep <= 2 ? rate.two : 1.)) + p.besides;
 }
 
 template <typename F> inline void each_split(long long steps, F f)
@@ -71,7 +80,7 @@ template <typename F> inline void each_split(long long steps, F f)
 }
 
 // the seconds of a product by itself: rounds of workgroups
-inline double time_alone(const GemmPlan& p) { return (double)(long long)((p.groups + 255) / 256) * p.cost + p.join; }
+inline double time_alone(const GemmPlan& p) { return (double)(long long)((p.groups + 255) / 256) * cost_of(p, p.groups) + p.join; }
 
 inline GemmPlan plan_shape(int shape, int elem, bool gated, long long I, long long J, long long R, int segs, int batch)
 {
@@ -109,9 +118,9 @@ inline void plan_two(int elem, long long M, int N, int K, int pairs, GemmPlan* d
             for (int b = 0; b < 2; ++b) {
                 // a unit takes the next workgroup when it is done with one: the last to be started end half of one's time
                 // after the average, and no sooner than they take
-                const double work = (x[a].groups * x[a].cost + w[b].groups * w[b].cost) / 256;
-                double t = work + 0.5 * w[b].cost;
-                if (t < x[a].cost) t = x[a].cost;
+                const double groups = x[a].groups + w[b].groups, cx = cost_of(x[a], groups), cw = cost_of(w[b], groups);
+                double t = (x[a].groups * cx + w[b].groups * cw) / 256 + 0.5 * cw;
+                if (t < cx) t = cx;
                 t += x[a].join + w[b].join;
                 if (dx->ti == 0 || t < best) {
                     best = t;
@@ -122,6 +131,8 @@ inline void plan_two(int elem, long long M, int N, int K, int pairs, GemmPlan* d
     }
 }
 
+// the sums of a split forward product joined, the epilogue
+template <typename T, bool GATED> hipError_t launch_join(const GemmArgs& G, hipStream_t st);
 template <typename T, int FORM, bool GATED> hipError_t launch_gemm(const GemmPlan& p, GemmArgs G, hipStream_t st);
 // both products of a backward pass in one launch
 template <typename T> hipError_t launch_two(const GemmPlan& px, GemmArgs X, const GemmPlan& pw, GemmArgs W, hipStream_t st);

@@ -4,7 +4,8 @@
 // gated pair) and its wavefronts share the reduction, 128 bytes of every row at a time in turn, so the workgroup walks 16 (32)
 // streams of whole lines.  W goes from memory straight to the registers that the matrix instruction reads: lane l holds 16 bytes of
 // row l % 16, the four lanes of a row 64 neighbouring ones, several steps in flight.  x is small and comes
-// from the caches.  The wavefronts' sums meet in LDS and are added in wavefront order.
+// from the caches.  The wavefronts' sums meet in LDS and are added in wavefront order.  Where W has few rows and long ones, several
+// workgroups share them, and gemm_join adds their sums.
 #pragma once
 
 #include "cgbn_gemm.h"
@@ -34,20 +35,20 @@ __global__ __launch_bounds__(NW * kWave) void gemm_rows(const GemmArgs G)
     constexpr int E = 16 / (int)sizeof(T), STEP = 8 * E, P = GATED ? 2 : 1, U = FM == 1 && !GATED ? 4 : 2;
     __shared__ f32x4 sums[NW][FM * P][kWave];
     const int l = (int)threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), t = l & 15, q = l >> 4;
-    const int j0 = (int)blockIdx.x * 16, i0 = (int)blockIdx.y * 16 * FM;
+    const int j0 = (int)blockIdx.x * 16;
     const T *pw[P], *px[FM];
 #pragma unroll
     for (int p = 0; p < P; ++p) pw[p] = static_cast<const T*>(G.B[p]) + (long long)min(j0 + t, G.J - 1) * G.ldb + q * E;
 #pragma unroll
-    for (int m = 0; m < FM; ++m) px[m] = static_cast<const T*>(G.A[0]) + (long long)min(i0 + m * 16 + t, G.I - 1) * G.lda + q * E;
+    for (int m = 0; m < FM; ++m) px[m] = static_cast<const T*>(G.A[0]) + (long long)min(m * 16 + t, G.I - 1) * G.lda + q * E;
 
     f32x4 acc[P][FM];
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
         for (int m = 0; m < FM; ++m) acc[p][m] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int steps = (G.R + STEP - 1) / STEP, full = G.R / STEP;
-    int s = wave;
+    const int begin = (int)blockIdx.y * G.per, steps = min(begin + G.per, (G.R + STEP - 1) / STEP), full = min(steps, G.R / STEP);
+    int s = begin + wave;
     for (; s + (U - 1) * NW < full; s += U * NW) {
         u32x4 w[U][P][2], x[U][FM][2];
 #pragma unroll
@@ -90,15 +91,8 @@ __global__ __launch_bounds__(NW * kWave) void gemm_rows(const GemmArgs G)
         for (int m = 0; m < FM; ++m) sums[wave][p * FM + m][l] = acc[p][m];
     __syncthreads();
     if (wave >= FM) return;
-    const int m = wave, i = i0 + m * 16 + t, j = j0 + q * 4;
+    const int m = wave, i = m * 16 + t, j = j0 + q * 4;
     if (i >= G.I || j >= G.J) return;
-    const long long o = (long long)i * G.ldc + j;
-    float extra[4];
-    if constexpr (!GATED) {
-        float bias[4];
-        load_bias<4>(G, bias, j, G.J - j);
-        load_extras<T, 4>(G, extra, bias, o, G.J - j);
-    }
     float v[P][4];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -107,6 +101,18 @@ __global__ __launch_bounds__(NW * kWave) void gemm_rows(const GemmArgs G)
         for (int k = 1; k < NW; ++k) a += sums[k][p * FM + m][l];
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[p][k] = a[k];
+    }
+    if (G.splits > 1) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) store_run<float, 4>(G.part + (((long long)blockIdx.y * P + p) * G.I + i) * G.J + j, v[p], G.J - j);
+        return;
+    }
+    const long long o = (long long)i * G.ldc + j;
+    float extra[4];
+    if constexpr (!GATED) {
+        float bias[4];
+        load_bias<4>(G, bias, j, G.J - j);
+        load_extras<T, 4>(G, extra, bias, o, G.J - j);
     }
     if constexpr (GATED) finish_gated<T, 4>(G, v[0], v[1], o, G.J - j);
     else finish_linear<T, 4>(G, v[0], extra, o, G.J - j);

@@ -50,23 +50,45 @@ template <typename T> __global__ __launch_bounds__(kThreads) void linear_dz(cons
     for (int e = 0; e < E; ++e) sum[e] = 0.f;
     const long long r0 = (long long)blockIdx.y * A.rows, r1 = min(r0 + A.rows, A.M);
     if (in) {
-        for (long long r = r0 + first; r < r1; r += stride) {
-            float g[E];
-            load_run<T, E>(static_cast<const T*>(A.dy) + r * A.N + c, g, valid);
+        const T *const dy = static_cast<const T*>(A.dy) + c, *const saved = static_cast<const T*>(A.saved) + c;
+        auto row = [&](long long r, float (&g)[E], const float (&z)[E]) {
+            // (where ReLU passes nothing dz is zero, not dy * 0: an infinity there does not become NaN)
             if (A.saved) {
-                float z[E];
-                load_run<T, E>(static_cast<const T*>(A.saved) + r * A.N + c, z, valid);
-                // (where ReLU passes nothing dz is zero, not dy * 0: an infinity there does not become NaN)
 #pragma unroll
                 for (int e = 0; e < E; ++e) g[e] = A.act == ACT_RELU ? (z[e] > 0.f ? g[e] : 0.f) : g[e] * act_slope(z[e], A.act);
             }
 #pragma unroll
             for (int e = 0; e < E; ++e) sum[e] += g[e];
-            if (A.dz) {
-                // (beyond the row the filling is zero: what was loaded there is)
-                store_run<T, E>(static_cast<T*>(A.dz) + r * A.ld + c, g, E);
-            }
+            // (beyond the row the filling is zero: what was loaded there is)
+            if (A.dz) store_run<T, E>(static_cast<T*>(A.dz) + r * A.ld + c, g, E);
             if (A.dresidual) store_run<T, E>(static_cast<T*>(A.dresidual) + r * A.N + c, g, valid);
+        };
+        if (valid >= E) {
+            // four rows at a time: the loads of all before the first is used (the last row's again where there are fewer)
+            constexpr int U = 4;
+            for (long long r = r0 + first; r < r1; r += U * stride) {
+                u32x4 wg[U], wz[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) wg[u] = *reinterpret_cast<const u32x4_any*>(dy + min(r + u * stride, r1 - 1) * A.N);
+                if (A.saved) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) wz[u] = *reinterpret_cast<const u32x4_any*>(saved + min(r + u * stride, r1 - 1) * A.N);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    float g[E], z[E];
+                    unpack_run<T>(wg[u], g);
+                    unpack_run<T>(wz[u], z);
+                    if (r + u * stride < r1) row(r + u * stride, g, z);
+                }
+            }
+        } else {
+            for (long long r = r0 + first; r < r1; r += stride) {
+                float g[E], z[E];
+                load_run<T, E>(dy + r * A.N, g, valid);
+                if (A.saved) load_run<T, E>(saved + r * A.N, z, valid);
+                row(r, g, z);
+            }
         }
     }
     if (!A.part) return;
@@ -179,9 +201,20 @@ ForwardPlan plan_forward(long long M, int N, int K, int dtype, bool gated)
     const Widths W(dtype);
     ForwardPlan p{};
     p.rows = M <= (gated ? kFewRowsGated : kFewRows);
-    if (p.rows) return p;
-    p.g = plan_gemm(W.elem, gated, M, N, K, 1, 1);
     Layout l;
+    if (p.rows) {
+        // Workgroups of 16 weight rows; where those are too few for the device and long, several share them: 20 us by 4 workgroups,
+        // 8 by 40 (the gated pair, 2 x 5248 x 64, float), and 11.1 by 64, 8.3 by 256 (1 x 8192 x 1024, bfloat16)
+        const int steps = (K * W.elem + 127) / 128, groups = (N + 15) / 16;
+        int want = groups <= 128 && steps >= 96 ? 256 / groups : 1;
+        if (want > steps / 16) want = steps / 16 > 1 ? steps / 16 : 1;
+        p.g.per = (steps + want - 1) / want;
+        p.g.splits = (steps + p.g.per - 1) / p.g.per;
+        p.part = l.take(p.g.splits > 1 ? (size_t)p.g.splits * (gated ? 2 : 1) * M * N * sizeof(float) : 0);
+        p.bytes = l.at;
+        return p;
+    }
+    p.g = plan_gemm(W.elem, gated, M, N, K, 1, 1);
     if (W.odd(K)) {
         p.x = l.take((size_t)M * W.padded(K) * W.elem);
         p.w = l.take((size_t)N * W.padded(K) * W.elem * (gated ? 2 : 1));
@@ -211,11 +244,11 @@ BackwardPlan plan_backward(long long M, int N, int K, int dtype, bool gated)
     }
     p.part_x = l.take(p.dx.part_bytes);
     p.part_w = l.take(p.dw.part_bytes);
-    // column sums: enough blocks of rows to fill the device, no block of fewer rows than a workgroup walks in eight passes
+    // column sums: enough blocks of rows to fill the device, no block of fewer rows than a workgroup takes at once
     const int vecs = W.padded(N) / W.E;
     p.tw = 1;
     while (p.tw < 64 && p.tw < vecs) p.tw *= 2;
-    const long long across = (vecs + p.tw - 1) / p.tw, least = 8ll * (kThreads / p.tw);
+    const long long across = (vecs + p.tw - 1) / p.tw, least = 4ll * (kThreads / p.tw);
     long long blocks = 1024 / across > 1 ? 1024 / across : 1;
     if (blocks > (M + least - 1) / least) blocks = (M + least - 1) / least;
     if (blocks < 1) blocks = 1;
@@ -243,12 +276,13 @@ template <typename T> hipError_t pad(const void* src, void* dst, long long rows,
 
 template <typename T, bool GATED> hipError_t launch_rows(const GemmArgs& G, hipStream_t st)
 {
-    const dim3 grid((unsigned)((G.J + 15) / 16));
+    const dim3 grid((unsigned)((G.J + 15) / 16), (unsigned)G.splits);
     // 16 wavefronts, each with all of its loads in flight at once or twice, where there are steps for them: 8.0 against 8.5 us with 8 of
     // them (one row, 4096 x 4096); with few steps they only wait for each other: 3.3 with 4 against 3.6 us (1024 x 1024)
     const bool many = (long long)G.R * (int)sizeof(T) >= 32 * 128;
 #define CGBN_ROWS(FM_, NW_) hipLaunchKernelGGL((gemm_rows<T, GATED, FM_, NW_>), grid, dim3(NW_ * kWave), 0, st, G)
-    if (G.I <= 16 && many) CGBN_ROWS(1, 16);
+    if (G.I <= 16 && many && sizeof(T) == 4) CGBN_ROWS(1, 8);          // 16.9 against 18.3 us (8 rows, 4096 x 4096)
+    else if (G.I <= 16 && many) CGBN_ROWS(1, 16);
     else if (G.I <= 16) CGBN_ROWS(1, 4);
     else if constexpr (!GATED) CGBN_ROWS(2, 16);
 #undef CGBN_ROWS
@@ -263,8 +297,12 @@ cgbn_status forward(GemmArgs G, const ForwardPlan& p, char* ws, hipStream_t st)
     G.segs = G.batch = 1;
     G.lda = G.ldb = K;
     G.ldc = G.J;
+    G.part = reinterpret_cast<float*>(ws + p.part);
     if (p.rows) {
+        G.splits = p.g.splits;
+        G.per = p.g.per;
         CGBN_HIP((launch_rows<T, GATED>(G, st)));
+        if (G.splits > 1) CGBN_HIP((launch_join<T, GATED>(G, st)));
         return CGBN_OK;
     }
     if (W.odd(K)) {
@@ -278,7 +316,6 @@ cgbn_status forward(GemmArgs G, const ForwardPlan& p, char* ws, hipStream_t st)
         }
         G.lda = G.ldb = kp;
     }
-    G.part = reinterpret_cast<float*>(ws + p.part);
     CGBN_HIP((launch_gemm<T, FORM_NT, GATED>(p.g, G, st)));
     return CGBN_OK;
 }
