@@ -43,6 +43,7 @@ struct GemmArgs {
     int segs, batch;            // segments of the reduction; products side by side
     int ti, tj, splits, per;    // tiles; splits of the reduction and steps (of 128 bytes) in each
     int act;
+    int nt;                     // results go past the caches
 };
 
 // ---- activations, on 32-bit values ----
@@ -123,7 +124,8 @@ template <typename T, int N> __device__ __forceinline__ void load_run(const T* p
     }
 }
 
-template <typename T, int N> __device__ __forceinline__ void store_run(T* p, const float (&v)[N], int valid)
+// NT: past the caches (a choice of the compiler's, not of the program's: of two stores under a condition it makes one without)
+template <typename T, int N, bool NT = false> __device__ __forceinline__ void store_run(T* p, const float (&v)[N], int valid)
 {
     constexpr int V = Elem<T>::VEC;
     if (valid >= N && N >= 4) {
@@ -136,7 +138,8 @@ template <typename T, int N> __device__ __forceinline__ void store_run(T* p, con
                     if constexpr (sizeof(T) == 2) w[e] = f32x2_to_bf16x2(v[k + 2 * e], v[k + 2 * e + 1]);
                     else w[e] = __float_as_uint(v[k + e]);
                 }
-                *reinterpret_cast<u32x4_any*>(p + k) = w;
+                if constexpr (NT) __builtin_nontemporal_store(w, reinterpret_cast<u32x4_any*>(p + k));
+                else *reinterpret_cast<u32x4_any*>(p + k) = w;
             }
         } else if constexpr (N == 4) {
             u32x2_any w;
@@ -331,16 +334,16 @@ template <int N> __device__ __forceinline__ void activate(float (&v)[N], int act
 }
 
 // v: the products; r: bias and residual.  o: the run's first element in the outputs
-template <typename T, int N>
+template <typename T, int N, bool NT = false>
 __device__ __forceinline__ void finish_linear(const GemmArgs& G, float (&v)[N], const float (&r)[N], long long o, int valid)
 {
     if (G.bias || G.residual) {
 #pragma unroll
         for (int k = 0; k < N; ++k) v[k] += r[k];
     }
-    if (G.Z[0]) store_run<T, N>(static_cast<T*>(G.Z[0]) + o, v, valid);
+    if (G.Z[0]) store_run<T, N, NT>(static_cast<T*>(G.Z[0]) + o, v, valid);
     activate(v, G.act);
-    store_run<T, N>(static_cast<T*>(G.C[0]) + o, v, valid);
+    store_run<T, N, NT>(static_cast<T*>(G.C[0]) + o, v, valid);
 }
 
 // what finish_linear adds
@@ -361,16 +364,16 @@ template <typename T, int N> __device__ __forceinline__ void load_extras(const G
     }
 }
 
-template <typename T, int N> __device__ __forceinline__ void finish_gated(const GemmArgs& G, float (&g)[N], const float (&u)[N], long long o, int valid)
+template <typename T, int N, bool NT = false> __device__ __forceinline__ void finish_gated(const GemmArgs& G, float (&g)[N], const float (&u)[N], long long o, int valid)
 {
     if (G.Z[0]) {
-        store_run<T, N>(static_cast<T*>(G.Z[0]) + o, g, valid);
-        store_run<T, N>(static_cast<T*>(G.Z[1]) + o, u, valid);
+        store_run<T, N, NT>(static_cast<T*>(G.Z[0]) + o, g, valid);
+        store_run<T, N, NT>(static_cast<T*>(G.Z[1]) + o, u, valid);
     }
     activate(g, G.act);
 #pragma unroll
     for (int k = 0; k < N; ++k) g[k] *= u[k];
-    store_run<T, N>(static_cast<T*>(G.C[0]) + o, g, valid);
+    store_run<T, N, NT>(static_cast<T*>(G.C[0]) + o, g, valid);
 }
 
 // ---- the product ----
@@ -580,7 +583,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
     const int l = (int)threadIdx.x % kWave, t = l & 15, q = l >> 4;
     lds_char* const mine = tile + wave * (FX * 16 * TJ * 4);
     typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
-    auto store_round = [&](int x0, auto PART) {
+    auto store_round = [&](int x0, auto PART, auto NT) {
         const int i_first = i0 + wi * TI + x0 * 16;
         constexpr int N = PART() ? 4 : Elem<T>::VEC, LANES = WIDE / N, ROWS = kWave / LANES, U = FX * 16 / ROWS < 4 ? FX * 16 / ROWS : 4;
         static_assert(FX * 16 % (ROWS * U) == 0, "whole rounds");
@@ -627,11 +630,11 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
                     store_run<float, N>(p, v, valid);
                     if constexpr (GATED) store_run<float, N>(p + (long long)G.I * G.J, up, valid);
                 } else if constexpr (GATED) {
-                    finish_gated<T, N>(G, v, up, o, valid);
+                    finish_gated<T, N, NT()>(G, v, up, o, valid);
                 } else if constexpr (FORM == FORM_NT) {
-                    finish_linear<T, N>(G, v, extra[u], o, valid);
+                    finish_linear<T, N, NT()>(G, v, extra[u], o, valid);
                 } else {
-                    store_run<T, N>(static_cast<T*>(G.C[w.z]) + o, v, valid);
+                    store_run<T, N, NT()>(static_cast<T*>(G.C[w.z]) + o, v, valid);
                 }
             }
         };
@@ -651,8 +654,9 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
 #pragma unroll
             for (int y = 0; y < FJ; ++y) *(lds_f32x4*)(mine + (x * 16 + t) * (TJ * 4) + (((y * 4 + q) ^ (t & 7)) << 4)) = acc[x0 + x][y];
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // (the lanes of a wavefront read each other's)
-        if (G.splits > 1) store_round(x0, yes());
-        else store_round(x0, no());
+        if (G.splits > 1) store_round(x0, yes(), no());
+        else if (G.nt) store_round(x0, no(), yes());
+        else store_round(x0, no(), no());
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 }
