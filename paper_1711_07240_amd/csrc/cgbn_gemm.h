@@ -101,6 +101,9 @@ template <typename T> __device__ __forceinline__ void unpack_run(const u32x4& w,
     else Elem<T>::unpack(__builtin_bit_cast(f32x4, w), v);
 }
 
+// 16 bytes that are read once
+template <typename T> __device__ __forceinline__ u32x4 load_once(const T* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p)); }
+
 template <typename T, int N> __device__ __forceinline__ void load_run(const T* p, float (&v)[N], int valid)
 {
     constexpr int V = Elem<T>::VEC;
@@ -449,7 +452,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
 #pragma unroll
             for (int k = 0; k < EARLY_N; ++k) {
                 const int i = i0 + wi * TI + k * EROWS + (int)threadIdx.x % kWave / ELANES;
-                if (i < G.I && j + EV <= G.J) early[k] = *reinterpret_cast<const u32x4_any*>(static_cast<const T*>(G.residual) + (long long)i * G.ldc + j);
+                if (i < G.I && j + EV <= G.J) early[k] = load_once(static_cast<const T*>(G.residual) + (long long)i * G.ldc + j);
             }
         }
     }

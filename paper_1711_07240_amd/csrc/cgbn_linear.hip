@@ -69,10 +69,10 @@ template <typename T> __global__ __launch_bounds__(kThreads) void linear_dz(cons
             for (long long r = r0 + first; r < r1; r += U * stride) {
                 u32x4 wg[U], wz[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) wg[u] = *reinterpret_cast<const u32x4_any*>(dy + min(r + u * stride, r1 - 1) * A.N);
+                for (int u = 0; u < U; ++u) wg[u] = load_once(dy + min(r + u * stride, r1 - 1) * A.N);
                 if (A.saved) {
 #pragma unroll
-                    for (int u = 0; u < U; ++u) wz[u] = *reinterpret_cast<const u32x4_any*>(saved + min(r + u * stride, r1 - 1) * A.N);
+                    for (int u = 0; u < U; ++u) wz[u] = load_once(saved + min(r + u * stride, r1 - 1) * A.N);
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
@@ -121,10 +121,18 @@ template <typename T> __global__ __launch_bounds__(kThreads) void gated_dz(const
         const long long r = id / chunks;
         const int c = (int)(id - r * chunks) * E, valid = A.F - c;
         const long long o = r * A.F + c;
+        const T *const ph = static_cast<const T*>(A.dh) + o, *const pg = static_cast<const T*>(A.gate) + o, *const pu = static_cast<const T*>(A.up) + o;
         float h[E], g[E], u[E];
-        load_run<T, E>(static_cast<const T*>(A.dh) + o, h, valid);
-        load_run<T, E>(static_cast<const T*>(A.gate) + o, g, valid);
-        load_run<T, E>(static_cast<const T*>(A.up) + o, u, valid);
+        if (valid >= E) {
+            const u32x4 wh = load_once(ph), wg = load_once(pg), wu = load_once(pu);
+            unpack_run<T>(wh, h);
+            unpack_run<T>(wg, g);
+            unpack_run<T>(wu, u);
+        } else {
+            load_run<T, E>(ph, h, valid);
+            load_run<T, E>(pg, g, valid);
+            load_run<T, E>(pu, u, valid);
+        }
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const float slope = act_slope(g[e], A.act), a = act_apply(g[e], A.act);
