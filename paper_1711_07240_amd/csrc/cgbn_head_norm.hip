@@ -562,15 +562,16 @@ template <typename T, int E, bool NT> void launch_backward(HeadArgs& A, int grou
         else hipLaunchKernelGGL((kernel_<T, kMaxD / kWave>), g_, dim3(kThreads), lds_, st, A);                         \
     } while (0)
 
-// Results of more than the caches next to the compute units hold go past them: 118 against 127 us, backward 106 against 112 (40 heads of
-// 128 bfloat16; 32768 and 16384 tokens); smaller ones stay there for whoever reads them next.
+// Results of more than the caches next to the compute units hold go past them: 119 against 127 us, backward 106 against 112 (40 heads of
+// 128 bfloat16; 32768 and 16384 tokens); smaller ones stay there for whoever reads them next.  Not from chunks of 8 bytes: 65 us through
+// the caches, 72 past them (5845 tokens, 144 heads of 80).
 template <typename T> bool past_caches(const HeadArgs& A) { return (double)A.T * (A.H[0] + A.H[1]) * A.D * sizeof(T) > 32e6; }
 
 template <typename T> cgbn_status run_forward(HeadArgs& A, hipStream_t st)
 {
     constexpr int E = 16 / (int)sizeof(T);
     if (plan_chunks<T>(&A, E, false)) past_caches<T>(A) ? launch_forward<T, E, true>(A, st) : launch_forward<T, E, false>(A, st);
-    else if (sizeof(T) == 2 && plan_chunks<T>(&A, 4, false)) past_caches<T>(A) ? launch_forward<T, 4, true>(A, st) : launch_forward<T, 4, false>(A, st);
+    else if (sizeof(T) == 2 && plan_chunks<T>(&A, 4, false)) launch_forward<T, 4, false>(A, st);
     else CGBN_ANY(head_forward_any, (A.T * (A.H[0] + A.H[1]) + 3) / 4, 0);
     return launched();
 }
@@ -581,8 +582,7 @@ template <typename T> cgbn_status run_backward(HeadArgs& A, float* dwq, float* d
     const int groups = backward_groups(A.T, A.H[0], A.H[1]);
     const size_t lds = (size_t)4 * A.D * sizeof(float);
     if (plan_chunks<T>(&A, E, true)) past_caches<T>(A) ? launch_backward<T, E, true>(A, groups, lds, st) : launch_backward<T, E, false>(A, groups, lds, st);
-    else if (sizeof(T) == 2 && plan_chunks<T>(&A, 4, true))
-        past_caches<T>(A) ? launch_backward<T, 4, true>(A, groups, lds, st) : launch_backward<T, 4, false>(A, groups, lds, st);
+    else if (sizeof(T) == 2 && plan_chunks<T>(&A, 4, true)) launch_backward<T, 4, false>(A, groups, lds, st);
     else CGBN_ANY(head_backward_any, groups, lds);
     if (launched() != CGBN_OK) return CGBN_ERR_HIP;
     const int n = A.H[1] ? 2 * A.D : A.D;
