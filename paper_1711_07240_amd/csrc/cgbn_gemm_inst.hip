@@ -22,7 +22,7 @@ template <typename T, int FORM, bool GATED> hipError_t join(const GemmArgs& G, h
     const int n = G.J % 4 == 0 ? 4 : 1;
     const long long threads = (long long)G.I * G.J * (GATED ? 1 : G.batch) / n;
     int lanes = 1;
-    while (lanes < 16 && lanes * 4 <= G.splits && threads * lanes < 256 * 1024) lanes *= 2;
+    while (lanes < 16 && lanes * 4 <= G.splits && threads * lanes < 128 * 1024) lanes *= 2;
     const dim3 grid((unsigned)((threads * lanes + kThreads - 1) / kThreads));
     if (n == 4) hipLaunchKernelGGL((gemm_join<T, FORM, GATED, 4>), grid, dim3(kThreads), 0, st, G, lanes);
     else hipLaunchKernelGGL((gemm_join<T, FORM, GATED, 1>), grid, dim3(kThreads), 0, st, G, lanes);
