@@ -95,7 +95,7 @@ typedef u32x4 u32x4_any __attribute__((aligned(2)));
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 
 // a whole 16 bytes
-template <typename T> __device__ __forceinline__ void unpack_run(const u32x4& w, float (&v)[16 / sizeof(T)])
+template <typename T> __device__ __forceinline__ void unpack_run(const u32x4 w, float (&v)[16 / sizeof(T)])
 {
     if constexpr (sizeof(T) == 2) Elem<T>::unpack(w, v);
     else Elem<T>::unpack(__builtin_bit_cast(f32x4, w), v);

@@ -168,9 +168,17 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 constexpr int kMaxWidth = 1 << 20;                  // of N, K, F: a tile's byte offsets stay within 32 bits
 constexpr long long kMaxRows = 1ll << 30;
 constexpr long long kMaxElements = 1ll << 38;       // of a matrix: grids stay within 31 bits
-// Up to here a forward product takes gemm_rows: 13.3 us against 14.8 with tiles (32 rows, 4096 x 4096), 48 rows 18.8 against 14.2; the
-// gated pair 38 against 49 us (4096 x 11264) with 16 rows, 61 against 49 with 32.
-constexpr int kFewRows = 32, kFewRowsGated = 16;
+
+// Whether a product takes gemm_rows.  Up to 16 rows it does: the gated pair 38 against 49 us with tiles (4096 x 11264, 16 rows), 61
+// against 49 with 32.  Beyond them it pays for every row again with all of the weights, so these have to be small.  bfloat16, against
+// tiles: 5.0 and 7.3 us (32 rows, 1024 x 1024), 11.1 and 12.1 (17, 4096 x 4096), 12.4 and 12.4 (24), 13.7 and 12.8 (32), 31 and 26.5
+// (17, 12288 x 4096).  Float, whose tiles multiply six times: 27 and 26.6 (32, 4096 x 4096), 58 and 64 (17, 12288 x 4096), 64.5 and
+// 64.3 (24), 73 and 66 (32).
+bool few_rows(long long M, int N, int K, int elem, bool gated)
+{
+    if (M <= 16) return true;
+    return !gated && M <= 32 && (double)M * N * K * elem <= (elem == 2 ? 0.8e9 : 4e9);
+}
 
 cgbn_status check_sizes(long long M, int N, int K, int dtype)
 {
@@ -208,11 +216,11 @@ ForwardPlan plan_forward(long long M, int N, int K, int dtype, bool gated)
 {
     const Widths W(dtype);
     ForwardPlan p{};
-    p.rows = M <= (gated ? kFewRowsGated : kFewRows);
+    p.rows = few_rows(M, N, K, W.elem, gated);
     Layout l;
     if (p.rows) {
-        // Workgroups of 16 weight rows; where those are too few for the device and long, several share them: 20 us by 4 workgroups,
-        // 8 by 40 (the gated pair, 2 x 5248 x 64, float), and 11.1 by 64, 8.3 by 256 (1 x 8192 x 1024, bfloat16)
+        // Workgroups of 16 weight rows; where those are too few for the device and long, several share them: 23.4 us by 4 workgroups,
+        // 7.2 by 40 (the gated pair, 2 x 5248 x 64, float), and 11.5 by 64, 9.4 by 256 (1 x 8192 x 1024, bfloat16)
         const int steps = (K * W.elem + 127) / 128, groups = (N + 15) / 16;
         int want = groups <= 128 && steps >= 96 ? 256 / groups : 1;
         if (want > steps / 16) want = steps / 16 > 1 ? steps / 16 : 1;
