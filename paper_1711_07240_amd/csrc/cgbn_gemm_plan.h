@@ -29,15 +29,16 @@ struct GemmPlan {
 // them; `start`, their prologue's time.
 struct TileShape {
     int bi, bj, waves;
+    int fit;                    // workgroups that a compute unit holds
     double start;
     struct { double full, one, two; } rate[2];          // bfloat16, float
 };
 inline const TileShape& tile_shape(int s)
 {
-    static const TileShape shapes[] = {{256, 256, 4, 7e-6, {{1450e12, 1., 1.}, {0., 0., 0.}}},
-                                       {128, 128, 4, 0.8e-6, {{1170e12, 0.68, 1.}, {198e12, 0.72, 1.}}},
-                                       {128, 64, 4, 0.5e-6, {{900e12, 0.55, 0.85}, {162e12, 0.5, 0.7}}},
-                                       {64, 64, 2, 0.3e-6, {{690e12, 0.85, 0.95}, {153e12, 0.47, 0.75}}}};
+    static const TileShape shapes[] = {{256, 256, 4, 1, 7e-6, {{1450e12, 1., 1.}, {0., 0., 0.}}},
+                                       {128, 128, 4, 2, 0.8e-6, {{1170e12, 0.68, 1.}, {198e12, 0.72, 1.}}},
+                                       {128, 64, 4, 3, 0.5e-6, {{900e12, 0.55, 0.85}, {162e12, 0.5, 0.7}}},
+                                       {64, 64, 2, 5, 0.3e-6, {{690e12, 0.85, 0.95}, {153e12, 0.47, 0.75}}}};
     return shapes[s];
 }
 constexpr int kTileShapes = 4;
@@ -58,7 +59,10 @@ inline bool plan_with(int shape, long long want, int elem, bool gated, long long
     const double bytes = (double)t.bi * per * 128 / (double)(tj < 8 ? tj : 8) + (double)t.bi * bj * (gated ? 2 : 1) * (splits > 1 ? 4 : elem * 1.25);
     p->besides = t.start + bytes / (5e12 / 256);
     p->work = per * 2. * t.bi * t.bj * step / (t.rate[elem == 4].full / 256);
-    p->join = splits > 1 ? 5e-6 + part * 2 / 4e12 : 0;
+    // (written and read back from the caches.  Of 282 forward products of 33 to 2048 rows, timed with every shape and split, those that
+    // this model takes are 4% off the best on the mean where it was chosen and 6% elsewhere, 5% and 7% with half of this rate; with 6e12
+    // 3000 x 768 x 768 float has dW split for nothing, 83 us for 69)
+    p->join = splits > 1 ? 5e-6 + part / 4e12 : 0;
     return true;
 }
 
@@ -104,30 +108,36 @@ inline GemmPlan plan_gemm(int elem, bool gated, long long I, long long J, long l
     return best;
 }
 
-// dx [M][K] = dz [M][N] W and dW [N][K] = dz^T x, `pairs` of them: with one shape, each split as it would be alone or not at all
+// dx [M][K] = dz [M][N] W and dW [N][K] = dz^T x, `pairs` of them, in one launch and with one shape
 inline void plan_two(int elem, long long M, int N, int K, int pairs, GemmPlan* dx, GemmPlan* dw)
 {
+    const int step = 128 / elem;
     double best = 0;
     dx->ti = 0;
     for (int s = 0; s < kTileShapes; ++s) {
-        GemmPlan x[2], w[2];
-        x[0] = plan_shape(s, elem, false, M, K, N, pairs, 1);
+        GemmPlan w[2], x;
         w[0] = plan_shape(s, elem, false, N, K, M, 1, pairs);
-        if (!x[0].ti || !w[0].ti || !plan_with(s, 1, elem, false, M, K, N, pairs, 1, &x[1]) || !plan_with(s, 1, elem, false, N, K, M, 1, pairs, &w[1])) continue;
-        for (int a = 0; a < 2; ++a)
+        if (!w[0].ti || !plan_with(s, 1, elem, false, N, K, M, 1, pairs, &w[1])) continue;
+        each_split((N + step - 1) / step * pairs, [&](long long want) {
+            if (!plan_with(s, want, elem, false, M, K, N, pairs, 1, &x)) return false;
             for (int b = 0; b < 2; ++b) {
-                // a unit takes the next workgroup when it is done with one: the last to be started end half of one's time
-                // after the average, and no sooner than they take
-                const double groups = x[a].groups + w[b].groups, cx = cost_of(x[a], groups), cw = cost_of(w[b], groups);
-                double t = (x[a].groups * cx + w[b].groups * cw) / 256 + 0.5 * cw;
-                if (t < cx) t = cx;
-                t += x[a].join + w[b].join;
+                const double groups = x.groups + w[b].groups, cx = cost_of(x, groups), cw = cost_of(w[b], groups);
+                // A unit takes the next workgroup when it is done with one: the last to be started end half of one's time after
+                // the average.  One that shares its unit takes as many times longer: a long one, dx unsplit for few rows, is then
+                // what the launch waits for (64 x 4096 x 4096 float 190 us with dx in 64 workgroups among 4096 of dW, 67 split).
+                const double most = groups / 256 < tile_shape(s).fit ? groups / 256 : tile_shape(s).fit, share = most > 1 ? most : 1;
+                double t = (x.groups * cx + w[b].groups * cw) / 256 + 0.5 * cw;
+                if (t < cx * share) t = cx * share;
+                if (t < cw * share) t = cw * share;
+                t += x.join + w[b].join;
                 if (dx->ti == 0 || t < best) {
                     best = t;
-                    *dx = x[a];
+                    *dx = x;
                     *dw = w[b];
                 }
             }
+            return true;
+        });
     }
 }
 
