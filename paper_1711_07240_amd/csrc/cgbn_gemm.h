@@ -383,10 +383,11 @@ template <typename T, int N, bool NT = false> __device__ __forceinline__ void fi
 
 constexpr int tile_lds(int bi, int bj) { return 2 * (bi + bj) * 128; }
 // wavefronts that a vector unit must have registers for, by the values that one accumulates
-constexpr int tile_waves(int values) { return values > 64 * 64 ? 1 : 2; }
+constexpr int tile_waves(int values) { return values > 96 * 64 ? 1 : 2; }
 
-// One workgroup's share, number `id` of `n`.
-template <typename T, int FORM, bool GATED, int BI, int BJ, int WI, int WJ>
+// One workgroup's share, number `id` of `n`.  EARLY: see below
+constexpr bool early_fits(int ti, int tj, int elem) { return ti * tj * elem / kWave <= 128; }
+template <typename T, int FORM, bool GATED, int BI, int BJ, int WI, int WJ, bool EARLY = FORM == FORM_NT && !GATED && early_fits(BI / WI, BJ / WJ, sizeof(T))>
 __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int id, int n)
 {
     constexpr int NT = WI * WJ * kWave, TI = BI / WI, FI = TI / 16, TJ = BJ / WJ, FJ = TJ / 16;
@@ -443,7 +444,6 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
     const int wave = (int)threadIdx.x / kWave, wi = wave / WJ, wj = wave % WJ;
     // A tile's residual is asked for before anything else where registers are left for it: with few steps there is nothing to hide
     // its way behind at the end.  (Laid out as store_round below takes it.)
-    constexpr bool EARLY = FORM == FORM_NT && !GATED && TI * TJ * (int)sizeof(T) / kWave <= 128;
     constexpr int EV = Elem<T>::VEC, ELANES = TJ / EV, EROWS = kWave / ELANES, EARLY_N = EARLY ? TI / EROWS : 1;
     u32x4 early[EARLY_N];
     if constexpr (EARLY) {
@@ -588,7 +588,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
     typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
     auto store_round = [&](int x0, auto PART, auto NT) {
         const int i_first = i0 + wi * TI + x0 * 16;
-        constexpr int N = PART() ? 4 : Elem<T>::VEC, LANES = WIDE / N, ROWS = kWave / LANES, U = FX * 16 / ROWS < 4 ? FX * 16 / ROWS : 4;
+        constexpr int N = PART() ? 4 : Elem<T>::VEC, LANES = WIDE / N, ROWS = kWave / LANES, RUNS = FX * 16 / ROWS, U = RUNS < 4 ? RUNS : RUNS % 4 == 0 ? 4 : 3;
         static_assert(FX * 16 % (ROWS * U) == 0, "whole rounds");
         constexpr bool EXTRAS = FORM == FORM_NT && !PART() && !GATED;
         const int j = j0 + wj * WIDE + (l % LANES) * N, valid = G.J - j;
@@ -669,6 +669,15 @@ __global__ __launch_bounds__(WI * WJ * kWave, tile_waves(BI * BJ / (WI * WJ))) v
 {
     __shared__ __attribute__((aligned(1024))) char lds[tile_lds(BI, BJ)];
     tile_product<T, FORM, GATED, BI, BJ, WI, WJ>(G, lds, (int)blockIdx.x, (int)gridDim.x);
+}
+
+// The same for a forward product with many tiles and a short reduction (short_shape says when).  Its epilogue counts, so a residual, asked for
+// early, has a kernel of its own: without one the registers are better left free (67200 x 64 x 1024 50 us, and 56 with them).
+template <typename T, int BI, int BJ, int WI, int WJ, bool RESIDUAL>
+__global__ __launch_bounds__(WI * WJ * kWave, tile_waves(BI * BJ / (WI * WJ))) void gemm_short(const GemmArgs G)
+{
+    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(BI, BJ)];
+    tile_product<T, FORM_NT, false, BI, BJ, WI, WJ, RESIDUAL>(G, lds, (int)blockIdx.x, (int)gridDim.x);
 }
 
 // dx = dz W and dW = dz^T x in one launch: neither needs the other, and the second's workgroups fill the compute units that

@@ -32,6 +32,15 @@ template <typename T, int FORM, bool GATED> hipError_t join(const GemmArgs& G, h
 template <typename T, int FORM, bool GATED> hipError_t launch_one(const GemmPlan& p, GemmArgs G, hipStream_t st)
 {
     take(p, &G);
+    if constexpr (sizeof(T) == 2 && FORM == FORM_NT && !GATED) {
+        if (short_shape(p.shape, G.splits, G.I, G.J, G.R, G.residual != nullptr)) {
+            G.ti = (G.I + kShortI - 1) / kShortI;
+            G.tj = (G.J + kShortJ - 1) / kShortJ;
+            if (G.residual) hipLaunchKernelGGL((gemm_short<T, kShortI, kShortJ, 2, 2, true>), dim3(groups_of(G)), dim3(4 * kWave), 0, st, G);
+            else hipLaunchKernelGGL((gemm_short<T, kShortI, kShortJ, 2, 2, false>), dim3(groups_of(G)), dim3(4 * kWave), 0, st, G);
+            return hipGetLastError();
+        }
+    }
 #define CGBN_CASE(n_, BI_, BJ_, WI_, WJ_) \
     case n_: hipLaunchKernelGGL((gemm_tile<T, FORM, GATED, BI_, BJ_, WI_, WJ_>), dim3(groups_of(G)), dim3(WI_ * WJ_ * kWave), 0, st, G); break;
     if constexpr (sizeof(T) == 2) switch (p.shape) { CGBN_TILE_SHAPES(CGBN_CASE) }

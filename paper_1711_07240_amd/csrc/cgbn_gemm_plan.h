@@ -43,6 +43,20 @@ inline const TileShape& tile_shape(int s)
 }
 constexpr int kTileShapes = 4;
 
+// Forward products of bfloat16 with short reductions and many tiles take a tile of their own instead of 128 x 128 or 256 x 256: two
+// workgroups just fit the LDS of a compute unit, so that one multiplies while the other's results travel, and they read a fifth less from LDS
+// than with 128 x 128.  Microseconds without it and with it, without residual and with one:
+//   67200 x 64 x 1024    57, 50; 78, 75      67200 x 512 x 1024   119, 104; 118, 113     67200 x 1024 x 1024   184, 160; 187, 169
+//   16384 x 64 x 4096    54, 50; 94, 73      16384 x 512 x 4096   103, 90; 194, 113      16384 x 2048 x 4096   -; 320, 273
+// Not where rows of the result do not start on lines of 128 bytes and there is little else to do: 9000 x 64 x 9000 85, 94 and 128, 132;
+// 9000 x 1000 x 9000 227, 210 and 255, 247.  Longer reductions are 256 x 256's: 8192 x 8192 x 8192 870 with this tile, 772.
+constexpr int kShortI = 192, kShortJ = 128;
+inline bool short_shape(int shape, int splits, long long I, long long J, long long R, bool residual)
+{
+    return shape <= 1 && splits == 1 && R <= (residual ? 2048 : 1024) && (R >= 512 || J % 64 == 0) &&
+           (I + kShortI - 1) / kShortI * ((J + kShortJ - 1) / kShortJ) >= 2048;
+}
+
 // the plan with one shape and one number of splits; false: more than can be
 inline bool plan_with(int shape, long long want, int elem, bool gated, long long I, long long J, long long R, int segs, int batch, GemmPlan* p)
 {

@@ -6,7 +6,8 @@ import numpy as np
 import pytest
 import torch
 
-from layers_harness import DEV, F, Gated, Linear, f64, normal
+from layers_harness import ACT_ERR, DEV, F, STEEP, UNIT, Gated, Linear, f64, near, normal
+from oracle import layers_oracle as Y
 from paper_1711_07240_amd import cgbn as L
 from test_gpu_head_norm import Heads
 
@@ -57,6 +58,33 @@ def test_large_gradients(size, dtype):
 @pytest.mark.parametrize("size,dtype", [((4100, 4100, 40), "bf16"), ((8300, 2051, 24), "bf16"), ((2100, 4097, 16), "f32")], ids=str)
 def test_large_gated_results(size, dtype):
     Gated(*size, dtype).check_forward("silu")
+
+
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("size", [(196700, 256, 40), (98400, 512, 129), (131100, 330, 513), (12389, 4096, 64), (66000, 767, 1000)], ids=str)
+def test_many_tiles_and_a_short_reduction(size, residual):
+    M, N, K = size
+    gen = torch.Generator(device=DEV).manual_seed(K)
+    x, w = (torch.randn(r, K, device=DEV, generator=gen).to(torch.bfloat16) for r in (M, N))
+    bias, res = torch.randn(N, device=DEV, generator=gen), torch.randn(M, N, device=DEV, generator=gen).to(torch.bfloat16)
+    y, z = (torch.full((M + 1, N), 7.0, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    ws = torch.empty(L.cgbn_linear_workspace_bytes(M, N, K, "bf16", False), dtype=torch.uint8, device=DEV)
+    L.cgbn_linear_forward(x, w, bias, res if residual else None, M, N, K, "gelu", y, z, "bf16", ws)
+    assert bool((y[M] == 7.0).all()) and bool((z[M] == 7.0).all())
+    # some rows exactly, the edges among them; every row against a product in float on the device, twice as far off at most
+    rows = torch.unique(torch.cat([torch.arange(200), torch.arange(M - 200, M), torch.randint(0, M, (600,), generator=torch.Generator().manual_seed(1))]))
+    xs, ws64, b, r = f64(x[rows.to(DEV)]), f64(w), f64(bias), f64(res[rows.to(DEV)]) if residual else 0.0
+    want = Y.linear_forward(xs, ws64, b, r if residual else None, "gelu")
+    err = (K + 8) * F * (np.abs(xs) @ np.abs(ws64).T + np.abs(b) + np.abs(r))
+    u = UNIT["bf16"]
+    near(z[rows.to(DEV)], want[1], err + u * np.abs(want[1]) + 1e-37, "z")
+    near(y[rows.to(DEV)], want[0], STEEP * err * (1 + u) + u * np.abs(want[0]) + ACT_ERR * (1 + np.abs(want[1])) + 1e-37, "y")
+    wf = w.float().t().contiguous()
+    for at in range(0, M, 8192):
+        to = min(M, at + 8192)
+        full = x[at:to].float() @ wf + bias + (res[at:to].float() if residual else 0.0)
+        tol = 2 * (K + 8) * F * (x[at:to].float().abs() @ wf.abs() + bias.abs() + (res[at:to].float().abs() if residual else 0.0)) + u * full.abs()
+        assert bool(((z[at:to].float() - full).abs() <= tol).all()), at
 
 
 @pytest.mark.parametrize("style", ["halves", "interleaved"])
