@@ -13,6 +13,16 @@ namespace {
 
 // ---- small kernels around the products ----
 
+// A row's last values: `valid` of them, at least one and fewer than E; zeros for the others.  The last one is asked for again where there is none,
+// without a branch: all of the loads are on their way before the first is waited for.
+template <typename T, int E> __device__ __forceinline__ void load_end(const T* p, float (&v)[E], int valid)
+{
+#pragma unroll
+    for (int k = 0; k < E; ++k) v[k] = Elem<T>::load1(p + min(k, valid - 1));
+#pragma unroll
+    for (int k = 0; k < E; ++k) v[k] = k < valid ? v[k] : 0.f;
+}
+
 // rows of n elements to rows of np, the filling zero: operands whose rows do not start on 16 bytes
 template <typename T> __global__ __launch_bounds__(kThreads) void pad_rows(const T* src, T* dst, long long rows, int n, int np)
 {
@@ -26,6 +36,12 @@ template <typename T> __global__ __launch_bounds__(kThreads) void pad_rows(const
     load_run<T, E>(src + r * n + c, v, n - c);
     store_run<T, E>(dst + r * np + c, v, E);
 }
+
+// the E values of a run: one decision for all of them
+#define CGBN_EACH(act_, which_, ...)                          \
+    if (act_ == which_) {                                     \
+        _Pragma("unroll") for (int e = 0; e < E; ++e) { __VA_ARGS__; } \
+    }
 
 struct DzArgs {
     const void *dy, *saved;        // [M][N]; saved null: act none
@@ -54,8 +70,9 @@ template <typename T> __global__ __launch_bounds__(kThreads) void linear_dz(cons
         auto row = [&](long long r, float (&g)[E], const float (&z)[E]) {
             // (where ReLU passes nothing dz is zero, not dy * 0: an infinity there does not become NaN)
             if (A.saved) {
-#pragma unroll
-                for (int e = 0; e < E; ++e) g[e] = A.act == ACT_RELU ? (z[e] > 0.f ? g[e] : 0.f) : g[e] * act_slope(z[e], A.act);
+                CGBN_EACH(A.act, ACT_RELU, g[e] = z[e] > 0.f ? g[e] : 0.f)
+                CGBN_EACH(A.act, ACT_GELU, g[e] *= act_slope(z[e], ACT_GELU))
+                CGBN_EACH(A.act, ACT_SILU, g[e] *= act_slope(z[e], ACT_SILU))
             }
 #pragma unroll
             for (int e = 0; e < E; ++e) sum[e] += g[e];
@@ -129,16 +146,14 @@ template <typename T> __global__ __launch_bounds__(kThreads) void gated_dz(const
             unpack_run<T>(wg, g);
             unpack_run<T>(wu, u);
         } else {
-            load_run<T, E>(ph, h, valid);
-            load_run<T, E>(pg, g, valid);
-            load_run<T, E>(pu, u, valid);
+            load_end<T, E>(ph, h, valid);
+            load_end<T, E>(pg, g, valid);
+            load_end<T, E>(pu, u, valid);
         }
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float slope = act_slope(g[e], A.act), a = act_apply(g[e], A.act);
-            g[e] = A.act == ACT_RELU && !(g[e] > 0.f) ? 0.f : h[e] * u[e] * slope;
-            u[e] = h[e] * a;
-        }
+        CGBN_EACH(A.act, ACT_NONE, const float a = g[e]; g[e] = h[e] * u[e]; u[e] = h[e] * a)
+        CGBN_EACH(A.act, ACT_RELU, const float a = act_apply(g[e], ACT_RELU); g[e] = g[e] > 0.f ? h[e] * u[e] : 0.f; u[e] = h[e] * a)
+        CGBN_EACH(A.act, ACT_GELU, const float z = g[e]; g[e] = h[e] * u[e] * act_slope(z, ACT_GELU); u[e] = h[e] * act_apply(z, ACT_GELU))
+        CGBN_EACH(A.act, ACT_SILU, const float z = g[e]; g[e] = h[e] * u[e] * act_slope(z, ACT_SILU); u[e] = h[e] * act_apply(z, ACT_SILU))
         store_run<T, E>(static_cast<T*>(A.dg) + r * A.ld + c, g, E);
         store_run<T, E>(static_cast<T*>(A.du) + r * A.ld + c, u, E);
     }
