@@ -8,9 +8,10 @@
 // lane, chosen so that the values that are turned together are in the same lane: with halves, chunk c and the one R/2 values
 // on; with pairs any two.  So nothing but the row's sums crosses lanes.  A wavefront takes heads of ONE token: cosines and sines,
 // which in float are twice the bytes of a bfloat16 row, and the weights are fetched once for all of them.
-// Chunks are 8 bytes where bfloat16 rows, strides, addresses or halves do not go in 16 (heads of 80 values, 40 of them turned: 348 us
-// value by value, 65 in chunks of 8 bytes; 5845 tokens of 144 heads); where they do not go in either, a wavefront takes a row, a value a lane
-// and step, and reads partners again from the cache (`_any`).
+// Chunks are as wide as rows, strides, addresses and halves allow, 16 bytes, 8, two values or one (value by value a wavefront to a row, and
+// in chunks: 144 heads of 80 bfloat16, 40 turned, 5845 tokens, 348 and 65 us; 24 of 82, 40 turned, 8000 tokens, 77 and 21, backward 230 and 48;
+// 80 of 39, 15994 tokens, 276 and 70, backward 606 and 170).  Rows of more than 64 pairs of chunks a wavefront takes one at a time, a value a
+// lane and step, and reads partners again from the cache (`_any`).
 //
 // Sums are float: a row's over at most 16 values a lane, then a fixed tree; the weights' gradients per lane over the rows a wavefront
 // walks, then over wavefronts in order, then over workgroups in double precision.  No atomics.
@@ -34,7 +35,7 @@ struct HeadArgs {
     int H[2], D, R, table;
     int style;                         // CGBN_ROTATE_*
     float eps, inv_D;
-    int pairs, lead, far, rest;        // chunk pairs of a row; those turned together as halves, chunks between them; see chunks_of()
+    int pairs, lead, step, far, rest;  // chunk pairs of a row; those turned together, chunks from one to the next and within one; see chunks_of()
     int parts;                         // wavefronts that share a token's heads
 };
 
@@ -52,15 +53,15 @@ template <int L> __device__ __forceinline__ float group_sum(float v)
     return v;
 }
 
-// The first elements of a lane's two chunks (-1: none).  As halves: `lead` pairs of chunks `far` apart, then the `rest` chunks
-// that are not turned, first half with second half.
+// The first elements of a lane's two chunks (-1: none).  Turned together as halves, or chunks of one value: `lead` pairs of chunks `far`
+// apart, then the `rest` chunks that are not turned, first half with second half.
 template <int E> __device__ __forceinline__ void chunks_of(const HeadArgs& A, int p, int* c0, int* c1)
 {
     *c0 = *c1 = -1;
     if (p >= A.pairs) return;
     if (p < A.lead) {
-        *c0 = p * E;
-        *c1 = (p + A.far) * E;
+        *c0 = p * A.step * E;
+        *c1 = *c0 + A.far * E;
     } else {
         const int k = p - A.lead, first = 2 * A.lead, half = (A.rest + 1) / 2;
         *c0 = (first + k) * E;
@@ -78,6 +79,8 @@ template <int N> __device__ __forceinline__ void load_floats(const float* p, flo
             const f32x4_any t = *reinterpret_cast<const f32x4_any*>(p + k);
             v[k] = t.x; v[k + 1] = t.y; v[k + 2] = t.z; v[k + 3] = t.w;
         }
+    } else if constexpr (N == 1) {
+        v[0] = *p;
     } else {
         static_assert(N == 2, "");
         typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
@@ -87,9 +90,10 @@ template <int N> __device__ __forceinline__ void load_floats(const float* p, flo
 }
 
 // cosines and sines of a lane's chunks.  Halves: of value e of both chunks; pairs: of values 2e, 2e + 1 of chunk 0 in the first
-// half, of chunk 1 in the second.  Not turned: 1 and 0.
+// half, of chunk 1 in the second.  Chunks of one value are turned as halves are.  Not turned: 1 and 0.
 template <int E> struct Turn {
     float c[E], s[E];
+    static __device__ __forceinline__ bool across(int style) { return E == 1 || style == CGBN_ROTATE_HALVES; }
     __device__ __forceinline__ void load(const HeadArgs& A, long long token, int p, int c0, int c1)
     {
 #pragma unroll
@@ -99,11 +103,11 @@ template <int E> struct Turn {
         const bool in = pos >= 0 && pos < A.table;
         const long long row = in ? pos * (A.R / 2) : 0;
         const float bad = __int_as_float(0x7fc00000);
-        if (A.style == CGBN_ROTATE_HALVES) {
+        if (across(A.style)) {
             if (c0 < 0 || p >= A.lead) return;
-            load_floats<E>(A.cos + row + c0, c);
-            load_floats<E>(A.sin + row + c0, s);
-        } else {
+            load_floats<E>(A.cos + row + p * E, c);
+            load_floats<E>(A.sin + row + p * E, s);
+        } else if constexpr (E > 1) {
             // (chunks that are turned in part: the angles of those of their pairs that are)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -124,7 +128,7 @@ template <int E> struct Turn {
         if (!in) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const bool turned = A.style == CGBN_ROTATE_HALVES || (e < E / 2 ? c0 >= 0 && c0 + 2 * e < A.R : c1 >= 0 && c1 + 2 * (e - E / 2) < A.R);
+                const bool turned = across(A.style) || (e < E / 2 ? c0 >= 0 && c0 + 2 * e < A.R : c1 >= 0 && c1 + 2 * (e - E / 2) < A.R);
                 if (turned) c[e] = s[e] = bad;
             }
         }
@@ -132,14 +136,14 @@ template <int E> struct Turn {
     // sign 1: turn; -1: turn back
     template <int SIGN> __device__ __forceinline__ void apply(int style, float (&a)[E], float (&b)[E]) const
     {
-        if (style == CGBN_ROTATE_HALVES) {
+        if (across(style)) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const float u = a[e], v = b[e], t = SIGN * s[e];
                 a[e] = u * c[e] - v * t;
                 b[e] = v * c[e] + u * t;
             }
-        } else {
+        } else if constexpr (E > 1) {
 #pragma unroll
             for (int e = 0; e < E / 2; ++e) {
                 const float t = SIGN * s[e], u = a[2 * e], v = a[2 * e + 1];
@@ -153,7 +157,7 @@ template <int E> struct Turn {
     }
 };
 
-// E values as they are stored: 16 bytes, or 4 bfloat16 where rows or halves go in no whole 16 bytes
+// E values as they are stored: 16 bytes, or fewer where rows or halves do not go in those
 template <typename T, int E> struct Chunk {
     static_assert(E * sizeof(T) == 16, "");
     typedef typename Elem<T>::Raw Raw;
@@ -186,6 +190,40 @@ template <> struct Chunk<bf16_t, 4> {
         if constexpr (NT) __builtin_nontemporal_store(v, reinterpret_cast<u32x2*>(p));
         else *reinterpret_cast<u32x2*>(p) = v;
     }
+};
+
+template <> struct Chunk<bf16_t, 2> {
+    typedef uint32_t Raw;
+    static __device__ __forceinline__ Raw load(const bf16_t* p) { return *reinterpret_cast<const uint32_t*>(p); }
+    static __device__ __forceinline__ void unpack(const Raw& v, float (&f)[2])
+    {
+        f[0] = __uint_as_float(v << 16);
+        f[1] = __uint_as_float(v & 0xffff0000u);
+    }
+    template <bool> static __device__ __forceinline__ void store(bf16_t* p, const float (&f)[2])
+    {
+        *reinterpret_cast<uint32_t*>(p) = f32x2_to_bf16x2(f[0], f[1]);
+    }
+};
+template <> struct Chunk<float, 2> {
+    typedef float2 Raw;
+    static __device__ __forceinline__ Raw load(const float* p) { return *reinterpret_cast<const float2*>(p); }
+    static __device__ __forceinline__ void unpack(const Raw& v, float (&f)[2]) { f[0] = v.x; f[1] = v.y; }
+    template <bool> static __device__ __forceinline__ void store(float* p, const float (&f)[2]) { *reinterpret_cast<float2*>(p) = make_float2(f[0], f[1]); }
+};
+// (bits, as a 32-bit register holds them: a value that is converted where it is loaded, or kept in 16, is waited for there: 80 heads of 39,
+// 15994 tokens, backward 553 and 269 us, and so 170)
+template <> struct Chunk<bf16_t, 1> {
+    typedef uint32_t Raw;
+    static __device__ __forceinline__ Raw load(const bf16_t* p) { return p->bits; }
+    static __device__ __forceinline__ void unpack(const Raw& v, float (&f)[1]) { f[0] = __uint_as_float(v << 16); }
+    template <bool> static __device__ __forceinline__ void store(bf16_t* p, const float (&f)[1]) { Elem<bf16_t>::store1(p, f[0]); }
+};
+template <> struct Chunk<float, 1> {
+    typedef float Raw;
+    static __device__ __forceinline__ Raw load(const float* p) { return *p; }
+    static __device__ __forceinline__ void unpack(const Raw& v, float (&f)[1]) { f[0] = v; }
+    template <bool> static __device__ __forceinline__ void store(float* p, const float (&f)[1]) { *p = f[0]; }
 };
 
 template <typename T, int E> __device__ __forceinline__ typename Chunk<T, E>::Raw load_chunk(const T* row, int c)
@@ -505,23 +543,30 @@ template <typename T> bool plan_chunks(HeadArgs* A, int E, bool backward)
     }
     const int chunks = A->D / E;
     A->lead = A->far = 0;
+    A->step = 1;
     if (A->style == CGBN_ROTATE_HALVES && A->R) {
         if ((A->R / 2) % E != 0) return false;
         A->lead = A->far = A->R / 2 / E;
+    } else if (E == 1 && A->R) {                // a pair is two chunks side by side
+        A->lead = A->R / 2;
+        A->step = 2;
+        A->far = 1;
     }
     A->rest = chunks - 2 * A->lead;
     A->pairs = A->lead + (A->rest + 1) / 2;
     return A->pairs <= kWave;
 }
 
-int lanes_of(int pairs)
+// (rows in chunks of one or two values are no shorter than that: where one is, its lanes idle)
+template <int E> int lanes_of(int pairs)
 {
-    int l = 1;
+    int l = E <= 2 ? 16 : 1;
     while (l < pairs) l *= 2;
     return l;
 }
 
-#define CGBN_LANES(X_) X_(1) X_(2) X_(4) X_(8) X_(16) X_(32) X_(64)
+#define CGBN_LANES(X_) X_(1) X_(2) X_(4) X_(8)
+#define CGBN_LANES_LONG(X_) X_(16) X_(32) X_(64)
 
 // a wavefront takes all heads of its token unless there are too few tokens to fill the device with
 void deal_heads(HeadArgs* A, int G)
@@ -534,22 +579,24 @@ void deal_heads(HeadArgs* A, int G)
 
 template <typename T, int E, bool NT> void launch_forward(HeadArgs& A, hipStream_t st)
 {
-    const int L = lanes_of(A.pairs);
+    const int L = lanes_of<E>(A.pairs);
     deal_heads(&A, kWave / L);
     const dim3 grid((unsigned)((A.T * A.parts + 3) / 4));
 #define CGBN_CASE(L_) \
     case L_: hipLaunchKernelGGL((head_forward<T, E, L_, NT>), grid, dim3(kThreads), 0, st, A); break;
-    switch (L) { CGBN_LANES(CGBN_CASE) }
+    if constexpr (E <= 2) switch (L) { CGBN_LANES_LONG(CGBN_CASE) }
+    else switch (L) { CGBN_LANES(CGBN_CASE) CGBN_LANES_LONG(CGBN_CASE) }
 #undef CGBN_CASE
 }
 
 template <typename T, int E, bool NT> void launch_backward(HeadArgs& A, int groups, size_t lds, hipStream_t st)
 {
-    const int L = lanes_of(A.pairs);
+    const int L = lanes_of<E>(A.pairs);
     deal_heads(&A, kWave / L);
 #define CGBN_CASE(L_) \
     case L_: hipLaunchKernelGGL((head_backward<T, E, L_, NT>), dim3((unsigned)groups), dim3(kThreads), lds, st, A); break;
-    switch (L) { CGBN_LANES(CGBN_CASE) }
+    if constexpr (E <= 2) switch (L) { CGBN_LANES_LONG(CGBN_CASE) }
+    else switch (L) { CGBN_LANES(CGBN_CASE) CGBN_LANES_LONG(CGBN_CASE) }
 #undef CGBN_CASE
 }
 
@@ -572,6 +619,8 @@ template <typename T> cgbn_status run_forward(HeadArgs& A, hipStream_t st)
     constexpr int E = 16 / (int)sizeof(T);
     if (plan_chunks<T>(&A, E, false)) past_caches<T>(A) ? launch_forward<T, E, true>(A, st) : launch_forward<T, E, false>(A, st);
     else if (sizeof(T) == 2 && plan_chunks<T>(&A, 4, false)) launch_forward<T, 4, false>(A, st);
+    else if (plan_chunks<T>(&A, 2, false)) launch_forward<T, 2, false>(A, st);
+    else if (plan_chunks<T>(&A, 1, false)) launch_forward<T, 1, false>(A, st);
     else CGBN_ANY(head_forward_any, (A.T * (A.H[0] + A.H[1]) + 3) / 4, 0);
     return launched();
 }
@@ -583,6 +632,8 @@ template <typename T> cgbn_status run_backward(HeadArgs& A, float* dwq, float* d
     const size_t lds = (size_t)4 * A.D * sizeof(float);
     if (plan_chunks<T>(&A, E, true)) past_caches<T>(A) ? launch_backward<T, E, true>(A, groups, lds, st) : launch_backward<T, E, false>(A, groups, lds, st);
     else if (sizeof(T) == 2 && plan_chunks<T>(&A, 4, true)) launch_backward<T, 4, false>(A, groups, lds, st);
+    else if (plan_chunks<T>(&A, 2, true)) launch_backward<T, 2, false>(A, groups, lds, st);
+    else if (plan_chunks<T>(&A, 1, true)) launch_backward<T, 1, false>(A, groups, lds, st);
     else CGBN_ANY(head_backward_any, groups, lds);
     if (launched() != CGBN_OK) return CGBN_ERR_HIP;
     const int n = A.H[1] ? 2 * A.D : A.D;

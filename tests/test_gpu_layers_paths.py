@@ -96,6 +96,34 @@ def test_rows_in_chunks_of_8_bytes(shape, lead, gap, style):
     p.check_backward()
 
 
+@pytest.mark.parametrize("style", ["halves", "interleaved"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape,lead,gap", [((60, 5, 3, 39, 0), 0, 0), ((60, 5, 3, 39, 38), 0, 0), ((60, 5, 3, 39, 20), 1, 0), ((40, 9, 2, 82, 40), 0, 0), ((40, 9, 2, 82, 42), 2, 4),
+                                            ((33, 3, 1, 127, 126), 0, 0), ((33, 3, 1, 128, 2), 3, 0), ((17, 3, 1, 129, 128), 0, 0), ((17, 3, 1, 254, 250), 0, 2),
+                                            ((9, 40, 2, 3, 2), 0, 0), ((5000, 2, 1, 33, 32), 0, 0), ((1, 1, 1, 35, 34), 0, 0)], ids=str)
+def test_rows_in_chunks_of_two_values_and_of_one(shape, lead, gap, dtype, style):
+    p = Heads(*shape, style, dtype, lead, gap)
+    p.check_forward()
+    p.check_backward()
+
+
+@pytest.mark.parametrize("shape", [(40, 6, 2, 39, 38), (40, 6, 2, 82, 40)], ids=str)
+def test_odd_heads_in_place_and_outside_the_table(shape):
+    for style in ("halves", "interleaved"):
+        p = Heads(*shape, style, "bf16")
+        y, (dx, dwq, dwk) = p.forward(), p.backward()
+        p.pos[3], p.pos[7] = -1, p.cos.shape[0]
+        bad = p.forward()[:, :p.nq + p.nk].view(40, 8, p.D)
+        assert not torch.isfinite(bad[[3, 7], :, :p.R]).any() and torch.equal(bad[:3], y[:3, :p.nq + p.nk].view(3, 8, p.D))
+        assert torch.equal(bad[3, :, p.R:], y[3, :p.nq + p.nk].view(8, p.D)[:, p.R:])
+        p = Heads(*shape, style, "bf16")
+        keep = p.x.clone()
+        assert torch.equal(p.forward(out=p.x)[:, :p.nq + p.nk], y[:, :p.nq + p.nk])
+        p.x.copy_(keep)
+        got, gq, gk = p.backward(dx=p.dy)
+        assert torch.equal(got[:, :p.nq + p.nk], dx[:, :p.nq + p.nk]) and torch.equal(gq, dwq) and torch.equal(gk, dwk)
+
+
 @pytest.mark.parametrize("shape,dtype", [((2000, 40, 32, 128, 64), "bf16"), ((1100, 70, 2, 256, 256), "bf16"), ((3000, 30, 6, 80, 32), "f32"),
                                          ((3001, 70, 2, 80, 40), "bf16")], ids=str)
 def test_large_norms(shape, dtype):
