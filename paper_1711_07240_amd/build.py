@@ -4,8 +4,10 @@ The host code and the multi-sweep kernels are one translation unit; the NCHW
 single-launch kernels are instantiated in ten more (element type x direction
 x activation), the column-slab kernels in eight (element type x direction x
 register limit),
-compiled side by side, then everything is linked into one shared library.  The
-binding's extension is one C file."""
+compiled side by side; the layers beside the normalization are a unit for their
+host code and small kernels, one for the head norm, and six for the matrix
+products (element type x forward, gated, backward).  Then everything is linked
+into one shared library.  The binding's extension is one C file."""
 
 from __future__ import annotations
 

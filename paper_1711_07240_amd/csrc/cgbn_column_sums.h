@@ -8,7 +8,7 @@ namespace {
 
 // Sums over `rows` of part[row * ld + n], n < N, in double precision: n < n0 to out0, the others to out1.  A workgroup takes 16
 // columns (64 bytes a row) with 64 threads each, a thread's rows eight at a time: the sums are few and what they take is the
-// loads' way.
+// loads' way (1023 rows of 128: 7 us, 512 of 160: 4.7; a launch is 3 of them).
 constexpr int kSumThreads = 1024;
 __global__ __launch_bounds__(kSumThreads) void column_sums(const float* part, int rows, int ld, int N, float* out0, int n0, float* out1)
 {

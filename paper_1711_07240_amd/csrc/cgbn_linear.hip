@@ -23,7 +23,8 @@ template <typename T, int E> __device__ __forceinline__ void load_end(const T* p
     for (int k = 0; k < E; ++k) v[k] = k < valid ? v[k] : 0.f;
 }
 
-// rows of n elements to rows of np, the filling zero: operands whose rows do not start on 16 bytes
+// rows of n elements to rows of np, the filling zero: operands whose rows do not start on 16 bytes, which a load to LDS has to.  Bound by memory
+// where it is not the launch, 3 us (6832 x 267 float, 7.3 MB read and written, 5.8 us).
 template <typename T> __global__ __launch_bounds__(kThreads) void pad_rows(const T* src, T* dst, long long rows, int n, int np)
 {
     constexpr int E = 16 / (int)sizeof(T);
@@ -52,8 +53,10 @@ struct DzArgs {
     int tw, rows;                  // vectors of a row that a workgroup covers (a power of two, at most 64); rows of a block
 };
 
-// dz = dy * act'(saved), and its column sums.  Memory bound: one read of dy and saved, one write of dz.  A thread stays in
-// one column vector and walks rows; its sums are of at most rows * tw / 256 values, in float.
+// dz = dy * act'(saved), and its column sums.  Memory bound: one read of dy and saved, one write of dz (268800 x 128 bfloat16, ReLU: 38
+// us, 5.4 TB/s).  A thread stays in one column vector and walks rows; its sums are of at most rows * tw / 256 values, in float, and column_sums
+// adds those of the workgroups.  dz is rounded to the operands' type, which is what the matrix cores multiply: half the bytes of a float dz,
+// written once and read twice; the column sums are of the values before it.
 template <typename T> __global__ __launch_bounds__(kThreads) void linear_dz(const DzArgs A)
 {
     constexpr int E = 16 / (int)sizeof(T);
@@ -128,7 +131,7 @@ struct GateArgs {
 };
 
 // dg = dh * up * act'(gate), du = dh * act(gate), rounded to the operands' type for the products that follow (as they would be
-// had they been tensors of the layer): memory bound, three reads and two writes.
+// had they been tensors of the layer): memory bound, three reads and two writes (5003 x 5461 bfloat16, rows on no 16 bytes, GELU: 48 us, 5.7 TB/s).
 template <typename T> __global__ __launch_bounds__(kThreads) void gated_dz(const GateArgs A)
 {
     constexpr int E = 16 / (int)sizeof(T);
