@@ -29,8 +29,38 @@ template <typename T> __device__ __forceinline__ u32x4 row_chunk(const T* p, int
     return v;
 }
 
-// FM: 16-row blocks of x; NW: wavefronts
-template <typename T, bool GATED, int FM, int NW>
+// 16 bytes of an operand's row, of a step that lies within the row.  HALF: of rows of an odd number of bfloat16, every other one of which starts
+// between two words, where a load takes twice as long.  The words from the one it starts in, and one more, which holds the row's own last value of
+// the 8 and the next (the row has one: its length is odd, whole steps are even); rows that start on a word ask for their last word again instead.
+template <typename T, bool HALF> struct RowPiece {
+    u32x4 v;
+    uint32_t next;
+    __device__ __forceinline__ void load(const T* p)
+    {
+        if constexpr (HALF) {
+            typedef uint32_t u32x4_word __attribute__((ext_vector_type(4), aligned(4)));
+            const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(p) & 2;
+            const char* const a = reinterpret_cast<const char*>(p) - off;
+            v = *reinterpret_cast<const u32x4_word*>(a);
+            next = *reinterpret_cast<const uint32_t*>(a + 12 + 2 * off);
+        } else {
+            v = *reinterpret_cast<const u32x4_any*>(p);
+        }
+    }
+    __device__ __forceinline__ u32x4 get(const T* p) const
+    {
+        if constexpr (HALF) {
+            const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(p) & 2;
+            return u32x4{__builtin_amdgcn_alignbyte(v[1], v[0], off), __builtin_amdgcn_alignbyte(v[2], v[1], off), __builtin_amdgcn_alignbyte(v[3], v[2], off),
+                         __builtin_amdgcn_alignbyte(next, v[3], off)};
+        } else {
+            return v;
+        }
+    }
+};
+
+// FM: 16-row blocks of x; NW: wavefronts; HALF: see RowPiece
+template <typename T, bool GATED, int FM, int NW, bool HALF>
 __global__ __launch_bounds__(NW * kWave) void gemm_rows(const GemmArgs G)
 {
     constexpr int E = 16 / (int)sizeof(T), STEP = 8 * E, P = GATED ? 2 : 1, U = FM == 1 && !GATED ? 4 : 2;
@@ -51,16 +81,16 @@ __global__ __launch_bounds__(NW * kWave) void gemm_rows(const GemmArgs G)
     const int begin = (int)blockIdx.y * G.per, steps = min(begin + G.per, (G.R + STEP - 1) / STEP), full = min(steps, G.R / STEP);
     int s = begin + wave;
     for (; s + (U - 1) * NW < full; s += U * NW) {
-        u32x4 w[U][P][2], x[U][FM][2];
+        RowPiece<T, HALF> w[U][P][2], x[U][FM][2];
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int r = (s + u * NW) * STEP + h * 4 * E;
 #pragma unroll
-                for (int p = 0; p < P; ++p) w[u][p][h] = row_chunk<T>(pw[p] + r, E);
+                for (int p = 0; p < P; ++p) w[u][p][h].load(pw[p] + r);
 #pragma unroll
-                for (int m = 0; m < FM; ++m) x[u][m][h] = row_chunk<T>(px[m] + r, E);
+                for (int m = 0; m < FM; ++m) x[u][m][h].load(px[m] + r);
             }
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -69,18 +99,25 @@ __global__ __launch_bounds__(NW * kWave) void gemm_rows(const GemmArgs G)
 #pragma unroll
                 for (int p = 0; p < P; ++p)
 #pragma unroll
-                    for (int m = 0; m < FM; ++m) acc[p][m] = multiply<T>(w[u][p][h], x[u][m][h], acc[p][m]);
+                    for (int m = 0; m < FM; ++m) acc[p][m] = multiply<T>(w[u][p][h].get(pw[p]), x[u][m][h].get(px[m]), acc[p][m]);
     }
     for (; s < steps; s += NW) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int r = s * STEP + h * 4 * E, left = G.R - r - q * E;
+            const bool whole = HALF && s < full;
+            auto chunk = [&](const T* row) {
+                if (!whole) return row_chunk<T>(row + r, left);
+                RowPiece<T, HALF> piece;
+                piece.load(row + r);
+                return piece.get(row);
+            };
             u32x4 x[FM];
 #pragma unroll
-            for (int m = 0; m < FM; ++m) x[m] = row_chunk<T>(px[m] + r, left);
+            for (int m = 0; m < FM; ++m) x[m] = chunk(px[m]);
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const u32x4 w = row_chunk<T>(pw[p] + r, left);
+                const u32x4 w = chunk(pw[p]);
 #pragma unroll
                 for (int m = 0; m < FM; ++m) acc[p][m] = multiply<T>(w, x[m], acc[p][m]);
             }

@@ -314,7 +314,12 @@ template <typename T, bool GATED> hipError_t launch_rows(const GemmArgs& G, hipS
     // 16 wavefronts, each with all of its loads in flight at once or twice, where there are steps for them: 8.0 against 8.5 us with 8 of
     // them (one row, 4096 x 4096); with few steps they only wait for each other: 3.3 with 4 against 3.6 us (1024 x 1024)
     const bool many = (long long)G.R * (int)sizeof(T) >= 32 * 128;
-#define CGBN_ROWS(FM_, NW_) hipLaunchKernelGGL((gemm_rows<T, GATED, FM_, NW_>), grid, dim3(NW_ * kWave), 0, st, G)
+    const bool half = sizeof(T) == 2 && G.R % 2 != 0;
+#define CGBN_ROWS(FM_, NW_)                                                                                             \
+    do {                                                                                                                \
+        if (sizeof(T) == 2 && half) hipLaunchKernelGGL((gemm_rows<T, GATED, FM_, NW_, sizeof(T) == 2>), grid, dim3(NW_ * kWave), 0, st, G); \
+        else hipLaunchKernelGGL((gemm_rows<T, GATED, FM_, NW_, false>), grid, dim3(NW_ * kWave), 0, st, G);              \
+    } while (0)
     if (G.I <= 16 && many && sizeof(T) == 4) CGBN_ROWS(1, 8);          // 16.9 against 18.3 us (8 rows, 4096 x 4096)
     else if (G.I <= 16 && many) CGBN_ROWS(1, 16);
     else if (G.I <= 16) CGBN_ROWS(1, 4);

@@ -31,6 +31,14 @@ def test_few_rows_of_a_long_gated_reduction(size, dtype):
     p.check_forward("gelu", save=False)
 
 
+@pytest.mark.parametrize("size", [(1, 1, 65), (1, 17, 127), (3, 33, 1025), (8, 40, 4069), (16, 50, 2113), (17, 100, 1001), (32, 31, 4097), (2, 16, 8193)], ids=str)
+def test_few_rows_of_odd_length(size):
+    Linear(*size, "bf16").check_forward("silu")
+    p = Linear(*size, "bf16", seed=1)
+    p.check_forward("none", bias=False, residual=False, save=False)
+    Gated(*size, "bf16").check_forward("gelu")
+
+
 @pytest.mark.parametrize("size,dtype", [((17, 8192, 4096), "bf16"), ((31, 6000, 4104), "bf16"), ((32, 4097, 4100), "bf16"), ((32, 8192, 4096), "f32")],
                          ids=str)
 def test_some_rows_with_large_weights(size, dtype):
