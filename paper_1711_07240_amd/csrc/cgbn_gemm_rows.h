@@ -13,18 +13,23 @@
 
 namespace cgbn {
 
-// 16 bytes of an operand's row, zero beyond `left` elements
+// 16 bytes of an operand's row of which `left` elements remain (none or fewer: the row ended before); zeros beyond.  What is not there is the row's
+// last element again, so that no branch keeps one load from following the other.
 template <typename T> __device__ __forceinline__ u32x4 row_chunk(const T* p, int left)
 {
     constexpr int E = 16 / (int)sizeof(T);
     if (left >= E) return *reinterpret_cast<const u32x4_any*>(p);
-    u32x4 v = {0, 0, 0, 0};
+    uint32_t t[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        if (e < left) {
-            if constexpr (sizeof(T) == 2) v[e / 2] |= (uint32_t)p[e].bits << (16 * (e & 1));
-            else v[e] = __float_as_uint(p[e]);
-        }
+        if constexpr (sizeof(T) == 2) t[e] = p[min(e, left - 1)].bits;
+        else t[e] = __float_as_uint(p[min(e, left - 1)]);
+    }
+    u32x4 v;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if constexpr (sizeof(T) == 2) v[k] = (2 * k < left ? t[2 * k] : 0) | (2 * k + 1 < left ? t[2 * k + 1] << 16 : 0);
+        else v[k] = k < left ? t[k] : 0;
     }
     return v;
 }
