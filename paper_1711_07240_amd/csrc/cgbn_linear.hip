@@ -238,9 +238,11 @@ ForwardPlan plan_forward(long long M, int N, int K, int dtype, bool gated)
     Layout l;
     if (p.rows) {
         // Workgroups of 16 weight rows; where those are too few for the device and long, several share them: 23.4 us by 4 workgroups,
-        // 7.2 by 40 (the gated pair, 2 x 5248 x 64, float), and 11.5 by 64, 9.4 by 256 (1 x 8192 x 1024, bfloat16)
+        // 7.2 by 40 (the gated pair, 2 x 5248 x 64, float); bfloat16, 1 x 4096 x 64 6.5 and 5.4, 16 x 4096 x 256 9.1 and 6.4, gated 13.2 and
+        // 8.0.  Not for less: 16 x 3008 x 256 is 7.4 and 7.0, 1 x 2048 x 256 4.5 and 5.3.  Where only two can, the joining has to pay: 1 x 4096 x 2048 7.3
+        // and 9.3; 1 x 8192 x 1024 11.5 and 9.4.
         const int steps = (K * W.elem + 127) / 128, groups = (N + 15) / 16;
-        int want = groups <= 128 && steps >= 96 ? 256 / groups : 1;
+        int want = groups <= 128 && steps >= (groups <= 64 || gated ? 48 : 96) ? 256 / groups : 1;
         if (want > steps / 16) want = steps / 16 > 1 ? steps / 16 : 1;
         p.g.per = (steps + want - 1) / want;
         p.g.splits = (steps + p.g.per - 1) / p.g.per;
