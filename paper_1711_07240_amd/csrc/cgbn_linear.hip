@@ -23,19 +23,30 @@ template <typename T, int E> __device__ __forceinline__ void load_end(const T* p
     for (int k = 0; k < E; ++k) v[k] = k < valid ? v[k] : 0.f;
 }
 
-// rows of n elements to rows of np, the filling zero: operands whose rows do not start on 16 bytes, which a load to LDS has to.  Bound by memory
-// where it is not the launch, 3 us (6832 x 267 float, 7.3 MB read and written, 5.8 us).
-template <typename T> __global__ __launch_bounds__(kThreads) void pad_rows(const T* src, T* dst, long long rows, int n, int np)
+// Rows of n elements to rows of np, the filling zero: operands whose rows do not start on 16 bytes, which a load to LDS has to.  All operands of a
+// call in one launch.  Bound by memory where it is not the launch, 3 us (6832 x 267 float, 7.3 MB read and written, 5.8 us).
+struct PadArgs {
+    const void* src[3];
+    void* dst[3];
+    long long end[3];              // 16-byte chunks up to the end of each operand
+    int n, np;
+};
+template <typename T> __global__ __launch_bounds__(kThreads) void pad_rows(const PadArgs A)
 {
     constexpr int E = 16 / (int)sizeof(T);
-    const int chunks = np / E;
-    const long long id = (long long)blockIdx.x * kThreads + threadIdx.x;
-    if (id >= rows * chunks) return;
+    const int chunks = A.np / E;
+    long long id = (long long)blockIdx.x * kThreads + threadIdx.x;
+    if (id >= A.end[2]) return;
+    const int k = id < A.end[0] ? 0 : id < A.end[1] ? 1 : 2;
+    id -= k == 0 ? 0 : k == 1 ? A.end[0] : A.end[1];
+    const T* const src = static_cast<const T*>(k == 0 ? A.src[0] : k == 1 ? A.src[1] : A.src[2]);
+    T* const dst = static_cast<T*>(k == 0 ? A.dst[0] : k == 1 ? A.dst[1] : A.dst[2]);
     const long long r = id / chunks;
-    const int c = (int)(id - r * chunks) * E;
+    const int c = (int)(id - r * chunks) * E, valid = A.n - c;
     float v[E];
-    load_run<T, E>(src + r * n + c, v, n - c);
-    store_run<T, E>(dst + r * np + c, v, E);
+    if (valid >= E) load_run<T, E>(src + r * A.n + c, v, valid);
+    else load_end<T, E>(src + r * A.n + c, v, valid);
+    store_run<T, E>(dst + r * A.np + c, v, E);
 }
 
 // the E values of a run: one decision for all of them
@@ -302,13 +313,29 @@ cgbn_status check_workspace(size_t need, const void* workspace, size_t have)
     return CGBN_OK;
 }
 
-template <typename T> hipError_t pad(const void* src, void* dst, long long rows, int n, int np, hipStream_t st)
-{
-    const long long ids = rows * (np / (16 / (int)sizeof(T)));
-    hipLaunchKernelGGL(pad_rows<T>, dim3((unsigned)((ids + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, static_cast<const T*>(src),
-                       static_cast<T*>(dst), rows, n, np);
-    return hipGetLastError();
-}
+// the operands of a call that are laid out anew, one after the other
+struct Pads {
+    PadArgs A;
+    int count;
+    Pads() { std::memset(this, 0, sizeof(*this)); }
+    // (three at the most: x and a gated pair's weights)
+    const void* add(const void* src, void* dst, long long rows, int chunks)
+    {
+        A.src[count] = src;
+        A.dst[count] = dst;
+        for (int k = 2; k > count; --k) A.end[k] += rows * chunks;
+        A.end[count++] += rows * chunks;
+        return dst;
+    }
+    template <typename T> hipError_t launch(int n, int np, hipStream_t st)
+    {
+        if (count == 0) return hipSuccess;
+        A.n = n;
+        A.np = np;
+        hipLaunchKernelGGL(pad_rows<T>, dim3((unsigned)((A.end[2] + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, A);
+        return hipGetLastError();
+    }
+};
 
 template <typename T, bool GATED> hipError_t launch_rows(const GemmArgs& G, hipStream_t st)
 {
@@ -347,14 +374,11 @@ cgbn_status forward(GemmArgs G, const ForwardPlan& p, char* ws, hipStream_t st)
         return CGBN_OK;
     }
     if (W.odd(K)) {
-        const int kp = W.padded(K);
-        CGBN_HIP(pad<T>(G.A[0], ws + p.x, G.I, K, kp, st));
-        G.A[0] = ws + p.x;
-        for (int k = 0; k < (GATED ? 2 : 1); ++k) {
-            char* to = ws + p.w + (size_t)k * G.J * kp * sizeof(T);
-            CGBN_HIP(pad<T>(G.B[k], to, G.J, K, kp, st));
-            G.B[k] = to;
-        }
+        const int kp = W.padded(K), chunks = kp / W.E;
+        Pads pads;
+        G.A[0] = pads.add(G.A[0], ws + p.x, G.I, chunks);
+        for (int k = 0; k < (GATED ? 2 : 1); ++k) G.B[k] = pads.add(G.B[k], ws + p.w + (size_t)k * G.J * kp * sizeof(T), G.J, chunks);
+        CGBN_HIP(pads.launch<T>(K, kp, st));
         G.lda = G.ldb = kp;
     }
     CGBN_HIP((launch_gemm<T, FORM_NT, GATED>(p.g, G, st)));
@@ -368,6 +392,7 @@ cgbn_status products(const void* const dz[2], int ldz, int pairs, const void* x,
 {
     const Widths W(sizeof(T) == 4 ? CGBN_F32 : CGBN_BF16);
     const int kp = W.padded(K);
+    Pads pads;
     GemmArgs X, G;              // dx, dW
     std::memset(&X, 0, sizeof(X));
     X.J = K;
@@ -377,14 +402,7 @@ cgbn_status products(const void* const dz[2], int ldz, int pairs, const void* x,
     G = X;
     for (int k = 0; k < pairs; ++k) X.A[k] = G.A[k] = dz[k];
     if (dx) {
-        for (int k = 0; k < pairs; ++k) {
-            X.B[k] = w[k];
-            if (W.odd(K)) {
-                char* to = ws + p.w + (size_t)k * N * kp * sizeof(T);
-                CGBN_HIP(pad<T>(w[k], to, N, K, kp, st));
-                X.B[k] = to;
-            }
-        }
+        for (int k = 0; k < pairs; ++k) X.B[k] = W.odd(K) ? pads.add(w[k], ws + p.w + (size_t)k * N * kp * sizeof(T), N, kp / W.E) : w[k];
         X.C[0] = dx;
         X.I = (int)M;
         X.R = N;
@@ -393,10 +411,7 @@ cgbn_status products(const void* const dz[2], int ldz, int pairs, const void* x,
         X.part = reinterpret_cast<float*>(ws + p.part_x);
     }
     if (dw[0]) {
-        if (W.odd(K)) {
-            CGBN_HIP(pad<T>(x, ws + p.x, M, K, kp, st));
-            x = ws + p.x;
-        }
+        if (W.odd(K)) x = pads.add(x, ws + p.x, M, kp / W.E);
         for (int k = 0; k < pairs; ++k) {
             G.B[k] = x;
             G.C[k] = dw[k];
@@ -407,6 +422,7 @@ cgbn_status products(const void* const dz[2], int ldz, int pairs, const void* x,
         G.batch = pairs;
         G.part = reinterpret_cast<float*>(ws + p.part_w);
     }
+    CGBN_HIP(pads.launch<T>(K, kp, st));
     if (dx && dw[0]) CGBN_HIP(launch_two<T>(p.dx, X, p.dw, G, st));
     else if (dx) CGBN_HIP((launch_gemm<T, FORM_NN, false>(p.dx, X, st)));
     else if (dw[0]) CGBN_HIP((launch_gemm<T, FORM_TN, false>(p.dw, G, st)));
