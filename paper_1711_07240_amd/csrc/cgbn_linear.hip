@@ -68,7 +68,8 @@ struct DzArgs {
 // us, 5.4 TB/s).  A thread stays in one column vector and walks rows; its sums are of at most rows * tw / 256 values, in float, and column_sums
 // adds those of the workgroups.  dz is rounded to the operands' type, which is what the matrix cores multiply: half the bytes of a float dz,
 // written once and read twice; the column sums are of the values before it.
-template <typename T> __global__ __launch_bounds__(kThreads) void linear_dz(const DzArgs A)
+// ENDS: rows are no whole number of vectors.  (A kernel each: the registers that ends are loaded to cost the others 209 us for 205.)
+template <typename T, bool ENDS> __global__ __launch_bounds__(kThreads) void linear_dz(const DzArgs A)
 {
     constexpr int E = 16 / (int)sizeof(T);
     __shared__ float red[kThreads * E];
@@ -94,31 +95,27 @@ template <typename T> __global__ __launch_bounds__(kThreads) void linear_dz(cons
             if (A.dz) store_run<T, E>(static_cast<T*>(A.dz) + r * A.ld + c, g, E);
             if (A.dresidual) store_run<T, E>(static_cast<T*>(A.dresidual) + r * A.N + c, g, valid);
         };
-        if (valid >= E) {
-            // four rows at a time: the loads of all before the first is used (the last row's again where there are fewer)
-            constexpr int U = 4;
-            for (long long r = r0 + first; r < r1; r += U * stride) {
-                u32x4 wg[U], wz[U];
+        // four rows at a time: the loads of all before the first is used (the last row's again where there are fewer)
+        constexpr int U = 4;
+        for (long long r = r0 + first; r < r1; r += U * stride) {
+            u32x4 wg[U], wz[U];
+            auto load = [&](const T* p, u32x4 (&w)[U]) {
+                if (!ENDS || valid >= E) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) wg[u] = load_once(dy + min(r + u * stride, r1 - 1) * A.N);
-                if (A.saved) {
+                    for (int u = 0; u < U; ++u) w[u] = load_once(p + min(r + u * stride, r1 - 1) * A.N);
+                } else {
 #pragma unroll
-                    for (int u = 0; u < U; ++u) wz[u] = load_once(saved + min(r + u * stride, r1 - 1) * A.N);
+                    for (int u = 0; u < U; ++u) w[u] = row_chunk<T>(p + min(r + u * stride, r1 - 1) * A.N, valid);
                 }
+            };
+            load(dy, wg);
+            if (A.saved) load(saved, wz);
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    float g[E], z[E];
-                    unpack_run<T>(wg[u], g);
-                    unpack_run<T>(wz[u], z);
-                    if (r + u * stride < r1) row(r + u * stride, g, z);
-                }
-            }
-        } else {
-            for (long long r = r0 + first; r < r1; r += stride) {
+            for (int u = 0; u < U; ++u) {
                 float g[E], z[E];
-                load_run<T, E>(dy + r * A.N, g, valid);
-                if (A.saved) load_run<T, E>(saved + r * A.N, z, valid);
-                row(r, g, z);
+                unpack_run<T>(wg[u], g);
+                unpack_run<T>(wz[u], z);
+                if (r + u * stride < r1) row(r + u * stride, g, z);
             }
         }
     }
@@ -472,7 +469,8 @@ cgbn_status linear_backward(const void* dy, const void* x, const void* w, const 
         A.tw = p.tw; A.rows = p.sum_rows;
         const int vecs = np / W.E;
         const dim3 grid((unsigned)((vecs + p.tw - 1) / p.tw), (unsigned)p.sum_blocks);
-        hipLaunchKernelGGL(linear_dz<T>, grid, dim3(kThreads), 0, st, A);
+        if (W.odd(N)) hipLaunchKernelGGL((linear_dz<T, true>), grid, dim3(kThreads), 0, st, A);
+        else hipLaunchKernelGGL((linear_dz<T, false>), grid, dim3(kThreads), 0, st, A);
         CGBN_HIP(hipGetLastError());
         if (dbias) {
             hipLaunchKernelGGL(column_sums, dim3((unsigned)((N + 15) / 16)), dim3(kSumThreads), 0, st, A.part, p.sum_blocks, N, N, dbias, N, nullptr);
