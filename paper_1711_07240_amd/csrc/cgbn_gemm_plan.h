@@ -92,8 +92,8 @@ inline double cost_of(const GemmPlan& p, double groups)
 
 template <typename F> inline void each_split(long long steps, F f)
 {
-    // (a split of fewer than four steps is all prologue)
-    for (long long want = 1; want == 1 || (want <= 256 && steps / want >= 4); want = want < 4 ? want + 1 : want + want / 4)
+    // (a split of fewer than four steps is all prologue; powers of two fill 256 compute units evenly)
+    for (long long want = 1, by = 1; want == 1 || (want <= 256 && steps / want >= 4); want += by, by = want >= 8 * by ? 2 * by : by)
         if (!f(want)) break;
 }
 
