@@ -699,7 +699,7 @@ __global__ __launch_bounds__(WI * WJ * kWave, tile_waves(BI * BJ / (WI * WJ))) v
 
 // Partial sums of a split reduction, added in a fixed order, then the epilogue.  N values a thread (4 where J allows whole vectors).
 // Where there are few values and many splits, `lanes` threads (a power of two) share a value's splits: 128 x 512 values of 120
-// splits took 31 us with one thread each, 7 with several; 512 x 1024 values of few splits want one (85.5 us with the product, 90 with two).
+// splits took 31 us with one thread each, 7 with several; 512 x 1024 values of few splits want one (85 us with the product, 90 with two).
 template <typename T, int FORM, bool GATED, int N>
 __global__ __launch_bounds__(kThreads) void gemm_join(const GemmArgs G, int lanes)
 {
