@@ -226,3 +226,52 @@ def test_norm_gradients_against_differences(style):
     loss()
     dx, dwq, dwk = p.backward()
     _check(loss, [("x", p.x, dx), ("wq", p.wq, dwq), ("wk", p.wk, dwk)], 16, p.dy, y)
+
+
+@pytest.mark.parametrize("size", [(98400, 512, 64), (66000, 767, 1000), (16500, 1024, 40), (20, 1000, 8191)], ids=str)
+def test_results_over_the_residual(size):
+    """y may be the residual's own buffer: the same bits as elsewhere, and the same in every run."""
+    M, N, K = size
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    x, w, res = (torch.randn(a, b, device=DEV, generator=gen).to(torch.bfloat16) for a, b in ((M, K), (N, K), (M, N)))
+    ws = torch.empty(L.cgbn_linear_workspace_bytes(M, N, K, "bf16", False), dtype=torch.uint8, device=DEV)
+    y = torch.empty_like(res)
+    L.cgbn_linear_forward(x, w, None, res, M, N, K, "relu", y, None, "bf16", ws)
+    for _ in range(3):
+        over = res.clone()
+        L.cgbn_linear_forward(x, w, None, over, M, N, K, "relu", over, None, "bf16", ws)
+        assert torch.equal(over, y)
+
+
+def test_graph_replays_of_shared_and_padded_work():
+    """Few rows of a long odd reduction, padded operands, dx split beside dW, odd heads: captured once, replayed with other work between."""
+    calls, outs = [], []
+    gen = torch.Generator(device=DEV).manual_seed(8)
+    rand = lambda *s: torch.randn(*s, device=DEV, generator=gen).to(torch.bfloat16)
+    for M, N, K in ((3, 64, 4069), (300, 264, 131), (64, 2048, 512)):
+        x, w, dy, b = rand(M, K), rand(N, K), rand(M, N), torch.randn(N, device=DEV, generator=gen)
+        y, z, dx, dw, db = torch.empty_like(dy), torch.empty_like(dy), torch.empty_like(x), torch.empty_like(w), torch.empty_like(b)
+        ws = torch.empty(max(L.cgbn_linear_workspace_bytes(M, N, K, "bf16", k) for k in (False, True)), dtype=torch.uint8, device=DEV)
+        calls.append(lambda M=M, N=N, K=K, x=x, w=w, dy=dy, b=b, y=y, z=z, dx=dx, dw=dw, db=db, ws=ws: (
+            L.cgbn_linear_forward(x, w, b, None, M, N, K, "silu", y, z, "bf16", ws),
+            L.cgbn_linear_backward(dy, x, w, z, M, N, K, "silu", dx, dw, db, None, "bf16", ws)))
+        outs += [y, z, dx, dw, db]
+    p = Heads(40, 5, 3, 39, 38, "halves", "bf16")
+    heads = torch.zeros_like(p.x)
+    (q, k), (yq, yk) = p.split(p.x), p.split(heads)
+    calls.append(lambda: L.cgbn_head_norm_forward(q, p.row, k, p.row, p.T, p.Hq, p.Hk, p.D, *p.turn(), p.wq, p.wk, 1e-5, yq, p.row, yk, p.row, "bf16"))
+    outs.append(heads)
+    for call in calls:
+        call()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outs]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        for call in calls:
+            call()
+    for _ in range(4):
+        for t in outs[:-1]:
+            t.fill_(3.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
