@@ -72,8 +72,10 @@ __device__ __forceinline__ float normal_tail(float z, float e)
 __device__ __forceinline__ float act_apply(float z, int act)
 {
     if (act == ACT_RELU) return z < 0.f ? 0.f : z;
-    // z Phi(z), which is z - z Phi(-z); the positive part by its bits, as an integer (where z is NaN the other term is)
-    if (act == ACT_GELU) return fmaf(-fabsf(z), normal_tail(z, bell(z)), __int_as_float(max(__float_as_int(z), 0)));
+    // z Phi(z), which is z - z Phi(-z); the positive part by its bits, as an integer (where z is NaN the other term is).  Where z is large the tail is
+    // zero, and what it is multiplied by is kept finite, by its bits too, for an infinite z.
+    if (act == ACT_GELU)
+        return fmaf(-fabsf(__int_as_float(min(__float_as_int(z), 0x7149f2ca))), normal_tail(z, bell(z)), __int_as_float(max(__float_as_int(z), 0)));
     if (act == ACT_SILU) return z * __builtin_amdgcn_rcpf(1.f + exp_of(-z));
     return z;
 }

@@ -1,0 +1,67 @@
+"""The layers beside the normalization where values, sizes or buffers are at an end of what they may be."""
+
+import pytest
+import torch
+
+from layers_harness import DEV, TORCH, Linear
+from paper_1711_07240_amd import cgbn as L
+
+pytestmark = pytest.mark.gpu
+INF = float("inf")
+
+
+def _linear(x, w, bias, act, dtype, z=None):
+    M, K, N = *x.shape, w.shape[0]
+    y = torch.full((M, N), 7.0, dtype=TORCH[dtype], device=DEV)
+    ws = torch.empty(L.cgbn_linear_workspace_bytes(M, N, K, dtype, False), dtype=torch.uint8, device=DEV)
+    L.cgbn_linear_forward(x, w, bias, None, M, N, K, act, y, z, dtype, ws)
+    return y
+
+
+def _backward(dy, x, w, dtype, saved=None, act="none", dresidual=None):
+    M, N, K = *dy.shape, x.shape[1]
+    dx, dw = torch.full_like(x, 7.0), torch.full_like(w, 7.0)
+    ws = torch.empty(L.cgbn_linear_workspace_bytes(M, N, K, dtype, True), dtype=torch.uint8, device=DEV)
+    L.cgbn_linear_backward(dy, x, w, saved, M, N, K, act, dx, dw, None, dresidual, dtype, ws)
+    return dx, dw
+
+
+def _gated(x, wg, wu, act, dtype, gate=None, up=None):
+    M, K, N = *x.shape, wg.shape[0]
+    h = torch.full((M, N), 7.0, dtype=TORCH[dtype], device=DEV)
+    ws = torch.empty(L.cgbn_gated_workspace_bytes(M, N, K, dtype, False), dtype=torch.uint8, device=DEV)
+    L.cgbn_gated_forward(x, wg, wu, M, N, K, act, h, gate, up, dtype, ws)
+    return h
+
+
+# few rows, few rows shared by workgroups, tiles, a split reduction
+WAYS = [(5, 40, 64), (2, 64, 8192), (140, 72, 96), (70, 64, 8192)]
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu", "relu"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", WAYS, ids=str)
+def test_activations_at_the_ends(size, dtype, act):
+    """z Phi(z) and its like of +infinity are infinite, of large values those values, and of large negative ones nothing."""
+    p = Linear(*size, dtype, seed=11)
+    p.bias[1], p.bias[2], p.bias[3], p.bias[4], p.bias[5] = INF, 1e30, -1e30, 3e38, float("nan")
+    y = _linear(p.x, p.w, p.bias, act, dtype).float()
+    assert bool((y[:, 1] == INF).all())
+    for col in (2, 4):
+        assert torch.equal(y[:, col], p.bias[col].to(TORCH[dtype]).float().expand(size[0]))
+    assert bool((y[:, 3] == 0).all()) and bool(torch.isnan(y[:, 5]).all())
+    rest = [c for c in range(size[1]) if not 1 <= c <= 5]
+    assert bool(torch.isfinite(y[:, rest]).all())
+    # the gated pair: an infinite gate times a finite value
+    x, wg = p.x.clone(), p.w.clone()
+    wu = torch.zeros_like(wg)
+    x[:, 1], wg[:, 0], wu[:, 1] = 1, 1, 2
+    x[3 % size[0], 0] = INF
+    h = _gated(x, wg, wu, act, dtype).float()
+    # (the row's product with wu is infinity times zero)
+    assert bool(torch.isnan(h[3 % size[0]]).all())
+    x[:, 0], wg[:, 0], wg[7, 2], x[:, 2] = 0, 0, INF, 1
+    h = _gated(x, wg, wu, act, dtype).float()
+    assert bool((h[:, 7] == INF).all())
+    h[:, 7] = 0
+    assert bool(torch.isfinite(h).all())
