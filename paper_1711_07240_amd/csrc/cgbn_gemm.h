@@ -295,12 +295,14 @@ template <typename T> __device__ __forceinline__ f32x4 multiply(const u32x4& a, 
 }
 
 // Float values as sums of three bfloat16, which is exact: 24 bits are 8 and 8 and 8, each cut off and the rest, without rounding, kept.
-// (Parts below the smallest normal number are lost: values under 1e-33 have fewer than 24 bits.)  8 values of a lane, from two chunks.
+// (Parts below the smallest normal number are lost: values under 1e-33 have fewer than 24 bits.)  A NaN whose upper half alone would be an infinity
+// is made quiet first: the bit that says so is in the upper half.  8 values of a lane, from two chunks.
 __device__ __forceinline__ void split_float(const u32x4& lo, const u32x4& hi, u32x4 (&part)[3])
 {
+    auto quiet = [](uint32_t v) { return __float_as_uint(__builtin_canonicalizef(__uint_as_float(v))); };
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const uint32_t x = k < 2 ? lo[2 * k] : hi[2 * k - 4], y = k < 2 ? lo[2 * k + 1] : hi[2 * k - 3];
+        const uint32_t x = quiet(k < 2 ? lo[2 * k] : hi[2 * k - 4]), y = quiet(k < 2 ? lo[2 * k + 1] : hi[2 * k - 3]);
         const float xr = __uint_as_float(x) - __uint_as_float(x & 0xffff0000u), yr = __uint_as_float(y) - __uint_as_float(y & 0xffff0000u);
         const float xs = xr - __uint_as_float(__float_as_uint(xr) & 0xffff0000u), ys = yr - __uint_as_float(__float_as_uint(yr) & 0xffff0000u);
         part[0][k] = __builtin_amdgcn_perm(y, x, 0x07060302);                                            // the upper halves of both

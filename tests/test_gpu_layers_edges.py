@@ -65,3 +65,24 @@ def test_activations_at_the_ends(size, dtype, act):
     assert bool((h[:, 7] == INF).all())
     h[:, 7] = 0
     assert bool(torch.isfinite(h).all())
+
+
+def _bits(t, index, pattern):
+    t.view(torch.int32)[index] = pattern - (1 << 32 if pattern >> 31 else 0)
+
+
+# a NaN is one by any of its 23 bits, the lowest alone among them
+@pytest.mark.parametrize("pattern", [0x7f800001, 0xff800001, 0x7f80ffff, 0x7fc00000, 0xffffffff], ids=hex)
+def test_float_nans_of_any_bits(pattern):
+    for size in ((5, 40, 70), (140, 72, 96), (70, 66, 8192)):
+        p = Linear(*size, "f32", seed=12)
+        clean, clean_h = _linear(p.x, p.w, None, "none", "f32"), _gated(p.x, p.w, p.w, "none", "f32")
+        _bits(p.x, (3, 5), pattern)
+        _bits(p.w, (9, 2), pattern)
+        touched = torch.zeros_like(clean, dtype=torch.bool)
+        touched[3], touched[:, 9] = True, True
+        for got, want in ((_linear(p.x, p.w, None, "none", "f32"), clean), (_gated(p.x, p.w, p.w, "none", "f32"), clean_h)):
+            assert bool(torch.isnan(got[touched]).all()) and torch.equal(got[~touched], want[~touched])
+        dx, dw = _backward(p.dy, p.x, p.w, "f32")
+        assert bool(torch.isnan(dx[:, 2]).all()) and bool(torch.isnan(dw[:, 5]).all())
+        assert bool(torch.isfinite(dx[:, 3:]).all()) and bool(torch.isfinite(dw[:, 6:]).all())
