@@ -294,19 +294,22 @@ template <typename T> __device__ __forceinline__ f32x4 multiply(const u32x4& a, 
     }
 }
 
-// Float values as sums of three bfloat16, which is exact: 24 bits are 8 and 8 and 8, each cut off and the rest, without rounding, kept.
+// Float values as sums of three bfloat16, which is exact: the first is cut off (rounded, the type's largest values would become infinities), the second
+// is what is left rounded to nearest, so that the third has either sign and what a product drops no preferred one.
 // (Parts below the smallest normal number are lost: values under 1e-33 have fewer than 24 bits.)  A NaN whose upper half alone would be an infinity
 // is made quiet first: the bit that says so is in the upper half.  8 values of a lane, from two chunks.
 __device__ __forceinline__ void split_float(const u32x4& lo, const u32x4& hi, u32x4 (&part)[3])
 {
-    auto quiet = [](uint32_t v) { return __float_as_uint(__builtin_canonicalizef(__uint_as_float(v))); };
+    auto quiet = [](uint32_t v) { return __builtin_canonicalizef(__uint_as_float(v)); };
+    auto upper = [](float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); };
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const uint32_t x = quiet(k < 2 ? lo[2 * k] : hi[2 * k - 4]), y = quiet(k < 2 ? lo[2 * k + 1] : hi[2 * k - 3]);
-        const float xr = __uint_as_float(x) - __uint_as_float(x & 0xffff0000u), yr = __uint_as_float(y) - __uint_as_float(y & 0xffff0000u);
-        const float xs = xr - __uint_as_float(__float_as_uint(xr) & 0xffff0000u), ys = yr - __uint_as_float(__float_as_uint(yr) & 0xffff0000u);
-        part[0][k] = __builtin_amdgcn_perm(y, x, 0x07060302);                                            // the upper halves of both
-        part[1][k] = __builtin_amdgcn_perm(__float_as_uint(yr), __float_as_uint(xr), 0x07060302);
+        const float x = quiet(k < 2 ? lo[2 * k] : hi[2 * k - 4]), y = quiet(k < 2 ? lo[2 * k + 1] : hi[2 * k - 3]);
+        const float xr = x - upper(x), yr = y - upper(y);
+        const uint32_t mid = f32x2_to_bf16x2(xr, yr);
+        const float xs = xr - __uint_as_float(mid << 16), ys = yr - __uint_as_float(mid & 0xffff0000u);
+        part[0][k] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302);           // the upper halves of both
+        part[1][k] = mid;
         part[2][k] = __builtin_amdgcn_perm(__float_as_uint(ys), __float_as_uint(xs), 0x07060302);
     }
 }
@@ -477,7 +480,8 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
     typedef std::integral_constant<bool, false> no;
     if constexpr (sizeof(T) == 4) {
         // Float: each value as three bfloat16 (split_float), of whose nine products the six that count run on the bfloat16
-        // instructions, 16 times the rate of those for float.  What is dropped is below 2^-23 of a product, less than its rounding.
+        // instructions, 16 times the rate of those for float.  What is dropped, second by third parts, is below 2^-22 of a product (2^-7 by 2^-16 of its
+        // factors, twice), on either side.
         // The leading products have accumulators of their own: where an infinity makes one of those infinite, the others, in which it may
         // have met a zero, have no say.
         f32x4 rest[FI][FJ];

@@ -1,9 +1,10 @@
 """The layers beside the normalization where values, sizes or buffers are at an end of what they may be."""
 
+import numpy as np
 import pytest
 import torch
 
-from layers_harness import DEV, TORCH, Linear
+from layers_harness import DEV, TORCH, F, Linear, f64
 from paper_1711_07240_amd import cgbn as L
 
 pytestmark = pytest.mark.gpu
@@ -86,3 +87,47 @@ def test_float_nans_of_any_bits(pattern):
         dx, dw = _backward(p.dy, p.x, p.w, "f32")
         assert bool(torch.isnan(dx[:, 2]).all()) and bool(torch.isnan(dw[:, 5]).all())
         assert bool(torch.isfinite(dx[:, 3:]).all()) and bool(torch.isfinite(dw[:, 6:]).all())
+
+
+def _products(x, w):
+    """x[i] w[j] by every form of the tiles, each the only product of its sum."""
+    n, m = len(x), len(w)
+    yield "forward", _linear(x.view(n, 1), w.view(m, 1), None, "none", "f32")
+    yield "dx", _backward(x.view(n, 1), torch.ones(n, m, device=DEV), w.view(1, m), "f32")[0]
+    yield "dw", _backward(x.view(1, n), w.view(1, m), torch.ones(n, m, device=DEV), "f32")[1]
+    gate, up = torch.empty(n, m, device=DEV), torch.empty(n, m, device=DEV)
+    _gated(x.view(n, 1), w.view(m, 1), w.view(m, 1), "none", "f32", gate, up)
+    yield "gate", gate
+    yield "up", up
+
+
+def test_float_products_are_off_by_less_than_stated():
+    """Values whose second and third parts are as large as they come, and random ones.  What a product drops is less than 2^-22 of it, and two
+    roundings (of the parts' sum, and of the whole) are at most 2^-24 each, the first of a small part.  Nor is it always dropped on one
+    side: over random products the mean of the errors is that of parts whose signs are random, 0.05 units of 2^-24 in 257 rows and
+    columns (parts cut off, all of the product's sign, would make it 0.7)."""
+    rng = np.random.default_rng(13)
+    ends = [2 ** 16 * a + b for a in (0x3f80, 0x3f81, 0x3fff, 0x3fc0) for b in (0xffff, 0xff80, 0xff7f, 0x8000, 0x7fff, 0x7f80, 0x0080, 0x007f, 0xfe80, 1, 0)]
+    ends = np.array(ends, np.uint32).view(np.float32)
+    random = rng.uniform(1, 2, 257).astype(np.float32), rng.uniform(1, 2, 257).astype(np.float32)
+    for a, b in ((ends, ends), random):
+        x, w = torch.from_numpy(a).to(DEV), torch.from_numpy(b).to(DEV)
+        for name, got in _products(x, w):
+            want = np.outer(a.astype(np.float64), b.astype(np.float64))
+            off = (f64(got) - want) / want
+            assert np.abs(off).max() < 2.0 ** -22 + 1.1 * F, (name, np.abs(off).max() / F)
+            if a is not b:
+                assert abs(off.mean()) < 0.3 * F, (name, off.mean() / F)
+
+
+def test_float_products_of_the_largest_values():
+    """The type's lowest value, as masks hold it, is no infinity on its way through the products."""
+    big = float(np.finfo(np.float32).max)
+    x, w = torch.zeros(140, 96, device=DEV), torch.zeros(72, 96, device=DEV)
+    x[:, 3], w[:, 3] = -big, torch.linspace(0.25, 1.0, 72, device=DEV)
+    y = _linear(x, w, None, "none", "f32")
+    want = -big * w[:, 3].double()
+    assert bool(((y.double() - want).abs() <= 2.0 ** -21 * want.abs()).all())
+    x[5, 3], w[9, 3] = -INF, 1.0
+    y = _linear(x, w, None, "none", "f32")
+    assert bool((y[5] == -INF).all()) and bool(torch.isfinite(y[:5]).all()) and bool(torch.isfinite(y[6:]).all())
