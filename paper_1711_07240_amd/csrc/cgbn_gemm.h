@@ -296,15 +296,15 @@ template <typename T> __device__ __forceinline__ f32x4 multiply(const u32x4& a, 
 
 // Float values as sums of three bfloat16, which is exact: the first is cut off (rounded, the type's largest values would become infinities), the second
 // is what is left rounded to nearest, so that the third has either sign and what a product drops no preferred one.
-// (Parts below the smallest normal number are lost: values under 1e-33 have fewer than 24 bits.)  A NaN whose upper half alone would be an infinity
-// is made quiet first: the bit that says so is in the upper half.  8 values of a lane, from two chunks.
-__device__ __forceinline__ void split_float(const u32x4& lo, const u32x4& hi, u32x4 (&part)[3])
+// (Parts below the smallest normal number are lost: values under 1e-33 have fewer than 24 bits.)  8 values of a lane, from two chunks.
+// QUIET: a NaN whose upper half alone would be an infinity keeps to be one: the bit that makes it quiet is in the upper half.
+template <bool QUIET> __device__ __forceinline__ void split_float(const u32x4& lo, const u32x4& hi, u32x4 (&part)[3])
 {
-    auto quiet = [](uint32_t v) { return __builtin_canonicalizef(__uint_as_float(v)); };
+    auto value = [](uint32_t v) { return QUIET ? __builtin_canonicalizef(__uint_as_float(v)) : __uint_as_float(v); };
     auto upper = [](float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); };
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const float x = quiet(k < 2 ? lo[2 * k] : hi[2 * k - 4]), y = quiet(k < 2 ? lo[2 * k + 1] : hi[2 * k - 3]);
+        const float x = value(k < 2 ? lo[2 * k] : hi[2 * k - 4]), y = value(k < 2 ? lo[2 * k + 1] : hi[2 * k - 3]);
         const float xr = x - upper(x), yr = y - upper(y);
         const uint32_t mid = f32x2_to_bf16x2(xr, yr);
         const float xs = xr - __uint_as_float(mid << 16), ys = yr - __uint_as_float(mid & 0xffff0000u);
@@ -394,7 +394,8 @@ template <typename T, int N, bool NT = false> __device__ __forceinline__ void fi
 
 // ---- the product ----
 
-constexpr int tile_lds(int bi, int bj) { return 2 * (bi + bj) * 128; }
+// (float: and a word of each wavefront)
+constexpr int tile_lds(int bi, int bj, int elem) { return 2 * (bi + bj) * 128 + (elem == 4 ? 16 : 0); }
 // wavefronts that a vector unit must have registers for, by the values that one accumulates
 constexpr int tile_waves(int values) { return values > 96 * 64 ? 1 : 2; }
 
@@ -408,7 +409,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
     typedef Operand<T, ACOLS, BI, NT, false> OA;
     typedef Operand<T, BCOLS, BJ, NT, GATED> OB;
     constexpr int STAGE = OA::BYTES + OB::BYTES;
-    static_assert(2 * STAGE == tile_lds(BI, BJ), "two steps");
+    static_assert(2 * STAGE == tile_lds(BI, BJ, 2) && WI * WJ <= 4, "two steps");
     lds_char* const tile = (lds_char*)lds;
     const uint32_t lds0 = (uint32_t)(uintptr_t)tile;
 
@@ -422,9 +423,19 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
     const int first = w.split * G.per, last = min(first + G.per, seg_steps * G.segs);
 
     // The next step to be staged: where its data starts, and the r that remain in its segment.
-    int seg = first >= seg_steps, left = G.R - (first - seg * seg_steps) * OA::STEP;
-    const char *pa = OA::at(G.A[seg + w.z], i0, first - seg * seg_steps, G.lda), *pb = OB::at(GATED ? G.B[0] : G.B[seg + w.z], j0, first - seg * seg_steps, G.ldb),
-               *pb2 = GATED ? OB::at(G.B[1], j0, first, G.ldb) : pb;
+    int seg, left;
+    const char *pa, *pb, *pb2;
+    auto from_the_first = [&] {
+        seg = first >= seg_steps;
+        left = G.R - (first - seg * seg_steps) * OA::STEP;
+        pa = OA::at(G.A[seg + w.z], i0, first - seg * seg_steps, G.lda);
+        pb = OB::at(GATED ? G.B[0] : G.B[seg + w.z], j0, first - seg * seg_steps, G.ldb);
+        pb2 = GATED ? OB::at(G.B[1], j0, first, G.ldb) : pb;
+        // (an address must not be read by a load within five wait states of the vector unit's writing it; from here on only the scalar
+        // unit touches these)
+        asm volatile("s_nop 4" : "+s"(pa), "+s"(pb), "+s"(pb2));
+    };
+    from_the_first();
     const char *const next_a = OA::at(G.A[1], i0, 0, G.lda), *const next_b = OB::at(G.B[1], j0, 0, G.ldb);
     const long long da = OA::advance(G.lda), db = OB::advance(G.ldb);
     auto staged = [&] {
@@ -434,9 +445,6 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
     };
     constexpr int PASSES = OA::IT + OB::IT;
     const uint32_t lds_wave = lds0 + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave) * (kWave * 16);
-    // (an address must not be read by a load within five wait states of the vector unit's writing it; from here on only the scalar
-    // unit touches these)
-    asm volatile("s_nop 4" : "+s"(pa), "+s"(pb), "+s"(pb2));
     auto pass = [&](int buf, int p, bool whole) {
         const uint32_t to = buf * STAGE + (p < OA::IT ? 0 : OA::BYTES);
         if (p < OA::IT) {
@@ -485,35 +493,59 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
         // The leading products have accumulators of their own: where an infinity makes one of those infinite, the others, in which it may
         // have met a zero, have no say.
         f32x4 rest[FI][FJ];
+        auto sums = [&](auto QUIET) {
 #pragma unroll
-        for (int x = 0; x < FI; ++x)
+            for (int x = 0; x < FI; ++x)
 #pragma unroll
-            for (int y = 0; y < FJ; ++y) rest[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (first < last) stage(0);
-        for (int s = first, buf = 0; s < last; ++s, buf ^= 1) {
-            dma_wait_and_meet();
-            if (s + 1 < last) stage(buf ^ 1);
-            const lds_char* const ta = tile + buf * STAGE;
-            u32x4 pb[FJ][3];
+                for (int y = 0; y < FJ; ++y) acc[x][y] = rest[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (first < last) stage(0);
+            for (int s = first, buf = 0; s < last; ++s, buf ^= 1) {
+                dma_wait_and_meet();
+                if (s + 1 < last) stage(buf ^ 1);
+                const lds_char* const ta = tile + buf * STAGE;
+                u32x4 pb[FJ][3];
 #pragma unroll
-            for (int y = 0; y < FJ; ++y) {
-                const int at = bbase + (GATED && y >= FJ / 2 ? BJ / 2 : 0), f = GATED ? y % (FJ / 2) : y;
-                split_float(fragment<T, BCOLS, BJ>(ta + OA::BYTES, at, f, 0), fragment<T, BCOLS, BJ>(ta + OA::BYTES, at, f, 1), pb[y]);
-            }
+                for (int y = 0; y < FJ; ++y) {
+                    const int at = bbase + (GATED && y >= FJ / 2 ? BJ / 2 : 0), f = GATED ? y % (FJ / 2) : y;
+                    split_float<QUIET()>(fragment<T, BCOLS, BJ>(ta + OA::BYTES, at, f, 0), fragment<T, BCOLS, BJ>(ta + OA::BYTES, at, f, 1), pb[y]);
+                }
 #pragma unroll
-            for (int x = 0; x < FI; ++x) {
-                u32x4 pa[3];
-                split_float(fragment<T, ACOLS, BI>(ta, abase, x, 0), fragment<T, ACOLS, BI>(ta, abase, x, 1), pa);
+                for (int x = 0; x < FI; ++x) {
+                    u32x4 pa[3];
+                    split_float<QUIET()>(fragment<T, ACOLS, BI>(ta, abase, x, 0), fragment<T, ACOLS, BI>(ta, abase, x, 1), pa);
 #pragma unroll
-                for (int k = 0; k < 6; ++k) {
-                    constexpr int ka[6] = {0, 2, 1, 0, 1, 0}, kb[6] = {2, 0, 1, 1, 0, 0};          // small ones first
+                    for (int k = 0; k < 6; ++k) {
+                        constexpr int ka[6] = {0, 2, 1, 0, 1, 0}, kb[6] = {2, 0, 1, 1, 0, 0};          // small ones first
 #pragma unroll
-                    for (int y = 0; y < FJ; ++y) {
-                        f32x4& to = k == 5 ? acc[x][y] : rest[x][y];
-                        to = multiply<bf16_t>(pb[y][kb[k]], pa[ka[k]], to);
+                        for (int y = 0; y < FJ; ++y) {
+                            f32x4& to = k == 5 ? acc[x][y] : rest[x][y];
+                            to = multiply<bf16_t>(pb[y][kb[k]], pa[ka[k]], to);
+                        }
                     }
                 }
             }
+        };
+        sums(no());
+        // A leading sum that is not finite may hold a NaN that was cut to an infinity: where a workgroup has one it forms its sums once more, of values
+        // that are made quiet.  (In every sum that takes an instruction a value, 5% of a product.)
+        f32x4 finite = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < FI; ++x)
+#pragma unroll
+            for (int y = 0; y < FJ; ++y)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) finite[k] = fmaf(acc[x][y][k], 0.f, finite[k]);
+        typedef __attribute__((address_space(3))) uint32_t lds_word;
+        lds_word* const doubts = (lds_word*)(tile + 2 * STAGE);
+        const bool doubt = __any(!(finite[0] + finite[1] + finite[2] + finite[3] == 0.f));
+        if ((int)threadIdx.x % kWave == 0) doubts[wave] = doubt;
+        dma_wait_and_meet();                            // ... and everyone has read the last step
+        uint32_t again = 0;
+#pragma unroll
+        for (int k = 0; k < WI * WJ; ++k) again |= doubts[k];
+        if (__builtin_amdgcn_readfirstlane(again)) {
+            from_the_first();
+            sums(yes());
         }
 #pragma unroll
         for (int x = 0; x < FI; ++x)
@@ -681,7 +713,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& G, char* lds, int i
 template <typename T, int FORM, bool GATED, int BI, int BJ, int WI, int WJ>
 __global__ __launch_bounds__(WI * WJ * kWave, tile_waves(BI * BJ / (WI * WJ))) void gemm_tile(const GemmArgs G)
 {
-    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(BI, BJ)];
+    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(BI, BJ, sizeof(T))];
     tile_product<T, FORM, GATED, BI, BJ, WI, WJ>(G, lds, (int)blockIdx.x, (int)gridDim.x);
 }
 
@@ -690,7 +722,7 @@ __global__ __launch_bounds__(WI * WJ * kWave, tile_waves(BI * BJ / (WI * WJ))) v
 template <typename T, int BI, int BJ, int WI, int WJ, bool RESIDUAL>
 __global__ __launch_bounds__(WI * WJ * kWave, tile_waves(BI * BJ / (WI * WJ))) void gemm_short(const GemmArgs G)
 {
-    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(BI, BJ)];
+    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(BI, BJ, sizeof(T))];
     tile_product<T, FORM_NT, false, BI, BJ, WI, WJ, RESIDUAL>(G, lds, (int)blockIdx.x, (int)gridDim.x);
 }
 
@@ -700,7 +732,7 @@ __global__ __launch_bounds__(WI * WJ * kWave, tile_waves(BI * BJ / (WI * WJ))) v
 template <typename T, int BI, int BJ, int WI, int WJ>
 __global__ __launch_bounds__(WI * WJ * kWave, tile_waves(BI * BJ / (WI * WJ))) void gemm_two(const GemmArgs X, const GemmArgs W, int nx)
 {
-    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(BI, BJ)];
+    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(BI, BJ, sizeof(T))];
     if ((int)blockIdx.x < nx) tile_product<T, FORM_NN, false, BI, BJ, WI, WJ>(X, lds, (int)blockIdx.x, nx);
     else tile_product<T, FORM_TN, false, BI, BJ, WI, WJ>(W, lds, (int)blockIdx.x - nx, (int)gridDim.x - nx);
 }

@@ -87,6 +87,17 @@ def test_float_nans_of_any_bits(pattern):
         dx, dw = _backward(p.dy, p.x, p.w, "f32")
         assert bool(torch.isnan(dx[:, 2]).all()) and bool(torch.isnan(dw[:, 5]).all())
         assert bool(torch.isfinite(dx[:, 3:]).all()) and bool(torch.isfinite(dw[:, 6:]).all())
+        # dx of the gated pair: two products in one sum
+        wu, gate, up = p.w.roll(1, 0), p.dy.roll(1, 0), p.dy.roll(2, 0)
+        dx, dwg, dwu = torch.empty_like(p.x), torch.empty_like(p.w), torch.empty_like(p.w)
+        ws = torch.empty(L.cgbn_gated_workspace_bytes(*size, "f32", True), dtype=torch.uint8, device=DEV)
+        L.cgbn_gated_backward(p.dy, p.x, p.w, wu, gate, up, *size, "none", dx, dwg, dwu, "f32", ws)
+        assert bool(torch.isnan(dx[:, 2]).all()) and bool(torch.isfinite(dx[:, 3:]).all())
+        for dw in (dwg, dwu):
+            assert bool(torch.isnan(dw[:, 5]).all()) and bool(torch.isfinite(dw[:, 6:]).all())
+        p.w[9, 2] = 0
+        L.cgbn_gated_backward(p.dy, p.x, p.w, wu, gate, up, *size, "none", dx, dwg, dwu, "f32", ws)
+        assert bool(torch.isnan(dx[:, 2]).all()) and bool(torch.isfinite(dx[:, 3:]).all())
 
 
 def _products(x, w):
