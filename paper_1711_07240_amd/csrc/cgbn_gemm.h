@@ -53,43 +53,77 @@ struct GemmArgs {
 };
 
 // ---- activations, on 32-bit values ----
+//
+// FINE: for float results, which show what the shorter forms leave out.  Those are for bfloat16, at most 2.7e-7 off (GELU, near zero).
 
 // exp(x): the hardware's 2^y
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
 
-// exp(-z^2 / 2)
-__device__ __forceinline__ float bell(float z) { return __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f); }
-
-// Phi(-|z|), e being exp(-z^2 / 2): the rational approximation of the complementary error function that Abramowitz and Stegun give as
-// 7.1.26 (after Hastings), off by at most 7.5e-8 here.  It counts: an epilogue is bound by its instructions, 13 a value for GELU, 53 us
-// of 534 at 16384 x 2048 x 8192 (with the library's erff, 45 and 150).
-__device__ __forceinline__ float normal_tail(float z, float e)
+// exp(x) with what is lost of the product, and of log2(e), made good; x within [-150, 100], beyond which it is 0 and infinity
+__device__ __forceinline__ float exp_fine(float x)
 {
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.23164189f, fabsf(z), 1.f));         // 0.3275911 / sqrt(2)
-    return e * (t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5307027145f, -0.7265760135f), 0.7107068705f), -0.142248368f), 0.127414796f));
+    x = __builtin_amdgcn_fmed3f(x, -150.f, 100.f);
+    const float y = x * 1.4426950408889634f, lost = fmaf(x, 1.9259629911266175e-8f, fmaf(x, 1.4426950408889634f, -y));
+    return __builtin_amdgcn_exp2f(y) * fmaf(lost, 0.6931471805599453f, 1.f);
 }
 
-__device__ __forceinline__ float act_apply(float z, int act)
+// exp(-z^2 / 2)
+template <bool FINE> __device__ __forceinline__ float bell(float z)
+{
+    if constexpr (!FINE) return __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
+    z = fminf(fabsf(z), 30.f);
+    const float s = z * z, y = s * -0.72134752044448170f;
+    const float lost = fmaf(fmaf(z, z, -s), -0.72134752044448170f, fmaf(s, -9.629814955633087e-9f, fmaf(s, -0.72134752044448170f, -y)));
+    return __builtin_amdgcn_exp2f(y) * fmaf(lost, 0.6931471805599453f, 1.f);
+}
+
+// Phi(-|z|), e being exp(-z^2 / 2).  Short: the rational approximation of the complementary error function that Abramowitz and Stegun give as
+// 7.1.26 (after Hastings).  It counts: an epilogue is bound by its instructions, 14 a value for GELU, 53 us of 534 at 16384 x 2048 x 8192 (with the
+// library's erff, 45 and 150).  Fine: of the same form, t = 1 / (1 + 0.35 |z|), a polynomial of degree 8 fitted to Phi(-z) / (e t) over z in
+// [0, 14] for the least largest relative error, 3.2e-8; evaluated in 32 bits it is off by 7 units of 2^-24 of itself.
+template <bool FINE> __device__ __forceinline__ float normal_tail(float z, float e)
+{
+    if constexpr (!FINE) {
+        const float t = __builtin_amdgcn_rcpf(fmaf(0.23164189f, fabsf(z), 1.f));         // 0.3275911 / sqrt(2)
+        return e * (t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5307027145f, -0.7265760135f), 0.7107068705f), -0.142248368f), 0.127414796f));
+    }
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.35f, fminf(fabsf(z), 30.f), 1.f));
+    constexpr float c[9] = {0.13962140679359436f, 0.13986186683177948f, 0.11983287334442139f, 0.1055079847574234f, -0.023109780624508858f,
+                            0.1591740846633911f, -0.25571417808532715f, 0.14397166669368744f, -0.029145922511816025f};
+    float p = c[8];
+#pragma unroll
+    for (int k = 7; k >= 0; --k) p = fmaf(t, p, c[k]);
+    return e * (t * p);
+}
+
+template <bool FINE> __device__ __forceinline__ float act_apply(float z, int act)
 {
     if (act == ACT_RELU) return z < 0.f ? 0.f : z;
     // z Phi(z), which is z - z Phi(-z); the positive part by its bits, as an integer (where z is NaN the other term is).  Where z is large the tail is
     // zero, and what it is multiplied by is kept finite, by its bits too, for an infinite z.
-    if (act == ACT_GELU)
-        return fmaf(-fabsf(__int_as_float(min(__float_as_int(z), 0x7149f2ca))), normal_tail(z, bell(z)), __int_as_float(max(__float_as_int(z), 0)));
-    if (act == ACT_SILU) return z * __builtin_amdgcn_rcpf(1.f + exp_of(-z));
+    if (act == ACT_GELU) {
+        const float finite = FINE ? (z > 1e30f ? 1e30f : z) : __int_as_float(min(__float_as_int(z), 0x7149f2ca));
+        return fmaf(-fabsf(finite), normal_tail<FINE>(z, bell<FINE>(z)), __int_as_float(max(__float_as_int(z), 0)));
+    }
+    if (act == ACT_SILU) return FINE ? z / (1.f + exp_fine(-z)) : z * __builtin_amdgcn_rcpf(1.f + exp_of(-z));
     return z;
 }
 
 // act'(z)
-__device__ __forceinline__ float act_slope(float z, int act)
+template <bool FINE> __device__ __forceinline__ float act_slope(float z, int act)
 {
     if (act == ACT_RELU) return z > 0.f ? 1.f : 0.f;
     if (act == ACT_GELU) {
-        const float e = bell(z);
-        const float p = normal_tail(z, e);
+        const float e = bell<FINE>(z);
+        const float p = normal_tail<FINE>(z, e);
         return (z < 0.f ? p : 1.f - p) + z * 0.39894228040143268f * e;
     }
     if (act == ACT_SILU) {
+        if constexpr (FINE) {
+            // (1 - s is e s: where z is positive the difference would lose its bits)
+            const float e = exp_fine(-z), s = 1.f / (1.f + e);
+            return fmaf(z * s, z > 0.f ? e * s : 1.f - s, s);
+        }
         const float s = __builtin_amdgcn_rcpf(1.f + exp_of(-z));
         return s + z * s * (1.f - s);
     }
@@ -337,11 +371,11 @@ __device__ __forceinline__ TileId tile_of(const GemmArgs& G, int id, int n)
 
 // ---- epilogues: a run of N neighbours of a row ----
 
-template <int N> __device__ __forceinline__ void activate(float (&v)[N], int act)
+template <bool FINE, int N> __device__ __forceinline__ void activate(float (&v)[N], int act)
 {
 #define CGBN_ACTIVATE(act_)                                   \
     if (act == act_) {                                        \
-        _Pragma("unroll") for (int k = 0; k < N; ++k) v[k] = act_apply(v[k], act_); \
+        _Pragma("unroll") for (int k = 0; k < N; ++k) v[k] = act_apply<FINE>(v[k], act_); \
     }
     CGBN_ACTIVATE(ACT_RELU)
     CGBN_ACTIVATE(ACT_GELU)
@@ -358,7 +392,7 @@ __device__ __forceinline__ void finish_linear(const GemmArgs& G, float (&v)[N], 
         for (int k = 0; k < N; ++k) v[k] += r[k];
     }
     if (G.Z[0]) store_run<T, N, NT>(static_cast<T*>(G.Z[0]) + o, v, valid);
-    activate(v, G.act);
+    activate<sizeof(T) == 4>(v, G.act);
     store_run<T, N, NT>(static_cast<T*>(G.C[0]) + o, v, valid);
 }
 
@@ -386,7 +420,7 @@ template <typename T, int N, bool NT = false> __device__ __forceinline__ void fi
         store_run<T, N, NT>(static_cast<T*>(G.Z[0]) + o, g, valid);
         store_run<T, N, NT>(static_cast<T*>(G.Z[1]) + o, u, valid);
     }
-    activate(g, G.act);
+    activate<sizeof(T) == 4>(g, G.act);
 #pragma unroll
     for (int k = 0; k < N; ++k) g[k] *= u[k];
     store_run<T, N, NT>(static_cast<T*>(G.C[0]) + o, g, valid);

@@ -86,8 +86,8 @@ template <typename T, bool ENDS> __global__ __launch_bounds__(kThreads) void lin
             // (where ReLU passes nothing dz is zero, not dy * 0: an infinity there does not become NaN)
             if (A.saved) {
                 CGBN_EACH(A.act, ACT_RELU, g[e] = z[e] > 0.f ? g[e] : 0.f)
-                CGBN_EACH(A.act, ACT_GELU, g[e] *= act_slope(z[e], ACT_GELU))
-                CGBN_EACH(A.act, ACT_SILU, g[e] *= act_slope(z[e], ACT_SILU))
+                CGBN_EACH(A.act, ACT_GELU, g[e] *= act_slope<sizeof(T) == 4>(z[e], ACT_GELU))
+                CGBN_EACH(A.act, ACT_SILU, g[e] *= act_slope<sizeof(T) == 4>(z[e], ACT_SILU))
             }
 #pragma unroll
             for (int e = 0; e < E; ++e) sum[e] += g[e];
@@ -162,9 +162,9 @@ template <typename T> __global__ __launch_bounds__(kThreads) void gated_dz(const
             load_end<T, E>(pu, u, valid);
         }
         CGBN_EACH(A.act, ACT_NONE, const float a = g[e]; g[e] = h[e] * u[e]; u[e] = h[e] * a)
-        CGBN_EACH(A.act, ACT_RELU, const float a = act_apply(g[e], ACT_RELU); g[e] = g[e] > 0.f ? h[e] * u[e] : 0.f; u[e] = h[e] * a)
-        CGBN_EACH(A.act, ACT_GELU, const float z = g[e]; g[e] = h[e] * u[e] * act_slope(z, ACT_GELU); u[e] = h[e] * act_apply(z, ACT_GELU))
-        CGBN_EACH(A.act, ACT_SILU, const float z = g[e]; g[e] = h[e] * u[e] * act_slope(z, ACT_SILU); u[e] = h[e] * act_apply(z, ACT_SILU))
+        CGBN_EACH(A.act, ACT_RELU, const float a = act_apply<sizeof(T) == 4>(g[e], ACT_RELU); g[e] = g[e] > 0.f ? h[e] * u[e] : 0.f; u[e] = h[e] * a)
+        CGBN_EACH(A.act, ACT_GELU, const float z = g[e]; g[e] = h[e] * u[e] * act_slope<sizeof(T) == 4>(z, ACT_GELU); u[e] = h[e] * act_apply<sizeof(T) == 4>(z, ACT_GELU))
+        CGBN_EACH(A.act, ACT_SILU, const float z = g[e]; g[e] = h[e] * u[e] * act_slope<sizeof(T) == 4>(z, ACT_SILU); u[e] = h[e] * act_apply<sizeof(T) == 4>(z, ACT_SILU))
         store_run<T, E>(static_cast<T*>(A.dg) + r * A.ld + c, g, E);
         store_run<T, E>(static_cast<T*>(A.du) + r * A.ld + c, u, E);
     }

@@ -1,10 +1,13 @@
 """The layers beside the normalization where values, sizes or buffers are at an end of what they may be."""
 
+import math
+
 import numpy as np
 import pytest
 import torch
 
 from layers_harness import DEV, TORCH, F, Linear, f64
+from oracle import layers_oracle as Y
 from paper_1711_07240_amd import cgbn as L
 
 pytestmark = pytest.mark.gpu
@@ -142,3 +145,36 @@ def test_float_products_of_the_largest_values():
     x[5, 3], w[9, 3] = -INF, 1.0
     y = _linear(x, w, None, "none", "f32")
     assert bool((y[5] == -INF).all()) and bool(torch.isfinite(y[:5]).all()) and bool(torch.isfinite(y[6:]).all())
+
+
+_phi = np.vectorize(lambda t: 0.5 * math.erfc(-t / math.sqrt(2.0)), otypes=[np.float64])
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("M", [3, 70])
+def test_float_activations_keep_their_bits(M, act):
+    """act(z) and act'(z) of float results.  The normal distribution's tail is off by at most 16 units of 2^-24 of itself (of the
+    approximation 0.6; its polynomial's, the exponential's and the reciprocal's roundings), the logistic function by 8; what they enter is
+    rounded once or twice more.  (1e-35: results under the smallest normal number are lost.)"""
+    N = 4096
+    z = torch.linspace(-20, 20, N, device=DEV)
+    x, w = torch.zeros(M, 8, device=DEV), torch.zeros(N, 8, device=DEV)
+    v = f64(z)
+    y = f64(_linear(x, w, z, act, "f32"))
+    tail, logistic = _phi(-np.abs(v)), Y.sigmoid(v)
+    if act == "gelu":
+        bell = np.exp(-0.5 * v * v) / np.sqrt(2 * np.pi)
+        want, want_slope = v * _phi(v), _phi(v) + v * bell
+        off, slope_off = 16 * np.abs(v) * tail + np.abs(want), 16 * (tail + np.abs(v) * bell) + 2
+    else:
+        want, want_slope = v * logistic, logistic * (1 + v * Y.sigmoid(-v))
+        off, slope_off = 9 * np.abs(want), 16 * logistic * (1 + np.abs(v) * Y.sigmoid(-v))
+    assert (np.abs(y - want) <= off * F + 1e-35).all()
+    saved, slope = z.expand(M, N).contiguous(), torch.empty(M, N, device=DEV)
+    _backward(torch.ones(M, N, device=DEV), x, w, "f32", saved, act, slope)
+    assert (np.abs(f64(slope) - want_slope) <= slope_off * F + 1e-35).all()
+    # the gated pair: a gate of z beside an up of 1, and back
+    x[:, 0], w[:, 0] = 1, z
+    one = torch.zeros_like(w)
+    one[:, 0] = 1
+    assert (np.abs(f64(_gated(x, w, one, act, "f32")) - want) <= (off + np.abs(want)) * F + 1e-35).all()
