@@ -668,7 +668,17 @@ cgbn_status check_call(const HeadArgs& A, cgbn_dtype dtype, cgbn_rotation style,
         if (A.T && A.out[t] == in && A.T > 1 && A.ldo[t] != ld) return CGBN_ERR_ALIAS;
         if (A.T && backward && A.out[t] == A.x[t] && A.T > 1 && A.ldo[t] != A.ldx[t]) return CGBN_ERR_ALIAS;
     }
-    if (A.T && A.H[1] && A.out[0] == A.out[1]) return CGBN_ERR_ALIAS;
+    if (A.T && A.H[1]) {
+        if (A.out[0] == A.out[1]) return CGBN_ERR_ALIAS;
+        // the one's results over what the other's come from
+        for (int t = 0; t < 2; ++t)
+            if (A.out[t] == A.x[1 - t] || (backward && A.out[t] == A.dy[1 - t])) return CGBN_ERR_ALIAS;
+    }
+    for (int t = 0; A.T && t < (A.H[1] ? 2 : 1); ++t) {
+        const void* const out = A.out[t];
+        if (out == A.w[0] || (A.H[1] && out == A.w[1]) || (A.R && (out == A.cos || out == A.sin || (A.positions && out == A.positions))))
+            return CGBN_ERR_ALIAS;
+    }
     return CGBN_OK;
 }
 
@@ -718,6 +728,8 @@ cgbn_status cgbn_head_norm_backward(const void* dyq, long long lddyq, const void
     if (s != CGBN_OK) return s;
     if (!dwq || (Hk && !dwk)) return CGBN_ERR_NULL;
     if (dwq == dwk) return CGBN_ERR_ALIAS;
+    for (int t = 0; T && t < (Hk ? 2 : 1); ++t)
+        if (A.out[t] == dwq || (Hk && A.out[t] == dwk)) return CGBN_ERR_ALIAS;
     const size_t need = cgbn_head_norm_workspace_bytes(T, Hq, Hk, D, dtype);
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need) return CGBN_ERR_WORKSPACE;
     A.part = static_cast<float*>(workspace);

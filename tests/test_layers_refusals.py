@@ -1,0 +1,41 @@
+"""Refusals of the layers' entry points beyond those of test_layers_abi.py: buffers that are also another argument's, sizes, workspaces.
+Without a GPU: a call that is refused never gets to one."""
+
+import pytest
+import torch
+
+from paper_1711_07240_amd import cgbn as L
+from test_layers_abi import CALLS, P, _code
+
+# (a call that is wrongly taken would follow addresses that are none)
+pytestmark = pytest.mark.skipif(torch.cuda.is_available(), reason="for machines without a GPU")
+
+
+def _refused(fn, changes, status):
+    for change in changes:
+        kw = {**CALLS[fn], **change}
+        assert _code(fn, kw) == status, (fn, change)
+        assert getattr(L.lib(), fn)(*kw.values()) == status, (fn, change)
+
+
+# the tables' and weights' addresses apart from the tensors'
+APART = dict(positions=20 * P, cos=21 * P, sin=22 * P, wq=23 * P, wk=24 * P)
+
+
+def test_head_norm_results_over_the_other_heads_inputs_or_constants():
+    """Queries' results over keys that are still to be read, and the other way; results over the tables."""
+    fwd = [{"yq": 2 * P}, {"yk": P}, {"yk": P, "ldyk": 64}, {"yq": 2 * P, "ldyq": 64}]
+    fwd += [{**APART, name: P * at} for name in ("yq", "yk") for at in (20, 21, 22, 23, 24)]
+    _refused("cgbn_head_norm_forward", fwd, 11)
+    bwd = [{"dq": 2 * P}, {"dq": 4 * P}, {"dk": P}, {"dk": 3 * P}, {"dwq": 5 * P}, {"dwk": 6 * P}, {"dwq": 6 * P}, {"dwk": 5 * P}]
+    bwd += [{**APART, name: P * at} for name in ("dq", "dk") for at in (20, 21, 22, 23, 24)]
+    _refused("cgbn_head_norm_backward", bwd, 11)
+
+
+def test_head_norm_takes_what_is_not_wrong():
+    """In place each over its own, and addresses of what is not read: these calls are refused for their workspace alone, the last thing that is looked
+    at."""
+    back = {**CALLS["cgbn_head_norm_backward"], **APART, "dwq": 25 * P, "dwk": 26 * P, "workspace_bytes": 0}
+    for change in ({}, {"dq": P, "dk": 2 * P, "lddk": 32}, {"dq": 3 * P}, {"Hk": 0, "dq": 2 * P}, {"Hk": 0, "dq": 4 * P}, {"Hk": 0, "dq": 24 * P},
+                   {"R": 0, "dq": 21 * P}, {"dk": 4 * P, "lddk": 64}, {"T": 0, "dq": 2 * P}):
+        assert _code("cgbn_head_norm_backward", {**back, **change}) == 6, change
