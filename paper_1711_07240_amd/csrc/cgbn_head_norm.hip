@@ -248,12 +248,16 @@ template <int E> __device__ __forceinline__ void load_weights(const float* w, in
 // four, and angles and weights by vectors, 5.4 and 4.5 (bfloat16, 40 heads of 128 values; 32768 and 16384 tokens).
 constexpr int kAhead = 4;
 
+// A launch has less than 2^32 threads along each of its axes (of more the runtime starts some, without an error), so many workgroups take two.
+constexpr long long kGridX = 1 << 23;
+__device__ __forceinline__ long long workgroup() { return (long long)blockIdx.y * kGridX + blockIdx.x; }
+
 // L: lanes of a row; NT: results go past the caches
 template <typename T, int E, int L, bool NT> __global__ __launch_bounds__(kThreads) void head_forward(const HeadArgs A)
 {
     constexpr int G = kWave / L;
     const int lane = (int)threadIdx.x % kWave, p = lane % L, g = lane / L;
-    const long long wave = (long long)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
+    const long long wave = workgroup() * (kThreads / kWave) + threadIdx.x / kWave;
     const long long token = wave / A.parts;
     const int part = (int)(wave - token * A.parts);
     if (token >= A.T) return;
@@ -419,7 +423,7 @@ struct Angles {
 template <typename T, int kSlots> __global__ __launch_bounds__(kThreads) void head_forward_any(const HeadArgs A)
 {
     const int lane = (int)threadIdx.x % kWave, heads = A.H[0] + A.H[1];
-    const long long row = (long long)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
+    const long long row = workgroup() * (kThreads / kWave) + threadIdx.x / kWave;
     if (row >= A.T * heads) return;
     const long long token = row / heads;
     int h = (int)(row - token * heads);
@@ -523,7 +527,7 @@ cgbn_status check_sizes(long long T, int Hq, int Hk, int D, int dtype)
 {
     if (dtype != CGBN_F32 && dtype != CGBN_BF16) return CGBN_ERR_ENUM;
     if (T < 0 || T > kMaxTokens || Hq < 1 || Hq > kMaxHeads || Hk < 0 || Hk > kMaxHeads || D < 1 || D > kMaxD) return CGBN_ERR_SHAPE;
-    if (T * (Hq + Hk) > (1ll << 33)) return CGBN_ERR_SHAPE;            // grids stay within 31 bits
+    if (T * (Hq + Hk) > (1ll << 33)) return CGBN_ERR_SHAPE;            // 2^8 times kGridX workgroups at the most
     return CGBN_OK;
 }
 
@@ -571,6 +575,9 @@ template <int E> int lanes_of(int pairs)
 #define CGBN_LANES(X_) X_(1) X_(2) X_(4) X_(8)
 #define CGBN_LANES_LONG(X_) X_(16) X_(32) X_(64)
 
+// workgroups that know themselves by workgroup(); the last of them may be beyond the work
+dim3 grid_of(long long groups) { return groups <= kGridX ? dim3((unsigned)groups) : dim3((unsigned)kGridX, (unsigned)((groups + kGridX - 1) / kGridX)); }
+
 // a wavefront takes all heads of its token unless there are too few tokens to fill the device with
 void deal_heads(HeadArgs* A, int G)
 {
@@ -584,7 +591,7 @@ template <typename T, int E, bool NT> void launch_forward(HeadArgs& A, hipStream
 {
     const int L = lanes_of<E>(A.pairs);
     deal_heads(&A, kWave / L);
-    const dim3 grid((unsigned)((A.T * A.parts + 3) / 4));
+    const dim3 grid = grid_of((A.T * A.parts + 3) / 4);
 #define CGBN_CASE(L_) \
     case L_: hipLaunchKernelGGL((head_forward<T, E, L_, NT>), grid, dim3(kThreads), 0, st, A); break;
     if constexpr (E <= 2) switch (L) { CGBN_LANES_LONG(CGBN_CASE) }
@@ -605,7 +612,7 @@ template <typename T, int E, bool NT> void launch_backward(HeadArgs& A, int grou
 
 #define CGBN_ANY(kernel_, grid_, lds_)                                                                                 \
     do {                                                                                                               \
-        const dim3 g_((unsigned)(grid_));                                                                              \
+        const dim3 g_ = grid_;                                                                                         \
         if (A.D <= 64) hipLaunchKernelGGL((kernel_<T, 1>), g_, dim3(kThreads), lds_, st, A);                           \
         else if (A.D <= 128) hipLaunchKernelGGL((kernel_<T, 2>), g_, dim3(kThreads), lds_, st, A);                     \
         else if (A.D <= 256) hipLaunchKernelGGL((kernel_<T, 4>), g_, dim3(kThreads), lds_, st, A);                     \
@@ -624,7 +631,7 @@ template <typename T> cgbn_status run_forward(HeadArgs& A, hipStream_t st)
     else if (sizeof(T) == 2 && plan_chunks<T>(&A, 4, false)) launch_forward<T, 4, false>(A, st);
     else if (plan_chunks<T>(&A, 2, false)) launch_forward<T, 2, false>(A, st);
     else if (plan_chunks<T>(&A, 1, false)) launch_forward<T, 1, false>(A, st);
-    else CGBN_ANY(head_forward_any, (A.T * (A.H[0] + A.H[1]) + 3) / 4, 0);
+    else CGBN_ANY(head_forward_any, grid_of((A.T * (A.H[0] + A.H[1]) + 3) / 4), 0);
     return launched();
 }
 
@@ -637,7 +644,7 @@ template <typename T> cgbn_status run_backward(HeadArgs& A, float* dwq, float* d
     else if (sizeof(T) == 2 && plan_chunks<T>(&A, 4, true)) launch_backward<T, 4, false>(A, groups, lds, st);
     else if (plan_chunks<T>(&A, 2, true)) launch_backward<T, 2, false>(A, groups, lds, st);
     else if (plan_chunks<T>(&A, 1, true)) launch_backward<T, 1, false>(A, groups, lds, st);
-    else CGBN_ANY(head_backward_any, groups, lds);
+    else CGBN_ANY(head_backward_any, dim3((unsigned)groups), lds);
     if (launched() != CGBN_OK) return CGBN_ERR_HIP;
     const int n = A.H[1] ? 2 * A.D : A.D;
     // (a workgroup's row of partial sums has both weights' side by side; without keys the second half is zero and stays unread)

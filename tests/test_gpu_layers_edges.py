@@ -178,3 +178,35 @@ def test_float_activations_keep_their_bits(M, act):
     one = torch.zeros_like(w)
     one[:, 0] = 1
     assert (np.abs(f64(_gated(x, w, one, act, "f32")) - want) <= (off + np.abs(want)) * F + 1e-35).all()
+
+
+def _rows_again(T, Hq, D, block):
+    """T tokens that repeat `block`'s, and the library's own answer for one block."""
+    x = torch.empty(T, Hq * D, dtype=torch.bfloat16, device=DEV)
+    for at in range(0, T, len(block)):
+        x[at:at + len(block)] = block[:T - at]
+    return x
+
+
+@pytest.mark.parametrize("Hq,D,T", [(1, 8, (1 << 26) + 1001), (32, 129, (1 << 21) + 77)], ids=["chunks", "value by value"])
+def test_more_threads_than_a_launch_has(Hq, D, T):
+    """A wavefront to a token, or to a row of an odd length: 2^32 threads and more."""
+    torch.cuda.empty_cache()
+    gen = torch.Generator(device=DEV).manual_seed(14)
+    block = torch.randn((1 << 21) // Hq, Hq * D, device=DEV, generator=gen).to(torch.bfloat16)
+    w = torch.rand(D, device=DEV, generator=gen) + 0.5
+
+    def norm(x):
+        y = torch.full_like(x, 7.0)
+        L.cgbn_head_norm_forward(x, Hq * D, None, 0, len(x), Hq, 0, D, 0, "halves", None, None, None, 0, w, None, 1e-5, y, Hq * D, None, 0, "bf16")
+        return y
+
+    want = norm(block)
+    v = block[:300].double().view(300, Hq, D)
+    exact = (v / (v.square().mean(-1, keepdim=True) + 1e-5).sqrt() * w.double()).view(300, -1)
+    assert bool(((want[:300].double() - exact).abs() <= (2.0 ** -8 + (D + 32) * F) * exact.abs()).all())
+    y = norm(_rows_again(T, Hq, D, block))
+    for at in range(0, T, len(block)):
+        assert torch.equal(y[at:at + len(block)], want[:T - at]), at
+    del y
+    torch.cuda.empty_cache()
