@@ -16,6 +16,9 @@ namespace cgbn {
     X_(2, 128, 64, 4, 1)           \
     X_(3, 64, 64, 2, 1)
 
+// of a launch's axis (of more the runtime starts some, without an error)
+constexpr double kMaxThreads = 4294967295.;
+
 struct GemmPlan {
     int shape, elem, ti, tj, splits, per;
     size_t part_bytes;          // of workspace, 0 where the reduction is not split
@@ -54,7 +57,8 @@ constexpr int kShortI = 192, kShortJ = 128;
 inline bool short_shape(int shape, int splits, long long I, long long J, long long R, bool residual)
 {
     return shape <= 1 && splits == 1 && R <= (residual ? 2048 : 1024) && (R >= 512 || J % 64 == 0) &&
-           (I + kShortI - 1) / kShortI * ((J + kShortJ - 1) / kShortJ) >= 2048;
+           (I + kShortI - 1) / kShortI * ((J + kShortJ - 1) / kShortJ) >= 2048 &&
+           (double)((I + kShortI - 1) / kShortI * ((J + kShortJ - 1) / kShortJ)) * 4 * kWave <= kMaxThreads;
 }
 
 // the plan with one shape and one number of splits; false: more than can be
@@ -66,7 +70,7 @@ inline bool plan_with(int shape, long long want, int elem, bool gated, long long
     const long long steps = (R + step - 1) / step * segs, per = (steps + want - 1) / want, splits = (steps + per - 1) / per;
     const double part = splits > 1 ? (double)splits * batch * (gated ? 2 : 1) * I * J * 4 : 0;
     const long long ti = (I + t.bi - 1) / t.bi, tj = (J + bj - 1) / bj;
-    if (part > 1e9 || (double)ti * tj * splits * batch > 1e9) return false;
+    if (part > 1e9 || (double)ti * tj * splits * batch * t.waves * kWave > kMaxThreads) return false;
     *p = GemmPlan{shape, elem, (int)ti, (int)tj, (int)splits, (int)per, (size_t)part, (double)ti * tj * splits * batch, 0, 0, 0};
     // (what a workgroup does besides: its first loads' way, and its rows of A, which it shares with the tiles beside it, and its
     // results, at the rate of memory)
@@ -135,7 +139,9 @@ inline void plan_two(int elem, long long M, int N, int K, int pairs, GemmPlan* d
         each_split((N + step - 1) / step * pairs, [&](long long want) {
             if (!plan_with(s, want, elem, false, M, K, N, pairs, 1, &x)) return false;
             for (int b = 0; b < 2; ++b) {
-                const double groups = x.groups + w[b].groups, cx = cost_of(x, groups), cw = cost_of(w[b], groups);
+                const double groups = x.groups + w[b].groups;
+                if (groups * tile_shape(s).waves * kWave > kMaxThreads) continue;
+                const double cx = cost_of(x, groups), cw = cost_of(w[b], groups);
                 // A unit takes the next workgroup when it is done with one: the last to be started end half of one's time after
                 // the average.  One that shares its unit takes as many times longer: a long one, dx unsplit for few rows, is then
                 // what the launch waits for (64 x 4096 x 4096 float 190 us with dx in 64 workgroups among 4096 of dW, 67 split).

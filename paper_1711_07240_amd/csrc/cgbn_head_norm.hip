@@ -20,6 +20,7 @@
 // walks, then over wavefronts in order, then over workgroups in double precision.  No atomics.
 #include "cgbn.h"
 #include "cgbn_column_sums.h"
+#include "cgbn_grid.h"
 
 #include <cmath>
 #include <cstring>
@@ -247,10 +248,6 @@ template <int E> __device__ __forceinline__ void load_weights(const float* w, in
 // Rows whose chunks are asked for before the first of them is used: with one at a time 4.4 TB/s forward and 2.6 backward, with
 // four, and angles and weights by vectors, 5.4 and 4.5 (bfloat16, 40 heads of 128 values; 32768 and 16384 tokens).
 constexpr int kAhead = 4;
-
-// A launch has less than 2^32 threads along each of its axes (of more the runtime starts some, without an error), so many workgroups take two.
-constexpr long long kGridX = 1 << 23;
-__device__ __forceinline__ long long workgroup() { return (long long)blockIdx.y * kGridX + blockIdx.x; }
 
 // L: lanes of a row; NT: results go past the caches
 template <typename T, int E, int L, bool NT> __global__ __launch_bounds__(kThreads) void head_forward(const HeadArgs A)
@@ -527,7 +524,7 @@ cgbn_status check_sizes(long long T, int Hq, int Hk, int D, int dtype)
 {
     if (dtype != CGBN_F32 && dtype != CGBN_BF16) return CGBN_ERR_ENUM;
     if (T < 0 || T > kMaxTokens || Hq < 1 || Hq > kMaxHeads || Hk < 0 || Hk > kMaxHeads || D < 1 || D > kMaxD) return CGBN_ERR_SHAPE;
-    if (T * (Hq + Hk) > (1ll << 33)) return CGBN_ERR_SHAPE;            // 2^8 times kGridX workgroups at the most
+    if (T * (Hq + Hk) > (1ll << 33)) return CGBN_ERR_SHAPE;            // 2^31 workgroups at the most
     return CGBN_OK;
 }
 
@@ -574,9 +571,6 @@ template <int E> int lanes_of(int pairs)
 
 #define CGBN_LANES(X_) X_(1) X_(2) X_(4) X_(8)
 #define CGBN_LANES_LONG(X_) X_(16) X_(32) X_(64)
-
-// workgroups that know themselves by workgroup(); the last of them may be beyond the work
-dim3 grid_of(long long groups) { return groups <= kGridX ? dim3((unsigned)groups) : dim3((unsigned)kGridX, (unsigned)((groups + kGridX - 1) / kGridX)); }
 
 // a wavefront takes all heads of its token unless there are too few tokens to fill the device with
 void deal_heads(HeadArgs* A, int G)

@@ -5,6 +5,7 @@
 #include "cgbn_gemm_plan.h"
 #include "cgbn_gemm_rows.h"
 #include "cgbn_column_sums.h"
+#include "cgbn_grid.h"
 
 #include <cstring>
 
@@ -35,7 +36,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void pad_rows(const
 {
     constexpr int E = 16 / (int)sizeof(T);
     const int chunks = A.np / E;
-    long long id = (long long)blockIdx.x * kThreads + threadIdx.x;
+    long long id = workgroup() * kThreads + threadIdx.x;
     if (id >= A.end[2]) return;
     const int k = id < A.end[0] ? 0 : id < A.end[1] ? 1 : 2;
     id -= k == 0 ? 0 : k == 1 ? A.end[0] : A.end[1];
@@ -172,7 +173,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void gated_dz(const
 
 template <typename T> __global__ __launch_bounds__(kThreads) void fill_zero(T* p, long long n)
 {
-    const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
+    const long long i = workgroup() * kThreads + threadIdx.x;
     if (i < n) p[i] = T{};
 }
 
@@ -193,7 +194,7 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 constexpr int kMaxWidth = 1 << 20;                  // of N, K, F: a tile's byte offsets stay within 32 bits
 constexpr long long kMaxRows = 1ll << 30;
-constexpr long long kMaxElements = 1ll << 38;       // of a matrix: grids stay within 31 bits
+constexpr long long kMaxElements = 1ll << 38;       // of a matrix: grids stay within 31 bits (and what a product's tiles have for threads, see plan_with)
 
 // Whether a product takes gemm_rows.  Up to 16 rows it does: the gated pair 38 against 49 us with tiles (4096 x 11264, 16 rows), 61
 // against 49 with 32.  Beyond them it pays for every row again with all of the weights, so these have to be small.  bfloat16, against
@@ -234,6 +235,7 @@ struct Widths {
 
 struct ForwardPlan {
     bool rows;                  // gemm_rows
+    bool none;                  // more tiles than a launch has
     GemmPlan g;
     size_t x, w, part, bytes;   // padded copies of x and of the weights; partial sums
 };
@@ -259,6 +261,7 @@ ForwardPlan plan_forward(long long M, int N, int K, int dtype, bool gated)
         return p;
     }
     p.g = plan_gemm(W.elem, gated, M, N, K, 1, 1);
+    p.none = p.g.ti == 0;
     if (W.odd(K)) {
         p.x = l.take((size_t)M * W.padded(K) * W.elem);
         p.w = l.take((size_t)N * W.padded(K) * W.elem * (gated ? 2 : 1));
@@ -272,6 +275,7 @@ struct BackwardPlan {
     GemmPlan dx, dw;
     size_t dz, x, w, part_x, part_w, sums, bytes;
     int sum_blocks, sum_rows, tw;
+    bool none;
 };
 
 // (one plan whichever of dx and dW a call wants: it is what the workspace is sized by)
@@ -280,6 +284,7 @@ BackwardPlan plan_backward(long long M, int N, int K, int dtype, bool gated)
     const Widths W(dtype);
     BackwardPlan p{};
     plan_two(W.elem, M, N, K, gated ? 2 : 1, &p.dx, &p.dw);
+    p.none = p.dx.ti == 0;
     Layout l;
     p.dz = l.take((size_t)M * W.padded(N) * W.elem * (gated ? 2 : 1));
     if (W.odd(K)) {
@@ -301,6 +306,21 @@ BackwardPlan plan_backward(long long M, int N, int K, int dtype, bool gated)
     if (!gated) p.sums = l.take((size_t)p.sum_blocks * N * sizeof(float));
     p.bytes = l.at;
     return p;
+}
+
+size_t workspace_of(long long M, int N, int K, int dtype, bool gated, bool backward)
+{
+    size_t bytes;
+    if (backward) {
+        const BackwardPlan p = plan_backward(M, N, K, dtype, gated);
+        if (p.none) return 0;
+        bytes = p.bytes;
+    } else {
+        const ForwardPlan p = plan_forward(M, N, K, dtype, gated);
+        if (p.none) return 0;
+        bytes = p.bytes;
+    }
+    return bytes ? bytes : 256;
 }
 
 cgbn_status check_workspace(size_t need, const void* workspace, size_t have)
@@ -329,7 +349,7 @@ struct Pads {
         if (count == 0) return hipSuccess;
         A.n = n;
         A.np = np;
-        hipLaunchKernelGGL(pad_rows<T>, dim3((unsigned)((A.end[2] + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, A);
+        hipLaunchKernelGGL(pad_rows<T>, grid_of((A.end[2] + kThreads - 1) / kThreads), dim3(kThreads), 0, st, A);
         return hipGetLastError();
     }
 };
@@ -429,7 +449,7 @@ cgbn_status products(const void* const dz[2], int ldz, int pairs, const void* x,
 template <typename T> hipError_t zero(void* p, long long n, hipStream_t st)
 {
     if (!p || n == 0) return hipSuccess;
-    hipLaunchKernelGGL(fill_zero<T>, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, static_cast<T*>(p), n);
+    hipLaunchKernelGGL(fill_zero<T>, grid_of((n + kThreads - 1) / kThreads), dim3(kThreads), 0, st, static_cast<T*>(p), n);
     return hipGetLastError();
 }
 
@@ -517,8 +537,7 @@ size_t cgbn_linear_workspace_bytes(long long M, int N, int K, cgbn_dtype dtype, 
 {
     if (check_sizes(M, N, K, dtype) != CGBN_OK) return 0;
     if (M == 0) return 256;
-    const size_t b = backward ? plan_backward(M, N, K, dtype, false).bytes : plan_forward(M, N, K, dtype, false).bytes;
-    return b ? b : 256;
+    return workspace_of(M, N, K, dtype, false, backward);
 }
 
 cgbn_status cgbn_linear_forward(const void* x, const void* w, const float* bias, const void* residual, long long M, int N, int K, cgbn_activation act,
@@ -531,6 +550,7 @@ cgbn_status cgbn_linear_forward(const void* x, const void* w, const float* bias,
     if (!aligned16(x) || !aligned16(w) || !aligned16(y) || !aligned16(residual) || !aligned16(z)) return CGBN_ERR_ALIGN;
     if (y == z || y == x || z == x || y == w || z == w) return CGBN_ERR_ALIAS;
     const ForwardPlan p = plan_forward(M, N, K, dtype, false);
+    if (p.none) return CGBN_ERR_SHAPE;
     CGBN_TRY(check_workspace(p.bytes, workspace, workspace_bytes));
     GemmArgs G;
     std::memset(&G, 0, sizeof(G));
@@ -554,7 +574,11 @@ cgbn_status cgbn_linear_backward(const void* dy, const void* x, const void* w, c
     if (M != 0 && dx && (dx == dw || dx == dresidual || dx == dy || dx == x || dx == w)) return CGBN_ERR_ALIAS;
     if (M != 0 && dw && (dw == dresidual || dw == dy || dw == x || dw == w)) return CGBN_ERR_ALIAS;
     if (M != 0 && dresidual && (dresidual == x || dresidual == w)) return CGBN_ERR_ALIAS;
-    if (M > 0) CGBN_TRY(check_workspace(plan_backward(M, N, K, dtype, false).bytes, workspace, workspace_bytes));
+    if (M > 0) {
+        const BackwardPlan p = plan_backward(M, N, K, dtype, false);
+        if (p.none) return CGBN_ERR_SHAPE;
+        CGBN_TRY(check_workspace(p.bytes, workspace, workspace_bytes));
+    }
     hipStream_t st = static_cast<hipStream_t>(stream);
     char* ws = static_cast<char*>(workspace);
     return dtype == CGBN_F32 ? linear_backward<float>(dy, x, w, saved, M, N, K, act, dx, dw, dbias, dresidual, ws, st)
@@ -565,8 +589,7 @@ size_t cgbn_gated_workspace_bytes(long long M, int F, int K, cgbn_dtype dtype, i
 {
     if (check_sizes(M, F, K, dtype) != CGBN_OK) return 0;
     if (M == 0) return 256;
-    const size_t b = backward ? plan_backward(M, F, K, dtype, true).bytes : plan_forward(M, F, K, dtype, true).bytes;
-    return b ? b : 256;
+    return workspace_of(M, F, K, dtype, true, backward);
 }
 
 cgbn_status cgbn_gated_forward(const void* x, const void* w_gate, const void* w_up, long long M, int F, int K, cgbn_activation act, void* h,
@@ -581,6 +604,7 @@ cgbn_status cgbn_gated_forward(const void* x, const void* w_gate, const void* w_
     for (int k = 0; k < 3; ++k)
         if (outs[k] && (outs[k] == x || outs[k] == w_gate || outs[k] == w_up || outs[k] == outs[(k + 1) % 3])) return CGBN_ERR_ALIAS;
     const ForwardPlan p = plan_forward(M, F, K, dtype, true);
+    if (p.none) return CGBN_ERR_SHAPE;
     CGBN_TRY(check_workspace(p.bytes, workspace, workspace_bytes));
     GemmArgs G;
     std::memset(&G, 0, sizeof(G));
@@ -606,7 +630,11 @@ cgbn_status cgbn_gated_backward(const void* dh, const void* x, const void* w_gat
         if (outs[k] && (outs[k] == x || outs[k] == w_gate || outs[k] == w_up || outs[k] == dh || outs[k] == gate || outs[k] == up ||
                         outs[k] == outs[(k + 1) % 3]))
             return CGBN_ERR_ALIAS;
-    if (M > 0) CGBN_TRY(check_workspace(plan_backward(M, F, K, dtype, true).bytes, workspace, workspace_bytes));
+    if (M > 0) {
+        const BackwardPlan p = plan_backward(M, F, K, dtype, true);
+        if (p.none) return CGBN_ERR_SHAPE;
+        CGBN_TRY(check_workspace(p.bytes, workspace, workspace_bytes));
+    }
     hipStream_t st = static_cast<hipStream_t>(stream);
     char* ws = static_cast<char*>(workspace);
     return dtype == CGBN_F32 ? gated_backward<float>(dh, x, w_gate, w_up, gate, up, M, F, K, act, dx, dw_gate, dw_up, ws, st)

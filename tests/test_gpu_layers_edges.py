@@ -210,3 +210,59 @@ def test_more_threads_than_a_launch_has(Hq, D, T):
         assert torch.equal(y[at:at + len(block)], want[:T - at]), at
     del y
     torch.cuda.empty_cache()
+
+
+def test_no_rows_and_weights_of_2_to_the_32():
+    torch.cuda.empty_cache()
+    dw = torch.full(((1 << 16) + 1, 1 << 16), 7.0, dtype=torch.bfloat16, device=DEV)
+    w = torch.empty(8, dtype=torch.bfloat16, device=DEV)               # (not read: there are no rows)
+    L.cgbn_linear_backward(None, None, w, None, 0, dw.shape[0], dw.shape[1], "none", None, dw, None, None, "bf16")
+    assert not bool(dw.view(torch.int16).any())
+    L.cgbn_gated_backward(None, None, w, w, None, None, 0, 8, 16, "silu", None, dw[0], dw[1], "bf16")
+    del dw
+    torch.cuda.empty_cache()
+
+
+def test_rows_laid_out_anew_of_2_to_the_32_chunks():
+    """2^30 rows of 25 values, which take four chunks each."""
+    torch.cuda.empty_cache()
+    M, N, K = 1 << 30, 1, 25
+    need = M * K * 2 + M * 32 * 2 + M * N * 2 + (8 << 30)
+    if torch.cuda.mem_get_info()[0] < need:
+        pytest.skip(f"{need >> 30} GiB of memory are not free")
+    x = torch.zeros(M, K, dtype=torch.bfloat16, device=DEV)
+    gen = torch.Generator(device=DEV).manual_seed(15)
+    rows = torch.cat([torch.arange(3), torch.arange(M // 2 - 2, M // 2 + 2), torch.arange(M - 5, M)]).to(DEV)
+    x[rows] = torch.randint(-3, 4, (len(rows), K), device=DEV, generator=gen).to(torch.bfloat16)
+    w = torch.randint(-3, 4, (N, K), device=DEV, generator=gen).to(torch.bfloat16)
+    y = torch.full((M, N), 7.0, dtype=torch.bfloat16, device=DEV)
+    ws = torch.empty(L.cgbn_linear_workspace_bytes(M, N, K, "bf16", False), dtype=torch.uint8, device=DEV)
+    L.cgbn_linear_forward(x, w, None, None, M, N, K, "none", y, None, "bf16", ws)
+    assert torch.equal(y[rows].double(), x[rows].double() @ w.double().t())
+    y[rows] = 0
+    assert not bool(y.view(torch.int16).any())
+    del x, y, ws
+    torch.cuda.empty_cache()
+
+
+def test_more_tiles_than_a_launch_has_threads_for():
+    """2^30 rows of 65 values of the gated pair: tiles of 128 x 32 of each would be 1.5 times 2^32 threads."""
+    torch.cuda.empty_cache()
+    M, F_, K = 1 << 30, 65, 1
+    need = M * F_ * 2 + M * 18 + (12 << 30)
+    if torch.cuda.mem_get_info()[0] < need:
+        pytest.skip(f"{need >> 30} GiB of memory are not free")
+    x = torch.zeros(M, K, dtype=torch.bfloat16, device=DEV)
+    rows = torch.cat([torch.arange(3), torch.arange(M // 2 - 2, M // 2 + 2), torch.arange(M - 5, M)]).to(DEV)
+    x[rows] = torch.arange(1, len(rows) + 1, device=DEV, dtype=torch.bfloat16)[:, None]
+    wg, wu = (torch.arange(F_, device=DEV, dtype=torch.bfloat16).add_(k)[:, None] for k in (1, 2))
+    h = torch.full((M, F_), 7.0, dtype=torch.bfloat16, device=DEV)
+    ws = torch.empty(L.cgbn_gated_workspace_bytes(M, F_, K, "bf16", False), dtype=torch.uint8, device=DEV)
+    L.cgbn_gated_forward(x, wg, wu, M, F_, K, "none", h, None, None, "bf16", ws)
+    v = x[rows].double()
+    assert torch.equal(h[rows], (v * wg.double().t() * (v * wu.double().t())).float().to(torch.bfloat16))
+    h[rows] = 0
+    for at in range(0, M, 1 << 26):
+        assert not bool(h[at:at + (1 << 26)].view(torch.int16).any()), at
+    del x, h, ws
+    torch.cuda.empty_cache()

@@ -39,3 +39,14 @@ def test_head_norm_takes_what_is_not_wrong():
     for change in ({}, {"dq": P, "dk": 2 * P, "lddk": 32}, {"dq": 3 * P}, {"Hk": 0, "dq": 2 * P}, {"Hk": 0, "dq": 4 * P}, {"Hk": 0, "dq": 24 * P},
                    {"R": 0, "dq": 21 * P}, {"dk": 4 * P, "lddk": 64}, {"T": 0, "dq": 2 * P}):
         assert _code("cgbn_head_norm_backward", {**back, **change}) == 6, change
+
+
+def test_more_tiles_than_a_launch_has():
+    """Sizes of which no tile shape fits a launch (2^30 rows of 200 floats and more): refused, not done in part."""
+    assert L.cgbn_linear_workspace_bytes(1 << 30, 200, 8, "f32", False) == 0
+    assert L.cgbn_gated_workspace_bytes(1 << 30, 200, 8, "f32", False) == 0
+    big = {"M": 1 << 30, "K": 8, "dtype": 0}
+    _refused("cgbn_linear_forward", [{**big, "N": 200}], 2)
+    _refused("cgbn_gated_forward", [{**big, "F": 200}], 2)
+    # as tall, with a shape that does
+    assert L.cgbn_linear_workspace_bytes(1 << 30, 200, 8, "bf16", False) and L.cgbn_linear_workspace_bytes(1 << 30, 128, 8, "f32", False)
