@@ -535,6 +535,9 @@ int backward_groups(long long T, int Hq, int Hk)
     return (int)(groups < kBackwardGroups ? (groups < 1 ? 1 : groups) : kBackwardGroups);
 }
 
+// bytes of a backward call's partial sums
+size_t partial_sums(long long T, int Hq, int Hk, int D) { return (size_t)backward_groups(T, Hq, Hk) * 2 * D * sizeof(float); }
+
 // rows in chunks of E values
 template <typename T> bool plan_chunks(HeadArgs* A, int E, bool backward)
 {
@@ -710,7 +713,8 @@ cgbn_status cgbn_head_norm_forward(const void* q, long long ldq, const void* k, 
 size_t cgbn_head_norm_workspace_bytes(long long T, int Hq, int Hk, int D, cgbn_dtype dtype)
 {
     if (check_sizes(T, Hq, Hk, D, dtype) != CGBN_OK) return 0;
-    return ((size_t)backward_groups(T, Hq, Hk) * 2 * D * sizeof(float) + 255) / 256 * 256;
+    const size_t bytes = (partial_sums(T, Hq, Hk, D) + 255) / 256 * 256;
+    return bytes > 256 ? bytes : 512;          // (of 256 or less a program may pass none)
 }
 
 cgbn_status cgbn_head_norm_backward(const void* dyq, long long lddyq, const void* dyk, long long lddyk, const void* q, long long ldq, const void* k,
@@ -731,7 +735,7 @@ cgbn_status cgbn_head_norm_backward(const void* dyq, long long lddyq, const void
     if (dwq == dwk) return CGBN_ERR_ALIAS;
     for (int t = 0; T && t < (Hk ? 2 : 1); ++t)
         if (A.out[t] == dwq || (Hk && A.out[t] == dwk)) return CGBN_ERR_ALIAS;
-    const size_t need = cgbn_head_norm_workspace_bytes(T, Hq, Hk, D, dtype);
+    const size_t need = partial_sums(T, Hq, Hk, D);
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need) return CGBN_ERR_WORKSPACE;
     A.part = static_cast<float*>(workspace);
     A.inv_D = 1.f / (float)D;

@@ -320,7 +320,8 @@ size_t workspace_of(long long M, int N, int K, int dtype, bool gated, bool backw
         if (p.none) return 0;
         bytes = p.bytes;
     }
-    return bytes ? bytes : 256;
+    // (256 says that none is needed: a program may then pass none)
+    return bytes == 0 ? 256 : bytes > 256 ? bytes : 512;
 }
 
 cgbn_status check_workspace(size_t need, const void* workspace, size_t have)

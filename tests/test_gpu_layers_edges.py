@@ -266,3 +266,24 @@ def test_more_tiles_than_a_launch_has_threads_for():
         assert not bool(h[at:at + (1 << 26)].view(torch.int16).any()), at
     del x, h, ws
     torch.cuda.empty_cache()
+
+
+def test_calls_without_a_workspace():
+    """Where the size asked for is 256 bytes none is needed; the results are those with one."""
+    asked = 0
+    for M, N, K in ((1, 1, 4096), (1, 8, 8192), (3, 40, 64), (16, 64, 1024), (65, 128, 64), (33, 64, 72), (257, 256, 512)):
+        for dtype in ("bf16", "f32"):
+            p = Linear(M, N, K, dtype, seed=16)
+            want = _linear(p.x, p.w, p.bias, "relu", dtype)
+            if L.cgbn_linear_workspace_bytes(M, N, K, dtype, False) <= 256:
+                y = torch.full_like(want, 7.0)
+                L.cgbn_linear_forward(p.x, p.w, p.bias, None, M, N, K, "relu", y, None, dtype)
+                assert torch.equal(y, want)
+                asked += 1
+            want = _gated(p.x, p.w, p.w, "silu", dtype)
+            if L.cgbn_gated_workspace_bytes(M, N, K, dtype, False) <= 256:
+                h = torch.full_like(want, 7.0)
+                L.cgbn_gated_forward(p.x, p.w, p.w, M, N, K, "silu", h, None, None, dtype)
+                assert torch.equal(h, want)
+                asked += 1
+    assert asked > 4

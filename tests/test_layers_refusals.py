@@ -50,3 +50,28 @@ def test_more_tiles_than_a_launch_has():
     _refused("cgbn_gated_forward", [{**big, "F": 200}], 2)
     # as tall, with a shape that does
     assert L.cgbn_linear_workspace_bytes(1 << 30, 200, 8, "bf16", False) and L.cgbn_linear_workspace_bytes(1 << 30, 128, 8, "f32", False)
+
+
+def test_a_workspace_that_is_asked_for_is_more_than_256_bytes():
+    """Sizes up to 256 say that a call may go without one: a call that refuses to was answered with more."""
+    seen = 0
+    for dtype in ("f32", "bf16"):
+        for M, N, K in ((1, 1, 4096), (1, 8, 8192), (2, 3, 4096), (1, 16, 4096), (1, 8, 8), (1, 64, 8), (33, 3, 5), (16, 8, 8192)):
+            for back in (False, True):
+                size = {"M": M, "K": K, "dtype": dtype, "workspace": None, "workspace_bytes": 0}
+                for fn, width, ask in (("cgbn_linear", "N", L.cgbn_linear_workspace_bytes), ("cgbn_gated", "F", L.cgbn_gated_workspace_bytes)):
+                    nbytes = ask(M, N, K, dtype, back)
+                    fn += "_backward" if back else "_forward"
+                    if nbytes > 256:
+                        assert _code(fn, {**CALLS[fn], **size, width: N, "act": "relu"}) == 6, (fn, M, N, K, dtype)
+                        seen += nbytes == 512
+                    else:
+                        assert not back
+        for T, Hq, Hk, D in ((0, 1, 0, 1), (1, 1, 0, 8), (1, 1, 1, 32), (5, 2, 1, 16)):
+            nbytes = L.cgbn_head_norm_workspace_bytes(T, Hq, Hk, D, dtype)
+            kw = {**CALLS["cgbn_head_norm_backward"], "T": T, "Hq": Hq, "Hk": Hk, "D": D, "R": 0, "dtype": dtype, "workspace": None, "workspace_bytes": 0}
+            assert nbytes > 256 and _code("cgbn_head_norm_backward", kw) == 6
+    assert seen > 8
+    # a call that does without, and one that does not, as they came with 256 bytes each
+    assert L.cgbn_linear_workspace_bytes(1, 16, 64, "bf16", False) == 256 and L.cgbn_linear_workspace_bytes(1, 16, 4096, "bf16", False) == 512
+    assert L.cgbn_gated_workspace_bytes(1, 8, 8, "bf16", True) > 256
