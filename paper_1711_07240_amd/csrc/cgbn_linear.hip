@@ -549,7 +549,7 @@ cgbn_status cgbn_linear_forward(const void* x, const void* w, const float* bias,
     if (act < CGBN_ACT_NONE || act > CGBN_ACT_SILU) return CGBN_ERR_ACTIVATION;
     if (M == 0) return CGBN_OK;
     if (!aligned16(x) || !aligned16(w) || !aligned16(y) || !aligned16(residual) || !aligned16(z)) return CGBN_ERR_ALIGN;
-    if (y == z || y == x || z == x || y == w || z == w) return CGBN_ERR_ALIAS;
+    if (y == z || y == x || z == x || y == w || z == w || (bias && (y == bias || z == bias))) return CGBN_ERR_ALIAS;
     const ForwardPlan p = plan_forward(M, N, K, dtype, false);
     if (p.none) return CGBN_ERR_SHAPE;
     CGBN_TRY(check_workspace(p.bytes, workspace, workspace_bytes));
@@ -575,6 +575,10 @@ cgbn_status cgbn_linear_backward(const void* dy, const void* x, const void* w, c
     if (M != 0 && dx && (dx == dw || dx == dresidual || dx == dy || dx == x || dx == w)) return CGBN_ERR_ALIAS;
     if (M != 0 && dw && (dw == dresidual || dw == dy || dw == x || dw == w)) return CGBN_ERR_ALIAS;
     if (M != 0 && dresidual && (dresidual == x || dresidual == w)) return CGBN_ERR_ALIAS;
+    // (without rows, too: these are set to zero)
+    if (dw && dw == w) return CGBN_ERR_ALIAS;
+    if (dbias && (dbias == w || dbias == dw)) return CGBN_ERR_ALIAS;
+    if (M != 0 && dbias && (dbias == dx || dbias == dresidual || dbias == dy || dbias == x || (act != CGBN_ACT_NONE && dbias == saved))) return CGBN_ERR_ALIAS;
     if (M > 0) {
         const BackwardPlan p = plan_backward(M, N, K, dtype, false);
         if (p.none) return CGBN_ERR_SHAPE;

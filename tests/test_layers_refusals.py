@@ -75,3 +75,14 @@ def test_a_workspace_that_is_asked_for_is_more_than_256_bytes():
     # a call that does without, and one that does not, as they came with 256 bytes each
     assert L.cgbn_linear_workspace_bytes(1, 16, 64, "bf16", False) == 256 and L.cgbn_linear_workspace_bytes(1, 16, 4096, "bf16", False) == 512
     assert L.cgbn_gated_workspace_bytes(1, 8, 8, "bf16", True) > 256
+
+
+def test_linear_results_over_the_bias_and_the_bias_gradient_over_others():
+    _refused("cgbn_linear_forward", [{"bias": 7 * P, "y": 7 * P}, {"bias": 7 * P, "z": 7 * P}], 11)
+    _refused("cgbn_linear_backward", [{"dbias": P * at} for at in (1, 2, 3, 4, 5, 6, 8)], 11)
+    # no rows: the weights' gradient is zero, and so would the weights be
+    _refused("cgbn_linear_backward", [{"M": 0, "dw": 3 * P}, {"M": 0, "dbias": 3 * P}, {"M": 0, "dbias": 6 * P}], 11)
+    # what is not wrong is refused for the workspace alone
+    for change in ({"dresidual": P}, {"dx": 4 * P}, {"act": 0, "dbias": 4 * P}):
+        assert _code("cgbn_linear_backward", {**CALLS["cgbn_linear_backward"], **change, "workspace": None}) == 6, change
+    assert _code("cgbn_linear_forward", {**CALLS["cgbn_linear_forward"], "M": 100, "K": 33, "y": 3 * P, "bias": 7 * P, "workspace": None}) == 6
