@@ -287,3 +287,47 @@ def test_calls_without_a_workspace():
                 assert torch.equal(h, want)
                 asked += 1
     assert asked > 4
+
+
+def _whole(gen, *shape, most, dtype):
+    return torch.randint(-most, most + 1, shape, device=DEV, generator=gen).to(TORCH[dtype])
+
+
+def _rounded(a, dtype):
+    """The nearest value of the type to a whole number below 2^24."""
+    return torch.from_numpy(a.astype(np.float32)).to(TORCH[dtype])
+
+
+@pytest.mark.parametrize("act", ["none", "relu"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [(1, 64, 64), (16, 40, 8200), (33, 65, 520), (257, 300, 264), (3000, 8, 40), (5000, 129, 64), (300, 72, 2056), (70, 3001, 24),
+                                  (130, 4096, 130), (64, 64, 8192)], ids=str)
+def test_sums_of_whole_numbers_are_exact(size, dtype, act):
+    """Of whole numbers every product and sum is exact in 32 bits, in any order: a term lost, doubled or taken from the wrong place shows,
+    however long the sum."""
+    M, N, K = size
+    gen = torch.Generator(device=DEV).manual_seed(sum(size))
+    x, w, dy = (_whole(gen, *s, most=3, dtype=dtype) for s in ((M, K), (N, K), (M, N)))
+    bias, saved = _whole(gen, N, most=9, dtype="f32"), _whole(gen, M, N, most=2, dtype=dtype)
+    x64, w64, b64, dy64, s64 = (f64(t) for t in (x, w, bias, dy, saved))
+    z = torch.empty(M, N, dtype=TORCH[dtype], device=DEV)
+    y = _linear(x, w, bias, act, dtype, z)
+    want = x64 @ w64.T + b64
+    assert torch.equal(z.cpu(), _rounded(want, dtype)) and torch.equal(y.cpu(), _rounded(np.maximum(want, 0) if act == "relu" else want, dtype))
+    dresidual = torch.empty_like(dy)
+    dx, dw = _backward(dy, x, w, dtype, saved if act == "relu" else None, act, dresidual)
+    dz = dy64 * (s64 > 0) if act == "relu" else dy64
+    assert torch.equal(dresidual.cpu(), _rounded(dz, dtype))
+    assert torch.equal(dx.cpu(), _rounded(dz @ w64, dtype)) and torch.equal(dw.cpu(), _rounded(dz.T @ x64, dtype))
+    # the gated pair: gate and up of up to 2, so that dg and du are whole numbers of few bits
+    wu, up = _whole(gen, N, K, most=3, dtype=dtype), _whole(gen, M, N, most=2, dtype=dtype)
+    gate_out, up_out = torch.empty_like(z), torch.empty_like(z)
+    _gated(x, w, wu, act, dtype, gate_out, up_out)
+    assert torch.equal(gate_out.cpu(), _rounded(x64 @ w64.T, dtype)) and torch.equal(up_out.cpu(), _rounded(x64 @ f64(wu).T, dtype))
+    a64, u64, wu64 = (np.maximum(s64, 0) if act == "relu" else s64), f64(up), f64(wu)
+    dg, du = dy64 * u64 * ((s64 > 0) if act == "relu" else 1), dy64 * a64
+    gx, gw, gu = torch.empty_like(x), torch.empty_like(w), torch.empty_like(w)
+    ws = torch.empty(L.cgbn_gated_workspace_bytes(M, N, K, dtype, True), dtype=torch.uint8, device=DEV)
+    L.cgbn_gated_backward(dy, x, w, wu, saved, up, M, N, K, act, gx, gw, gu, dtype, ws)
+    assert torch.equal(gx.cpu(), _rounded(dg @ w64 + du @ wu64, dtype))
+    assert torch.equal(gw.cpu(), _rounded(dg.T @ x64, dtype)) and torch.equal(gu.cpu(), _rounded(du.T @ x64, dtype))
