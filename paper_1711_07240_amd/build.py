@@ -37,8 +37,8 @@ FLAGS = [
     "-I", os.path.join(ROOT, "include"), "-I", CSRC,
 ]
 
-# the column-slab kernels keep their unit in registers: one whose registers spill is a build error (but for those held to half the
-# registers on purpose)
+# the column-slab kernels keep their unit in registers, the matrix products their sums: one whose registers spill is a build error (but for
+# the slab kernels held to half the registers on purpose)
 NO_SCRATCH = ["-Xarch_device", "-Wframe-larger-than=0", "-Xarch_device", "-Werror=frame-larger-than"]
 
 
@@ -49,7 +49,7 @@ def _units(obj_dir):
     for tname, t in (("f32", "float"), ("bf16", "bf16_t")):
         for form, fname in enumerate(("forward", "gated", "backward")):
             units.append((os.path.join(OBJ, f"gemm_{tname}_{fname}.o"), os.path.join(CSRC, "cgbn_gemm_inst.hip"),
-                          [f"-DCGBN_INST_T={t}", f"-DCGBN_INST_FORM={form}"]))
+                          [f"-DCGBN_INST_T={t}", f"-DCGBN_INST_FORM={form}"] + NO_SCRATCH))
     for tname, t in (("f32", "float"), ("bf16", "bf16_t")):
         for fwd in (1, 0):
             for act in ((0, 1, 2) if fwd else (0, 1)):       # forward: plain, ReLU, shortcut + ReLU

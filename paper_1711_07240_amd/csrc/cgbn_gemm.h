@@ -203,8 +203,10 @@ template <typename T, int N, bool NT = false> __device__ __forceinline__ void st
 
 // 16 bytes a lane from base + off to LDS at `lds` + 16 * lane.  Written out because the compiler, which cannot tell the two
 // halves of the buffer apart, would have every LDS read wait for the loads in flight into the other half.  No register is
-// written (but m0, in which the compiler keeps nothing); dma_wait_and_meet() below makes the bytes visible.  The wait state is what m0
-// needs before the load.
+// written but m0, which the compiler reserves: it writes it before each use of its own and keeps nothing in it (nor does it take it for a clobber).
+// dma_wait_and_meet() below makes the bytes visible.  The wait state is what the load needs after m0 is written.  Five are needed after the VECTOR unit
+// has written a scalar of the address, where a spilled one is brought back, say; waited for here, in every load, that is 2% of a product
+// (8192 x 8192 x 8192 774 and 794 us).  No kernel does so: tests/test_product_code.py reads it from their code.
 __device__ __forceinline__ void dma16(uint32_t lds, const char* base, uint32_t off)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
