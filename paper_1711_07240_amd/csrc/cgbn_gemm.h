@@ -21,7 +21,7 @@
 // 8192 x 4096 x 14336, 1430 us, 1345 TF); short ones with wide results the results' way to memory (16384 x 2048 x 8192 with z kept 518 us, 1061 TF and
 // 537 MB written; 67200 x 256 x 1024 with a residual 93.5 us, 3.3 TB/s, the matrix cores busy 15%).  Tiles of 256 x 256 read the least from
 // LDS for each product, but fill a compute unit alone, so that nothing is multiplied while their results leave; smaller ones run side by
-// side.  No bank conflicts (counted).  Float, three bfloat16 parts a value: 8192 x 8192 x 2048 198 TF, 12544-long 512 x 1024 85 us, 154 TF.
+// side.  No bank conflicts (counted).  Float, three bfloat16 parts a value: 8192 x 8192 x 2048 1382 us, 199 TF, 12544-long 512 x 1024 87 us, 152 TF.
 //
 // Sums are held in 32 bits throughout.  Where tiles are too few for 256 compute units the reduction is split and the partial
 // sums, float, are joined by gemm_join in split order: results never depend on the order in which workgroups end.
@@ -78,8 +78,8 @@ template <bool FINE> __device__ __forceinline__ float bell(float z)
 }
 
 // Phi(-|z|), e being exp(-z^2 / 2).  Short: the rational approximation of the complementary error function that Abramowitz and Stegun give as
-// 7.1.26 (after Hastings).  It counts: an epilogue is bound by its instructions, 14 a value for GELU, 53 us of 534 at 16384 x 2048 x 8192 (with the
-// library's erff, 45 and 150).  Fine: of the same form, t = 1 / (1 + 0.35 |z|), a polynomial of degree 8 fitted to Phi(-z) / (e t) over z in
+// 7.1.26 (after Hastings).  It counts: an epilogue is bound by its instructions, 14 a value for GELU, 40 us of 520 at 16384 x 2048 x 8192 (the
+// library's erff cost about three times as much).  Fine: of the same form, t = 1 / (1 + 0.35 |z|), a polynomial of degree 8 fitted to Phi(-z) / (e t) over z in
 // [0, 14] for the least largest relative error, 3.2e-8; evaluated in 32 bits it is off by 7 units of 2^-24 of itself.
 template <bool FINE> __device__ __forceinline__ float normal_tail(float z, float e)
 {
@@ -333,7 +333,7 @@ template <typename T> __device__ __forceinline__ f32x4 multiply(const u32x4& a, 
 // Float values as sums of three bfloat16, which is exact: the first is cut off (rounded, the type's largest values would become infinities), the second
 // is what is left rounded to nearest, so that the third has either sign and what a product drops no preferred one.
 // (Parts below the smallest normal number are lost: values under 1e-33 have fewer than 24 bits.)  8 values of a lane, from two chunks.
-// QUIET: a NaN whose upper half alone would be an infinity keeps to be one: the bit that makes it quiet is in the upper half.
+// QUIET: a NaN whose upper half alone would be an infinity stays a NaN: the bit that makes it quiet is in the upper half.
 template <bool QUIET> __device__ __forceinline__ void split_float(const u32x4& lo, const u32x4& hi, u32x4 (&part)[3])
 {
     auto value = [](uint32_t v) { return QUIET ? __builtin_canonicalizef(__uint_as_float(v)) : __uint_as_float(v); };
