@@ -1252,6 +1252,9 @@ SweepArgs sweep_args(const Plan& p)
     return A;
 }
 
+// A launch has less than 2^32 threads: of more the runtime starts some, without an error.  (2^26 planes of a wavefront each, say.)
+bool launchable(long long groups) { return groups < (1LL << 32) / kThreads; }
+
 template <typename T, int OP> void launch_reduce_t(const Plan& p, const SweepArgs& A, hipStream_t st)
 {
     dim3 grid((unsigned)p.grid), block(kThreads);
@@ -1294,6 +1297,7 @@ template <typename T, int EL> void launch_map_t(const Plan& p, const SweepArgs& 
 cgbn_status launch_reduce(int op, const Plan& p, const SweepArgs& A, hipStream_t st)
 {
     const bool f32 = p.dtype == CGBN_F32;
+    if (!launchable(p.grid)) return CGBN_ERR_SHAPE;
     switch (op) {
     case OP_SUM:   f32 ? launch_reduce_t<float, OP_SUM>(p, A, st)   : launch_reduce_t<bf16_t, OP_SUM>(p, A, st); break;
     case OP_SQDEV: f32 ? launch_reduce_t<float, OP_SQDEV>(p, A, st) : launch_reduce_t<bf16_t, OP_SQDEV>(p, A, st); break;
@@ -1307,6 +1311,7 @@ cgbn_status launch_reduce(int op, const Plan& p, const SweepArgs& A, hipStream_t
 cgbn_status launch_map(int el, const Plan& p, const SweepArgs& A, hipStream_t st)
 {
     const bool f32 = p.dtype == CGBN_F32;
+    if (!launchable(p.layout == CGBN_NCHW ? p.grid : p.map[el_has_3(el) ? 2 : el_has_2(el) ? 1 : 0].grid)) return CGBN_ERR_SHAPE;
     switch (el) {
     case EL_NORM:   f32 ? launch_map_t<float, EL_NORM>(p, A, st)   : launch_map_t<bf16_t, EL_NORM>(p, A, st); break;
     case EL_DX:     f32 ? launch_map_t<float, EL_DX>(p, A, st)     : launch_map_t<bf16_t, EL_DX>(p, A, st); break;
