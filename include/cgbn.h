@@ -79,7 +79,7 @@ enum {
     CGBN_ERR_MOMENTUM = 10,  /* momentum outside [0, 1] */
     CGBN_ERR_ALIAS = 11,     /* two outputs that must differ are the same buffer */
     CGBN_ERR_SCRATCH = 12,   /* cgbn_forward_static: the problem needs more than CGBN_STATIC_SCRATCH_BYTES */
-    CGBN_ERR_ACTIVATION = 13, /* an activation or rotation that is not in its list */
+    CGBN_ERR_ACTIVATION = 13, /* an activation, rotation or scaling that is not in its list */
     CGBN_ERR_STRIDE = 14     /* rows of a strided tensor overlap */
 };
 
@@ -332,6 +332,75 @@ cgbn_status cgbn_head_norm_backward(const void* dyq, long long lddyq, const void
                                     int table_rows, const float* wq, const float* wk, float eps, void* dq, long long lddq,
                                     void* dk, long long lddk, float* dwq, float* dwk, cgbn_dtype dtype,
                                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- Serving: rotation by position without a norm, a cache of keys and values in pages, attention over it.  The conventions of the layers
+ * above hold (types, alignment, sums in 32 bits, statuses, streams; calls on different streams may overlap, each with its own workspace).
+ * The cache of one layer is two pools of `pages` pages, k_pages and v_pages[pages][Hk][page][D]: a page holds `page` tokens (a power of two up to 1024),
+ * head by head.  A request's tokens lie in the pages that its row of `table` names, in order; the prefix that all requests of a
+ * batch share lies in the pages of a table of its own, is `prefix` tokens long and precedes the first token of each.  A place (slot) in the pools is page id * page + token
+ * in page; pages * page < 2^31.  Page ids outside [0, pages) are no error: they stand for pages that are not there. ---- */
+
+/* How the frequencies of a rotation are stretched for contexts longer than those a model was trained on, by `factor` >= 1 (f[i] = base^(-2i / R)):
+ * f / factor; with base * factor^(R / (R - 2)) for the base; by parts, g f + (1 - g) f / factor with g = (turns - slow) / (fast - slow)
+ * within [0, 1] and turns = trained f / (2 pi), the turns that a pair made over the `trained` positions. */
+typedef int cgbn_scaling;
+enum { CGBN_SCALE_NONE = 0, CGBN_SCALE_POSITIONS = 1, CGBN_SCALE_BASE = 2, CGBN_SCALE_PARTS = 3 };
+
+/* The R/2 frequencies, radians a position, to HOST memory.  Host-only, launches nothing.  base > 1; trained, fast and slow (trained >= 1,
+ * fast > slow >= 0) are looked at by parts alone. */
+cgbn_status cgbn_rotary_frequencies(int R, double base, cgbn_scaling scaling, double factor, double trained, double fast, double slow,
+                                    double* freq);
+
+/* The first R values of every head of D are turned by the token's position (a, b) -> magnitude (a cos t - b sin t, b cos t + a sin t) with t = p freq[i],
+ * p = positions[token] (any int; the token's own index if positions is NULL), freq[R/2] a DEVICE vector of doubles; the others are copied.  Rows, heads, strides and
+ * `style` as in cgbn_head_norm_forward; Hk may be 0; yq may be exactly q (with its stride), yk exactly k.  Turns are counted in 64 bits: angles are as exact
+ * at position 2^31 as at 0, up to the product's own rounding. */
+cgbn_status cgbn_rotate_forward(const void* q, long long ldq, const void* k, long long ldk, long long T, int Hq, int Hk, int D, int R,
+                                cgbn_rotation style, const int* positions, const double* freq, float magnitude, void* yq, long long ldyq,
+                                void* yk, long long ldyk, cgbn_dtype dtype, void* stream);
+
+/* Its backward: gradients turned back, times magnitude.  dq may be exactly dyq (with its stride), dk exactly dyk. */
+cgbn_status cgbn_rotate_backward(const void* dyq, long long lddyq, const void* dyk, long long lddyk, long long T, int Hq, int Hk, int D, int R,
+                                 cgbn_rotation style, const int* positions, const double* freq, float magnitude, void* dq, long long lddq,
+                                 void* dk, long long lddk, cgbn_dtype dtype, void* stream);
+
+/* Bytes of workspace of a plan. */
+size_t cgbn_page_plan_workspace_bytes(int B, long long T);
+
+/* The plan of a step: request b has have[b] tokens of its own in the cache and gets fresh[b] (either may be 0; less counts as 0).  All of it on the device.
+ *   rows[B + 1]     where each request's new tokens start among the step's T rows, in order; tokens beyond row T are cut off
+ *   lengths[B]      tokens of its own after the step
+ *   table[B][max_pages]  in and out: pages that a request needs beyond those that have[b] tokens take come from free_pages[free_count], in order,
+ *                   from the taken[0]-th on, first request first; where the list or the row of the table is at its end there are none (-1 in the table)
+ *   slots[T], positions[T]   each row's place in the cache (-1: it has none) and its position, `before` (the prefix's length) + its index
+ *                   in its request; rows behind the last token: -1 and 0
+ *   counts[2]       pages of the list that are taken now; new tokens that got no place or no row (at most 2^31 - 1).  counts may be exactly taken.
+ * have[b] is cut to max_pages * page.  0 <= before <= 2^30, B <= 2^20, T <= 2^29, 1 <= max_pages <= 2^16. */
+cgbn_status cgbn_page_plan(const int* have, const int* fresh, int B, int before, const int* free_pages, int free_count, const int* taken,
+                           int* counts, int* table, int max_pages, int pages, int page, long long T, int* rows, int* lengths, int* slots,
+                           int* positions, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Puts T tokens' keys and values (Hk heads of D values side by side, row to row ldk and ldv elements, rows on 16 bytes) to their places in
+ * the pages; tokens whose slot is outside the pools are left out.  Two tokens of one call have different slots (of equal ones either may stay, in parts).
+ * D a multiple of 8 up to 256. */
+cgbn_status cgbn_page_store(const void* k, long long ldk, const void* v, long long ldv, long long T, int Hk, int D, const int* slots,
+                            void* k_pages, void* v_pages, int pages, int page, cgbn_dtype dtype, void* stream);
+
+/* Bytes of workspace of the attention below; capacity: max_pages * page. */
+size_t cgbn_prefix_attention_workspace_bytes(long long T, int B, int Hq, int Hk, int D, long long prefix, long long capacity,
+                                             cgbn_dtype dtype);
+
+/* out = softmax(scale q k^T) v, head by head, of the T rows' queries (Hq heads of D values, Hq a multiple of Hk: head h reads keys of head h / (Hq / Hk)).
+ * Request b's queries are rows rows[b] ... rows[b + 1] - 1 (rows[0] = 0, ascending), its last tokens: the j-th of n sees the prefix and its request's tokens up to
+ * itself, the first lengths[b] - n + j + 1.  rows may be NULL: one row each, T = B.  Rows behind rows[B] are left as they were.
+ * A row that sees no key is zero.  lse[T][Hq], if not NULL: the logarithm of the sum of the exponentials of a row's scores, -infinity where there is no key.
+ *   Keys beyond lengths[b], in pages that are not there, or later than a row's own are not looked at, whatever their places hold.  max_pages = 0: no own tokens,
+ *   table and lengths are not read.  Weights are rounded to bfloat16 for the products of bfloat16 tensors, their sum is not.
+ *   D a multiple of 8 up to 256; rows of q and out on 16 bytes; T * Hq < 2^26 - 3. */
+cgbn_status cgbn_prefix_attention(const void* q, long long ldq, long long T, int B, const int* rows, const int* lengths, int Hq, int Hk,
+                                  int D, float scale, const void* k_pages, const void* v_pages, int pages, int page,
+                                  const int* prefix_table, int prefix, const int* table, int max_pages, void* out, long long ldo,
+                                  float* lse, cgbn_dtype dtype, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- housekeeping ---- */
 

@@ -6,7 +6,9 @@ x activation), the column-slab kernels in eight (element type x direction x
 register limit),
 compiled side by side; the layers beside the normalization are a unit for their
 host code and small kernels, one for the head norm, and six for the matrix
-products (element type x forward, gated, backward).  Then everything is linked
+products (element type x forward, gated, backward); the serving operators are
+one each for the rotation, the pages and the attention's host code, and two for
+its kernels (element type).  Then everything is linked
 into one shared library.  The binding's extension is one C file."""
 
 from __future__ import annotations
@@ -45,7 +47,9 @@ NO_SCRATCH = ["-Xarch_device", "-Wframe-larger-than=0", "-Xarch_device", "-Werro
 def _units(obj_dir):
     """(object file, source, extra flags) of every translation unit."""
     OBJ = obj_dir
-    units = [(os.path.join(OBJ, name + ".o"), os.path.join(CSRC, name + ".hip"), []) for name in ("cgbn", "cgbn_linear", "cgbn_head_norm")]
+    units = [(os.path.join(OBJ, name + ".o"), os.path.join(CSRC, name + ".hip"), []) for name in ("cgbn", "cgbn_linear", "cgbn_head_norm", "cgbn_rotate", "cgbn_pages", "cgbn_attention")]
+    for tname, t in (("f32", "float"), ("bf16", "bf16_t")):
+        units.append((os.path.join(OBJ, f"attention_{tname}.o"), os.path.join(CSRC, "cgbn_attention_inst.hip"), [f"-DCGBN_INST_T={t}"]))
     for tname, t in (("f32", "float"), ("bf16", "bf16_t")):
         for form, fname in enumerate(("forward", "gated", "backward")):
             units.append((os.path.join(OBJ, f"gemm_{tname}_{fname}.o"), os.path.join(CSRC, "cgbn_gemm_inst.hip"),

@@ -28,9 +28,10 @@ LAYOUTS = {"NCHW": CGBN_NCHW, "NHWC": CGBN_NHWC}
 DTYPES = {"f32": CGBN_F32, "bf16": CGBN_BF16}
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 ROTATIONS = {"halves": 0, "interleaved": 1}
+SCALINGS = {"none": 0, "positions": 1, "base": 2, "parts": 3}
 
-_c_int, _c_ll, _c_f, _c_sz, _c_p = (ctypes.c_int, ctypes.c_longlong, ctypes.c_float,
-                                     ctypes.c_size_t, ctypes.c_void_p)
+_c_int, _c_ll, _c_f, _c_sz, _c_p, _c_d = (ctypes.c_int, ctypes.c_longlong, ctypes.c_float,
+                                           ctypes.c_size_t, ctypes.c_void_p, ctypes.c_double)
 
 # name -> (restype, argtypes); mirrors include/cgbn.h declaration by declaration
 SIGNATURES = {
@@ -72,6 +73,15 @@ SIGNATURES = {
     "cgbn_head_norm_workspace_bytes": (_c_sz, [_c_ll, _c_int, _c_int, _c_int, _c_int]),
     "cgbn_head_norm_backward": (_c_int, [_c_p, _c_ll] * 4 + [_c_ll] + [_c_int] * 5 + [_c_p] * 3 + [_c_int, _c_p, _c_p, _c_f]
                                 + [_c_p, _c_ll] * 2 + [_c_p, _c_p, _c_int, _c_p, _c_sz, _c_p]),
+    "cgbn_rotary_frequencies": (_c_int, [_c_int, _c_d, _c_int] + [_c_d] * 4 + [_c_p]),
+    "cgbn_rotate_forward": (_c_int, [_c_p, _c_ll] * 2 + [_c_ll] + [_c_int] * 5 + [_c_p] * 2 + [_c_f] + [_c_p, _c_ll] * 2 + [_c_int, _c_p]),
+    "cgbn_rotate_backward": (_c_int, [_c_p, _c_ll] * 2 + [_c_ll] + [_c_int] * 5 + [_c_p] * 2 + [_c_f] + [_c_p, _c_ll] * 2 + [_c_int, _c_p]),
+    "cgbn_page_plan_workspace_bytes": (_c_sz, [_c_int, _c_ll]),
+    "cgbn_page_plan": (_c_int, [_c_p] * 2 + [_c_int] * 2 + [_c_p, _c_int] + [_c_p] * 3 + [_c_int] * 3 + [_c_ll] + [_c_p] * 5 + [_c_sz, _c_p]),
+    "cgbn_page_store": (_c_int, [_c_p, _c_ll] * 2 + [_c_ll, _c_int, _c_int] + [_c_p] * 3 + [_c_int] * 3 + [_c_p]),
+    "cgbn_prefix_attention_workspace_bytes": (_c_sz, [_c_ll] + [_c_int] * 4 + [_c_ll] * 2 + [_c_int]),
+    "cgbn_prefix_attention": (_c_int, [_c_p, _c_ll, _c_ll, _c_int, _c_p, _c_p] + [_c_int] * 3 + [_c_f, _c_p, _c_p] + [_c_int] * 2 + [_c_p, _c_int]
+                              + [_c_p, _c_int, _c_p, _c_ll, _c_p, _c_int, _c_p, _c_sz, _c_p]),
     "cgbn_calibration_copy": (_c_int, [_c_p, _c_p, _c_sz, _c_p]),
     "cgbn_status_string": (ctypes.c_char_p, [_c_int]),
     "cgbn_set_tuning": (_c_int, [ctypes.c_char_p, _c_ll]),
@@ -87,6 +97,7 @@ class _ByCtypes:
     """In the place of the extension where it is not built for this Python: every call goes through ctypes."""
     forward = forward_relu = backward = backward_relu = frozen_forward = frozen_backward = staticmethod(lambda *_: NotImplemented)
     linear_forward = linear_backward = gated_forward = gated_backward = head_norm_forward = head_norm_backward = forward
+    rotate_forward = rotate_backward = page_plan = page_store = prefix_attention = forward
 
 
 class CgbnError(RuntimeError):
@@ -125,6 +136,7 @@ def _load_extension(handle):
               _stream)
     call.bind_layers(addresses("linear_forward", "linear_backward", "gated_forward", "gated_backward", "head_norm_forward",
                                "head_norm_backward"), ACTIVATIONS, ROTATIONS)
+    call.bind_serving(addresses("rotate_forward", "rotate_backward", "page_plan", "page_store", "prefix_attention"))
     return call
 
 
@@ -423,6 +435,73 @@ def cgbn_head_norm_backward(dyq, lddyq, dyk, lddyk, q, ldq, k, ldk, T, Hq, Hk, D
             _stream(stream))
     if code:
         _check(code, "cgbn_head_norm_backward")
+
+
+def cgbn_rotary_frequencies(R, base, scaling, factor, trained, fast, slow, freq) -> None:
+    """freq: R/2 doubles in host memory (an array or CPU tensor with a data_ptr(), or an address)."""
+    _check(lib().cgbn_rotary_frequencies(R, float(base), _enum(SCALINGS, scaling), float(factor), float(trained), float(fast), float(slow),
+                                         _ptr(freq)), "cgbn_rotary_frequencies")
+
+
+def cgbn_rotate_forward(q, ldq, k, ldk, T, Hq, Hk, D, R, style, positions, freq, magnitude, yq, ldyq, yk, ldyk, dtype="f32", stream=None) -> None:
+    code = (_call or _calls()).rotate_forward(q, ldq, k, ldk, T, Hq, Hk, D, R, style, positions, freq, magnitude, yq, ldyq, yk, ldyk, dtype, stream)
+    if code is NotImplemented:
+        code = lib().cgbn_rotate_forward(_ptr(q), ldq, _ptr(k), ldk, T, Hq, Hk, D, R, _enum(ROTATIONS, style), _ptr(positions), _ptr(freq),
+            float(magnitude), _ptr(yq), ldyq, _ptr(yk), ldyk, _enum(DTYPES, dtype), _stream(stream))
+    if code:
+        _check(code, "cgbn_rotate_forward")
+
+
+def cgbn_rotate_backward(dyq, lddyq, dyk, lddyk, T, Hq, Hk, D, R, style, positions, freq, magnitude, dq, lddq, dk, lddk, dtype="f32",
+                         stream=None) -> None:
+    code = (_call or _calls()).rotate_backward(dyq, lddyq, dyk, lddyk, T, Hq, Hk, D, R, style, positions, freq, magnitude, dq, lddq, dk, lddk, dtype,
+                                               stream)
+    if code is NotImplemented:
+        code = lib().cgbn_rotate_backward(_ptr(dyq), lddyq, _ptr(dyk), lddyk, T, Hq, Hk, D, R, _enum(ROTATIONS, style), _ptr(positions), _ptr(freq),
+            float(magnitude), _ptr(dq), lddq, _ptr(dk), lddk, _enum(DTYPES, dtype), _stream(stream))
+    if code:
+        _check(code, "cgbn_rotate_backward")
+
+
+def cgbn_page_plan_workspace_bytes(B, T) -> int:
+    return int(lib().cgbn_page_plan_workspace_bytes(B, T))
+
+
+def cgbn_page_plan(have, fresh, B, before, free_pages, free_count, taken, counts, table, max_pages, pages, page, T, rows, lengths, slots, positions,
+                   workspace=None, workspace_bytes=None, stream=None) -> None:
+    code = (_call or _calls()).page_plan(have, fresh, B, before, free_pages, free_count, taken, counts, table, max_pages, pages, page, T, rows, lengths,
+                                         slots, positions, workspace, workspace_bytes, stream)
+    if code is NotImplemented:
+        code = lib().cgbn_page_plan(_ptr(have), _ptr(fresh), B, before, _ptr(free_pages), free_count, _ptr(taken), _ptr(counts), _ptr(table), max_pages,
+            pages, page, T, _ptr(rows), _ptr(lengths), _ptr(slots), _ptr(positions), _ptr(workspace),
+            _room(workspace, workspace_bytes), _stream(stream))
+    if code:
+        _check(code, "cgbn_page_plan")
+
+
+def cgbn_page_store(k, ldk, v, ldv, T, Hk, D, slots, k_pages, v_pages, pages, page, dtype="f32", stream=None) -> None:
+    code = (_call or _calls()).page_store(k, ldk, v, ldv, T, Hk, D, slots, k_pages, v_pages, pages, page, dtype, stream)
+    if code is NotImplemented:
+        code = lib().cgbn_page_store(_ptr(k), ldk, _ptr(v), ldv, T, Hk, D, _ptr(slots), _ptr(k_pages), _ptr(v_pages), pages, page,
+            _enum(DTYPES, dtype), _stream(stream))
+    if code:
+        _check(code, "cgbn_page_store")
+
+
+def cgbn_prefix_attention_workspace_bytes(T, B, Hq, Hk, D, prefix, capacity, dtype) -> int:
+    return int(lib().cgbn_prefix_attention_workspace_bytes(T, B, Hq, Hk, D, prefix, capacity, _enum(DTYPES, dtype)))
+
+
+def cgbn_prefix_attention(q, ldq, T, B, rows, lengths, Hq, Hk, D, scale, k_pages, v_pages, pages, page, prefix_table, prefix, table, max_pages, out, ldo,
+                          lse=None, dtype="f32", workspace=None, workspace_bytes=None, stream=None) -> None:
+    code = (_call or _calls()).prefix_attention(q, ldq, T, B, rows, lengths, Hq, Hk, D, scale, k_pages, v_pages, pages, page, prefix_table, prefix,
+                                                table, max_pages, out, ldo, lse, dtype, workspace, workspace_bytes, stream)
+    if code is NotImplemented:
+        code = lib().cgbn_prefix_attention(_ptr(q), ldq, T, B, _ptr(rows), _ptr(lengths), Hq, Hk, D, float(scale), _ptr(k_pages), _ptr(v_pages), pages,
+            page, _ptr(prefix_table), prefix, _ptr(table), max_pages, _ptr(out), ldo, _ptr(lse), _enum(DTYPES, dtype),
+            _ptr(workspace), _room(workspace, workspace_bytes), _stream(stream))
+    if code:
+        _check(code, "cgbn_prefix_attention")
 
 
 def cgbn_calibration_copy(src, dst, nbytes, stream=None) -> None:

@@ -1,0 +1,129 @@
+// Attention over a shared prefix and pages of each request's own: arguments and the choice of tiles.  The kernels are in cgbn_attention.h.
+#include "cgbn.h"
+#include "cgbn_attention.h"
+
+#include <cstring>
+
+namespace cgbn {
+namespace {
+
+constexpr int kMaxHeads = 1 << 10, kMaxRequests = 1 << 20, kMaxPage = 1024, kMaxTable = 1 << 20;
+constexpr long long kMaxKeys = 1ll << 30, kMaxRows = 1ll << 26;          // rows: heads of tokens
+
+struct Plan {
+    int way, prefix_splits, prefix_per, own_splits, prefix_tiles, own_tiles, whole;
+    long long prefix_jobs, jobs;
+    int parts() const { return prefix_splits + own_splits; }
+};
+
+bool sizes_fit(long long T, int B, int Hq, int Hk, int D, long long prefix, long long capacity)
+{
+    if (T < 0 || B < 0 || B > kMaxRequests || Hk < 1 || Hq < Hk || Hq > kMaxHeads || Hq % Hk != 0 || D < 8 || D > 256 || D % 8 != 0) return false;
+    return T <= (kMaxRows - 4) / Hq && prefix >= 0 && prefix < kMaxKeys && capacity >= 0 && capacity < kMaxKeys;
+}
+
+long long up(long long a, long long b) { return (a + b - 1) / b; }
+
+// What the device has to know of the lengths stays there: ranges of a request's own keys are cut by its length where they are read, `own_splits` of
+// them.  `several`: requests may have more rows than one.
+Plan plan(long long T, int B, int Hq, int Hk, long long prefix, long long capacity, bool several)
+{
+    Plan p;
+    std::memset(&p, 0, sizeof(p));
+    const long long g = Hq / Hk, rows = T * g, each = several ? up(rows, B) : g;
+    // tiles of rows: no more of them empty than has to be
+    if (each > 32) p.way = WAY_128_128;
+    else if (each > 16) p.way = rows > 32 ? WAY_128_32 : WAY_32_32;
+    else p.way = rows > 32 ? WAY_128_16 : rows > 16 ? WAY_32_16 : WAY_16_16;
+    p.prefix_tiles = (int)up(rows, kPrefixRows[p.way]);
+    const long long own_tiles = several ? rows / kOwnRows[p.way] + B : B * up(g, kOwnRows[p.way]);
+    p.own_tiles = (int)own_tiles;
+    if (p.way == WAY_128_128 && own_tiles * Hk >= 256) {
+        p.whole = 1;
+        p.own_splits = 1;
+        p.prefix_tiles = 0;
+        p.jobs = own_tiles * Hk;
+        return p;
+    }
+    p.own_splits = prefix ? 0 : 1;         // (without any keys rows are zero)
+    if (capacity) {
+        long long s = 1024 / (own_tiles * Hk);
+        if (s > up(capacity, 256)) s = up(capacity, 256);
+        p.own_splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+    }
+    if (prefix) {
+        long long s = 512 / ((long long)p.prefix_tiles * Hk);
+        if (s > up(prefix, 256)) s = up(prefix, 256);
+        s = s < 1 ? 1 : s > 64 ? 64 : s;
+        p.prefix_per = (int)up(up(prefix, s), 128) * 128;
+        p.prefix_splits = (int)up(prefix, p.prefix_per);
+    }
+    p.prefix_jobs = (long long)p.prefix_tiles * p.prefix_splits * Hk;
+    p.jobs = p.prefix_jobs + own_tiles * p.own_splits * Hk;
+    return p;
+}
+
+// bytes of the parts
+size_t scratch(const Plan& p, long long T, int Hq, int D) { return p.parts() <= 1 ? 0 : (size_t)p.parts() * T * Hq * (D + 2) * sizeof(float); }
+
+}  // namespace
+}  // namespace cgbn
+
+using namespace cgbn;
+
+extern "C" {
+
+size_t cgbn_prefix_attention_workspace_bytes(long long T, int B, int Hq, int Hk, int D, long long prefix, long long capacity, cgbn_dtype dtype)
+{
+    if ((dtype != CGBN_F32 && dtype != CGBN_BF16) || !sizes_fit(T, B, Hq, Hk, D, prefix, capacity)) return 0;
+    if (T == 0 || B == 0) return 256;
+    // requests of one row each go in other tiles when it is said that they are
+    size_t most = scratch(plan(T, B, Hq, Hk, prefix, capacity, true), T, Hq, D);
+    if (T == B) {
+        const size_t single = scratch(plan(T, B, Hq, Hk, prefix, capacity, false), T, Hq, D);
+        if (single > most) most = single;
+    }
+    const size_t bytes = (most + 255) / 256 * 256;
+    return most == 0 ? 256 : bytes > 256 ? bytes : 512;          // (of 256 or less a program may pass none)
+}
+
+cgbn_status cgbn_prefix_attention(const void* q, long long ldq, long long T, int B, const int* rows, const int* lengths, int Hq, int Hk, int D, float scale,
+                                  const void* k_pages, const void* v_pages, int pages, int page, const int* prefix_table, int prefix, const int* table,
+                                  int max_pages, void* out, long long ldo, float* lse, cgbn_dtype dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (dtype != CGBN_F32 && dtype != CGBN_BF16) return CGBN_ERR_ENUM;
+    if (page < 1 || page > kMaxPage || (page & (page - 1)) || pages < 0 || (long long)pages * page >= (1ll << 31) || max_pages < 0 || max_pages > kMaxTable) return CGBN_ERR_SHAPE;
+    const long long capacity = (long long)max_pages * page;
+    if (!sizes_fit(T, B, Hq, Hk, D, prefix, capacity) || (!rows && T != B)) return CGBN_ERR_SHAPE;
+    if (T == 0 || B == 0) return CGBN_OK;
+    if (!q || !out || (pages && (!k_pages || !v_pages)) || (prefix && !prefix_table) || (max_pages && (!table || !lengths))) return CGBN_ERR_NULL;
+    const long long elem = dtype == CGBN_F32 ? 4 : 2, width = (long long)Hq * D;
+    if (ldq > (1ll << 32) || ldo > (1ll << 32)) return CGBN_ERR_SHAPE;
+    if (T > 1 && (ldq < width || ldo < width)) return CGBN_ERR_STRIDE;
+    const uintptr_t sixteen = reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(k_pages) | reinterpret_cast<uintptr_t>(v_pages);
+    const uintptr_t four = reinterpret_cast<uintptr_t>(rows) | reinterpret_cast<uintptr_t>(lengths) | reinterpret_cast<uintptr_t>(prefix_table) |
+                           reinterpret_cast<uintptr_t>(table) | reinterpret_cast<uintptr_t>(lse);
+    if (sixteen % 16 || four % 4 || (T > 1 && (ldq * elem % 16 || ldo * elem % 16))) return CGBN_ERR_ALIGN;
+    const void* const in[] = {q, rows, lengths, k_pages, v_pages, prefix_table, table, workspace};
+    for (const void* p : in)
+        if (p && (p == out || p == lse)) return CGBN_ERR_ALIAS;
+    if (out == lse) return CGBN_ERR_ALIAS;
+    const Plan p = plan(T, B, Hq, Hk, prefix, capacity, rows != nullptr);
+    if (p.jobs >= (1ll << 24)) return CGBN_ERR_SHAPE;           // 2^32 threads
+    AttendArgs A;
+    std::memset(&A, 0, sizeof(A));
+    const size_t need = scratch(p, T, Hq, D);
+    if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need)) return CGBN_ERR_WORKSPACE;
+    A.part_o = static_cast<float*>(workspace);
+    A.part_ml = reinterpret_cast<float2*>(A.part_o + (size_t)p.parts() * T * Hq * D);
+    A.q = static_cast<const char*>(q); A.k_pages = static_cast<const char*>(k_pages); A.v_pages = static_cast<const char*>(v_pages);
+    A.out = static_cast<char*>(out); A.lse = lse; A.rows = rows; A.lengths = lengths; A.prefix_table = prefix_table; A.table = table;
+    A.ldq = ldq; A.ldo = ldo; A.T = T; A.B = B; A.Hq = Hq; A.Hk = Hk; A.g = Hq / Hk; A.D = D; A.pages = pages; A.prefix = prefix; A.max_pages = max_pages;
+    while ((1 << A.page_bits) < page) ++A.page_bits;
+    A.prefix_splits = p.prefix_splits; A.prefix_per = p.prefix_per; A.own_splits = p.own_splits; A.prefix_tiles = p.prefix_tiles; A.own_tiles = p.own_tiles;
+    A.prefix_jobs = (int)p.prefix_jobs; A.jobs = (int)p.jobs; A.whole = p.whole; A.direct = p.parts() <= 1; A.scale = scale * 1.4426950408889634f;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return dtype == CGBN_F32 ? launch_attend<float>(A, p.way, st) : launch_attend<bf16_t>(A, p.way, st);
+}
+
+}  // extern "C"

@@ -37,6 +37,19 @@ typedef cgbn_status (*head_norm_backward_fn)(const void*, long long, const void*
                                              int, int, int, int, cgbn_rotation, const int*, const float*, const float*, int, const float*,
                                              const float*, float, void*, long long, void*, long long, float*, float*, cgbn_dtype, void*, size_t, void*);
 
+typedef cgbn_status (*rotate_fn)(const void*, long long, const void*, long long, long long, int, int, int, int, cgbn_rotation, const int*, const double*,
+                                 float, void*, long long, void*, long long, cgbn_dtype, void*);
+typedef cgbn_status (*page_plan_fn)(const int*, const int*, int, int, const int*, int, const int*, int*, int*, int, int, int, long long, int*, int*, int*,
+                                    int*, void*, size_t, void*);
+typedef cgbn_status (*page_store_fn)(const void*, long long, const void*, long long, long long, int, int, const int*, void*, void*, int, int, cgbn_dtype,
+                                     void*);
+typedef cgbn_status (*prefix_attention_fn)(const void*, long long, long long, int, const int*, const int*, int, int, int, float, const void*, const void*,
+                                           int, int, const int*, int, const int*, int, void*, long long, float*, cgbn_dtype, void*, size_t, void*);
+
+static rotate_fn g_rotate_forward, g_rotate_backward;
+static page_plan_fn g_page_plan;
+static page_store_fn g_page_store;
+static prefix_attention_fn g_prefix_attention;
 static linear_forward_fn g_linear_forward;
 static linear_backward_fn g_linear_backward;
 static gated_forward_fn g_gated_forward;
@@ -349,6 +362,114 @@ static PyObject* head_norm_backward(PyObject* self, PyObject* const* a, Py_ssize
                               lddk, dwq, dwk, dtype, ws, bytes, st));
 }
 
+#define SERVING_ARGS(count_)                                                                             \
+    LAYER_ARGS(count_)                                                                                   \
+    if (!g_rotate_forward) { PyErr_SetString(PyExc_RuntimeError, "bind_serving() first"); return NULL; }
+
+static PyObject* rotate(PyObject* const* a, Py_ssize_t n, rotate_fn* fn)
+{
+    SERVING_ARGS(19)
+    const void* q = ptr(a[0], &plain);
+    const long long ldq = wide(a[1], &plain);
+    const void* k = ptr(a[2], &plain);
+    const long long ldk = wide(a[3], &plain), T = wide(a[4], &plain);
+    const int Hq = num(a[5], &plain), Hk = num(a[6], &plain), D = num(a[7], &plain), R = num(a[8], &plain), style = name(g_rotations, a[9], &plain);
+    const int* positions = ptr(a[10], &plain);
+    const double* freq = ptr(a[11], &plain);
+    const float magnitude = real(a[12], &plain);
+    void* yq = ptr(a[13], &plain);
+    const long long ldyq = wide(a[14], &plain);
+    void* yk = ptr(a[15], &plain);
+    const long long ldyk = wide(a[16], &plain);
+    const int dtype = name(g_dtypes, a[17], &plain);
+    void* st = stream(a[18], &plain);
+    CALL((*fn)(q, ldq, k, ldk, T, Hq, Hk, D, R, style, positions, freq, magnitude, yq, ldyq, yk, ldyk, dtype, st));
+}
+static PyObject* rotate_forward(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    (void)self;
+    return rotate(a, n, &g_rotate_forward);
+}
+static PyObject* rotate_backward(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    (void)self;
+    return rotate(a, n, &g_rotate_backward);
+}
+static PyObject* page_plan(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    (void)self;
+    SERVING_ARGS(20)
+    const int *have = ptr(a[0], &plain), *fresh = ptr(a[1], &plain);
+    const int B = num(a[2], &plain), before = num(a[3], &plain);
+    const int* free_pages = ptr(a[4], &plain);
+    const int free_count = num(a[5], &plain);
+    const int* taken = ptr(a[6], &plain);
+    int *counts = ptr(a[7], &plain), *table = ptr(a[8], &plain);
+    const int max_pages = num(a[9], &plain), pages = num(a[10], &plain), page = num(a[11], &plain);
+    const long long T = wide(a[12], &plain);
+    int *rows = ptr(a[13], &plain), *lengths = ptr(a[14], &plain), *slots = ptr(a[15], &plain), *positions = ptr(a[16], &plain);
+    void* ws = ptr(a[17], &plain);
+    const size_t bytes = room(a[17], a[18], &plain);
+    void* st = stream(a[19], &plain);
+    CALL(g_page_plan(have, fresh, B, before, free_pages, free_count, taken, counts, table, max_pages, pages, page, T, rows, lengths, slots, positions, ws,
+                     bytes, st));
+}
+static PyObject* page_store(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    (void)self;
+    SERVING_ARGS(14)
+    const void* k = ptr(a[0], &plain);
+    const long long ldk = wide(a[1], &plain);
+    const void* v = ptr(a[2], &plain);
+    const long long ldv = wide(a[3], &plain), T = wide(a[4], &plain);
+    const int Hk = num(a[5], &plain), D = num(a[6], &plain);
+    const int* slots = ptr(a[7], &plain);
+    void *k_pages = ptr(a[8], &plain), *v_pages = ptr(a[9], &plain);
+    const int pages = num(a[10], &plain), page = num(a[11], &plain), dtype = name(g_dtypes, a[12], &plain);
+    void* st = stream(a[13], &plain);
+    CALL(g_page_store(k, ldk, v, ldv, T, Hk, D, slots, k_pages, v_pages, pages, page, dtype, st));
+}
+static PyObject* prefix_attention(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    (void)self;
+    SERVING_ARGS(25)
+    const void* q = ptr(a[0], &plain);
+    const long long ldq = wide(a[1], &plain), T = wide(a[2], &plain);
+    const int B = num(a[3], &plain);
+    const int *rows = ptr(a[4], &plain), *lengths = ptr(a[5], &plain);
+    const int Hq = num(a[6], &plain), Hk = num(a[7], &plain), D = num(a[8], &plain);
+    const float scale = real(a[9], &plain);
+    const void *k_pages = ptr(a[10], &plain), *v_pages = ptr(a[11], &plain);
+    const int pages = num(a[12], &plain), page = num(a[13], &plain);
+    const int* prefix_table = ptr(a[14], &plain);
+    const int prefix = num(a[15], &plain);
+    const int* table = ptr(a[16], &plain);
+    const int max_pages = num(a[17], &plain);
+    void* out = ptr(a[18], &plain);
+    const long long ldo = wide(a[19], &plain);
+    float* lse = ptr(a[20], &plain);
+    const int dtype = name(g_dtypes, a[21], &plain);
+    void* ws = ptr(a[22], &plain);
+    const size_t bytes = room(a[22], a[23], &plain);
+    void* st = stream(a[24], &plain);
+    CALL(g_prefix_attention(q, ldq, T, B, rows, lengths, Hq, Hk, D, scale, k_pages, v_pages, pages, page, prefix_table, prefix, table, max_pages, out, ldo,
+                            lse, dtype, ws, bytes, st));
+}
+
+/* bind_serving(addresses of the five functions), after bind_layers() */
+static PyObject* bind_serving(PyObject* self, PyObject* args)
+{
+    unsigned long long f[5];
+    (void)self;
+    if (!PyArg_ParseTuple(args, "(KKKKK)", &f[0], &f[1], &f[2], &f[3], &f[4])) return NULL;
+    g_rotate_forward = (rotate_fn)(uintptr_t)f[0];
+    g_rotate_backward = (rotate_fn)(uintptr_t)f[1];
+    g_page_plan = (page_plan_fn)(uintptr_t)f[2];
+    g_page_store = (page_store_fn)(uintptr_t)f[3];
+    g_prefix_attention = (prefix_attention_fn)(uintptr_t)f[4];
+    Py_RETURN_NONE;
+}
+
 /* bind_layers(addresses of the six functions of the layers, activations, rotations), after bind() */
 static PyObject* bind_layers(PyObject* self, PyObject* args)
 {
@@ -406,6 +527,12 @@ static PyMethodDef methods[] = {
     {"gated_backward", (PyCFunction)(void (*)(void))gated_backward, METH_FASTCALL, NULL},
     {"head_norm_forward", (PyCFunction)(void (*)(void))head_norm_forward, METH_FASTCALL, NULL},
     {"head_norm_backward", (PyCFunction)(void (*)(void))head_norm_backward, METH_FASTCALL, NULL},
+    {"bind_serving", bind_serving, METH_VARARGS, NULL},
+    {"rotate_forward", (PyCFunction)(void (*)(void))rotate_forward, METH_FASTCALL, NULL},
+    {"rotate_backward", (PyCFunction)(void (*)(void))rotate_backward, METH_FASTCALL, NULL},
+    {"page_plan", (PyCFunction)(void (*)(void))page_plan, METH_FASTCALL, NULL},
+    {"page_store", (PyCFunction)(void (*)(void))page_store, METH_FASTCALL, NULL},
+    {"prefix_attention", (PyCFunction)(void (*)(void))prefix_attention, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL},
 };
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_cgbn_call", NULL, -1, methods, NULL, NULL, NULL, NULL};

@@ -1,0 +1,290 @@
+// A cache in pages: the plan of a step from the requests' lengths, and the store of its keys and values.
+//
+// page_plan.  Two running sums over the requests: new tokens (cut at T, the rows there are), which give each request's rows, and the new pages that
+// its length then takes beyond those it holds, which give its place in the free list.  After that every row is on its own: its request by bisection
+// of the rows' starts, its key's page from the table or, if the request did not hold it before, from the free list; the row
+// whose key is a page's first writes the new entry (a page that is new has its first key in this step).  So nothing is read that another row writes.
+// Bound by latency: a launch and two dependent reads, 2 sums by one workgroup.  Few requests with few rows are done by that
+// workgroup alone, the others' rows by a second launch.
+//
+// page_store.  Bound by memory: one read and one write of the rows, 16 bytes a lane.  Pages hold a head's keys side by side ([page][head][key][D]), so
+// that attention, which reads one head at a time, finds whole pages of it in one run; a row is written in runs of D.
+#include "cgbn.h"
+#include "cgbn_grid.h"
+#include "cgbn_kernels.h"
+
+#include <cstring>
+
+namespace cgbn {
+namespace {
+
+struct PlanArgs {
+    const int *have, *fresh, *free_pages, *taken;
+    int *counts, *table, *rows, *lengths, *slots, *positions;
+    int* first;                    // [B]: place in the free list of a request's first new page
+    long long T;
+    int B, before, free_count, max_pages, pages, page_bits;
+};
+
+constexpr int kPlanThreads = 1024;
+constexpr int kMost = (1 << 30) - 1;          // sums stop here: more tokens or pages than there can be
+
+__device__ __forceinline__ int add_most(int a, int b, int most) { return min(a + b, most); }          // (both at most 2^30 - 1: no overflow)
+
+// Running sums over the workgroup, the own value left out, stopping at `most`; *total: of all
+__device__ __forceinline__ int scan_before(int v, int most, int* lds, int* total)
+{
+    const int lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
+    int sum = v;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+        const int o = __shfl_up(sum, d);
+        if (lane >= d) sum = add_most(sum, o, most);
+    }
+    __syncthreads();
+    if (lane == kWave - 1) lds[wave] = sum;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < kPlanThreads / kWave; ++w) {
+        if (w == wave) before = all;
+        all = add_most(all, lds[w], most);
+    }
+    *total = all;
+    const int own = __shfl_up(sum, 1);
+    return add_most(before, lane ? own : 0, most);
+}
+
+__device__ __forceinline__ int held_by(const PlanArgs& A, int b) { return min(max(A.have[b], 0), A.max_pages << A.page_bits); }
+__device__ __forceinline__ int pages_of(const PlanArgs& A, int keys) { return min((keys + (1 << A.page_bits) - 1) >> A.page_bits, A.max_pages); }
+
+// One row.  start: the request's first row; first: its place in the free list
+__device__ __forceinline__ void fill_row(const PlanArgs& A, int t, int b, int start, int first)
+{
+    const int have = held_by(A, b), key = have + (t - start), at = key >> A.page_bits, held = pages_of(A, have);
+    int id = -1;
+    if (at < A.max_pages) {
+        int* const entry = A.table + (long long)b * A.max_pages + at;
+        if (at < held) {
+            id = *entry;
+        } else {
+            const int from = first + (at - held);
+            if (from < A.free_count) id = A.free_pages[from];
+        }
+        if (id < 0 || id >= A.pages) id = -1;
+        if (at >= held && (key & ((1 << A.page_bits) - 1)) == 0) *entry = id;
+    }
+    A.slots[t] = id < 0 ? -1 : (id << A.page_bits) + (key & ((1 << A.page_bits) - 1));
+    A.positions[t] = A.before + key;
+}
+
+// The last request that starts at row t or before it: the one whose row it is, if it is any's
+__device__ __forceinline__ int request_of(const int* starts, int B, int t)
+{
+    int lo = 0, hi = B;            // starts[lo] <= t < starts[hi], if it has a request at all
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (starts[mid] <= t) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// The sums, and with ALL every row (B at most kPlanThreads)
+template <bool ALL> __global__ __launch_bounds__(kPlanThreads) void plan_sums(const PlanArgs A)
+{
+    __shared__ int lds[kPlanThreads / kWave], starts[ALL ? kPlanThreads + 1 : 1], firsts[ALL ? kPlanThreads : 1];
+    __shared__ long long left_out;
+    const int T = (int)A.T, each = (A.B + kPlanThreads - 1) / kPlanThreads;
+    const int b0 = min((int)threadIdx.x * each, A.B), b1 = min(b0 + each, A.B);
+    const int taken = min(max(A.taken[0], 0), A.free_count);
+    if (threadIdx.x == 0) left_out = 0;
+    int sum = 0, total;
+    for (int b = b0; b < b1; ++b) sum = add_most(sum, min(max(A.fresh[b], 0), kMost), kMost);
+    const int row0 = min(scan_before(sum, kMost, lds, &total), T);
+    int row = row0, wanted = 0;
+    for (int b = b0; b < b1; ++b) {
+        const int have = held_by(A, b), next = min(add_most(row, min(max(A.fresh[b], 0), kMost), kMost), T);
+        wanted = add_most(wanted, max(pages_of(A, have + (next - row)) - pages_of(A, have), 0), kMost);
+        row = next;
+    }
+    int first = add_most(taken, scan_before(wanted, kMost, lds, &total), kMost);
+    row = row0;
+    long long out = 0;
+    for (int b = b0; b < b1; ++b) {
+        const int have = held_by(A, b), fresh = max(A.fresh[b], 0), next = min(add_most(row, min(fresh, kMost), kMost), T);
+        const int length = have + (next - row), held = pages_of(A, have), want = max(pages_of(A, length) - held, 0);
+        const int given = min(want, max(A.free_count - first, 0));
+        out += fresh - max(min((held + given) << A.page_bits, length) - have, 0);
+        A.rows[b] = row;
+        A.lengths[b] = length;
+        if (ALL) {
+            starts[b] = row;
+            firsts[b] = first;
+        } else {
+            A.first[b] = first;
+        }
+        row = next;
+        first = add_most(first, want, kMost);
+    }
+    if (out) atomicAdd(reinterpret_cast<unsigned long long*>(&left_out), (unsigned long long)out);          // (whole numbers: in any order the same)
+    if (b1 == A.B && (b0 < b1 || (A.B == 0 && threadIdx.x == 0))) {
+        A.rows[A.B] = row;
+        if (ALL) starts[A.B] = row;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        A.counts[0] = min(add_most(taken, total, kMost), A.free_count);
+        A.counts[1] = (int)min(left_out, (long long)0x7fffffff);
+    }
+    if constexpr (ALL) {
+        const int end = starts[A.B];
+        for (int t = (int)threadIdx.x; t < T; t += kPlanThreads) {
+            if (t >= end) {
+                A.slots[t] = -1;
+                A.positions[t] = 0;
+                continue;
+            }
+            const int b = request_of(starts, A.B, t);
+            fill_row(A, t, b, starts[b], firsts[b]);
+        }
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void plan_rows(const PlanArgs A)
+{
+    const int t = (int)(blockIdx.x * kThreads + threadIdx.x);
+    if (t >= A.T) return;
+    if (t >= A.rows[A.B]) {
+        A.slots[t] = -1;
+        A.positions[t] = 0;
+        return;
+    }
+    const int b = request_of(A.rows, A.B, t);
+    fill_row(A, t, b, A.rows[b], A.first[b]);
+}
+
+struct StoreArgs {
+    const char* x[2];              // k, v
+    char* pool[2];
+    const int* slots;
+    long long ldx[2];              // bytes
+    long long T;
+    int heads, chunks;             // 16-byte chunks of a head's row
+    int places, page_bits, per;    // tokens of a workgroup
+};
+
+__global__ __launch_bounds__(kThreads) void page_store(const StoreArgs A)
+{
+    const int row = A.heads * A.chunks, all = A.per * 2 * row;
+    const long long t0 = workgroup() * A.per;
+    for (int i = (int)threadIdx.x; i < all; i += kThreads) {
+        const int local = (unsigned)i / (unsigned)(2 * row), j = i - local * 2 * row, which = j >= row, c = which ? j - row : j;
+        const long long t = t0 + local;
+        if (t >= A.T) return;
+        const int slot = A.slots[t];
+        if (slot < 0 || slot >= A.places) continue;
+        const int h = (unsigned)c / (unsigned)A.chunks, part = c - h * A.chunks;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(A.x[which] + t * A.ldx[which] + (long long)c * 16);
+        const long long at = (((((long long)(slot >> A.page_bits) * A.heads + h) << A.page_bits) + (slot & ((1 << A.page_bits) - 1))) * A.chunks + part) * 16;
+        *reinterpret_cast<u32x4*>(A.pool[which] + at) = v;
+    }
+}
+
+// ---- host ----
+
+cgbn_status launched() { return hipGetLastError() == hipSuccess ? CGBN_OK : CGBN_ERR_HIP; }
+
+constexpr int kMaxRequests = 1 << 20, kMaxPage = 1024, kMaxTable = 1 << 16, kMaxRows = 1 << 29;
+constexpr int kAlone = 4096;       // rows that the workgroup of the sums fills itself
+
+bool page_fits(int page, int pages) { return page >= 1 && page <= kMaxPage && (page & (page - 1)) == 0 && pages >= 0 && (long long)pages * page < (1ll << 31); }
+bool alone(int B, long long T) { return B <= kPlanThreads && T <= kAlone; }
+int bits_of(int page)
+{
+    int b = 0;
+    while ((1 << b) < page) ++b;
+    return b;
+}
+
+}  // namespace
+}  // namespace cgbn
+
+using namespace cgbn;
+
+extern "C" {
+
+size_t cgbn_page_plan_workspace_bytes(int B, long long T)
+{
+    if (B < 0 || B > kMaxRequests || T < 0 || T > kMaxRows) return 0;
+    if (alone(B, T)) return 256;
+    const size_t bytes = ((size_t)B * sizeof(int) + 255) / 256 * 256;
+    return bytes > 256 ? bytes : 512;          // (of 256 or less a program may pass none)
+}
+
+cgbn_status cgbn_page_plan(const int* have, const int* fresh, int B, int before, const int* free_pages, int free_count, const int* taken, int* counts,
+                           int* table, int max_pages, int pages, int page, long long T, int* rows, int* lengths, int* slots, int* positions,
+                           void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (B < 0 || B > kMaxRequests || T < 0 || T > kMaxRows || before < 0 || before > (1 << 30) || max_pages < 1 || max_pages > kMaxTable) return CGBN_ERR_SHAPE;
+    if (!page_fits(page, pages) || free_count < 0 || free_count > kMost) return CGBN_ERR_SHAPE;
+    if (!taken || !counts || !rows || (B && (!have || !fresh || !table || !lengths)) || (free_count && !free_pages) || (T && (!slots || !positions)))
+        return CGBN_ERR_NULL;
+    const void* const all[] = {have, fresh, free_pages, taken, counts, table, rows, lengths, slots, positions};
+    for (const void* p : all)
+        if (reinterpret_cast<uintptr_t>(p) % 4) return CGBN_ERR_ALIGN;
+    // results over each other or over what is still to be read (the pages taken may be counted in place)
+    const void* const out[] = {counts, B ? table : nullptr, rows, B ? lengths : nullptr, T ? slots : nullptr, T ? positions : nullptr};
+    const void* const in[] = {B ? have : nullptr, B ? fresh : nullptr, free_count ? free_pages : nullptr};
+    for (int i = 0; i < 6; ++i) {
+        if (!out[i]) continue;
+        for (int j = 0; j < i; ++j)
+            if (out[i] == out[j]) return CGBN_ERR_ALIAS;
+        for (const void* p : in)
+            if (out[i] == p) return CGBN_ERR_ALIAS;
+        if (i && out[i] == taken) return CGBN_ERR_ALIAS;
+    }
+    const bool one = alone(B, T);
+    if (!one && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < (size_t)B * sizeof(int))) return CGBN_ERR_WORKSPACE;
+    PlanArgs A;
+    std::memset(&A, 0, sizeof(A));
+    A.have = have; A.fresh = fresh; A.free_pages = free_pages; A.taken = taken; A.counts = counts; A.table = table; A.rows = rows; A.lengths = lengths;
+    A.slots = slots; A.positions = positions; A.first = static_cast<int*>(workspace); A.T = T; A.B = B; A.before = before; A.free_count = free_count;
+    A.max_pages = max_pages; A.pages = pages; A.page_bits = bits_of(page);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (one) {
+        hipLaunchKernelGGL(plan_sums<true>, dim3(1), dim3(kPlanThreads), 0, st, A);
+        return launched();
+    }
+    hipLaunchKernelGGL(plan_sums<false>, dim3(1), dim3(kPlanThreads), 0, st, A);
+    if (launched() != CGBN_OK) return CGBN_ERR_HIP;
+    if (T) hipLaunchKernelGGL(plan_rows, dim3((unsigned)((T + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, A);
+    return launched();
+}
+
+cgbn_status cgbn_page_store(const void* k, long long ldk, const void* v, long long ldv, long long T, int Hk, int D, const int* slots, void* k_pages,
+                            void* v_pages, int pages, int page, cgbn_dtype dtype, void* stream)
+{
+    if (dtype != CGBN_F32 && dtype != CGBN_BF16) return CGBN_ERR_ENUM;
+    if (T < 0 || T > (1 << 30) || Hk < 1 || Hk > (1 << 10) || D < 8 || D > 256 || D % 8 != 0 || !page_fits(page, pages)) return CGBN_ERR_SHAPE;
+    if (T == 0) return CGBN_OK;
+    if (!k || !v || !slots || (pages && (!k_pages || !v_pages))) return CGBN_ERR_NULL;
+    const long long elem = dtype == CGBN_F32 ? 4 : 2, width = (long long)Hk * D;
+    if (ldk > (1ll << 32) || ldv > (1ll << 32)) return CGBN_ERR_SHAPE;
+    if (T > 1 && (ldk < width || ldv < width)) return CGBN_ERR_STRIDE;
+    const uintptr_t sixteen = reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(k_pages) | reinterpret_cast<uintptr_t>(v_pages);
+    if (sixteen % 16 || (T > 1 && (ldk * elem % 16 || ldv * elem % 16)) || reinterpret_cast<uintptr_t>(slots) % 4) return CGBN_ERR_ALIGN;
+    if (pages && (k_pages == v_pages || k_pages == k || k_pages == v || v_pages == k || v_pages == v || k_pages == slots || v_pages == slots)) return CGBN_ERR_ALIAS;
+    StoreArgs A;
+    std::memset(&A, 0, sizeof(A));
+    A.x[0] = static_cast<const char*>(k); A.x[1] = static_cast<const char*>(v);
+    A.pool[0] = static_cast<char*>(k_pages); A.pool[1] = static_cast<char*>(v_pages);
+    A.slots = slots; A.ldx[0] = ldk * elem; A.ldx[1] = ldv * elem; A.T = T; A.heads = Hk; A.chunks = (int)(D * elem / 16);
+    A.places = pages * page; A.page_bits = bits_of(page);
+    const int row = Hk * A.chunks;
+    A.per = 4 * kThreads / (2 * row);
+    if (A.per < 1) A.per = 1;
+    hipLaunchKernelGGL(page_store, grid_of((T + A.per - 1) / A.per), dim3(kThreads), 0, static_cast<hipStream_t>(stream), A);
+    return launched();
+}
+
+}  // extern "C"
