@@ -35,16 +35,50 @@ struct AttendArgs {
     float scale;                       // times log2(e)
 };
 
-// T: element type; DP: D up to the next tile width; WR: wavefronts side by side in rows (the others side by side in keys); QT: 16-row tiles of a wavefront
-template <typename T, int DP, int WR, int QT> struct Attend {
-    static constexpr int EB = (int)sizeof(T), WK = 4 / WR, ROWS = WR * QT * 16;
-    static constexpr int KW = (WK == 1 ? 128 : 64) / EB, KT = KW * WK;          // keys of a wavefront, of a tile
-    static constexpr int KROW = DP * EB + 16, VROW = DP * EB + (EB == 2 ? 32 : 16);        // rows apart in banks, see the reads
-    static constexpr int CH = DP * EB / 16, KS = DP * EB / 64, NT = KW / 16, ND = DP / 16;
-    static constexpr int V0 = KT * KROW, FLAGS = V0 + KT * VROW, KEYS = FLAGS + KT * 4;
+// How many rows a tile has, and how it is dealt to the four wavefronts: FEW (one row's worth: a request's heads), SOME, MANY.  `line`: bytes from key to key
+// in LDS.  Wavefronts side by side in keys (wk of them) read each key once from LDS, and have sums to join at the end; side by side in rows (wr) they
+// read the same keys.  A tile's keys and values are 32 KiB, two of them in LDS, so that two workgroups share a compute unit.
+enum { FEW = 0, SOME = 1, MANY = 2 };
+constexpr int width_of(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : D <= 192 ? 192 : 256; }
+constexpr int line_of(int D, int elem) { return D * elem <= 64 ? 64 : D * elem <= 128 ? 128 : D * elem <= 256 ? 256 : D * elem <= 512 ? 512 : 1024; }
+constexpr int keys_of(int kind, int line) { return line >= 256 ? 16384 / line : kind == MANY ? 64 : 128; }
+constexpr int wk_of(int kind, int line) { return kind == MANY || line == 1024 ? 1 : line == 512 ? 2 : 4; }
+// 16-row tiles of a wavefront: what is left of its registers decides where rows are long
+constexpr int qt_of(int kind, int line, int elem) { return kind == FEW ? 1 : line <= 256 ? 2 : kind == MANY && line == 512 && elem == 4 ? 2 : 1; }
+constexpr int rows_of(int kind, int line, int elem) { return 4 / wk_of(kind, line) * qt_of(kind, line, elem) * 16; }
+
+constexpr int kPlaces = 1024;          // pages whose addresses a workgroup has at hand
+
+// T: element type; DP: D up to the next tile width
+template <typename T, int DP, int KIND> struct Attend {
+    static constexpr int EB = (int)sizeof(T), LINE = line_of(DP, EB), WK = wk_of(KIND, LINE), WR = 4 / WK, QT = qt_of(KIND, LINE, EB), ROWS = rows_of(KIND, LINE, EB);
+    static constexpr int KT = keys_of(KIND, LINE), KW = KT / WK;                 // keys of a tile, of a wavefront
+    static constexpr int CH = LINE / 16, PASS = kThreads / CH, PASSES = KT / PASS;         // chunks of a line; keys of a pass of the workgroup's loads
+    static constexpr int KS = DP * EB / 64, NT = KW / 16, ND = DP / 16, NP = EB == 2 && NT > 1 ? NT / 2 : NT;
+    static constexpr int HALF = KT * LINE, STAGE = 2 * HALF, PLACES = 2 * STAGE;
     static constexpr int MERGE = WK == 1 ? 0 : 4 * QT * 16 * (DP + 2) * 4;
-    static constexpr int LDS = KEYS > MERGE ? KEYS : MERGE;
+    static constexpr int LDS = PLACES + kPlaces * 8 > MERGE ? PLACES + kPlaces * 8 : MERGE;
+    static_assert(ROWS == WR * QT * 16 && KT % PASS == 0 && KW % 16 == 0 && KT <= 128, "");
 };
+
+// 16 bytes a lane to LDS at `lds` + 16 * lane, from an address of the lane's own; see dma16
+__device__ __forceinline__ void dma16_from(uint32_t lds, const char* from)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+}
+
+// The larger of the four lanes that hold a row: lanes 16 and 32 apart, by the instructions that swap rows of 16 lanes and halves
+__device__ __forceinline__ float row_max(float v)
+{
+    typedef unsigned u32x2_hw __attribute__((ext_vector_type(2)));
+    const u32x2_hw a = __builtin_bit_cast(u32x2_hw, __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+    v = fmaxf(__uint_as_float(a.x), __uint_as_float(a.y));
+    const u32x2_hw b = __builtin_bit_cast(u32x2_hw, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+    return fmaxf(__uint_as_float(b.x), __uint_as_float(b.y));
+}
+
+// xor number of a key's line of 64 ... 1024 bytes: the 16 keys that a read of a fragment touches at once spread over all banks
+template <int LINE> __device__ __forceinline__ int line_key(int key) { return LINE >= 256 ? key & 15 : LINE == 128 ? (key >> 1) & 7 : (key >> 2) & 3; }
 
 __device__ __forceinline__ bool finite16(uint32_t pair, int hi) { return ((pair >> (hi ? 16 : 0)) & 0x7f80u) != 0x7f80u; }
 template <typename T> __device__ __forceinline__ bool all_finite(const u32x4& v)
@@ -96,11 +130,13 @@ __device__ __forceinline__ int request_of_tile(const AttendArgs& A, int i, int r
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
-template <typename T, int DP, int WR, int QT> __device__ void attend(const AttendArgs& A, char* lds, int id, bool prefix_job)
+template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(const AttendArgs& A, char* lds, int id, bool prefix_job)
 {
-    typedef Attend<T, DP, WR, QT> C;
+    typedef Attend<T, DP, KIND> C;
+    constexpr int QT = C::QT, WR = C::WR;
     const int tid = (int)threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave), wr = w % WR, wk = w / WR, col = lane & 15, grp = lane >> 4;
-    lds_char* const tile = (lds_char*)lds;
+    lds_char* const base = (lds_char*)lds;
+    const char** const places = reinterpret_cast<const char**>(lds + C::PLACES);
     const int head = id % A.Hk;
     id /= A.Hk;
 
@@ -147,7 +183,8 @@ template <typename T, int DP, int WR, int QT> __device__ void attend(const Atten
         for (int s = 0; s < C::KS; ++s) {
             const int c = s * 64 + grp * 16;
             Q[t][s] = u32x4{0, 0, 0, 0};
-            if (in && c < A.D * C::EB) Q[t][s] = *reinterpret_cast<const u32x4*>(at + c);
+            if (in && c < A.D * C::EB && A.scale != 0.f) Q[t][s] = *reinterpret_cast<const u32x4*>(at + c);
+            if (A.scale < 0.f) Q[t][s] ^= C::EB == 2 ? 0x80008000u : 0x80000000u;          // the scale's sign goes with the queries, and so does a scale of zero
         }
     }
 
@@ -160,6 +197,17 @@ template <typename T, int DP, int WR, int QT> __device__ void attend(const Atten
 #pragma unroll
         for (int d = 0; d < C::ND; ++d) O[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+
+    const float scale = A.scale == 0.f ? 1.f : fabsf(A.scale);
+
+    // this thread's part of a tile's loads: key r0 + pass * PASS, chunk `chunk` of its line, which goes to place tid of the pass.  A load writes its
+    // wavefront's lanes side by side, so the chunks of a line change places (xor a number of the key) instead of leaving gaps, for the reads below.
+    const int load_row = tid / C::CH, line = A.D * C::EB;
+    auto chunk = [&](int pass) { return ((tid % C::CH) ^ line_key<C::LINE>(pass * C::PASS + load_row)) * 16; };
+    if (A.D < DP || DP * C::EB < C::LINE) {                       // places that no load reaches
+        for (int i = tid; i < 2 * C::STAGE / 16; i += kThreads) *reinterpret_cast<u32x4*>(lds + i * 16) = u32x4{0, 0, 0, 0};
+    }
+    const long long values = A.v_pages - A.k_pages;
 
     int dirty_from = 0, dirty_to = 0;     // own keys whose infinities and NaN stay out of the products, see below
     for (int own = prefix_job || A.whole ? 0 : 1; own < (prefix_job ? 1 : 2); ++own) {
@@ -183,29 +231,83 @@ template <typename T, int DP, int WR, int QT> __device__ void attend(const Atten
                 end = min(begin + per, end);
             }
         }
-        for (int key0 = begin; key0 < end; key0 += C::KT) {
-            __syncthreads();
-            const bool edge = own && least < end && key0 + C::KT > least;
-            int bad = 0;
-            for (int i = tid; i < C::KT * C::CH; i += kThreads) {
-                const int r = i / C::CH, c = i % C::CH, key = key0 + r;
-                const long long at = key < end ? key_at<T>(A, table, head, key) : -1;
-                u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
-                if (at >= 0 && c * 16 < A.D * C::EB) {
-                    k = *reinterpret_cast<const u32x4*>(A.k_pages + at + c * 16);
-                    v = *reinterpret_cast<const u32x4*>(A.v_pages + at + c * 16);
+        if (begin >= end) continue;
+
+        int first = 0, stop = begin;      // keys whose pages' addresses are at hand
+        unsigned long long there[2], next[2];          // keys of the tile that is there, and of the next, that exist
+        // Starts the loads of the tile at `key0`
+        auto issue = [&](int key0, int stage) {
+            if (key0 + C::KT > stop && stop < end) {
+                first = key0 >> A.page_bits;
+                const int n = min(kPlaces, ((end - 1) >> A.page_bits) - first + 1);
+                stop = (first + kPlaces) << A.page_bits;
+                if (stop < 0 || stop > end) stop = end;
+                __syncthreads();
+                for (int i = tid; i < n; i += kThreads) {
+                    const int page = table[first + i];
+                    places[i] = page < 0 || page >= A.pages ? nullptr : A.k_pages + ((((long long)page * A.Hk + head) << A.page_bits) * line);
                 }
-                *reinterpret_cast<u32x4*>(lds + r * C::KROW + c * 16) = k;
-                *reinterpret_cast<u32x4*>(lds + C::V0 + r * C::VROW + c * 16) = v;
-                if (c == 0) *reinterpret_cast<int*>(lds + C::FLAGS + r * 4) = at < 0;
-                if (edge) bad |= !all_finite<T>(v);
+                __syncthreads();
             }
-            // A product with a score of zero would carry an infinity or a NaN of v to rows that do not see its key.  Where rows of the tile see
+#pragma unroll
+            for (int h = 0; h < (C::KT + 63) / 64; ++h) {
+                const int key = key0 + h * 64 + lane;
+                next[h] = __ballot(h * 64 + lane < C::KT && key < end && places[(key >> A.page_bits) - first] != nullptr);
+            }
+            const bool full = next[0] == (C::KT >= 64 ? ~0ull : (1ull << (C::KT % 64)) - 1) && (C::KT <= 64 || next[1] == ~0ull);
+            const uint32_t to = (uint32_t)(uintptr_t)(base + stage * C::STAGE) + w * 1024;
+            const int mask = (1 << A.page_bits) - 1;
+            if (full) {
+                const char* at[C::PASSES];
+#pragma unroll
+                for (int i = 0; i < C::PASSES; ++i) {
+                    const int key = key0 + i * C::PASS + load_row;
+                    at[i] = places[(key >> A.page_bits) - first] + ((key & mask) * line + chunk(i));
+                }
+#pragma unroll
+                for (int i = 0; i < C::PASSES; ++i)
+                    if (chunk(i) < line) dma16_from(to + i * 4096, at[i]);
+#pragma unroll
+                for (int i = 0; i < C::PASSES; ++i)
+                    if (chunk(i) < line) dma16_from(to + C::HALF + i * 4096, at[i] + values);
+            } else {
+#pragma unroll
+                for (int i = 0; i < C::PASSES; ++i) {
+                    const int key = key0 + i * C::PASS + load_row;
+                    const char* const at = key < end ? places[(key >> A.page_bits) - first] : nullptr;
+                    if (at && chunk(i) < line) {
+                        dma16_from(to + i * 4096, at + ((key & mask) * line + chunk(i)));
+                        dma16_from(to + C::HALF + i * 4096, at + values + ((key & mask) * line + chunk(i)));
+                    } else {
+                        *reinterpret_cast<u32x4*>(lds + stage * C::STAGE + i * 4096 + tid * 16) = u32x4{0, 0, 0, 0};
+                        *reinterpret_cast<u32x4*>(lds + stage * C::STAGE + C::HALF + i * 4096 + tid * 16) = u32x4{0, 0, 0, 0};
+                    }
+                }
+            }
+        };
+
+        __syncthreads();                  // (LDS is read no more)
+        issue(begin, 0);
+        int stage = 0;
+        for (int key0 = begin; key0 < end; key0 += C::KT, stage ^= 1) {
+            there[0] = next[0];
+            there[1] = next[1];
+            dma_wait_and_meet();
+            if (key0 + C::KT < end) issue(key0 + C::KT, stage ^ 1);
+            const lds_char* const tile = base + stage * C::STAGE;
+            // A product with a weight of zero would carry an infinity or a NaN of v to rows that do not see its key.  Where rows of the tile see
             // different keys such values are left out of the products and added to the rows that do at the end.
-            const bool dirty = edge ? __syncthreads_or(bad) : (__syncthreads(), false);
-            if (dirty) {
-                if (dirty_to == 0) dirty_from = key0;
-                dirty_to = end;
+            const bool edge = own && least < end && key0 + C::KT > least;
+            bool dirty = false;
+            if (edge) {
+                int bad = 0;
+#pragma unroll
+                for (int i = 0; i < C::PASSES; ++i) bad |= !all_finite<T>(*reinterpret_cast<const u32x4*>(lds + stage * C::STAGE + C::HALF + i * 4096 + tid * 16));
+                dirty = __syncthreads_or(bad);
+                if (dirty) {
+                    if (dirty_to == 0) dirty_from = key0;
+                    dirty_to = end;
+                }
             }
 
             const int k0 = wk * C::KW;
@@ -218,72 +320,104 @@ template <typename T, int DP, int WR, int QT> __device__ void attend(const Atten
             for (int s = 0; s < C::KS; ++s)
 #pragma unroll
                 for (int n = 0; n < C::NT; ++n) {
-                    const u32x4 k = *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(tile + (k0 + n * 16 + col) * C::KROW + s * 64 + grp * 16);
+                    const u32x4 k = *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(
+                        tile + (k0 + n * 16 + col) * C::LINE + (((s * 4 + grp) ^ line_key<C::LINE>(col)) << 4));
 #pragma unroll
                     for (int t = 0; t < QT; ++t) S[t][n] = multiply<T>(k, Q[t][s], S[t][n]);
                 }
 
-            u32x4 P[QT][C::EB == 2 ? C::NT / 2 : C::NT];
+            const bool whole = there[0] == (C::KT >= 64 ? ~0ull : (1ull << (C::KT % 64)) - 1) && (C::KT <= 64 || there[1] == ~0ull) && !edge;
+            if (!whole) {
+                const unsigned seen = (unsigned)((C::KT > 64 && k0 >= 64 ? there[1] : there[0]) >> (k0 & 63) >> (grp * 4));
+                const unsigned seen2 = (unsigned)((C::KT > 64 && k0 >= 64 ? there[1] : there[0]) >> (k0 & 63) >> (grp * 4) >> 32);
+#pragma unroll
+                for (int t = 0; t < QT; ++t)
+#pragma unroll
+                    for (int n = 0; n < C::NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int key = key0 + k0 + n * 16 + grp * 4 + e;
+                            const bool hidden = !(((n < 2 ? seen : seen2) >> (n % 2 * 16 + e)) & 1) || (own && key >= sees[t]);
+                            if (hidden) S[t][n][e] = -INFINITY;
+                        }
+            }
+
+            // The weights, 2^(scale s - m).  m follows the largest score only where that is more than 2^8 times what m stands for: sums hold that and
+            // much more in 32 bits, and what is there already is seldom scaled.
+            u32x4 P[QT][C::NP];
 #pragma unroll
             for (int t = 0; t < QT; ++t) {
-                float top = -INFINITY;
+                float top = S[t][0][0];
 #pragma unroll
-                for (int n = 0; n < C::NT; ++n) {
-                    const u32x4 none = *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(tile + C::FLAGS + (k0 + n * 16 + grp * 4) * 4);
+                for (int n = 0; n < C::NT; ++n)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int key = key0 + k0 + n * 16 + grp * 4 + e;
-                        const bool hidden = none[e] || (own && key >= sees[t]);
-                        S[t][n][e] = hidden ? -INFINITY : S[t][n][e] * A.scale;
-                        top = fmaxf(top, S[t][n][e]);
-                    }
+                    for (int e = 0; e < 4; ++e) top = fmaxf(top, S[t][n][e]);
+                if (__any(top * scale > m[t] + 8.f)) {
+                    const float most = fmaxf(m[t], row_max(top * scale)), down = __builtin_amdgcn_exp2f(m[t] - (most == -INFINITY ? 0.f : most));
+                    m[t] = most;
+                    l[t] *= down;
+#pragma unroll
+                    for (int d = 0; d < C::ND; ++d) O[t][d] *= down;
                 }
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float most = fmaxf(m[t], top), from = most == -INFINITY ? 0.f : most, down = __builtin_amdgcn_exp2f(m[t] - from);
-                m[t] = most;
+                const float from = m[t] == -INFINITY ? 0.f : m[t];
                 float sum = 0.f;
 #pragma unroll
                 for (int n = 0; n < C::NT; ++n)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        S[t][n][e] = __builtin_amdgcn_exp2f(S[t][n][e] - from);
+                        S[t][n][e] = __builtin_amdgcn_exp2f(fmaf(S[t][n][e], scale, -from));
                         sum += S[t][n][e];
                     }
-                l[t] = l[t] * down + sum;
-#pragma unroll
-                for (int d = 0; d < C::ND; ++d) O[t][d] *= down;
+                l[t] += sum;
                 // bfloat16: the weights are rounded to 8 bits for the products (off by at most 2^-8 of themselves, with no preferred sign); their sum is not
-                if constexpr (C::EB == 2) {
 #pragma unroll
-                    for (int n = 0; n < C::NT / 2; ++n)
-                        P[t][n] = u32x4{f32x2_to_bf16x2(S[t][2 * n][0], S[t][2 * n][1]), f32x2_to_bf16x2(S[t][2 * n][2], S[t][2 * n][3]),
-                                        f32x2_to_bf16x2(S[t][2 * n + 1][0], S[t][2 * n + 1][1]), f32x2_to_bf16x2(S[t][2 * n + 1][2], S[t][2 * n + 1][3])};
-                } else {
-#pragma unroll
-                    for (int n = 0; n < C::NT; ++n)
+                for (int n = 0; n < C::NP; ++n) {
+                    if constexpr (C::EB == 2) {
+                        P[t][n].x = f32x2_to_bf16x2(S[t][2 * n][0], S[t][2 * n][1]);
+                        P[t][n].y = f32x2_to_bf16x2(S[t][2 * n][2], S[t][2 * n][3]);
+                        if constexpr (C::NT > 1) {
+                            P[t][n].z = f32x2_to_bf16x2(S[t][2 * n + 1][0], S[t][2 * n + 1][1]);
+                            P[t][n].w = f32x2_to_bf16x2(S[t][2 * n + 1][2], S[t][2 * n + 1][3]);
+                        }
+                    } else {
                         P[t][n] = u32x4{__float_as_uint(S[t][n][0]), __float_as_uint(S[t][n][1]), __float_as_uint(S[t][n][2]), __float_as_uint(S[t][n][3])};
+                    }
                 }
             }
+            const lds_char* const v_tile = tile + C::HALF;
 #pragma unroll
-            for (int n = 0; n < (C::EB == 2 ? C::NT / 2 : C::NT); ++n)
+            for (int n = 0; n < C::NP; ++n)
 #pragma unroll
                 for (int d = 0; d < C::ND; ++d) {
-                    u32x4 v;
+                    u32x4 v = {0, 0, 0, 0};
                     if constexpr (C::EB == 2) {
                         typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-                        const lds_char* const p = tile + C::V0 + (k0 + n * 32 + grp * 4 + (col >> 2)) * C::VROW + d * 32 + (col & 3) * 8;
+                        const int in = grp * 4 + (col >> 2);
+                        const lds_char* const p = v_tile + (k0 + n * 32 + in) * C::LINE + (((d * 2 + ((col >> 1) & 1)) ^ line_key<C::LINE>(in)) << 4) + (col & 1) * 8;
                         const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
-                        const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * C::VROW)));
-                        v = u32x4{lo.x, lo.y, hi.x, hi.y};
+                        v.x = lo.x;
+                        v.y = lo.y;
+                        if constexpr (C::NT > 1) {
+                            const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * C::LINE)));
+                            v.z = hi.x;
+                            v.w = hi.y;
+                        }
                     } else {
                         typedef const __attribute__((address_space(3))) uint32_t lds_u32;
-                        const lds_char* const p = tile + C::V0 + (k0 + n * 16 + grp * 4) * C::VROW + (d * 16 + col) * 4;
-                        v = u32x4{*(lds_u32*)p, *(lds_u32*)(p + C::VROW), *(lds_u32*)(p + 2 * C::VROW), *(lds_u32*)(p + 3 * C::VROW)};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int in = grp * 4 + e;
+                            v[e] = *(lds_u32*)(v_tile + (k0 + n * 16 + in) * C::LINE + (((d * 4 + (col >> 2)) ^ line_key<C::LINE>(in)) << 4) + (col & 3) * 4);
+                        }
                     }
                     if (dirty) v = only_finite<T>(v);
 #pragma unroll
-                    for (int t = 0; t < QT; ++t) O[t][d] = multiply<T>(v, P[t][n], O[t][d]);
+                    for (int t = 0; t < QT; ++t) {
+                        if constexpr (C::EB == 2 && C::NT == 1)
+                            O[t][d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, make_uint2(v.x, v.y)),
+                                                                                __builtin_bit_cast(s16x4, make_uint2(P[t][n].x, P[t][n].y)), O[t][d], 0, 0, 0);
+                        else O[t][d] = multiply<T>(v, P[t][n], O[t][d]);
+                    }
                 }
         }
     }
@@ -306,27 +440,29 @@ template <typename T, int DP, int WR, int QT> __device__ void attend(const Atten
         }
         return v;
     };
-    // one row's four values from d on: to the result or to this part's place
+    // where a row's results go, to the result or to this part's place, and its sums
     const long long part = prefix_job ? split : A.prefix_splits + split;
-    auto store = [&](long long r, int d, f32x4 o, float mm, float ll) {
-        if (r < 0) return;
-        if (d < A.D) {
-            if (A.direct) {
-                const float by = ll == 0.f ? 0.f : 1.f / ll;
+    auto place = [&](long long r) {
+        const int token = (int)((unsigned)r / (unsigned)A.Hq), h = (int)r - token * A.Hq;
+        return A.direct ? A.out + (token * A.ldo + h * A.D) * C::EB : reinterpret_cast<char*>(A.part_o + (part * A.T * A.Hq + r) * A.D);
+    };
+    auto store_sums = [&](long long r, float mm, float ll) {
+        if (!A.direct) A.part_ml[part * A.T * A.Hq + r] = make_float2(mm, ll);
+        else if (A.lse) A.lse[r] = ll == 0.f ? -INFINITY : 0.6931471805599453f * (mm + __builtin_amdgcn_logf(ll));
+    };
+    // four values from d on
+    auto store = [&](char* to, int d, f32x4 o, float ll) {
+        if (d >= A.D) return;
+        if (A.direct) {
+            const float by = 1.f / ll;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = ll == 0.f ? 0.f : o[e] * by;
-                const long long token = r / A.Hq;
-                T* const to = reinterpret_cast<T*>(A.out) + token * A.ldo + (r - token * A.Hq) * A.D + d;
-                if constexpr (C::EB == 2) *reinterpret_cast<uint2*>(to) = make_uint2(f32x2_to_bf16x2(o[0], o[1]), f32x2_to_bf16x2(o[2], o[3]));
-                else *reinterpret_cast<f32x4*>(to) = o;
-            } else {
-                *reinterpret_cast<f32x4*>(A.part_o + (part * A.T * A.Hq + r) * A.D + d) = o;
+            for (int e = 0; e < 4; ++e) o[e] = ll == 0.f ? 0.f : o[e] * by;
+            if constexpr (C::EB == 2) {
+                *reinterpret_cast<uint2*>(to + d * 2) = make_uint2(f32x2_to_bf16x2(o[0], o[1]), f32x2_to_bf16x2(o[2], o[3]));
+                return;
             }
         }
-        if (d == 0) {
-            if (!A.direct) A.part_ml[part * A.T * A.Hq + r] = make_float2(mm, ll);
-            else if (A.lse) A.lse[r] = ll == 0.f ? -INFINITY : 0.6931471805599453f * (mm + __builtin_amdgcn_logf(ll));
-        }
+        *reinterpret_cast<f32x4*>(to + d * 4) = o;
     };
     if constexpr (C::WK == 1) {
         for (int key = dirty_from; key < dirty_to; ++key)
@@ -338,9 +474,13 @@ template <typename T, int DP, int WR, int QT> __device__ void attend(const Atten
                     if (key < sees[t]) O[t][d] += v;
             }
 #pragma unroll
-        for (int t = 0; t < QT; ++t)
+        for (int t = 0; t < QT; ++t) {
+            if (row[t] < 0) continue;
+            char* const to = place(row[t]);
 #pragma unroll
-            for (int d = 0; d < C::ND; ++d) store(row[t], d * 16 + grp * 4, O[t][d], m[t], l[t]);
+            for (int d = 0; d < C::ND; ++d) store(to, d * 16 + grp * 4, O[t][d], l[t]);
+            if (grp == 0) store_sums(row[t], m[t], l[t]);
+        }
     } else {
         // the wavefronts' parts, in order
         constexpr int RW = QT * 16;
@@ -350,46 +490,48 @@ template <typename T, int DP, int WR, int QT> __device__ void attend(const Atten
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
 #pragma unroll
-            for (int d = 0; d < C::ND; ++d) *reinterpret_cast<f32x4*>(o + ((wk * RW + t * 16 + col) * DP + d * 16 + grp * 4)) = O[t][d];
+            for (int d = 0; d < C::ND; ++d) *reinterpret_cast<f32x4*>(o + ((w * RW + t * 16 + col) * DP + d * 16 + grp * 4)) = O[t][d];
             if (grp == 0) {
-                ml[(wk * RW + t * 16 + col) * 2] = m[t];
-                ml[(wk * RW + t * 16 + col) * 2 + 1] = l[t];
+                ml[(w * RW + t * 16 + col) * 2] = m[t];
+                ml[(w * RW + t * 16 + col) * 2 + 1] = l[t];
             }
         }
         __syncthreads();
-        for (int i = tid; i < RW * (DP / 4); i += kThreads) {
-            const int r = i / (DP / 4), d = i % (DP / 4) * 4;
+        for (int i = tid; i < C::ROWS * (DP / 4); i += kThreads) {
+            const int r = i / (DP / 4), d = i % (DP / 4) * 4, from = r / RW * RW + r % RW;          // (wavefront k * WR + r / RW has row r for its keys)
             float top = -INFINITY, ll = 0.f;
 #pragma unroll
-            for (int k = 0; k < C::WK; ++k) top = fmaxf(top, ml[(k * RW + r) * 2]);
+            for (int k = 0; k < C::WK; ++k) top = fmaxf(top, ml[(k * WR * RW + from) * 2]);
             f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < C::WK; ++k) {
-                if (ml[(k * RW + r) * 2 + 1] == 0.f) continue;          // (no key: what o holds is no sum)
-                const float f = __builtin_amdgcn_exp2f(ml[(k * RW + r) * 2] - top);
-                ll += f * ml[(k * RW + r) * 2 + 1];
-                sum += f * *reinterpret_cast<const f32x4*>(o + (k * RW + r) * DP + d);
+                const int at = k * WR * RW + from;
+                if (ml[at * 2 + 1] == 0.f) continue;          // (no key: what o holds is no sum)
+                const float f = __builtin_amdgcn_exp2f(ml[at * 2] - top);
+                ll += f * ml[at * 2 + 1];
+                sum += f * *reinterpret_cast<const f32x4*>(o + at * DP + d);
             }
-            const int at = r0 + r;
-            const int token = at / A.g;
-            const long long to = at < count ? (long long)(token0 + token) * A.Hq + head * A.g + (at - token * A.g) : -1;
+            const int at = r0 + r, token = at / A.g;
+            if (at >= count) continue;
             for (int key = dirty_from; key < min(dirty_to, length - fresh + token + 1); ++key) sum += left_out(key, d);
-            store(to, d, sum, top, ll);
+            const long long to = (long long)(token0 + token) * A.Hq + head * A.g + (at - token * A.g);
+            store(place(to), d, sum, ll);
+            if (d == 0) store_sums(to, top, ll);
         }
     }
 }
 
-// WP: the row wavefronts of a prefix tile; WO: of a tile of one request's rows.  One launch for both.
-template <typename T, int DP, int WP, int QP, int WO, int QO> __global__ __launch_bounds__(kThreads) void attend_keys(const AttendArgs A)
+// PREFIX: the kind of a tile of the prefix's rows; OWN: of a tile of one request's.  One launch for both.
+template <typename T, int DP, int PREFIX, int OWN> __global__ __launch_bounds__(kThreads, 2) void attend_keys(const AttendArgs A)
 {
-    constexpr int P = Attend<T, DP, WP, QP>::LDS, O = Attend<T, DP, WO, QO>::LDS;
+    constexpr int P = Attend<T, DP, PREFIX>::LDS, O = Attend<T, DP, OWN>::LDS;
     __shared__ __attribute__((aligned(1024))) char lds[P > O ? P : O];
     const int id = (int)blockIdx.x;
-    if constexpr (WP == WO && QP == QO) {
-        attend<T, DP, WP, QP>(A, lds, id < A.prefix_jobs ? id : id - A.prefix_jobs, id < A.prefix_jobs);
+    if constexpr (PREFIX == OWN) {
+        attend<T, DP, PREFIX>(A, lds, id < A.prefix_jobs ? id : id - A.prefix_jobs, id < A.prefix_jobs);
     } else {
-        if (id < A.prefix_jobs) attend<T, DP, WP, QP>(A, lds, id, true);
-        else attend<T, DP, WO, QO>(A, lds, id - A.prefix_jobs, false);
+        if (id < A.prefix_jobs) attend<T, DP, PREFIX>(A, lds, id, true);
+        else attend<T, DP, OWN>(A, lds, id - A.prefix_jobs, false);
     }
 }
 
@@ -424,10 +566,6 @@ template <typename T> __global__ __launch_bounds__(kThreads) void attend_join(co
     if (lane == 0 && A.lse) A.lse[r] = sum == 0.f ? -INFINITY : 0.6931471805599453f * (top + __builtin_amdgcn_logf(sum));
 }
 
-// ways: which tiles the rows go in, see plan()
-enum { WAY_16_16 = 0, WAY_32_16 = 1, WAY_128_16 = 2, WAY_32_32 = 3, WAY_128_32 = 4, WAY_128_128 = 5, WAYS = 6 };
-constexpr int kPrefixRows[WAYS] = {16, 32, 128, 32, 128, 128}, kOwnRows[WAYS] = {16, 16, 16, 32, 32, 128};
-
-template <typename T> cgbn_status launch_attend(const AttendArgs& A, int way, hipStream_t st);
+template <typename T> cgbn_status launch_attend(const AttendArgs& A, int prefix_kind, int own_kind, hipStream_t st);
 
 }  // namespace cgbn

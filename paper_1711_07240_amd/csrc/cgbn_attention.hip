@@ -11,7 +11,7 @@ constexpr int kMaxHeads = 1 << 10, kMaxRequests = 1 << 20, kMaxPage = 1024, kMax
 constexpr long long kMaxKeys = 1ll << 30, kMaxRows = 1ll << 26;          // rows: heads of tokens
 
 struct Plan {
-    int way, prefix_splits, prefix_per, own_splits, prefix_tiles, own_tiles, whole;
+    int prefix_kind, own_kind, prefix_splits, prefix_per, own_splits, prefix_tiles, own_tiles, whole;
     long long prefix_jobs, jobs;
     int parts() const { return prefix_splits + own_splits; }
 };
@@ -26,19 +26,20 @@ long long up(long long a, long long b) { return (a + b - 1) / b; }
 
 // What the device has to know of the lengths stays there: ranges of a request's own keys are cut by its length where they are read, `own_splits` of
 // them.  `several`: requests may have more rows than one.
-Plan plan(long long T, int B, int Hq, int Hk, long long prefix, long long capacity, bool several)
+Plan plan(long long T, int B, int Hq, int Hk, int line, int elem, long long prefix, long long capacity, bool several)
 {
     Plan p;
     std::memset(&p, 0, sizeof(p));
     const long long g = Hq / Hk, rows = T * g, each = several ? up(rows, B) : g;
     // tiles of rows: no more of them empty than has to be
-    if (each > 32) p.way = WAY_128_128;
-    else if (each > 16) p.way = rows > 32 ? WAY_128_32 : WAY_32_32;
-    else p.way = rows > 32 ? WAY_128_16 : rows > 16 ? WAY_32_16 : WAY_16_16;
-    p.prefix_tiles = (int)up(rows, kPrefixRows[p.way]);
-    const long long own_tiles = several ? rows / kOwnRows[p.way] + B : B * up(g, kOwnRows[p.way]);
+    auto kind_of = [&](long long n) { return n <= rows_of(FEW, line, elem) ? FEW : n <= rows_of(SOME, line, elem) ? SOME : MANY; };
+    p.own_kind = kind_of(each);
+    p.prefix_kind = kind_of(rows);
+    const int own_rows = rows_of(p.own_kind, line, elem);
+    p.prefix_tiles = (int)up(rows, rows_of(p.prefix_kind, line, elem));
+    const long long own_tiles = several ? rows / own_rows + B : B * up(g, own_rows);
     p.own_tiles = (int)own_tiles;
-    if (p.way == WAY_128_128 && own_tiles * Hk >= 256) {
+    if (p.own_kind == MANY && own_tiles * Hk >= 256) {
         p.whole = 1;
         p.own_splits = 1;
         p.prefix_tiles = 0;
@@ -77,10 +78,11 @@ size_t cgbn_prefix_attention_workspace_bytes(long long T, int B, int Hq, int Hk,
 {
     if ((dtype != CGBN_F32 && dtype != CGBN_BF16) || !sizes_fit(T, B, Hq, Hk, D, prefix, capacity)) return 0;
     if (T == 0 || B == 0) return 256;
+    const int elem = dtype == CGBN_F32 ? 4 : 2, line = line_of(width_of(D), elem);
     // requests of one row each go in other tiles when it is said that they are
-    size_t most = scratch(plan(T, B, Hq, Hk, prefix, capacity, true), T, Hq, D);
+    size_t most = scratch(plan(T, B, Hq, Hk, line, elem, prefix, capacity, true), T, Hq, D);
     if (T == B) {
-        const size_t single = scratch(plan(T, B, Hq, Hk, prefix, capacity, false), T, Hq, D);
+        const size_t single = scratch(plan(T, B, Hq, Hk, line, elem, prefix, capacity, false), T, Hq, D);
         if (single > most) most = single;
     }
     const size_t bytes = (most + 255) / 256 * 256;
@@ -97,7 +99,8 @@ cgbn_status cgbn_prefix_attention(const void* q, long long ldq, long long T, int
     if (!sizes_fit(T, B, Hq, Hk, D, prefix, capacity) || (!rows && T != B)) return CGBN_ERR_SHAPE;
     if (T == 0 || B == 0) return CGBN_OK;
     if (!q || !out || (pages && (!k_pages || !v_pages)) || (prefix && !prefix_table) || (max_pages && (!table || !lengths))) return CGBN_ERR_NULL;
-    const long long elem = dtype == CGBN_F32 ? 4 : 2, width = (long long)Hq * D;
+    const int elem = dtype == CGBN_F32 ? 4 : 2;
+    const long long width = (long long)Hq * D;
     if (ldq > (1ll << 32) || ldo > (1ll << 32)) return CGBN_ERR_SHAPE;
     if (T > 1 && (ldq < width || ldo < width)) return CGBN_ERR_STRIDE;
     const uintptr_t sixteen = reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(k_pages) | reinterpret_cast<uintptr_t>(v_pages);
@@ -108,7 +111,8 @@ cgbn_status cgbn_prefix_attention(const void* q, long long ldq, long long T, int
     for (const void* p : in)
         if (p && (p == out || p == lse)) return CGBN_ERR_ALIAS;
     if (out == lse) return CGBN_ERR_ALIAS;
-    const Plan p = plan(T, B, Hq, Hk, prefix, capacity, rows != nullptr);
+    const int line = line_of(width_of(D), elem);
+    const Plan p = plan(T, B, Hq, Hk, line, elem, prefix, capacity, rows != nullptr);
     if (p.jobs >= (1ll << 24)) return CGBN_ERR_SHAPE;           // 2^32 threads
     AttendArgs A;
     std::memset(&A, 0, sizeof(A));
@@ -123,7 +127,7 @@ cgbn_status cgbn_prefix_attention(const void* q, long long ldq, long long T, int
     A.prefix_splits = p.prefix_splits; A.prefix_per = p.prefix_per; A.own_splits = p.own_splits; A.prefix_tiles = p.prefix_tiles; A.own_tiles = p.own_tiles;
     A.prefix_jobs = (int)p.prefix_jobs; A.jobs = (int)p.jobs; A.whole = p.whole; A.direct = p.parts() <= 1; A.scale = scale * 1.4426950408889634f;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    return dtype == CGBN_F32 ? launch_attend<float>(A, p.way, st) : launch_attend<bf16_t>(A, p.way, st);
+    return dtype == CGBN_F32 ? launch_attend<float>(A, p.prefix_kind, p.own_kind, st) : launch_attend<bf16_t>(A, p.prefix_kind, p.own_kind, st);
 }
 
 }  // extern "C"

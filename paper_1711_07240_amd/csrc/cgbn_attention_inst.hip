@@ -4,28 +4,31 @@
 
 namespace cgbn {
 
-template <typename T, int DP> static void launch_width(const AttendArgs& A, int way, hipStream_t st)
+template <typename T, int DP> static void launch_width(const AttendArgs& A, int prefix, int own, hipStream_t st)
 {
     const dim3 grid((unsigned)A.jobs);
-    switch (way) {
-    case WAY_16_16: hipLaunchKernelGGL((attend_keys<T, DP, 1, 1, 1, 1>), grid, dim3(kThreads), 0, st, A); break;
-    case WAY_32_16: hipLaunchKernelGGL((attend_keys<T, DP, 1, 2, 1, 1>), grid, dim3(kThreads), 0, st, A); break;
-    case WAY_128_16: hipLaunchKernelGGL((attend_keys<T, DP, 4, 2, 1, 1>), grid, dim3(kThreads), 0, st, A); break;
-    case WAY_32_32: hipLaunchKernelGGL((attend_keys<T, DP, 1, 2, 1, 2>), grid, dim3(kThreads), 0, st, A); break;
-    case WAY_128_32: hipLaunchKernelGGL((attend_keys<T, DP, 4, 2, 1, 2>), grid, dim3(kThreads), 0, st, A); break;
-    case WAY_128_128: hipLaunchKernelGGL((attend_keys<T, DP, 4, 2, 4, 2>), grid, dim3(kThreads), 0, st, A); break;
-    }
+#define CGBN_CASE(prefix_, own_) \
+    if (prefix == prefix_ && own == own_) hipLaunchKernelGGL((attend_keys<T, DP, prefix_, own_>), grid, dim3(kThreads), 0, st, A);
+    CGBN_CASE(FEW, FEW)
+    CGBN_CASE(SOME, FEW)
+    CGBN_CASE(MANY, FEW)
+    CGBN_CASE(SOME, SOME)
+    CGBN_CASE(MANY, SOME)
+    CGBN_CASE(MANY, MANY)
+#undef CGBN_CASE
 }
 
-template <> cgbn_status launch_attend<CGBN_INST_T>(const AttendArgs& A, int way, hipStream_t st)
+template <> cgbn_status launch_attend<CGBN_INST_T>(const AttendArgs& A, int prefix, int own, hipStream_t st)
 {
     typedef CGBN_INST_T T;
-    if (A.D <= 32) launch_width<T, 32>(A, way, st);
-    else if (A.D <= 64) launch_width<T, 64>(A, way, st);
-    else if (A.D <= 96) launch_width<T, 96>(A, way, st);
-    else if (A.D <= 128) launch_width<T, 128>(A, way, st);
-    else if (A.D <= 192) launch_width<T, 192>(A, way, st);
-    else launch_width<T, 256>(A, way, st);
+    switch (width_of(A.D)) {
+    case 32: launch_width<T, 32>(A, prefix, own, st); break;
+    case 64: launch_width<T, 64>(A, prefix, own, st); break;
+    case 96: launch_width<T, 96>(A, prefix, own, st); break;
+    case 128: launch_width<T, 128>(A, prefix, own, st); break;
+    case 192: launch_width<T, 192>(A, prefix, own, st); break;
+    default: launch_width<T, 256>(A, prefix, own, st);
+    }
     if (hipGetLastError() != hipSuccess) return CGBN_ERR_HIP;
     if (!A.direct) {
         const long long rows = A.T * A.Hq;
