@@ -310,6 +310,7 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
                 }
             }
 
+            if (r0 + wr * (QT * 16) >= count) continue;          // none of this wavefront's rows are there
             const int k0 = wk * C::KW;
             f32x4 S[QT][C::NT];
 #pragma unroll
@@ -535,31 +536,74 @@ template <typename T, int DP, int PREFIX, int OWN> __global__ __launch_bounds__(
     }
 }
 
-// Joins a row's parts, a wavefront to a row, in their order.
-template <typename T> __global__ __launch_bounds__(kThreads) void attend_join(const AttendArgs A)
+constexpr int kMaxParts = 128;
+
+// Joins a row's parts: WAVES wavefronts to a row, lanes in groups of D / 4 (up to a power of two) that take every so manieth part; added part by part
+// within a group, then over the groups and the wavefronts in a fixed tree.  All of the parts' sums are fetched at once, and the products of four at a time.
+template <typename T, int LANES, int WAVES> __global__ __launch_bounds__(kThreads) void attend_join(const AttendArgs A)
 {
-    const long long r = (long long)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave, token = r / A.Hq;
-    const long long end = A.rows ? min(max((long long)A.rows[A.B], 0ll), A.T) : A.T;
-    if (token >= end) return;
-    const int lane = (int)threadIdx.x % kWave, parts = A.prefix_splits + A.own_splits, d = lane * 4;
-    float top = -INFINITY, sum = 0.f;
-    for (int p = 0; p < parts; ++p) {
-        const float2 ml = A.part_ml[p * A.T * A.Hq + r];
-        if (ml.y != 0.f) top = fmaxf(top, ml.x);
+    constexpr int GROUPS = kWave / LANES, STEP = GROUPS * WAVES, AHEAD = 4;
+    __shared__ float weights[4][kMaxParts];
+    __shared__ f32x4 joined[WAVES == 1 ? 1 : 4][LANES];
+    const int w = (int)threadIdx.x / kWave, lane = (int)threadIdx.x % kWave, parts = A.prefix_splits + A.own_splits;
+    const long long r = (long long)blockIdx.x * (4 / WAVES) + (WAVES == 1 ? w : 0);
+    const int token = (int)((unsigned)r / (unsigned)A.Hq);          // (rows are fewer than 2^26)
+    const long long end = A.rows ? min(max((long long)A.rows[A.B], 0ll), A.T) : A.T, all = A.T * A.Hq;
+    if (token >= end) return;                                       // (with several wavefronts to a row, all of the workgroup)
+    float top = -INFINITY;
+    float2 ml[kMaxParts / kWave];
+#pragma unroll
+    for (int k = 0; k < kMaxParts / kWave; ++k) {
+        ml[k] = make_float2(-INFINITY, 0.f);
+        if (k * kWave + lane < parts) ml[k] = A.part_ml[(k * kWave + lane) * all + r];
+        if (ml[k].y != 0.f) top = fmaxf(top, ml[k].x);
     }
+    top = row_max(top);
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < kMaxParts / kWave; ++k) {
+        const float f = ml[k].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[k].x - top);
+        sum += ml[k].y == 0.f ? 0.f : f * ml[k].y;
+        // (a part without keys weighs nothing, whatever it holds; one whose weight comes out as zero is there all the same)
+        weights[w][k * kWave + lane] = ml[k].y == 0.f ? -1.f : f;
+    }
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");              // (the lanes of a wavefront read each other's)
+
+    const int d = lane % LANES * 4, g = lane / LANES + (WAVES == 1 ? 0 : w * GROUPS);
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < parts; ++p) {
-        const float2 ml = A.part_ml[p * A.T * A.Hq + r];
-        if (ml.y == 0.f) continue;
-        const float f = __builtin_amdgcn_exp2f(ml.x - top);
-        sum += f * ml.y;
-        if (d < A.D) o += f * *reinterpret_cast<const f32x4*>(A.part_o + (p * A.T * A.Hq + r) * A.D + d);
+    for (int p0 = g; p0 < parts; p0 += AHEAD * STEP) {
+        f32x4 v[AHEAD];
+        float f[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int p = p0 + k * STEP;
+            f[k] = p < parts ? weights[w][p] : -1.f;
+            if (f[k] != -1.f && d < A.D) v[k] = *reinterpret_cast<const f32x4*>(A.part_o + (p * all + r) * A.D + d);
+            else v[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) o += (f[k] == -1.f ? 0.f : f[k]) * v[k];
     }
+#pragma unroll
+    for (int k = LANES; k < kWave; k *= 2)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], k);
+    if constexpr (WAVES > 1) {
+        if (lane < LANES) joined[w][lane] = o;
+        __syncthreads();
+        if (w) return;
+        o = (joined[0][lane % LANES] + joined[1][lane % LANES]) + (joined[2][lane % LANES] + joined[3][lane % LANES]);
+    }
+    if (lane >= LANES) return;
     if (d < A.D) {
         const float by = 1.f / sum;
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] = sum == 0.f ? 0.f : o[e] * by;
-        T* const to = reinterpret_cast<T*>(A.out) + token * A.ldo + (r - token * A.Hq) * A.D + d;
+        T* const to = reinterpret_cast<T*>(A.out) + token * A.ldo + ((int)r - token * A.Hq) * A.D + d;
         if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(f32x2_to_bf16x2(o[0], o[1]), f32x2_to_bf16x2(o[2], o[3]));
         else *reinterpret_cast<f32x4*>(to) = o;
     }

@@ -18,6 +18,14 @@ template <typename T, int DP> static void launch_width(const AttendArgs& A, int 
 #undef CGBN_CASE
 }
 
+// a workgroup to a row where it has many parts
+template <typename T, int LANES> static void launch_join(const AttendArgs& A, hipStream_t st)
+{
+    const long long rows = A.T * A.Hq;
+    if (A.prefix_splits + A.own_splits > 8 && rows < (1 << 20)) hipLaunchKernelGGL((attend_join<T, LANES, 4>), dim3((unsigned)rows), dim3(kThreads), 0, st, A);
+    else hipLaunchKernelGGL((attend_join<T, LANES, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(kThreads), 0, st, A);
+}
+
 template <> cgbn_status launch_attend<CGBN_INST_T>(const AttendArgs& A, int prefix, int own, hipStream_t st)
 {
     typedef CGBN_INST_T T;
@@ -31,8 +39,10 @@ template <> cgbn_status launch_attend<CGBN_INST_T>(const AttendArgs& A, int pref
     }
     if (hipGetLastError() != hipSuccess) return CGBN_ERR_HIP;
     if (!A.direct) {
-        const long long rows = A.T * A.Hq;
-        hipLaunchKernelGGL(attend_join<T>, dim3((unsigned)((rows + 3) / 4)), dim3(kThreads), 0, st, A);
+        if (A.D <= 32) launch_join<T, 8>(A, st);
+        else if (A.D <= 64) launch_join<T, 16>(A, st);
+        else if (A.D <= 128) launch_join<T, 32>(A, st);
+        else launch_join<T, 64>(A, st);
         if (hipGetLastError() != hipSuccess) return CGBN_ERR_HIP;
     }
     return CGBN_OK;
