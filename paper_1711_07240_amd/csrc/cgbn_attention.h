@@ -135,7 +135,6 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
     typedef Attend<T, DP, KIND> C;
     constexpr int QT = C::QT, WR = C::WR;
     const int tid = (int)threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave), wr = w % WR, wk = w / WR, col = lane & 15, grp = lane >> 4;
-    lds_char* const base = (lds_char*)lds;
     const char** const places = reinterpret_cast<const char**>(lds + C::PLACES);
     const int head = id % A.Hk;
     id /= A.Hk;
@@ -208,6 +207,8 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
         for (int i = tid; i < 2 * C::STAGE / 16; i += kThreads) *reinterpret_cast<u32x4*>(lds + i * 16) = u32x4{0, 0, 0, 0};
     }
     const long long values = A.v_pages - A.k_pages;
+    lds_char* const base = (lds_char*)lds;          // two tiles of keys, two of values
+    const int k0 = wk * C::KW;
 
     int dirty_from = 0, dirty_to = 0;     // own keys whose infinities and NaN stay out of the products, see below
     for (int own = prefix_job || A.whole ? 0 : 1; own < (prefix_job ? 1 : 2); ++own) {
@@ -234,14 +235,15 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
         if (begin >= end) continue;
 
         int first = 0, stop = begin;      // keys whose pages' addresses are at hand
-        unsigned long long there[2], next[2];          // keys of the tile that is there, and of the next, that exist
-        // Starts the loads of the tile at `key0`
-        auto issue = [&](int key0, int stage) {
+        const char* at[C::PASSES];        // the keys of the last tile whose loads were started: null where there is none
+        bool full = false;                // all of them are there
+        unsigned long long seen[2] = {0, 0};
+        const int mask = (1 << A.page_bits) - 1;
+        auto load_keys = [&](int key0, int stage) {
             if (key0 + C::KT > stop && stop < end) {
                 first = key0 >> A.page_bits;
                 const int n = min(kPlaces, ((end - 1) >> A.page_bits) - first + 1);
-                stop = (first + kPlaces) << A.page_bits;
-                if (stop < 0 || stop > end) stop = end;
+                stop = min((first + kPlaces) << A.page_bits, end);          // (below 2^30 + 2^20)
                 __syncthreads();
                 for (int i = tid; i < n; i += kThreads) {
                     const int page = table[first + i];
@@ -249,88 +251,98 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
                 }
                 __syncthreads();
             }
+            const uint32_t to = (uint32_t)(uintptr_t)base + stage * C::HALF + w * 1024;
+            int missing = 0;
 #pragma unroll
-            for (int h = 0; h < (C::KT + 63) / 64; ++h) {
-                const int key = key0 + h * 64 + lane;
-                next[h] = __ballot(h * 64 + lane < C::KT && key < end && places[(key >> A.page_bits) - first] != nullptr);
+            for (int i = 0; i < C::PASSES; ++i) {
+                const int key = min(key0 + i * C::PASS + load_row, end - 1);
+                const char* const place = places[(key >> A.page_bits) - first];
+                missing |= place == nullptr;
+                at[i] = place + ((key & mask) * line + chunk(i));
             }
-            const bool full = next[0] == (C::KT >= 64 ? ~0ull : (1ull << (C::KT % 64)) - 1) && (C::KT <= 64 || next[1] == ~0ull);
-            const uint32_t to = (uint32_t)(uintptr_t)(base + stage * C::STAGE) + w * 1024;
-            const int mask = (1 << A.page_bits) - 1;
+            full = key0 + C::KT <= end && !__any(missing);
             if (full) {
-                const char* at[C::PASSES];
-#pragma unroll
-                for (int i = 0; i < C::PASSES; ++i) {
-                    const int key = key0 + i * C::PASS + load_row;
-                    at[i] = places[(key >> A.page_bits) - first] + ((key & mask) * line + chunk(i));
-                }
 #pragma unroll
                 for (int i = 0; i < C::PASSES; ++i)
                     if (chunk(i) < line) dma16_from(to + i * 4096, at[i]);
+                return;
+            }
 #pragma unroll
-                for (int i = 0; i < C::PASSES; ++i)
-                    if (chunk(i) < line) dma16_from(to + C::HALF + i * 4096, at[i] + values);
-            } else {
+            for (int h = 0; h < (C::KT + 63) / 64; ++h) {
+                const int key = key0 + h * 64 + lane;
+                seen[h] = __ballot(h * 64 + lane < C::KT && key < end && places[(min(key, end - 1) >> A.page_bits) - first] != nullptr);
+            }
 #pragma unroll
-                for (int i = 0; i < C::PASSES; ++i) {
-                    const int key = key0 + i * C::PASS + load_row;
-                    const char* const at = key < end ? places[(key >> A.page_bits) - first] : nullptr;
-                    if (at && chunk(i) < line) {
-                        dma16_from(to + i * 4096, at + ((key & mask) * line + chunk(i)));
-                        dma16_from(to + C::HALF + i * 4096, at + values + ((key & mask) * line + chunk(i)));
-                    } else {
-                        *reinterpret_cast<u32x4*>(lds + stage * C::STAGE + i * 4096 + tid * 16) = u32x4{0, 0, 0, 0};
-                        *reinterpret_cast<u32x4*>(lds + stage * C::STAGE + C::HALF + i * 4096 + tid * 16) = u32x4{0, 0, 0, 0};
-                    }
-                }
+            for (int i = 0; i < C::PASSES; ++i) {
+                const int key = key0 + i * C::PASS + load_row;
+                if (key >= end || places[(key >> A.page_bits) - first] == nullptr) at[i] = nullptr;
+                if (at[i] && chunk(i) < line) dma16_from(to + i * 4096, at[i]);
+                else *reinterpret_cast<u32x4*>(lds + stage * C::HALF + i * 4096 + tid * 16) = u32x4{0, 0, 0, 0};
             }
         };
-
-        __syncthreads();                  // (LDS is read no more)
-        issue(begin, 0);
-        int stage = 0;
-        for (int key0 = begin; key0 < end; key0 += C::KT, stage ^= 1) {
-            there[0] = next[0];
-            there[1] = next[1];
-            dma_wait_and_meet();
-            if (key0 + C::KT < end) issue(key0 + C::KT, stage ^ 1);
-            const lds_char* const tile = base + stage * C::STAGE;
-            // A product with a weight of zero would carry an infinity or a NaN of v to rows that do not see its key.  Where rows of the tile see
-            // different keys such values are left out of the products and added to the rows that do at the end.
-            const bool edge = own && least < end && key0 + C::KT > least;
-            bool dirty = false;
-            if (edge) {
-                int bad = 0;
+        // ... of the values of the keys that the last call of load_keys() was for
+        auto load_values = [&](int stage) {
+            const uint32_t to = (uint32_t)(uintptr_t)base + (2 + stage) * C::HALF + w * 1024;
+            if (full) {
 #pragma unroll
-                for (int i = 0; i < C::PASSES; ++i) bad |= !all_finite<T>(*reinterpret_cast<const u32x4*>(lds + stage * C::STAGE + C::HALF + i * 4096 + tid * 16));
-                dirty = __syncthreads_or(bad);
-                if (dirty) {
-                    if (dirty_to == 0) dirty_from = key0;
-                    dirty_to = end;
-                }
+                for (int i = 0; i < C::PASSES; ++i)
+                    if (chunk(i) < line) dma16_from(to + i * 4096, at[i] + values);
+                return;
             }
-
-            if (r0 + wr * (QT * 16) >= count) continue;          // none of this wavefront's rows are there
-            const int k0 = wk * C::KW;
-            f32x4 S[QT][C::NT];
 #pragma unroll
-            for (int t = 0; t < QT; ++t)
-#pragma unroll
-                for (int n = 0; n < C::NT; ++n) S[t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < C::KS; ++s)
-#pragma unroll
-                for (int n = 0; n < C::NT; ++n) {
-                    const u32x4 k = *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(
-                        tile + (k0 + n * 16 + col) * C::LINE + (((s * 4 + grp) ^ line_key<C::LINE>(col)) << 4));
-#pragma unroll
-                    for (int t = 0; t < QT; ++t) S[t][n] = multiply<T>(k, Q[t][s], S[t][n]);
+            for (int i = 0; i < C::PASSES; ++i) {
+                if (at[i] && chunk(i) < line) dma16_from(to + i * 4096, at[i] + values);
+                else *reinterpret_cast<u32x4*>(lds + 2 * C::HALF + stage * C::HALF + i * 4096 + tid * 16) = u32x4{0, 0, 0, 0};
+            }
+        };
+        typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        typedef __attribute__((address_space(3))) uint32_t lds_u32;
+        // where this lane reads: line `col` of 16 keys; the values' line of its keys.  (xor of a chunk's number and xor of an address are the same: lines
+        // begin at multiples of their length)
+        const int k_from = (k0 + col) * C::LINE + ((grp ^ line_key<C::LINE>(col)) << 4);
+        const int v_line = grp * 4 + (C::EB == 2 ? col >> 2 : 0), v_chunk = C::EB == 2 ? (col >> 1) & 1 : col >> 2;
+        const int v_from = 2 * C::HALF + (k0 + v_line) * C::LINE + ((v_chunk ^ line_key<C::LINE>(v_line)) << 4) + (C::EB == 2 ? (col & 1) * 8 : (col & 3) * 4);
+        // fragment i of a tile's keys (16 of them, 64 bytes of each), of its values (the keys of a weights' register by 16 of D)
+        constexpr int K_STEPS = C::KS * C::NT, V_STEPS = C::NP * C::ND, AHEAD = K_STEPS < 4 ? K_STEPS : 4;
+        auto key_fragment = [&](int stage, int i) {
+            return *(const lds_u32x4*)(base + ((k_from + stage * C::HALF) ^ (i / C::NT << 6)) + i % C::NT * 16 * C::LINE);
+        };
+        auto value_fragment = [&](int stage, int i) {
+            const int n = i / C::ND, d = i % C::ND, from = v_from + stage * C::HALF;
+            u32x4 v = {0, 0, 0, 0};
+            if constexpr (C::EB == 2) {
+                lds_char* const p = base + (from ^ (d << 5)) + n * 32 * C::LINE;
+                const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
+                v.x = lo.x;
+                v.y = lo.y;
+                if constexpr (C::NT > 1) {
+                    const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * C::LINE)));
+                    v.z = hi.x;
+                    v.w = hi.y;
                 }
-
-            const bool whole = there[0] == (C::KT >= 64 ? ~0ull : (1ull << (C::KT % 64)) - 1) && (C::KT <= 64 || there[1] == ~0ull) && !edge;
-            if (!whole) {
-                const unsigned seen = (unsigned)((C::KT > 64 && k0 >= 64 ? there[1] : there[0]) >> (k0 & 63) >> (grp * 4));
-                const unsigned seen2 = (unsigned)((C::KT > 64 && k0 >= 64 ? there[1] : there[0]) >> (k0 & 63) >> (grp * 4) >> 32);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = *(const lds_u32*)(base + (from ^ (d << 6) ^ (line_key<C::LINE>(e) << 4)) + (n * 16 + e) * C::LINE);
+            }
+            return v;
+        };
+        auto largest = [&](const f32x4 (&S)[QT][C::NT], float (&top)[QT]) {
+#pragma unroll
+            for (int t = 0; t < QT; ++t) {
+                top[t] = S[t][0][0];
+#pragma unroll
+                for (int n = 0; n < C::NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) top[t] = fmaxf(top[t], S[t][n][e]);
+            }
+        };
+        // What rows do not see is -infinity, and m follows the largest score, of the tile at key0.  m follows only where that is more than 2^8 times what m stands for: sums
+        // hold that and much more in 32 bits, and what is there already is seldom scaled.
+        auto settle = [&](int key0, bool all, f32x4 (&S)[QT][C::NT], float (&top)[QT]) {
+            const bool edge = own && key0 + C::KT > least;
+            if (!all || edge) {
+                const unsigned long long bits = all ? ~0ull : (C::KT > 64 && k0 >= 64 ? seen[1] : seen[0]) >> (k0 & 63) >> (grp * 4);
 #pragma unroll
                 for (int t = 0; t < QT; ++t)
 #pragma unroll
@@ -338,88 +350,135 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const int key = key0 + k0 + n * 16 + grp * 4 + e;
-                            const bool hidden = !(((n < 2 ? seen : seen2) >> (n % 2 * 16 + e)) & 1) || (own && key >= sees[t]);
-                            if (hidden) S[t][n][e] = -INFINITY;
+                            if (!(((n < 2 ? (unsigned)bits : (unsigned)(bits >> 32)) >> (n % 2 * 16 + e)) & 1) || (own && key >= sees[t])) S[t][n][e] = -INFINITY;
                         }
+                largest(S, top);
             }
-
-            // The weights, 2^(scale s - m).  m follows the largest score only where that is more than 2^8 times what m stands for: sums hold that and
-            // much more in 32 bits, and what is there already is seldom scaled.
-            u32x4 P[QT][C::NP];
 #pragma unroll
-            for (int t = 0; t < QT; ++t) {
-                float top = S[t][0][0];
-#pragma unroll
-                for (int n = 0; n < C::NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) top = fmaxf(top, S[t][n][e]);
-                if (__any(top * scale > m[t] + 8.f)) {
-                    const float most = fmaxf(m[t], row_max(top * scale)), down = __builtin_amdgcn_exp2f(m[t] - (most == -INFINITY ? 0.f : most));
+            for (int t = 0; t < QT; ++t)
+                if (__any(top[t] * scale > m[t] + 8.f)) {
+                    const float most = fmaxf(m[t], row_max(top[t] * scale)), down = __builtin_amdgcn_exp2f(m[t] - (most == -INFINITY ? 0.f : most));
                     m[t] = most;
                     l[t] *= down;
 #pragma unroll
                     for (int d = 0; d < C::ND; ++d) O[t][d] *= down;
                 }
-                const float from = m[t] == -INFINITY ? 0.f : m[t];
-                float sum = 0.f;
+        };
+
+        // Keys are one tile ahead of values: while a tile's weights are formed, on the vector unit, and its values multiplied, the next one's scores are.
+        f32x4 S[QT][C::NT], next[QT][C::NT];
+        float top[QT];
+        __syncthreads();                  // (LDS is read no more)
+        load_keys(begin, 0);
+        bool all = full;                  // of the tile whose scores are in S
+        load_values(0);
+        dma_wait_and_meet();
+        const bool live = r0 + wr * (QT * 16) < count;          // this wavefront has rows
+        if (live) {
 #pragma unroll
-                for (int n = 0; n < C::NT; ++n)
+            for (int i = 0; i < K_STEPS; ++i) {
+                const u32x4 k = key_fragment(0, i);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        S[t][n][e] = __builtin_amdgcn_exp2f(fmaf(S[t][n][e], scale, -from));
-                        sum += S[t][n][e];
-                    }
-                l[t] += sum;
-                // bfloat16: the weights are rounded to 8 bits for the products (off by at most 2^-8 of themselves, with no preferred sign); their sum is not
+                for (int t = 0; t < QT; ++t) S[t][i % C::NT] = multiply<T>(k, Q[t][i / C::NT], i < C::NT ? f32x4{0.f, 0.f, 0.f, 0.f} : S[t][i % C::NT]);
+            }
+            largest(S, top);
+            settle(begin, all, S, top);
+        }
+        if (begin + C::KT < end) load_keys(begin + C::KT, 1);
+        int stage = 0;
+        for (int key0 = begin; key0 < end; key0 += C::KT, stage ^= 1) {
+            dma_wait_and_meet();
+            // (the keys' bits go with the next tile's scores, which are settled at the end of this pass: a tile further they are not asked for before)
+            const bool next_all = full;
+            unsigned long long next_seen[2] = {seen[0], seen[1]};
+            if (key0 + C::KT < end) load_values(stage ^ 1);
+            if (key0 + 2 * C::KT < end) load_keys(key0 + 2 * C::KT, stage);
+            // A product with a weight of zero would carry an infinity or a NaN of v to rows that do not see its key.  Where rows of the tile see
+            // different keys such values are taken out of the tile and added to the rows that do at the end.
+            if (own && least < end && key0 + C::KT > least) {
+                u32x4 v[C::PASSES];
+                int bad = 0;
 #pragma unroll
-                for (int n = 0; n < C::NP; ++n) {
-                    if constexpr (C::EB == 2) {
-                        P[t][n].x = f32x2_to_bf16x2(S[t][2 * n][0], S[t][2 * n][1]);
-                        P[t][n].y = f32x2_to_bf16x2(S[t][2 * n][2], S[t][2 * n][3]);
-                        if constexpr (C::NT > 1) {
-                            P[t][n].z = f32x2_to_bf16x2(S[t][2 * n + 1][0], S[t][2 * n + 1][1]);
-                            P[t][n].w = f32x2_to_bf16x2(S[t][2 * n + 1][2], S[t][2 * n + 1][3]);
-                        }
-                    } else {
-                        P[t][n] = u32x4{__float_as_uint(S[t][n][0]), __float_as_uint(S[t][n][1]), __float_as_uint(S[t][n][2]), __float_as_uint(S[t][n][3])};
-                    }
+                for (int i = 0; i < C::PASSES; ++i) {
+                    v[i] = *reinterpret_cast<const u32x4*>(lds + 2 * C::HALF + stage * C::HALF + i * 4096 + tid * 16);
+                    bad |= !all_finite<T>(v[i]);
+                }
+                if (__syncthreads_or(bad)) {
+                    if (dirty_to == 0) dirty_from = key0;
+                    dirty_to = end;
+#pragma unroll
+                    for (int i = 0; i < C::PASSES; ++i) *reinterpret_cast<u32x4*>(lds + 2 * C::HALF + stage * C::HALF + i * 4096 + tid * 16) = only_finite<T>(v[i]);
+                    __syncthreads();
                 }
             }
-            const lds_char* const v_tile = tile + C::HALF;
+            if (!live) continue;
+
+            // The order is held step by step (the compiler by itself asks LDS for an operand right before its product and then waits): operands are read some
+            // products ahead, and between the products of the next scores (behind the last tile: of what is there, and not used) goes the weights' arithmetic.
+            u32x4 P[QT][C::NP], k[K_STEPS], v[V_STEPS];
+            float from[QT];
 #pragma unroll
-            for (int n = 0; n < C::NP; ++n)
+            for (int t = 0; t < QT; ++t) from[t] = m[t] == -INFINITY ? 0.f : m[t];
+            constexpr int SLICES = QT * C::NT;
+            auto weights = [&](int j) {          // four keys of a row
+                const int t = j % QT, n = j / QT;
+                f32x4& x = S[t][n];
 #pragma unroll
-                for (int d = 0; d < C::ND; ++d) {
-                    u32x4 v = {0, 0, 0, 0};
-                    if constexpr (C::EB == 2) {
-                        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-                        const int in = grp * 4 + (col >> 2);
-                        const lds_char* const p = v_tile + (k0 + n * 32 + in) * C::LINE + (((d * 2 + ((col >> 1) & 1)) ^ line_key<C::LINE>(in)) << 4) + (col & 1) * 8;
-                        const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
-                        v.x = lo.x;
-                        v.y = lo.y;
-                        if constexpr (C::NT > 1) {
-                            const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * C::LINE)));
-                            v.z = hi.x;
-                            v.w = hi.y;
-                        }
-                    } else {
-                        typedef const __attribute__((address_space(3))) uint32_t lds_u32;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int in = grp * 4 + e;
-                            v[e] = *(lds_u32*)(v_tile + (k0 + n * 16 + in) * C::LINE + (((d * 4 + (col >> 2)) ^ line_key<C::LINE>(in)) << 4) + (col & 3) * 4);
-                        }
-                    }
-                    if (dirty) v = only_finite<T>(v);
-#pragma unroll
-                    for (int t = 0; t < QT; ++t) {
-                        if constexpr (C::EB == 2 && C::NT == 1)
-                            O[t][d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, make_uint2(v.x, v.y)),
-                                                                                __builtin_bit_cast(s16x4, make_uint2(P[t][n].x, P[t][n].y)), O[t][d], 0, 0, 0);
-                        else O[t][d] = multiply<T>(v, P[t][n], O[t][d]);
-                    }
+                for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], scale, -from[t]));
+                l[t] += (x[0] + x[1]) + (x[2] + x[3]);
+                // bfloat16: the weights are rounded to 8 bits for the products (off by at most 2^-8 of themselves, with no preferred sign); their sum is not
+                if constexpr (C::EB == 2) {
+                    P[t][n / 2][n % 2 * 2] = f32x2_to_bf16x2(x[0], x[1]);
+                    P[t][n / 2][n % 2 * 2 + 1] = f32x2_to_bf16x2(x[2], x[3]);
+                } else {
+                    P[t][n] = u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
                 }
+            };
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) k[i] = key_fragment(stage ^ 1, i);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < K_STEPS; ++i) {
+                if (i + AHEAD < K_STEPS) k[i + AHEAD] = key_fragment(stage ^ 1, i + AHEAD);
+                else if (i + AHEAD - K_STEPS < V_STEPS) v[i + AHEAD - K_STEPS] = value_fragment(stage, i + AHEAD - K_STEPS);
+#pragma unroll
+                for (int t = 0; t < QT; ++t) next[t][i % C::NT] = multiply<T>(k[i], Q[t][i / C::NT], i < C::NT ? f32x4{0.f, 0.f, 0.f, 0.f} : next[t][i % C::NT]);
+#pragma unroll
+                for (int j = i * SLICES / K_STEPS; j < (i + 1) * SLICES / K_STEPS; ++j) weights(j);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int t = 0; t < QT; ++t) top[t] = next[t][0][0];
+#pragma unroll
+            for (int i = 0; i < V_STEPS; ++i) {
+                if (i + AHEAD < V_STEPS) v[i + AHEAD] = value_fragment(stage, i + AHEAD);
+#pragma unroll
+                for (int t = 0; t < QT; ++t) {
+                    const int n = i / C::ND, d = i % C::ND;
+                    if constexpr (C::EB == 2 && C::NT == 1)
+                        O[t][d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, make_uint2(v[i].x, v[i].y)),
+                                                                            __builtin_bit_cast(s16x4, make_uint2(P[t][n].x, P[t][n].y)), O[t][d], 0, 0, 0);
+                    else O[t][d] = multiply<T>(v[i], P[t][n], O[t][d]);
+                }
+#pragma unroll
+                for (int j = i * SLICES / V_STEPS; j < (i + 1) * SLICES / V_STEPS; ++j) {
+                    const f32x4 x = next[j % QT][j / QT];
+                    top[j % QT] = fmaxf(fmaxf(fmaxf(top[j % QT], x[0]), fmaxf(x[1], x[2])), x[3]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (key0 + C::KT < end) {
+                unsigned long long later[2] = {seen[0], seen[1]};
+                seen[0] = next_seen[0];
+                seen[1] = next_seen[1];
+                settle(key0 + C::KT, next_all, next, top);
+                seen[0] = later[0];
+                seen[1] = later[1];
+            }
+#pragma unroll
+            for (int t = 0; t < QT; ++t)
+#pragma unroll
+                for (int n = 0; n < C::NT; ++n) S[t][n] = next[t][n];
         }
     }
 
