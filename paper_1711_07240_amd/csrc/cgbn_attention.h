@@ -235,9 +235,10 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
         if (begin >= end) continue;
 
         int first = 0, stop = begin;      // keys whose pages' addresses are at hand
+        bool holes = false;               // some of those pages are not there
         const char* at[C::PASSES];        // the keys of the last tile whose loads were started: null where there is none
         bool full = false;                // all of them are there
-        unsigned long long seen[2] = {0, 0};
+        unsigned long long seen[2] = {0, 0};          // which of them are there, if not all
         const int mask = (1 << A.page_bits) - 1;
         auto load_keys = [&](int key0, int stage) {
             if (key0 + C::KT > stop && stop < end) {
@@ -245,23 +246,23 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
                 const int n = min(kPlaces, ((end - 1) >> A.page_bits) - first + 1);
                 stop = min((first + kPlaces) << A.page_bits, end);          // (below 2^30 + 2^20)
                 __syncthreads();
+                int missing = 0;
                 for (int i = tid; i < n; i += kThreads) {
                     const int page = table[first + i];
-                    places[i] = page < 0 || page >= A.pages ? nullptr : A.k_pages + ((((long long)page * A.Hk + head) << A.page_bits) * line);
+                    const bool none = page < 0 || page >= A.pages;
+                    places[i] = none ? nullptr : A.k_pages + ((((long long)page * A.Hk + head) << A.page_bits) * line);
+                    missing |= none;
                 }
-                __syncthreads();
+                holes = __syncthreads_or(missing);
             }
             const uint32_t to = (uint32_t)(uintptr_t)base + stage * C::HALF + w * 1024;
-            int missing = 0;
-#pragma unroll
-            for (int i = 0; i < C::PASSES; ++i) {
-                const int key = min(key0 + i * C::PASS + load_row, end - 1);
-                const char* const place = places[(key >> A.page_bits) - first];
-                missing |= place == nullptr;
-                at[i] = place + ((key & mask) * line + chunk(i));
-            }
-            full = key0 + C::KT <= end && !__any(missing);
+            full = key0 + C::KT <= end && !holes;
             if (full) {
+#pragma unroll
+                for (int i = 0; i < C::PASSES; ++i) {
+                    const int key = key0 + i * C::PASS + load_row;
+                    at[i] = places[(key >> A.page_bits) - first] + ((key & mask) * line + chunk(i));
+                }
 #pragma unroll
                 for (int i = 0; i < C::PASSES; ++i)
                     if (chunk(i) < line) dma16_from(to + i * 4096, at[i]);
@@ -275,7 +276,8 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
 #pragma unroll
             for (int i = 0; i < C::PASSES; ++i) {
                 const int key = key0 + i * C::PASS + load_row;
-                if (key >= end || places[(key >> A.page_bits) - first] == nullptr) at[i] = nullptr;
+                const char* const place = key < end ? places[(key >> A.page_bits) - first] : nullptr;
+                at[i] = place ? place + ((key & mask) * line + chunk(i)) : nullptr;
                 if (at[i] && chunk(i) < line) dma16_from(to + i * 4096, at[i]);
                 else *reinterpret_cast<u32x4*>(lds + stage * C::HALF + i * 4096 + tid * 16) = u32x4{0, 0, 0, 0};
             }
@@ -342,16 +344,20 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
         auto settle = [&](int key0, bool all, f32x4 (&S)[QT][C::NT], float (&top)[QT]) {
             const bool edge = own && key0 + C::KT > least;
             if (!all || edge) {
-                const unsigned long long bits = all ? ~0ull : (C::KT > 64 && k0 >= 64 ? seen[1] : seen[0]) >> (k0 & 63) >> (grp * 4);
+                const unsigned long long there = all ? ~0ull : (C::KT > 64 && k0 >= 64 ? seen[1] : seen[0]) >> (k0 & 63) >> (grp * 4);
 #pragma unroll
-                for (int t = 0; t < QT; ++t)
+                for (int t = 0; t < QT; ++t) {
+                    // bit 16 n + e: key 16 n + e from this lane's first on
+                    const int below = own ? sees[t] - (key0 + k0 + grp * 4) : 64;
+                    const unsigned long long bits = there & (below <= 0 ? 0ull : below >= 64 ? ~0ull : (1ull << below) - 1);
 #pragma unroll
                     for (int n = 0; n < C::NT; ++n)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const int key = key0 + k0 + n * 16 + grp * 4 + e;
-                            if (!(((n < 2 ? (unsigned)bits : (unsigned)(bits >> 32)) >> (n % 2 * 16 + e)) & 1) || (own && key >= sees[t])) S[t][n][e] = -INFINITY;
+                            const unsigned half = n < 2 ? (unsigned)bits : (unsigned)(bits >> 32);
+                            S[t][n][e] = half & (1u << (n % 2 * 16 + e)) ? S[t][n][e] : -INFINITY;
                         }
+                }
                 largest(S, top);
             }
 #pragma unroll
