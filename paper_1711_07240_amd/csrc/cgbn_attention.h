@@ -341,7 +341,7 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
         };
         // What rows do not see is -infinity, and m follows the largest score, of the tile at key0.  m follows only where that is more than 2^8 times what m stands for: sums
         // hold that and much more in 32 bits, and what is there already is seldom scaled.
-        auto settle = [&](int key0, bool all, f32x4 (&S)[QT][C::NT], float (&top)[QT]) {
+        auto settle = [&](int key0, bool all, const unsigned long long (&seen)[2], f32x4 (&S)[QT][C::NT], float (&top)[QT]) {
             const bool edge = own && key0 + C::KT > least;
             if (!all || edge) {
                 const unsigned long long there = all ? ~0ull : (C::KT > 64 && k0 >= 64 ? seen[1] : seen[0]) >> (k0 & 63) >> (grp * 4);
@@ -376,8 +376,10 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
         float top[QT];
         __syncthreads();                  // (LDS is read no more)
         load_keys(begin, 0);
-        bool all = full;                  // of the tile whose scores are in S
+        const bool all = full;
+        const unsigned long long first_seen[2] = {seen[0], seen[1]};
         load_values(0);
+        if (begin + C::KT < end) load_keys(begin + C::KT, 1);
         dma_wait_and_meet();
         const bool live = r0 + wr * (QT * 16) < count;          // this wavefront has rows
         if (live) {
@@ -388,15 +390,13 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
                 for (int t = 0; t < QT; ++t) S[t][i % C::NT] = multiply<T>(k, Q[t][i / C::NT], i < C::NT ? f32x4{0.f, 0.f, 0.f, 0.f} : S[t][i % C::NT]);
             }
             largest(S, top);
-            settle(begin, all, S, top);
+            settle(begin, all, first_seen, S, top);
         }
-        if (begin + C::KT < end) load_keys(begin + C::KT, 1);
         int stage = 0;
         for (int key0 = begin; key0 < end; key0 += C::KT, stage ^= 1) {
             dma_wait_and_meet();
-            // (the keys' bits go with the next tile's scores, which are settled at the end of this pass: a tile further they are not asked for before)
-            const bool next_all = full;
-            unsigned long long next_seen[2] = {seen[0], seen[1]};
+            const bool next_all = full;          // of the next tile, before the one after it is asked for
+            const unsigned long long next_seen[2] = {seen[0], seen[1]};
             if (key0 + C::KT < end) load_values(stage ^ 1);
             if (key0 + 2 * C::KT < end) load_keys(key0 + 2 * C::KT, stage);
             // A product with a weight of zero would carry an infinity or a NaN of v to rows that do not see its key.  Where rows of the tile see
@@ -473,14 +473,7 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (key0 + C::KT < end) {
-                unsigned long long later[2] = {seen[0], seen[1]};
-                seen[0] = next_seen[0];
-                seen[1] = next_seen[1];
-                settle(key0 + C::KT, next_all, next, top);
-                seen[0] = later[0];
-                seen[1] = later[1];
-            }
+            if (key0 + C::KT < end) settle(key0 + C::KT, next_all, next_seen, next, top);
 #pragma unroll
             for (int t = 0; t < QT; ++t)
 #pragma unroll
@@ -592,12 +585,22 @@ template <typename T, int DP, int PREFIX, int OWN> __global__ __launch_bounds__(
 {
     constexpr int P = Attend<T, DP, PREFIX>::LDS, O = Attend<T, DP, OWN>::LDS;
     __shared__ __attribute__((aligned(1024))) char lds[P > O ? P : O];
-    const int id = (int)blockIdx.x;
-    if constexpr (PREFIX == OWN) {
-        attend<T, DP, PREFIX>(A, lds, id < A.prefix_jobs ? id : id - A.prefix_jobs, id < A.prefix_jobs);
+    // Workgroups of both kinds in turns of 256, as many as there are compute units, while there are both: products of the one and reads of the other side by side.
+    int id = (int)blockIdx.x;
+    const int turns = min(A.prefix_jobs, A.jobs - A.prefix_jobs) / 256, turn = id / 256;
+    bool prefix = turn % 2 == 0;
+    if (turn < 2 * turns) {
+        id = turn / 2 * 256 + id % 256;
     } else {
-        if (id < A.prefix_jobs) attend<T, DP, PREFIX>(A, lds, id, true);
-        else attend<T, DP, OWN>(A, lds, id - A.prefix_jobs, false);
+        id -= turns * 256;
+        prefix = id < A.prefix_jobs;
+        if (!prefix) id -= A.prefix_jobs - turns * 256;
+    }
+    if constexpr (PREFIX == OWN) {
+        attend<T, DP, PREFIX>(A, lds, id, prefix);
+    } else {
+        if (prefix) attend<T, DP, PREFIX>(A, lds, id, true);
+        else attend<T, DP, OWN>(A, lds, id, false);
     }
 }
 

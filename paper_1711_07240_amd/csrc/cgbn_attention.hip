@@ -32,9 +32,18 @@ Plan plan(long long T, int B, int Hq, int Hk, int line, int elem, long long pref
     std::memset(&p, 0, sizeof(p));
     const long long g = Hq / Hk, rows = T * g, each = several ? up(rows, B) : g;
     // tiles of rows: no more of them empty than has to be
-    auto kind_of = [&](long long n) { return n <= rows_of(FEW, line, elem) ? FEW : n <= rows_of(SOME, line, elem) ? SOME : MANY; };
+    auto kind_of = [&](long long n) {
+        int kind = n <= rows_of(FEW, line, elem) ? FEW : n <= rows_of(SOME, line, elem) ? SOME : MANY;
+        // float products take so much longer than what they are of that keys may as well be read again, if fewer empty rows are multiplied
+        auto work = [&](int k) { return up(n, rows_of(k, line, elem)) * qt_of(k, line, elem) * (4 / wk_of(k, line)); };
+        if (elem == 4)
+            for (int k = kind - 1; k >= FEW; --k)
+                if (work(k) < work(kind)) kind = k;
+        return kind;
+    };
     p.own_kind = kind_of(each);
     p.prefix_kind = kind_of(rows);
+    if (p.own_kind > p.prefix_kind) p.own_kind = p.prefix_kind;          // (one request's rows are no more than all rows; the other way there is no kernel)
     const int own_rows = rows_of(p.own_kind, line, elem);
     p.prefix_tiles = (int)up(rows, rows_of(p.prefix_kind, line, elem));
     const long long own_tiles = several ? rows / own_rows + B : B * up(g, own_rows);
@@ -47,13 +56,17 @@ Plan plan(long long T, int B, int Hq, int Hk, int line, int elem, long long pref
         return p;
     }
     p.own_splits = prefix ? 0 : 1;         // (without any keys rows are zero)
+    // Parts of a request's keys: so many that requests of unequal length, which the host does not know, keep the device busy to the end (24 requests of up to
+    // 1500 float keys, 20 heads: 512, 1024 and 2048 workgroups 129, 129 and 122 us; 64 of up to 2048 bfloat16 keys, 8 heads: 98, 100 and 105)
     if (capacity) {
-        long long s = 1024 / (own_tiles * Hk);
+        long long s = (elem == 4 ? 2048 : 1024) / (own_tiles * Hk);
         if (s > up(capacity, 256)) s = up(capacity, 256);
         p.own_splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
     }
+    // Parts of the prefix: a workgroup for each compute unit, which leaves room for one that reads beside it (64 rows, 32768 bfloat16 keys of 8 heads, 128, 256, 512 and
+    // 1024 workgroups: 112, 98, 105 and 130 us)
     if (prefix) {
-        long long s = 512 / ((long long)p.prefix_tiles * Hk);
+        long long s = 256 / ((long long)p.prefix_tiles * Hk);
         if (s > up(prefix, 256)) s = up(prefix, 256);
         s = s < 1 ? 1 : s > 64 ? 64 : s;
         p.prefix_per = (int)up(up(prefix, s), 128) * 128;
