@@ -31,7 +31,8 @@ struct AttendArgs {
     int prefix_tiles, own_tiles;       // tiles of rows
     int prefix_jobs, jobs;             // workgroups, those of the prefix first
     int whole;                         // a workgroup takes the prefix and then its request's own keys
-    int direct;                        // there is one part: it is the result
+    int cut, tail_splits;              // whole: from tile-and-head `cut` on workgroups share one, by its keys; their parts are [tile][part][row] from `cut` on
+    int direct;                        // there is one part: it is the result (whole: but for the last ones, see `cut`)
     float scale;                       // times log2(e)
 };
 
@@ -130,41 +131,54 @@ __device__ __forceinline__ int request_of_tile(const AttendArgs& A, int i, int r
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
+// The rows of a workgroup, from r0 on of `count`: of request b, of whose `fresh` tokens token0 is the first, or of all requests (prefix)
+struct RowsOf {
+    int r0, count, token0, length, fresh, b;
+    static __device__ __forceinline__ RowsOf of_prefix(const AttendArgs& A, int r0)
+    {
+        const int fresh = A.rows ? (int)min(max((long long)A.rows[A.B], 0ll), A.T) : (int)A.T;
+        return {r0, fresh * A.g, 0, 0, fresh, 0};          // (T * Hq stays below 2^26)
+    }
+    static __device__ __forceinline__ RowsOf of_tile(const AttendArgs& A, int i, int rows_of_a_tile)
+    {
+        RowsOf w;
+        if (A.rows) {
+            w.b = request_of_tile(A, i, rows_of_a_tile);
+            w.token0 = (int)min(max((long long)A.rows[w.b], 0ll), A.T);
+            w.fresh = max((int)min((long long)A.rows[w.b + 1], A.T) - w.token0, 0);
+            w.r0 = (i - (int)tiles_before(A, w.b, rows_of_a_tile)) * rows_of_a_tile;
+        } else {
+            const int per = (A.g + rows_of_a_tile - 1) / rows_of_a_tile;
+            w.b = i / per;
+            w.token0 = w.b;
+            w.fresh = 1;
+            w.r0 = (i - w.b * per) * rows_of_a_tile;
+        }
+        w.count = w.fresh * A.g;
+        w.length = A.max_pages ? (int)min((long long)max(A.lengths[w.b], 0), (long long)A.max_pages << A.page_bits) : 0;
+        return w;
+    }
+};
+
 template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(const AttendArgs& A, char* lds, int id, bool prefix_job)
 {
     typedef Attend<T, DP, KIND> C;
     constexpr int QT = C::QT, WR = C::WR;
     const int tid = (int)threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave), wr = w % WR, wk = w / WR, col = lane & 15, grp = lane >> 4;
     const char** const places = reinterpret_cast<const char**>(lds + C::PLACES);
-    const int head = id % A.Hk;
-    id /= A.Hk;
-
-    // the rows of this workgroup: from r0 on, of `count`; token0: the token of row 0
-    int r0, count, token0, length, fresh, split, b = 0;
-    if (prefix_job) {
-        r0 = id % A.prefix_tiles * C::ROWS;
-        split = id / A.prefix_tiles;
-        token0 = 0;
-        fresh = A.rows ? (int)min(max((long long)A.rows[A.B], 0ll), A.T) : (int)A.T;
-        length = 0;
-    } else {
-        split = id % A.own_splits;
-        const int i = id / A.own_splits;
-        if (A.rows) {
-            b = request_of_tile(A, i, C::ROWS);
-            token0 = (int)min(max((long long)A.rows[b], 0ll), A.T);
-            fresh = max((int)min((long long)A.rows[b + 1], A.T) - token0, 0);
-            r0 = (i - (int)tiles_before(A, b, C::ROWS)) * C::ROWS;
-        } else {
-            const int per = (A.g + C::ROWS - 1) / C::ROWS;
-            b = i / per;
-            token0 = b;
-            fresh = 1;
-            r0 = (i - b * per) * C::ROWS;
-        }
-        length = A.max_pages ? (int)min((long long)max(A.lengths[b], 0), (long long)A.max_pages << A.page_bits) : 0;
+    int split;
+    if (prefix_job) split = id / A.Hk / A.prefix_tiles;
+    else split = A.whole ? 0 : id / A.Hk % A.own_splits;
+    int job = id, parts = A.own_splits;          // whole: tile and head
+    if (A.whole && id >= A.cut) {
+        job = A.cut + (id - A.cut) / A.tail_splits;
+        split = (id - A.cut) % A.tail_splits;
+        parts = A.tail_splits;
     }
-    count = fresh * A.g;                  // (T * Hq stays below 2^31)
+    const bool direct = A.direct && parts == 1;
+    const int head = job % A.Hk;
+    const RowsOf rows = prefix_job ? RowsOf::of_prefix(A, job / A.Hk % A.prefix_tiles * C::ROWS) : RowsOf::of_tile(A, A.whole ? job / A.Hk : job / A.Hk / A.own_splits, C::ROWS);
+    const int r0 = rows.r0, count = rows.count, token0 = rows.token0, length = rows.length, fresh = rows.fresh, b = rows.b;
     if (r0 < 0 || r0 >= count) return;
 
     long long row[QT];                    // of [T][Hq]
@@ -213,24 +227,19 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
     int dirty_from = 0, dirty_to = 0;     // own keys whose infinities and NaN stay out of the products, see below
     for (int own = prefix_job || A.whole ? 0 : 1; own < (prefix_job ? 1 : 2); ++own) {
         const int* const table = own ? A.table + (long long)b * A.max_pages : A.prefix_table;
-        int begin = 0, end, least;        // this workgroup's keys; those below `least` are seen by all of its rows
-        if (!own) {
-            if (A.whole) {
-                end = A.prefix;
-            } else {
-                begin = split * A.prefix_per;
-                end = min(begin + A.prefix_per, A.prefix);
-            }
-            least = end;
-        } else {
-            const int last = min(r0 + C::ROWS, count) - 1;
-            end = min(max(length - fresh + last / A.g + 1, 0), length);
-            least = min(max(length - fresh + r0 / A.g + 1, 0), length);
-            if (A.own_splits > 1) {
-                const int per = ((end + A.own_splits - 1) / A.own_splits + 127) / 128 * 128;
-                begin = min(split * per, end);
-                end = min(begin + per, end);
-            }
+        int begin = 0, end = A.prefix, least;          // this workgroup's keys; those below `least` are seen by all of its rows
+        const int last = min(r0 + C::ROWS, count) - 1, own_end = min(max(length - fresh + last / A.g + 1, 0), length);
+        least = own ? min(max(length - fresh + r0 / A.g + 1, 0), length) : end;
+        if (own) end = own_end;
+        if (prefix_job) {
+            begin = split * A.prefix_per;
+            end = min(begin + A.prefix_per, A.prefix);
+        } else if (parts > 1) {
+            // equal parts of its own keys, or of those behind the prefix's (below 2^31 together)
+            const int before = A.whole ? A.prefix : 0, all = before + own_end, per = (int)(((unsigned)all + parts - 1) / parts + 127) / 128 * 128;
+            const int from = (int)min((long long)split * per, (long long)all) - (own ? before : 0), to = (int)min((long long)split * per + per, (long long)all) - (own ? before : 0);
+            begin = max(from, 0);
+            end = min(to, end);
         }
         if (begin >= end) continue;
 
@@ -499,20 +508,23 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
         }
         return v;
     };
-    // where a row's results go, to the result or to this part's place, and its sums
-    const long long part = prefix_job ? split : A.prefix_splits + split;
-    auto place = [&](long long r) {
-        const int token = (int)((unsigned)r / (unsigned)A.Hq), h = (int)r - token * A.Hq;
-        return A.direct ? A.out + (token * A.ldo + h * A.D) * C::EB : reinterpret_cast<char*>(A.part_o + (part * A.T * A.Hq + r) * A.D);
+    // where a row's results go (r of [T][Hq], `at` of this workgroup), to the result or to this part's place, and its sums
+    auto part_row = [&](long long r, int at) {
+        if (A.whole) return ((long long)(id - A.cut) * C::ROWS + at);
+        return (long long)(prefix_job ? split : A.prefix_splits + split) * A.T * A.Hq + r;
     };
-    auto store_sums = [&](long long r, float mm, float ll) {
-        if (!A.direct) A.part_ml[part * A.T * A.Hq + r] = make_float2(mm, ll);
+    auto place = [&](long long r, int at) {
+        const int token = (int)((unsigned)r / (unsigned)A.Hq), h = (int)r - token * A.Hq;
+        return direct ? A.out + (token * A.ldo + h * A.D) * C::EB : reinterpret_cast<char*>(A.part_o + part_row(r, at) * A.D);
+    };
+    auto store_sums = [&](long long r, int at, float mm, float ll) {
+        if (!direct) A.part_ml[part_row(r, at)] = make_float2(mm, ll);
         else if (A.lse) A.lse[r] = ll == 0.f ? -INFINITY : 0.6931471805599453f * (mm + __builtin_amdgcn_logf(ll));
     };
     // four values from d on
     auto store = [&](char* to, int d, f32x4 o, float ll) {
         if (d >= A.D) return;
-        if (A.direct) {
+        if (direct) {
             const float by = 1.f / ll;
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] = ll == 0.f ? 0.f : o[e] * by;
@@ -535,10 +547,11 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             if (row[t] < 0) continue;
-            char* const to = place(row[t]);
+            const int mine = (wr * QT + t) * 16 + col;
+            char* const to = place(row[t], mine);
 #pragma unroll
             for (int d = 0; d < C::ND; ++d) store(to, d * 16 + grp * 4, O[t][d], l[t]);
-            if (grp == 0) store_sums(row[t], m[t], l[t]);
+            if (grp == 0) store_sums(row[t], mine, m[t], l[t]);
         }
     } else {
         // the wavefronts' parts, in order
@@ -574,8 +587,8 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
             if (at >= count) continue;
             for (int key = dirty_from; key < min(dirty_to, length - fresh + token + 1); ++key) sum += left_out(key, d);
             const long long to = (long long)(token0 + token) * A.Hq + head * A.g + (at - token * A.g);
-            store(place(to), d, sum, ll);
-            if (d == 0) store_sums(to, top, ll);
+            store(place(to, r), d, sum, ll);
+            if (d == 0) store_sums(to, r, top, ll);
         }
     }
 }
@@ -676,6 +689,48 @@ template <typename T, int LANES, int WAVES> __global__ __launch_bounds__(kThread
         else *reinterpret_cast<f32x4*>(to) = o;
     }
     if (lane == 0 && A.lse) A.lse[r] = sum == 0.f ? -INFINITY : 0.6931471805599453f * (top + __builtin_amdgcn_logf(sum));
+}
+
+// Joins the parts of the tiles that workgroups share by keys: 32 rows of one, eight lanes to a row.
+constexpr int kTailRows = 32, kMaxTail = 8;
+template <typename T> __global__ __launch_bounds__(kThreads) void attend_join_tail(const AttendArgs A, int rows_of_a_tile)
+{
+    const int per = rows_of_a_tile / kTailRows, tile = (int)blockIdx.x / per, job = A.cut + tile, head = job % A.Hk;
+    const RowsOf w = RowsOf::of_tile(A, job / A.Hk, rows_of_a_tile);
+    const int at = (int)blockIdx.x % per * kTailRows + (int)threadIdx.x / 8, r = w.r0 + at;
+    if (w.r0 < 0 || r >= w.count) return;
+    const long long first = (long long)tile * A.tail_splits * rows_of_a_tile + at;
+    float2 ml[kMaxTail];
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int p = 0; p < kMaxTail; ++p) {
+        ml[p] = make_float2(-INFINITY, 0.f);
+        if (p < A.tail_splits) ml[p] = A.part_ml[first + p * rows_of_a_tile];
+        if (ml[p].y != 0.f) top = fmaxf(top, ml[p].x);
+    }
+#pragma unroll
+    for (int p = 0; p < kMaxTail; ++p) {
+        ml[p].x = ml[p].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[p].x - top);
+        if (ml[p].y != 0.f) sum += ml[p].x * ml[p].y;
+    }
+    const int token = w.token0 + r / A.g, h = head * A.g + r % A.g;
+    const float by = 1.f / sum;
+    for (int d = (int)threadIdx.x % 8 * 4; d < A.D; d += 32) {
+        f32x4 o = {0.f, 0.f, 0.f, 0.f}, v[kMaxTail];
+#pragma unroll
+        for (int p = 0; p < kMaxTail; ++p) {
+            v[p] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (ml[p].y != 0.f) v[p] = *reinterpret_cast<const f32x4*>(A.part_o + (first + p * rows_of_a_tile) * A.D + d);
+        }
+#pragma unroll
+        for (int p = 0; p < kMaxTail; ++p) o += ml[p].x * v[p];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = sum == 0.f ? 0.f : o[e] * by;
+        T* const to = reinterpret_cast<T*>(A.out) + token * A.ldo + h * A.D + d;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(f32x2_to_bf16x2(o[0], o[1]), f32x2_to_bf16x2(o[2], o[3]));
+        else *reinterpret_cast<f32x4*>(to) = o;
+    }
+    if (threadIdx.x % 8 == 0 && A.lse) A.lse[(long long)token * A.Hq + h] = sum == 0.f ? -INFINITY : 0.6931471805599453f * (top + __builtin_amdgcn_logf(sum));
 }
 
 template <typename T> cgbn_status launch_attend(const AttendArgs& A, int prefix_kind, int own_kind, hipStream_t st);

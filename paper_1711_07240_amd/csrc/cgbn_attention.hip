@@ -11,15 +11,15 @@ constexpr int kMaxHeads = 1 << 10, kMaxRequests = 1 << 20, kMaxPage = 1024, kMax
 constexpr long long kMaxKeys = 1ll << 30, kMaxRows = 1ll << 26;          // rows: heads of tokens
 
 struct Plan {
-    int prefix_kind, own_kind, prefix_splits, prefix_per, own_splits, prefix_tiles, own_tiles, whole;
-    long long prefix_jobs, jobs;
+    int prefix_kind, own_kind, prefix_splits, prefix_per, own_splits, prefix_tiles, own_tiles, whole, tail_splits;
+    long long prefix_jobs, jobs, cut;
     int parts() const { return prefix_splits + own_splits; }
 };
 
 bool sizes_fit(long long T, int B, int Hq, int Hk, int D, long long prefix, long long capacity)
 {
     if (T < 0 || B < 0 || B > kMaxRequests || Hk < 1 || Hq < Hk || Hq > kMaxHeads || Hq % Hk != 0 || D < 8 || D > 256 || D % 8 != 0) return false;
-    return T <= (kMaxRows - 4) / Hq && prefix >= 0 && prefix < kMaxKeys && capacity >= 0 && capacity < kMaxKeys;
+    return T <= (kMaxRows - 4) / Hq && (long long)B * Hk <= (1 << 22) && prefix >= 0 && prefix < kMaxKeys && capacity >= 0 && capacity < kMaxKeys;
 }
 
 long long up(long long a, long long b) { return (a + b - 1) / b; }
@@ -48,11 +48,26 @@ Plan plan(long long T, int B, int Hq, int Hk, int line, int elem, long long pref
     p.prefix_tiles = (int)up(rows, rows_of(p.prefix_kind, line, elem));
     const long long own_tiles = several ? rows / own_rows + B : B * up(g, own_rows);
     p.own_tiles = (int)own_tiles;
-    if (p.own_kind == MANY && own_tiles * Hk >= 256) {
-        p.whole = 1;
-        p.own_splits = 1;
+    // A workgroup to a tile of one request's rows and a head, prefix and own keys: where there are many, and where there are so few keys that one launch is the
+    // shorter way (3 requests, 100 keys of the prefix and up to 80 of their own: 7 us, in parts 9).
+    const long long whole = own_tiles * Hk, slots = 512;
+    const bool many = p.own_kind == MANY && whole >= 256;
+    if (many || prefix + capacity <= 512) {
+        p.whole = p.own_splits = 1;
+        p.prefix_kind = p.own_kind;
         p.prefix_tiles = 0;
-        p.jobs = own_tiles * Hk;
+        p.jobs = p.cut = whole;
+        // Two workgroups share each compute unit.  What is left behind the last full round of those is shared by more of them, in parts of 512 keys or more.
+        const long long left = whole % slots;
+        long long s = left ? 2 * slots / left : 1;
+        if (s > (prefix + capacity) / 512) s = (prefix + capacity) / 512;
+        if (s > kMaxTail) s = kMaxTail;
+        p.tail_splits = 1;
+        if (many && s > 1 && left * 4 <= slots * 3) {
+            p.tail_splits = (int)s;
+            p.cut = whole - left;
+            p.jobs = p.cut + left * s;
+        }
         return p;
     }
     p.own_splits = prefix ? 0 : 1;         // (without any keys rows are zero)
@@ -64,9 +79,9 @@ Plan plan(long long T, int B, int Hq, int Hk, int line, int elem, long long pref
         p.own_splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
     }
     // Parts of the prefix: a workgroup for each compute unit, which leaves room for one that reads beside it (64 rows, 32768 bfloat16 keys of 8 heads, 128, 256, 512 and
-    // 1024 workgroups: 112, 98, 105 and 130 us)
+    // 1024 workgroups: 112, 98, 105 and 130 us); with few rows reading is all there is to do, as above
     if (prefix) {
-        long long s = 256 / ((long long)p.prefix_tiles * Hk);
+        long long s = (rows > 32 ? 256 : 1024) / ((long long)p.prefix_tiles * Hk);
         if (s > up(prefix, 256)) s = up(prefix, 256);
         s = s < 1 ? 1 : s > 64 ? 64 : s;
         p.prefix_per = (int)up(up(prefix, s), 128) * 128;
@@ -78,7 +93,11 @@ Plan plan(long long T, int B, int Hq, int Hk, int line, int elem, long long pref
 }
 
 // bytes of the parts
-size_t scratch(const Plan& p, long long T, int Hq, int D) { return p.parts() <= 1 ? 0 : (size_t)p.parts() * T * Hq * (D + 2) * sizeof(float); }
+size_t scratch(const Plan& p, long long T, int Hq, int D, int line, int elem)
+{
+    const long long rows = p.whole ? (p.jobs - p.cut) * rows_of(p.own_kind, line, elem) : p.parts() <= 1 ? 0 : p.parts() * T * Hq;
+    return (size_t)rows * (D + 2) * sizeof(float);
+}
 
 }  // namespace
 }  // namespace cgbn
@@ -93,9 +112,9 @@ size_t cgbn_prefix_attention_workspace_bytes(long long T, int B, int Hq, int Hk,
     if (T == 0 || B == 0) return 256;
     const int elem = dtype == CGBN_F32 ? 4 : 2, line = line_of(width_of(D), elem);
     // requests of one row each go in other tiles when it is said that they are
-    size_t most = scratch(plan(T, B, Hq, Hk, line, elem, prefix, capacity, true), T, Hq, D);
+    size_t most = scratch(plan(T, B, Hq, Hk, line, elem, prefix, capacity, true), T, Hq, D, line, elem);
     if (T == B) {
-        const size_t single = scratch(plan(T, B, Hq, Hk, line, elem, prefix, capacity, false), T, Hq, D);
+        const size_t single = scratch(plan(T, B, Hq, Hk, line, elem, prefix, capacity, false), T, Hq, D, line, elem);
         if (single > most) most = single;
     }
     const size_t bytes = (most + 255) / 256 * 256;
@@ -129,16 +148,16 @@ cgbn_status cgbn_prefix_attention(const void* q, long long ldq, long long T, int
     if (p.jobs >= (1ll << 24)) return CGBN_ERR_SHAPE;           // 2^32 threads
     AttendArgs A;
     std::memset(&A, 0, sizeof(A));
-    const size_t need = scratch(p, T, Hq, D);
+    const size_t need = scratch(p, T, Hq, D, line, elem);
     if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need)) return CGBN_ERR_WORKSPACE;
     A.part_o = static_cast<float*>(workspace);
-    A.part_ml = reinterpret_cast<float2*>(A.part_o + (size_t)p.parts() * T * Hq * D);
+    A.part_ml = reinterpret_cast<float2*>(A.part_o + need / sizeof(float) / (D + 2) * D);
     A.q = static_cast<const char*>(q); A.k_pages = static_cast<const char*>(k_pages); A.v_pages = static_cast<const char*>(v_pages);
     A.out = static_cast<char*>(out); A.lse = lse; A.rows = rows; A.lengths = lengths; A.prefix_table = prefix_table; A.table = table;
     A.ldq = ldq; A.ldo = ldo; A.T = T; A.B = B; A.Hq = Hq; A.Hk = Hk; A.g = Hq / Hk; A.D = D; A.pages = pages; A.prefix = prefix; A.max_pages = max_pages;
     while ((1 << A.page_bits) < page) ++A.page_bits;
     A.prefix_splits = p.prefix_splits; A.prefix_per = p.prefix_per; A.own_splits = p.own_splits; A.prefix_tiles = p.prefix_tiles; A.own_tiles = p.own_tiles;
-    A.prefix_jobs = (int)p.prefix_jobs; A.jobs = (int)p.jobs; A.whole = p.whole; A.direct = p.parts() <= 1; A.scale = scale * 1.4426950408889634f;
+    A.prefix_jobs = (int)p.prefix_jobs; A.jobs = (int)p.jobs; A.whole = p.whole; A.cut = (int)p.cut; A.tail_splits = p.tail_splits; A.direct = p.parts() <= 1; A.scale = scale * 1.4426950408889634f;
     hipStream_t st = static_cast<hipStream_t>(stream);
     return dtype == CGBN_F32 ? launch_attend<float>(A, p.prefix_kind, p.own_kind, st) : launch_attend<bf16_t>(A, p.prefix_kind, p.own_kind, st);
 }

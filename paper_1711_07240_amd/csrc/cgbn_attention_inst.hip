@@ -38,6 +38,12 @@ template <> cgbn_status launch_attend<CGBN_INST_T>(const AttendArgs& A, int pref
     default: launch_width<T, 256>(A, prefix, own, st);
     }
     if (hipGetLastError() != hipSuccess) return CGBN_ERR_HIP;
+    if (A.whole && A.tail_splits > 1) {
+        const int rows = rows_of(own, line_of(width_of(A.D), sizeof(T)), sizeof(T));
+        const int tiles = (A.jobs - A.cut) / A.tail_splits;
+        hipLaunchKernelGGL(attend_join_tail<T>, dim3((unsigned)(tiles * (rows / kTailRows))), dim3(kThreads), 0, st, A, rows);
+        if (hipGetLastError() != hipSuccess) return CGBN_ERR_HIP;
+    }
     if (!A.direct) {
         if (A.D <= 32) launch_join<T, 8>(A, st);
         else if (A.D <= 64) launch_join<T, 16>(A, st);
