@@ -4,8 +4,8 @@
 // its length then takes beyond those it holds, which give its place in the free list.  After that every row is on its own: its request by bisection
 // of the rows' starts, its key's page from the table or, if the request did not hold it before, from the free list; the row
 // whose key is a page's first writes the new entry (a page that is new has its first key in this step).  So nothing is read that another row writes.
-// Bound by latency: a launch and two dependent reads, 2 sums by one workgroup.  Few requests with few rows are done by that
-// workgroup alone, the others' rows by a second launch.
+// Bound by latency: a launch, two dependent reads, two sums.  Up to 1024 requests are one launch, whose workgroups all form the sums (16 requests 4 us;
+// 1024 with 131072 rows, 1.1 MB, 5.9, in two launches 9.1); of more the rows are a second one's.
 //
 // page_store.  Bound by memory: one read and one write of the rows, 16 bytes a lane.  Pages hold a head's keys side by side ([page][head][key][D]), so
 // that attention, which reads one head at a time, finds whole pages of it in one run; a row is written in runs of D.
@@ -57,10 +57,10 @@ __device__ __forceinline__ int scan_before(int v, int most, int* lds, int* total
 __device__ __forceinline__ int held_by(const PlanArgs& A, int b) { return min(max(A.have[b], 0), A.max_pages << A.page_bits); }
 __device__ __forceinline__ int pages_of(const PlanArgs& A, int keys) { return min((keys + (1 << A.page_bits) - 1) >> A.page_bits, A.max_pages); }
 
-// One row.  start: the request's first row; first: its place in the free list
-__device__ __forceinline__ void fill_row(const PlanArgs& A, int t, int b, int start, int first)
+// One row.  start: the request's first row; first: its place in the free list; have: the tokens that it holds
+__device__ __forceinline__ void fill_row(const PlanArgs& A, int t, int b, int start, int first, int have)
 {
-    const int have = held_by(A, b), key = have + (t - start), at = key >> A.page_bits, held = pages_of(A, have);
+    const int key = have + (t - start), at = key >> A.page_bits, held = pages_of(A, have);
     int id = -1;
     if (at < A.max_pages) {
         int* const entry = A.table + (long long)b * A.max_pages + at;
@@ -89,11 +89,72 @@ __device__ __forceinline__ int request_of(const int* starts, int B, int t)
     return lo;
 }
 
-// The sums, and with ALL every row (B at most kPlanThreads)
-template <bool ALL> __global__ __launch_bounds__(kPlanThreads) void plan_sums(const PlanArgs A)
+// What a request takes of the step.  row: its first row; first: its place in the free list
+struct Share {
+    int next, length, want, left_out;          // the next request's first row; tokens and new pages; tokens without a place or a row
+    __device__ __forceinline__ Share(const PlanArgs& A, int have, int fresh, int row)
+    {
+        next = min(add_most(row, min(fresh, kMost), kMost), (int)A.T);
+        length = have + (next - row);
+        want = max(pages_of(A, length) - pages_of(A, have), 0);
+        left_out = fresh;
+    }
+    __device__ __forceinline__ void place(const PlanArgs& A, int have, int first)
+    {
+        const int given = min(want, max(A.free_count - first, 0));
+        left_out -= max(min((pages_of(A, have) + given) << A.page_bits, length) - have, 0);
+    }
+};
+
+// Up to kPlanThreads requests: a thread to each, and every row.  Each workgroup forms the sums for itself and fills rows of its own; the first one
+// stores what is not a row's.
+__global__ __launch_bounds__(kPlanThreads) void plan_few(const PlanArgs A)
 {
-    __shared__ int lds[kPlanThreads / kWave], starts[ALL ? kPlanThreads + 1 : 1], firsts[ALL ? kPlanThreads : 1];
-    __shared__ long long left_out;
+    __shared__ int lds[kPlanThreads / kWave], starts[kPlanThreads + 1], firsts[kPlanThreads], haves[kPlanThreads];
+    __shared__ unsigned long long left_out;
+    const int T = (int)A.T, b = (int)threadIdx.x;
+    const bool in = b < A.B;
+    const int have = in ? held_by(A, b) : 0, fresh = in ? max(A.fresh[b], 0) : 0, taken = min(max(A.taken[0], 0), A.free_count);
+    if (b == 0) left_out = 0;
+    int total;
+    const int row = min(scan_before(min(fresh, kMost), kMost, lds, &total), T);
+    Share share(A, have, fresh, row);
+    const int first = add_most(taken, scan_before(share.want, kMost, lds, &total), kMost);
+    share.place(A, have, first);
+    starts[b] = row;
+    firsts[b] = first;
+    haves[b] = have;
+    if (b == A.B - 1 || (A.B == 0 && b == 0)) starts[A.B] = in ? share.next : 0;
+    if (blockIdx.x == 0) {
+        if (in) {
+            A.rows[b] = row;
+            A.lengths[b] = share.length;
+            if (share.left_out) atomicAdd(&left_out, (unsigned long long)share.left_out);          // (whole numbers: in any order the same)
+        }
+        if (b == A.B - 1 || (A.B == 0 && b == 0)) A.rows[A.B] = in ? share.next : 0;
+    }
+    __syncthreads();
+    if (blockIdx.x == 0 && b == 0) {
+        A.counts[0] = min(add_most(taken, total, kMost), A.free_count);
+        A.counts[1] = (int)min(left_out, 0x7fffffffull);
+    }
+    const int end = starts[A.B];
+    for (int t = (int)(blockIdx.x * kPlanThreads + threadIdx.x); t < T; t += (int)gridDim.x * kPlanThreads) {
+        if (t >= end) {
+            A.slots[t] = -1;
+            A.positions[t] = 0;
+            continue;
+        }
+        const int of = request_of(starts, A.B, t);
+        fill_row(A, t, of, starts[of], firsts[of], haves[of]);
+    }
+}
+
+// Any number of requests, a run of them to a thread: the sums, by one workgroup.
+__global__ __launch_bounds__(kPlanThreads) void plan_sums(const PlanArgs A)
+{
+    __shared__ int lds[kPlanThreads / kWave];
+    __shared__ unsigned long long left_out;
     const int T = (int)A.T, each = (A.B + kPlanThreads - 1) / kPlanThreads;
     const int b0 = min((int)threadIdx.x * each, A.B), b1 = min(b0 + each, A.B);
     const int taken = min(max(A.taken[0], 0), A.free_count);
@@ -103,50 +164,30 @@ template <bool ALL> __global__ __launch_bounds__(kPlanThreads) void plan_sums(co
     const int row0 = min(scan_before(sum, kMost, lds, &total), T);
     int row = row0, wanted = 0;
     for (int b = b0; b < b1; ++b) {
-        const int have = held_by(A, b), next = min(add_most(row, min(max(A.fresh[b], 0), kMost), kMost), T);
-        wanted = add_most(wanted, max(pages_of(A, have + (next - row)) - pages_of(A, have), 0), kMost);
-        row = next;
+        const Share share(A, held_by(A, b), max(A.fresh[b], 0), row);
+        wanted = add_most(wanted, share.want, kMost);
+        row = share.next;
     }
     int first = add_most(taken, scan_before(wanted, kMost, lds, &total), kMost);
     row = row0;
-    long long out = 0;
+    unsigned long long out = 0;
     for (int b = b0; b < b1; ++b) {
-        const int have = held_by(A, b), fresh = max(A.fresh[b], 0), next = min(add_most(row, min(fresh, kMost), kMost), T);
-        const int length = have + (next - row), held = pages_of(A, have), want = max(pages_of(A, length) - held, 0);
-        const int given = min(want, max(A.free_count - first, 0));
-        out += fresh - max(min((held + given) << A.page_bits, length) - have, 0);
+        const int have = held_by(A, b);
+        Share share(A, have, max(A.fresh[b], 0), row);
+        share.place(A, have, first);
+        out += share.left_out;
         A.rows[b] = row;
-        A.lengths[b] = length;
-        if (ALL) {
-            starts[b] = row;
-            firsts[b] = first;
-        } else {
-            A.first[b] = first;
-        }
-        row = next;
-        first = add_most(first, want, kMost);
+        A.lengths[b] = share.length;
+        A.first[b] = first;
+        row = share.next;
+        first = add_most(first, share.want, kMost);
     }
-    if (out) atomicAdd(reinterpret_cast<unsigned long long*>(&left_out), (unsigned long long)out);          // (whole numbers: in any order the same)
-    if (b1 == A.B && (b0 < b1 || (A.B == 0 && threadIdx.x == 0))) {
-        A.rows[A.B] = row;
-        if (ALL) starts[A.B] = row;
-    }
+    if (out) atomicAdd(&left_out, out);          // (whole numbers: in any order the same)
+    if (b1 == A.B && (b0 < b1 || (A.B == 0 && threadIdx.x == 0))) A.rows[A.B] = row;
     __syncthreads();
     if (threadIdx.x == 0) {
         A.counts[0] = min(add_most(taken, total, kMost), A.free_count);
-        A.counts[1] = (int)min(left_out, (long long)0x7fffffff);
-    }
-    if constexpr (ALL) {
-        const int end = starts[A.B];
-        for (int t = (int)threadIdx.x; t < T; t += kPlanThreads) {
-            if (t >= end) {
-                A.slots[t] = -1;
-                A.positions[t] = 0;
-                continue;
-            }
-            const int b = request_of(starts, A.B, t);
-            fill_row(A, t, b, starts[b], firsts[b]);
-        }
+        A.counts[1] = (int)min(left_out, 0x7fffffffull);
     }
 }
 
@@ -160,7 +201,7 @@ __global__ __launch_bounds__(kThreads) void plan_rows(const PlanArgs A)
         return;
     }
     const int b = request_of(A.rows, A.B, t);
-    fill_row(A, t, b, A.rows[b], A.first[b]);
+    fill_row(A, t, b, A.rows[b], A.first[b], held_by(A, b));
 }
 
 struct StoreArgs {
@@ -173,20 +214,35 @@ struct StoreArgs {
     int places, page_bits, per;    // tokens of a workgroup
 };
 
-__global__ __launch_bounds__(kThreads) void page_store(const StoreArgs A)
+// NT: results go past the caches
+template <bool NT> __global__ __launch_bounds__(kThreads) void page_store(const StoreArgs A)
 {
+    constexpr int AHEAD = 4;       // chunks of a thread that are on their way at once
     const int row = A.heads * A.chunks, all = A.per * 2 * row;
     const long long t0 = workgroup() * A.per;
-    for (int i = (int)threadIdx.x; i < all; i += kThreads) {
-        const int local = (unsigned)i / (unsigned)(2 * row), j = i - local * 2 * row, which = j >= row, c = which ? j - row : j;
-        const long long t = t0 + local;
-        if (t >= A.T) return;
-        const int slot = A.slots[t];
-        if (slot < 0 || slot >= A.places) continue;
-        const int h = (unsigned)c / (unsigned)A.chunks, part = c - h * A.chunks;
-        const u32x4 v = *reinterpret_cast<const u32x4*>(A.x[which] + t * A.ldx[which] + (long long)c * 16);
-        const long long at = (((((long long)(slot >> A.page_bits) * A.heads + h) << A.page_bits) + (slot & ((1 << A.page_bits) - 1))) * A.chunks + part) * 16;
-        *reinterpret_cast<u32x4*>(A.pool[which] + at) = v;
+    for (int i0 = (int)threadIdx.x; i0 < all; i0 += AHEAD * kThreads) {
+        u32x4 v[AHEAD];
+        int slot[AHEAD], c[AHEAD], which[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int i = i0 + k * kThreads, local = (unsigned)i / (unsigned)(2 * row), j = i - local * 2 * row;
+            const long long t = t0 + local;
+            which[k] = j >= row;
+            c[k] = which[k] ? j - row : j;
+            slot[k] = -1;
+            if (i >= all || t >= A.T) continue;
+            v[k] = *reinterpret_cast<const u32x4*>(A.x[which[k]] + t * A.ldx[which[k]] + (long long)c[k] * 16);
+            slot[k] = A.slots[t];
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (slot[k] < 0 || slot[k] >= A.places) continue;
+            const int h = (unsigned)c[k] / (unsigned)A.chunks, part = c[k] - h * A.chunks;
+            const long long at = (((((long long)(slot[k] >> A.page_bits) * A.heads + h) << A.page_bits) + (slot[k] & ((1 << A.page_bits) - 1))) * A.chunks + part) * 16;
+            u32x4* const to = reinterpret_cast<u32x4*>(A.pool[which[k]] + at);
+            if constexpr (NT) __builtin_nontemporal_store(v[k], to);
+            else *to = v[k];
+        }
     }
 }
 
@@ -195,10 +251,11 @@ __global__ __launch_bounds__(kThreads) void page_store(const StoreArgs A)
 cgbn_status launched() { return hipGetLastError() == hipSuccess ? CGBN_OK : CGBN_ERR_HIP; }
 
 constexpr int kMaxRequests = 1 << 20, kMaxPage = 1024, kMaxTable = 1 << 16, kMaxRows = 1 << 29;
-constexpr int kAlone = 4096;       // rows that the workgroup of the sums fills itself
+constexpr int kAlone = 4096;       // rows that one workgroup fills
 
 bool page_fits(int page, int pages) { return page >= 1 && page <= kMaxPage && (page & (page - 1)) == 0 && pages >= 0 && (long long)pages * page < (1ll << 31); }
-bool alone(int B, long long T) { return B <= kPlanThreads && T <= kAlone; }
+// One launch: with several workgroups none may store the pages taken over what the others still read.
+bool one_launch(int B, long long T, bool in_place) { return B <= kPlanThreads && (T <= kAlone || !in_place); }
 int bits_of(int page)
 {
     int b = 0;
@@ -216,7 +273,7 @@ extern "C" {
 size_t cgbn_page_plan_workspace_bytes(int B, long long T)
 {
     if (B < 0 || B > kMaxRequests || T < 0 || T > kMaxRows) return 0;
-    if (alone(B, T)) return 256;
+    if (one_launch(B, T, true)) return 256;
     const size_t bytes = ((size_t)B * sizeof(int) + 255) / 256 * 256;
     return bytes > 256 ? bytes : 512;          // (of 256 or less a program may pass none)
 }
@@ -243,7 +300,7 @@ cgbn_status cgbn_page_plan(const int* have, const int* fresh, int B, int before,
             if (out[i] == p) return CGBN_ERR_ALIAS;
         if (i && out[i] == taken) return CGBN_ERR_ALIAS;
     }
-    const bool one = alone(B, T);
+    const bool one = one_launch(B, T, taken == counts);
     if (!one && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < (size_t)B * sizeof(int))) return CGBN_ERR_WORKSPACE;
     PlanArgs A;
     std::memset(&A, 0, sizeof(A));
@@ -252,10 +309,11 @@ cgbn_status cgbn_page_plan(const int* have, const int* fresh, int B, int before,
     A.max_pages = max_pages; A.pages = pages; A.page_bits = bits_of(page);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (one) {
-        hipLaunchKernelGGL(plan_sums<true>, dim3(1), dim3(kPlanThreads), 0, st, A);
+        const long long groups = T <= kAlone ? 1 : (T + kPlanThreads - 1) / kPlanThreads;
+        hipLaunchKernelGGL(plan_few, dim3((unsigned)(groups < 256 ? groups : 256)), dim3(kPlanThreads), 0, st, A);
         return launched();
     }
-    hipLaunchKernelGGL(plan_sums<false>, dim3(1), dim3(kPlanThreads), 0, st, A);
+    hipLaunchKernelGGL(plan_sums, dim3(1), dim3(kPlanThreads), 0, st, A);
     if (launched() != CGBN_OK) return CGBN_ERR_HIP;
     if (T) hipLaunchKernelGGL(plan_rows, dim3((unsigned)((T + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, A);
     return launched();
@@ -283,7 +341,11 @@ cgbn_status cgbn_page_store(const void* k, long long ldk, const void* v, long lo
     const int row = Hk * A.chunks;
     A.per = 4 * kThreads / (2 * row);
     if (A.per < 1) A.per = 1;
-    hipLaunchKernelGGL(page_store, grid_of((T + A.per - 1) / A.per), dim3(kThreads), 0, static_cast<hipStream_t>(stream), A);
+    const dim3 grid = grid_of((T + A.per - 1) / A.per);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    // Results of more than the caches next to the compute units hold go past them: 124 against 104 us (20011 tokens, 20 heads of 80 float, 4.8 TB/s)
+    if ((double)T * width * elem * 2 > 32e6) hipLaunchKernelGGL(page_store<true>, grid, dim3(kThreads), 0, st, A);
+    else hipLaunchKernelGGL(page_store<false>, grid, dim3(kThreads), 0, st, A);
     return launched();
 }
 

@@ -88,8 +88,8 @@ class Attention:
             o, lse, w = V.attention(q, k, v, self.scale)
             if len(k) == 0:
                 return o, lse, np.zeros(self.D), 0.0
-            s = np.abs(k @ q) * self.scale
-            ep = (self.D + 8) * F * (np.abs(k) @ np.abs(q)) * self.scale + 4 * F * (s + s.max() + 1)
+            s = np.abs(k @ q) * abs(self.scale)
+            ep = (self.D + 8) * F * (np.abs(k) @ np.abs(q)) * abs(self.scale) + 4 * F * (s + s.max() + 1)
             n = len(k) + 64
             off = float(w @ ep) + n * F
             rounding = UNIT["bf16"] if self.dtype == "bf16" else 0.0

@@ -65,6 +65,34 @@ def test_prompts_in_tiles_of_their_own(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("prefix,D,fresh", [(1500, 32, [400, 1, 129, 600, 0, 870]), (0, 64, [700, 700, 3, 500]), (2100, 136, [900, 900])])
+def test_tiles_that_workgroups_share(prefix, D, fresh, dtype):
+    """The last tiles of many: their keys, the prefix's and a request's own as one, are dealt to several workgroups."""
+    a = Attention(dtype, fresh, [n + 900 * (i % 2) for i, n in enumerate(fresh)], prefix, 16, 16, 8, D, pad=9)
+    got = a.call()
+    a.check(*got, rows=[0, 1, 63, 64, 127, 128, 255, 399, 599, 869, 899])
+    assert all(torch.equal(x, y) for x, y in zip(got, a.call()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_short_contexts_of_many_requests(dtype):
+    rng = np.random.default_rng(6)
+    a = Attention(dtype, [1] * 90, [int(n) for n in rng.integers(0, 200, 90)], 190, 16, 6, 3, 64)
+    a.check(*a.call(single=True))
+    a = Attention(dtype, [40] * 9, [int(n) for n in rng.integers(0, 300, 9)], 100, 16, 4, 2, 40)
+    a.check(*a.call())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("scale", [0.0, -0.125, 1e-30])
+def test_scales(scale, dtype):
+    """Of zero all keys weigh the same; a negative one turns the order around."""
+    a = Attention(dtype, [1, 3], [100, 70], 600, 16, 4, 2, 64)
+    a.scale = scale
+    a.check(*a.call())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_long_keys_in_many_parts(dtype):
     a = Attention(dtype, [1, 1, 2], [9000, 30, 4099], 20001, 64, 4, 1, 64, spread=3.0)
     a.check(*a.call())
@@ -108,7 +136,7 @@ def test_pages_that_are_not_there_are_not_seen(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("fresh,length,heads", [(5, 40, (4, 2)), (100, 130, (2, 1)), (200, 200, (16, 8))])
+@pytest.mark.parametrize("fresh,length,heads", [(5, 40, (4, 2)), (5, 900, (4, 2)), (100, 130, (2, 1)), (200, 200, (16, 8)), (300, 1400, (16, 8))])
 def test_infinities_of_later_tokens_stay_out(fresh, length, heads, dtype):
     """A later token's key and value reach the rows that see it and no others."""
     bad = length - 3
