@@ -160,28 +160,102 @@ struct RowsOf {
     }
 };
 
+// What a workgroup has to do: its rows, its keys, and where its results go.  ROWS: of a tile
+template <typename T, int ROWS> struct Job {
+    const AttendArgs& A;
+    int id, split, parts, head;        // parts: of its keys, if those are a request's
+    bool prefix, direct;
+    RowsOf rows;
+
+    __device__ __forceinline__ Job(const AttendArgs& args, int id_, bool prefix_job) : A(args), id(id_), parts(args.own_splits), prefix(prefix_job)
+    {
+        int tile_and_head = id;
+        split = prefix ? id / A.Hk / A.prefix_tiles : A.whole ? 0 : id / A.Hk % A.own_splits;
+        if (A.whole && id >= A.cut) {
+            tile_and_head = A.cut + (id - A.cut) / A.tail_splits;
+            split = (id - A.cut) % A.tail_splits;
+            parts = A.tail_splits;
+        }
+        direct = A.direct && parts == 1;
+        head = tile_and_head % A.Hk;
+        const int tile = tile_and_head / A.Hk;
+        rows = prefix ? RowsOf::of_prefix(A, tile % A.prefix_tiles * ROWS) : RowsOf::of_tile(A, A.whole ? tile : tile / A.own_splits, ROWS);
+    }
+    __device__ __forceinline__ bool none() const { return rows.r0 < 0 || rows.r0 >= rows.count; }
+    // of [T][Hq]; own keys that it sees
+    __device__ __forceinline__ long long row(int at) const
+    {
+        const int r = rows.r0 + at, token = r / A.g;
+        return r < rows.count ? (long long)(rows.token0 + token) * A.Hq + head * A.g + (r - token * A.g) : -1;
+    }
+    __device__ __forceinline__ int sees(int at) const
+    {
+        const int r = rows.r0 + at;
+        return r < rows.count ? min(max(rows.length - rows.fresh + r / A.g + 1, 0), rows.length) : 0;
+    }
+    // Its keys, the prefix's or the request's own; those below `least` are seen by all of its rows
+    __device__ __forceinline__ void keys(int own, int* begin, int* end, int* least) const
+    {
+        const int own_end = sees(min(ROWS, rows.count - rows.r0) - 1);
+        *begin = 0;
+        *end = own ? own_end : A.prefix;
+        if (prefix) {
+            *begin = split * A.prefix_per;
+            *end = min(*begin + A.prefix_per, A.prefix);
+        } else if (parts > 1) {
+            // equal parts of its own keys, or of those behind the prefix's (below 2^31 together)
+            const int before = A.whole ? A.prefix : 0, all = before + own_end, per = (int)(((unsigned)all + parts - 1) / parts + 127) / 128 * 128;
+            const int from = (int)min((long long)split * per, (long long)all) - (own ? before : 0), to = (int)min((long long)split * per + per, (long long)all) - (own ? before : 0);
+            *begin = max(from, 0);
+            *end = min(to, *end);
+        }
+        *least = own ? sees(0) : *end;
+    }
+    __device__ __forceinline__ const int* table(int own) const { return own ? A.table + (long long)rows.b * A.max_pages : A.prefix_table; }
+
+    // Where row r of [T][Hq], `at` of this workgroup, goes: to the result or to this part's place; its sums
+    __device__ __forceinline__ long long part_row(long long r, int at) const
+    {
+        if (A.whole) return (long long)(id - A.cut) * ROWS + at;
+        return (long long)(prefix ? split : A.prefix_splits + split) * A.T * A.Hq + r;
+    }
+    __device__ __forceinline__ char* place(long long r, int at) const
+    {
+        const int token = (int)((unsigned)r / (unsigned)A.Hq), h = (int)r - token * A.Hq;
+        return direct ? A.out + (token * A.ldo + h * A.D) * (long long)sizeof(T) : reinterpret_cast<char*>(A.part_o + part_row(r, at) * A.D);
+    }
+    __device__ __forceinline__ void store_sums(long long r, int at, float m, float l) const
+    {
+        if (!direct) A.part_ml[part_row(r, at)] = make_float2(m, l);
+        else if (A.lse) A.lse[r] = l == 0.f ? -INFINITY : 0.6931471805599453f * (m + __builtin_amdgcn_logf(l));
+    }
+    // four values from d on
+    __device__ __forceinline__ void store(char* to, int d, f32x4 o, float l) const
+    {
+        if (d >= A.D) return;
+        if (direct) {
+            const float by = 1.f / l;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = l == 0.f ? 0.f : o[e] * by;
+            if constexpr (sizeof(T) == 2) {
+                *reinterpret_cast<uint2*>(to + d * 2) = make_uint2(f32x2_to_bf16x2(o[0], o[1]), f32x2_to_bf16x2(o[2], o[3]));
+                return;
+            }
+        }
+        *reinterpret_cast<f32x4*>(to + d * 4) = o;
+    }
+};
+
 template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(const AttendArgs& A, char* lds, int id, bool prefix_job)
 {
     typedef Attend<T, DP, KIND> C;
     constexpr int QT = C::QT, WR = C::WR;
     const int tid = (int)threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave), wr = w % WR, wk = w / WR, col = lane & 15, grp = lane >> 4;
     const char** const places = reinterpret_cast<const char**>(lds + C::PLACES);
-    int split;
-    if (prefix_job) split = id / A.Hk / A.prefix_tiles;
-    else split = A.whole ? 0 : id / A.Hk % A.own_splits;
-    int job = id, parts = A.own_splits;          // whole: tile and head
-    if (A.whole && id >= A.cut) {
-        job = A.cut + (id - A.cut) / A.tail_splits;
-        split = (id - A.cut) % A.tail_splits;
-        parts = A.tail_splits;
-    }
-    const bool direct = A.direct && parts == 1;
-    const int head = job % A.Hk;
-    const RowsOf rows = prefix_job ? RowsOf::of_prefix(A, job / A.Hk % A.prefix_tiles * C::ROWS) : RowsOf::of_tile(A, A.whole ? job / A.Hk : job / A.Hk / A.own_splits, C::ROWS);
-    const int r0 = rows.r0, count = rows.count, token0 = rows.token0, length = rows.length, fresh = rows.fresh, b = rows.b;
-    if (r0 < 0 || r0 >= count) return;
+    const Job<T, C::ROWS> job(A, id, prefix_job);
+    if (job.none()) return;
+    const int count = job.rows.count, r0 = job.rows.r0, head = job.head;
 
-    long long row[QT];                    // of [T][Hq]
     int sees[QT];                         // own keys
     u32x4 Q[QT][C::KS];
 #pragma unroll
@@ -189,9 +263,8 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
         const int r = r0 + (wr * QT + t) * 16 + col;
         const bool in = r < count;
         const int token = in ? r / A.g : 0, h = in ? r - token * A.g : 0;
-        row[t] = in ? (long long)(token0 + token) * A.Hq + head * A.g + h : -1;
-        sees[t] = in ? min(max(length - fresh + token + 1, 0), length) : 0;
-        const char* const at = A.q + ((token0 + token) * A.ldq + (long long)(head * A.g + h) * A.D) * C::EB;
+        sees[t] = job.sees((wr * QT + t) * 16 + col);
+        const char* const at = A.q + ((job.rows.token0 + token) * A.ldq + (long long)(head * A.g + h) * A.D) * C::EB;
 #pragma unroll
         for (int s = 0; s < C::KS; ++s) {
             const int c = s * 64 + grp * 16;
@@ -226,21 +299,9 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
 
     int dirty_from = 0, dirty_to = 0;     // own keys whose infinities and NaN stay out of the products, see below
     for (int own = prefix_job || A.whole ? 0 : 1; own < (prefix_job ? 1 : 2); ++own) {
-        const int* const table = own ? A.table + (long long)b * A.max_pages : A.prefix_table;
-        int begin = 0, end = A.prefix, least;          // this workgroup's keys; those below `least` are seen by all of its rows
-        const int last = min(r0 + C::ROWS, count) - 1, own_end = min(max(length - fresh + last / A.g + 1, 0), length);
-        least = own ? min(max(length - fresh + r0 / A.g + 1, 0), length) : end;
-        if (own) end = own_end;
-        if (prefix_job) {
-            begin = split * A.prefix_per;
-            end = min(begin + A.prefix_per, A.prefix);
-        } else if (parts > 1) {
-            // equal parts of its own keys, or of those behind the prefix's (below 2^31 together)
-            const int before = A.whole ? A.prefix : 0, all = before + own_end, per = (int)(((unsigned)all + parts - 1) / parts + 127) / 128 * 128;
-            const int from = (int)min((long long)split * per, (long long)all) - (own ? before : 0), to = (int)min((long long)split * per + per, (long long)all) - (own ? before : 0);
-            begin = max(from, 0);
-            end = min(to, end);
-        }
+        const int* const table = job.table(own);
+        int begin, end, least;
+        job.keys(own, &begin, &end, &least);
         if (begin >= end) continue;
 
         int first = 0, stop = begin;      // keys whose pages' addresses are at hand
@@ -499,7 +560,7 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
     // what was left out of the products: a row's four values from d on of a key that it sees
     auto left_out = [&](int key, int d) {
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        const long long at = key_at<T>(A, A.table + (long long)b * A.max_pages, head, key);
+        const long long at = key_at<T>(A, job.table(1), head, key);
         if (at < 0 || d >= A.D) return v;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -507,33 +568,6 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
             v[e] = fabsf(x) < INFINITY ? 0.f : x;
         }
         return v;
-    };
-    // where a row's results go (r of [T][Hq], `at` of this workgroup), to the result or to this part's place, and its sums
-    auto part_row = [&](long long r, int at) {
-        if (A.whole) return ((long long)(id - A.cut) * C::ROWS + at);
-        return (long long)(prefix_job ? split : A.prefix_splits + split) * A.T * A.Hq + r;
-    };
-    auto place = [&](long long r, int at) {
-        const int token = (int)((unsigned)r / (unsigned)A.Hq), h = (int)r - token * A.Hq;
-        return direct ? A.out + (token * A.ldo + h * A.D) * C::EB : reinterpret_cast<char*>(A.part_o + part_row(r, at) * A.D);
-    };
-    auto store_sums = [&](long long r, int at, float mm, float ll) {
-        if (!direct) A.part_ml[part_row(r, at)] = make_float2(mm, ll);
-        else if (A.lse) A.lse[r] = ll == 0.f ? -INFINITY : 0.6931471805599453f * (mm + __builtin_amdgcn_logf(ll));
-    };
-    // four values from d on
-    auto store = [&](char* to, int d, f32x4 o, float ll) {
-        if (d >= A.D) return;
-        if (direct) {
-            const float by = 1.f / ll;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = ll == 0.f ? 0.f : o[e] * by;
-            if constexpr (C::EB == 2) {
-                *reinterpret_cast<uint2*>(to + d * 2) = make_uint2(f32x2_to_bf16x2(o[0], o[1]), f32x2_to_bf16x2(o[2], o[3]));
-                return;
-            }
-        }
-        *reinterpret_cast<f32x4*>(to + d * 4) = o;
     };
     if constexpr (C::WK == 1) {
         for (int key = dirty_from; key < dirty_to; ++key)
@@ -546,12 +580,13 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
             }
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            if (row[t] < 0) continue;
-            const int mine = (wr * QT + t) * 16 + col;
-            char* const to = place(row[t], mine);
+            const int at = (wr * QT + t) * 16 + col;
+            const long long row = job.row(at);
+            if (row < 0) continue;
+            char* const to = job.place(row, at);
 #pragma unroll
-            for (int d = 0; d < C::ND; ++d) store(to, d * 16 + grp * 4, O[t][d], l[t]);
-            if (grp == 0) store_sums(row[t], mine, m[t], l[t]);
+            for (int d = 0; d < C::ND; ++d) job.store(to, d * 16 + grp * 4, O[t][d], l[t]);
+            if (grp == 0) job.store_sums(row, at, m[t], l[t]);
         }
     } else {
         // the wavefronts' parts, in order
@@ -583,12 +618,11 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
                 ll += f * ml[at * 2 + 1];
                 sum += f * *reinterpret_cast<const f32x4*>(o + at * DP + d);
             }
-            const int at = r0 + r, token = at / A.g;
-            if (at >= count) continue;
-            for (int key = dirty_from; key < min(dirty_to, length - fresh + token + 1); ++key) sum += left_out(key, d);
-            const long long to = (long long)(token0 + token) * A.Hq + head * A.g + (at - token * A.g);
-            store(place(to, r), d, sum, ll);
-            if (d == 0) store_sums(to, r, top, ll);
+            const long long row = job.row(r);
+            if (row < 0) continue;
+            for (int key = dirty_from; key < min(dirty_to, job.sees(r)); ++key) sum += left_out(key, d);
+            job.store(job.place(row, r), d, sum, ll);
+            if (d == 0) job.store_sums(row, r, top, ll);
         }
     }
 }
