@@ -39,14 +39,17 @@ struct AttendArgs {
 // How many rows a tile has, and how it is dealt to the four wavefronts: FEW (one row's worth: a request's heads), SOME, MANY.  `line`: bytes from key to key
 // in LDS.  Wavefronts side by side in keys (wk of them) read each key once from LDS, and have sums to join at the end; side by side in rows (wr) they
 // read the same keys.  A tile's keys and values are 32 KiB, two of them in LDS, so that two workgroups share a compute unit.
-enum { FEW = 0, SOME = 1, MANY = 2 };
+// STREAM, float alone: up to four rows without LDS and matrix products, see stream() below.
+enum { STREAM = 0, FEW = 1, SOME = 2, MANY = 3 };
+constexpr int kStreamRows = 4;
+constexpr bool may_stream(int D, int elem) { return elem == 4 && D <= 128; }
 constexpr int width_of(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : D <= 192 ? 192 : 256; }
 constexpr int line_of(int D, int elem) { return D * elem <= 64 ? 64 : D * elem <= 128 ? 128 : D * elem <= 256 ? 256 : D * elem <= 512 ? 512 : 1024; }
 constexpr int keys_of(int kind, int line) { return line >= 256 ? 16384 / line : kind == MANY ? 64 : 128; }
 constexpr int wk_of(int kind, int line) { return kind == MANY || line == 1024 ? 1 : line == 512 ? 2 : 4; }
 // 16-row tiles of a wavefront: what is left of its registers decides where rows are long
 constexpr int qt_of(int kind, int line, int elem) { return kind == FEW ? 1 : line <= 256 ? 2 : kind == MANY && line == 512 && elem == 4 ? 2 : 1; }
-constexpr int rows_of(int kind, int line, int elem) { return 4 / wk_of(kind, line) * qt_of(kind, line, elem) * 16; }
+constexpr int rows_of(int kind, int line, int elem) { return kind == STREAM ? kStreamRows : 4 / wk_of(kind, line) * qt_of(kind, line, elem) * 16; }
 
 constexpr int kPlaces = 1024;          // pages whose addresses a workgroup has at hand
 
@@ -627,10 +630,176 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
     }
 }
 
+// Up to four rows of float: bound by memory, and by float matrix products if those were formed of 16 rows that are mostly empty.  No LDS, no barrier:
+// eight lanes hold a key, chunks of 16 bytes of it (lane p chunks p, p + 8, ...), so that they read whole lines; a wavefront takes eight keys at a time, the
+// workgroup 32, and DEPTH such steps' keys and values are on their way to registers while one is used.  A score is the sum over its eight lanes;
+// each group of lanes has maxima, sums and products of its own keys, which meet at the end, in LDS, in a fixed order.
+template <int DP> struct Stream {
+    static constexpr int NC = DP / 32, GROUPS = kThreads / 8, DEPTH = NC >= 4 ? 3 : NC == 3 ? 4 : 6;
+    static constexpr int LDS = GROUPS * kStreamRows * (DP + 2) * 4;
+};
+
+// the sum over eight lanes; all of them get it
+__device__ __forceinline__ float sum_of_8(float v)
+{
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xf, 0xf, true));       // lane ^ 1
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xf, 0xf, true));       // lane ^ 2
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, true));      // the other half of 8
+    return v;
+}
+
+template <int DP> __device__ __forceinline__ void stream(const AttendArgs& A, char* lds, int id, bool prefix_job)
+{
+    typedef Stream<DP> C;
+    constexpr int R = kStreamRows, NC = C::NC, DEPTH = C::DEPTH;
+    const int tid = (int)threadIdx.x, p = tid % 8, slot = tid / 8;
+    const Job<float, R> job(A, id, prefix_job);
+    if (job.none()) return;
+    const float scale = A.scale;
+
+    f32x4 Q[R][NC], O[R][NC];
+    float m[R], l[R];
+    int sees[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const long long row = job.row(r), token = row < 0 ? 0 : row / A.Hq;
+        sees[r] = job.sees(r);
+        const float* const at = reinterpret_cast<const float*>(A.q) + token * A.ldq + (row - token * A.Hq) * A.D;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int d = (c * 8 + p) * 4;
+            Q[r][c] = O[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (row >= 0 && d < A.D && scale != 0.f) Q[r][c] = *reinterpret_cast<const f32x4*>(at + d);
+        }
+        m[r] = -INFINITY;
+        l[r] = 0.f;
+    }
+    const float factor = scale == 0.f ? 1.f : scale;
+    const long long values = A.v_pages - A.k_pages;
+    for (int own = prefix_job || A.whole ? 0 : 1; own < (prefix_job ? 1 : 2); ++own) {
+        const int* const table = job.table(own);
+        int begin, end, least;
+        job.keys(own, &begin, &end, &least);
+        if (begin >= end) continue;
+        f32x4 K[DEPTH][NC], V[DEPTH][NC];
+        bool there[DEPTH];
+        int pages[DEPTH];
+        // a page's number is asked for DEPTH steps before its keys
+        auto page_of = [&](int key) { return key < end ? table[key >> A.page_bits] : -1; };
+        auto load = [&](int u, int key) {
+            const int page = pages[u];
+            there[u] = page >= 0 && page < A.pages;
+            const char* const at = A.k_pages + (((((long long)page * A.Hk + job.head) << A.page_bits) + (key & ((1 << A.page_bits) - 1))) * A.D + p * 4) * 4;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                K[u][c] = V[u][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (there[u] && (c * 8 + p) * 4 < A.D) {
+                    K[u][c] = *reinterpret_cast<const f32x4*>(at + c * 128);
+                    V[u][c] = *reinterpret_cast<const f32x4*>(at + c * 128 + values);
+                }
+            }
+        };
+        const int key0 = begin + slot;
+#pragma unroll
+        for (int u = 0; u < DEPTH; ++u) pages[u] = page_of(key0 + u * C::GROUPS);
+#pragma unroll
+        for (int u = 0; u < DEPTH; ++u) {
+            load(u, key0 + u * C::GROUPS);
+            pages[u] = page_of(key0 + (DEPTH + u) * C::GROUPS);
+        }
+        for (int step = begin; step < end; step += DEPTH * C::GROUPS)
+#pragma unroll
+            for (int u = 0; u < DEPTH; ++u) {
+                const int first = step + u * C::GROUPS, key = first + slot;
+                if (first >= end) break;
+                const bool edge = own && first + C::GROUPS > least;          // rows see different keys
+                float x[R];
+                bool hidden[R];
+                bool grows = false;
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    float s = 0.f;
+#pragma unroll
+                    for (int c = 0; c < NC; ++c)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s = fmaf(Q[r][c][e], K[u][c][e], s);
+                    hidden[r] = !there[u] || (edge && key >= sees[r]);
+                    x[r] = hidden[r] ? -INFINITY : sum_of_8(s) * factor;
+                    grows = grows || x[r] > m[r] + 8.f;
+                }
+                // m follows only where a score is more than 2^8 times what it stands for, see attend()
+                if (__any(grows)) {
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        const float most = fmaxf(m[r], x[r]), down = __builtin_amdgcn_exp2f(m[r] - (most == -INFINITY ? 0.f : most));
+                        m[r] = most;
+                        l[r] *= down;
+#pragma unroll
+                        for (int c = 0; c < NC; ++c) O[r][c] *= down;
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float w = __builtin_amdgcn_exp2f(x[r] - (m[r] == -INFINITY ? 0.f : m[r]));
+                    l[r] += w;
+                    if (edge && hidden[r]) continue;          // (what a row does not see does not reach it, whatever it is)
+#pragma unroll
+                    for (int c = 0; c < NC; ++c)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) O[r][c][e] = fmaf(w, V[u][c][e], O[r][c][e]);
+                }
+                load(u, key + DEPTH * C::GROUPS);
+                pages[u] = page_of(key + 2 * DEPTH * C::GROUPS);
+            }
+    }
+
+    float* const o = reinterpret_cast<float*>(lds);
+    float* const ml = o + C::GROUPS * R * DP;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) *reinterpret_cast<f32x4*>(o + (slot * R + r) * DP + (c * 8 + p) * 4) = O[r][c];
+        if (p == 0) {
+            ml[(slot * R + r) * 2] = m[r];
+            ml[(slot * R + r) * 2 + 1] = l[r];
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i < R * (DP / 4); i += kThreads) {
+        const int r = i / (DP / 4), d = i % (DP / 4) * 4;
+        const long long row = job.row(r);
+        if (row < 0) continue;
+        float top = -INFINITY, sum = 0.f;
+        for (int g = 0; g < C::GROUPS; ++g) top = fmaxf(top, ml[(g * R + r) * 2]);
+        f32x4 all = {0.f, 0.f, 0.f, 0.f};
+        for (int g = 0; g < C::GROUPS; ++g) {
+            const float part = ml[(g * R + r) * 2 + 1];
+            if (part == 0.f) continue;          // (no key)
+            const float f = __builtin_amdgcn_exp2f(ml[(g * R + r) * 2] - top);
+            sum += f * part;
+            all += f * *reinterpret_cast<const f32x4*>(o + (g * R + r) * DP + d);
+        }
+        job.store(job.place(row, r), d, all, sum);
+        if (d == 0) job.store_sums(row, r, top, sum);
+    }
+}
+
+template <typename T, int DP, int KIND> constexpr int lds_of()
+{
+    if constexpr (KIND == STREAM) return Stream<DP>::LDS;
+    else return Attend<T, DP, KIND>::LDS;
+}
+template <typename T, int DP, int KIND> __device__ __forceinline__ void do_job(const AttendArgs& A, char* lds, int id, bool prefix)
+{
+    if constexpr (KIND == STREAM) stream<DP>(A, lds, id, prefix);
+    else attend<T, DP, KIND>(A, lds, id, prefix);
+}
+
 // PREFIX: the kind of a tile of the prefix's rows; OWN: of a tile of one request's.  One launch for both.
 template <typename T, int DP, int PREFIX, int OWN> __global__ __launch_bounds__(kThreads, 2) void attend_keys(const AttendArgs A)
 {
-    constexpr int P = Attend<T, DP, PREFIX>::LDS, O = Attend<T, DP, OWN>::LDS;
+    constexpr int P = lds_of<T, DP, PREFIX>(), O = lds_of<T, DP, OWN>();
     __shared__ __attribute__((aligned(1024))) char lds[P > O ? P : O];
     // Workgroups of both kinds in turns of 256, as many as there are compute units, while there are both: products of the one and reads of the other side by side.
     int id = (int)blockIdx.x;
@@ -644,10 +813,10 @@ template <typename T, int DP, int PREFIX, int OWN> __global__ __launch_bounds__(
         if (!prefix) id -= A.prefix_jobs - turns * 256;
     }
     if constexpr (PREFIX == OWN) {
-        attend<T, DP, PREFIX>(A, lds, id, prefix);
+        do_job<T, DP, PREFIX>(A, lds, id, prefix);
     } else {
-        if (prefix) attend<T, DP, PREFIX>(A, lds, id, true);
-        else attend<T, DP, OWN>(A, lds, id, false);
+        if (prefix) do_job<T, DP, PREFIX>(A, lds, id, true);
+        else do_job<T, DP, OWN>(A, lds, id, false);
     }
 }
 

@@ -26,13 +26,14 @@ long long up(long long a, long long b) { return (a + b - 1) / b; }
 
 // What the device has to know of the lengths stays there: ranges of a request's own keys are cut by its length where they are read, `own_splits` of
 // them.  `several`: requests may have more rows than one.
-Plan plan(long long T, int B, int Hq, int Hk, int line, int elem, long long prefix, long long capacity, bool several)
+Plan plan(long long T, int B, int Hq, int Hk, int D, int line, int elem, long long prefix, long long capacity, bool several)
 {
     Plan p;
     std::memset(&p, 0, sizeof(p));
     const long long g = Hq / Hk, rows = T * g, each = several ? up(rows, B) : g;
     // tiles of rows: no more of them empty than has to be
     auto kind_of = [&](long long n) {
+        if (n <= kStreamRows && may_stream(D, elem)) return (int)STREAM;
         int kind = n <= rows_of(FEW, line, elem) ? FEW : n <= rows_of(SOME, line, elem) ? SOME : MANY;
         // float products take so much longer than what they are of that keys may as well be read again, if fewer empty rows are multiplied
         auto work = [&](int k) { return up(n, rows_of(k, line, elem)) * qt_of(k, line, elem) * (4 / wk_of(k, line)); };
@@ -112,9 +113,9 @@ size_t cgbn_prefix_attention_workspace_bytes(long long T, int B, int Hq, int Hk,
     if (T == 0 || B == 0) return 256;
     const int elem = dtype == CGBN_F32 ? 4 : 2, line = line_of(width_of(D), elem);
     // requests of one row each go in other tiles when it is said that they are
-    size_t most = scratch(plan(T, B, Hq, Hk, line, elem, prefix, capacity, true), T, Hq, D, line, elem);
+    size_t most = scratch(plan(T, B, Hq, Hk, D, line, elem, prefix, capacity, true), T, Hq, D, line, elem);
     if (T == B) {
-        const size_t single = scratch(plan(T, B, Hq, Hk, line, elem, prefix, capacity, false), T, Hq, D, line, elem);
+        const size_t single = scratch(plan(T, B, Hq, Hk, D, line, elem, prefix, capacity, false), T, Hq, D, line, elem);
         if (single > most) most = single;
     }
     const size_t bytes = (most + 255) / 256 * 256;
@@ -144,7 +145,7 @@ cgbn_status cgbn_prefix_attention(const void* q, long long ldq, long long T, int
         if (p && (p == out || p == lse)) return CGBN_ERR_ALIAS;
     if (out == lse) return CGBN_ERR_ALIAS;
     const int line = line_of(width_of(D), elem);
-    const Plan p = plan(T, B, Hq, Hk, line, elem, prefix, capacity, rows != nullptr);
+    const Plan p = plan(T, B, Hq, Hk, D, line, elem, prefix, capacity, rows != nullptr);
     if (p.jobs >= (1ll << 24)) return CGBN_ERR_SHAPE;           // 2^32 threads
     AttendArgs A;
     std::memset(&A, 0, sizeof(A));

@@ -9,6 +9,12 @@ template <typename T, int DP> static void launch_width(const AttendArgs& A, int 
     const dim3 grid((unsigned)A.jobs);
 #define CGBN_CASE(prefix_, own_) \
     if (prefix == prefix_ && own == own_) hipLaunchKernelGGL((attend_keys<T, DP, prefix_, own_>), grid, dim3(kThreads), 0, st, A);
+    if constexpr (may_stream(DP, sizeof(T))) {
+        CGBN_CASE(STREAM, STREAM)
+        CGBN_CASE(FEW, STREAM)
+        CGBN_CASE(SOME, STREAM)
+        CGBN_CASE(MANY, STREAM)
+    }
     CGBN_CASE(FEW, FEW)
     CGBN_CASE(SOME, FEW)
     CGBN_CASE(MANY, FEW)
