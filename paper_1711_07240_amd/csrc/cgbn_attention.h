@@ -631,28 +631,29 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
 }
 
 // Up to four rows of float: bound by memory, and by float matrix products if those were formed of 16 rows that are mostly empty.  No LDS, no barrier:
-// eight lanes hold a key, chunks of 16 bytes of it (lane p chunks p, p + 8, ...), so that they read whole lines; a wavefront takes eight keys at a time, the
-// workgroup 32, and DEPTH such steps' keys and values are on their way to registers while one is used.  A score is the sum over its eight lanes;
+// LANES lanes hold a key, chunks of 16 bytes of it (lane p chunks p, p + LANES, ...), so that they read whole lines; the workgroup takes GROUPS keys at a time,
+// and DEPTH such steps' keys and values are on their way to registers while one is used.  A score is the sum over its lanes;
 // each group of lanes has maxima, sums and products of its own keys, which meet at the end, in LDS, in a fixed order.
 template <int DP> struct Stream {
-    static constexpr int NC = DP / 32, GROUPS = kThreads / 8, DEPTH = NC >= 4 ? 3 : NC == 3 ? 4 : 6;
+    static constexpr int LANES = DP == 128 ? 16 : 8, NC = DP / 4 / LANES, GROUPS = kThreads / LANES, DEPTH = NC == 3 ? 3 : 4;
     static constexpr int LDS = GROUPS * kStreamRows * (DP + 2) * 4;
 };
 
-// the sum over eight lanes; all of them get it
-__device__ __forceinline__ float sum_of_8(float v)
+// the sum over 8 or 16 lanes; all of them get it
+template <int LANES> __device__ __forceinline__ float sum_over(float v)
 {
     v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xf, 0xf, true));       // lane ^ 1
     v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xf, 0xf, true));       // lane ^ 2
     v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, true));      // the other half of 8
+    if constexpr (LANES == 16) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xf, 0xf, true));      // the other half of 16
     return v;
 }
 
 template <int DP> __device__ __forceinline__ void stream(const AttendArgs& A, char* lds, int id, bool prefix_job)
 {
     typedef Stream<DP> C;
-    constexpr int R = kStreamRows, NC = C::NC, DEPTH = C::DEPTH;
-    const int tid = (int)threadIdx.x, p = tid % 8, slot = tid / 8;
+    constexpr int R = kStreamRows, NC = C::NC, DEPTH = C::DEPTH, LANES = C::LANES, G = C::GROUPS;
+    const int tid = (int)threadIdx.x, p = tid % LANES, slot = tid / LANES;
     const Job<float, R> job(A, id, prefix_job);
     if (job.none()) return;
     const float scale = A.scale;
@@ -667,7 +668,7 @@ template <int DP> __device__ __forceinline__ void stream(const AttendArgs& A, ch
         const float* const at = reinterpret_cast<const float*>(A.q) + token * A.ldq + (row - token * A.Hq) * A.D;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            const int d = (c * 8 + p) * 4;
+            const int d = (c * LANES + p) * 4;
             Q[r][c] = O[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
             if (row >= 0 && d < A.D && scale != 0.f) Q[r][c] = *reinterpret_cast<const f32x4*>(at + d);
         }
@@ -693,26 +694,26 @@ template <int DP> __device__ __forceinline__ void stream(const AttendArgs& A, ch
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 K[u][c] = V[u][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-                if (there[u] && (c * 8 + p) * 4 < A.D) {
-                    K[u][c] = *reinterpret_cast<const f32x4*>(at + c * 128);
-                    V[u][c] = *reinterpret_cast<const f32x4*>(at + c * 128 + values);
+                if (there[u] && (c * LANES + p) * 4 < A.D) {
+                    K[u][c] = *reinterpret_cast<const f32x4*>(at + c * (LANES * 16));
+                    V[u][c] = *reinterpret_cast<const f32x4*>(at + c * (LANES * 16) + values);
                 }
             }
         };
         const int key0 = begin + slot;
 #pragma unroll
-        for (int u = 0; u < DEPTH; ++u) pages[u] = page_of(key0 + u * C::GROUPS);
+        for (int u = 0; u < DEPTH; ++u) pages[u] = page_of(key0 + u * G);
 #pragma unroll
         for (int u = 0; u < DEPTH; ++u) {
-            load(u, key0 + u * C::GROUPS);
-            pages[u] = page_of(key0 + (DEPTH + u) * C::GROUPS);
+            load(u, key0 + u * G);
+            pages[u] = page_of(key0 + (DEPTH + u) * G);
         }
-        for (int step = begin; step < end; step += DEPTH * C::GROUPS)
+        for (int step = begin; step < end; step += DEPTH * G)
 #pragma unroll
             for (int u = 0; u < DEPTH; ++u) {
-                const int first = step + u * C::GROUPS, key = first + slot;
+                const int first = step + u * G, key = first + slot;
                 if (first >= end) break;
-                const bool edge = own && first + C::GROUPS > least;          // rows see different keys
+                const bool edge = own && first + G > least;          // rows see different keys
                 float x[R];
                 bool hidden[R];
                 bool grows = false;
@@ -723,8 +724,10 @@ template <int DP> __device__ __forceinline__ void stream(const AttendArgs& A, ch
                     for (int c = 0; c < NC; ++c)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) s = fmaf(Q[r][c][e], K[u][c][e], s);
+                    float y = sum_over<LANES>(s) * factor;
+                    asm("" : "+v"(y));          // (formed in any case: a branch around it is the longer way)
                     hidden[r] = !there[u] || (edge && key >= sees[r]);
-                    x[r] = hidden[r] ? -INFINITY : sum_of_8(s) * factor;
+                    x[r] = hidden[r] ? -INFINITY : y;
                     grows = grows || x[r] > m[r] + 8.f;
                 }
                 // m follows only where a score is more than 2^8 times what it stands for, see attend()
@@ -742,46 +745,72 @@ template <int DP> __device__ __forceinline__ void stream(const AttendArgs& A, ch
                 for (int r = 0; r < R; ++r) {
                     const float w = __builtin_amdgcn_exp2f(x[r] - (m[r] == -INFINITY ? 0.f : m[r]));
                     l[r] += w;
-                    if (edge && hidden[r]) continue;          // (what a row does not see does not reach it, whatever it is)
-#pragma unroll
-                    for (int c = 0; c < NC; ++c)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) O[r][c][e] = fmaf(w, V[u][c][e], O[r][c][e]);
+                    x[r] = w;
                 }
-                load(u, key + DEPTH * C::GROUPS);
-                pages[u] = page_of(key + 2 * DEPTH * C::GROUPS);
+                if (!edge) {
+#pragma unroll
+                    for (int r = 0; r < R; ++r)
+#pragma unroll
+                        for (int c = 0; c < NC; ++c)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) O[r][c][e] = fmaf(x[r], V[u][c][e], O[r][c][e]);
+                } else {          // what a row does not see does not reach it, whatever it is
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        if (hidden[r]) continue;
+#pragma unroll
+                        for (int c = 0; c < NC; ++c)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) O[r][c][e] = fmaf(x[r], V[u][c][e], O[r][c][e]);
+                    }
+                }
+                load(u, key + DEPTH * G);
+                pages[u] = page_of(key + 2 * DEPTH * G);
             }
     }
 
+    // The groups' parts: a wavefront to a row for what they weigh, then two threads to four values of a row, half of the groups each
     float* const o = reinterpret_cast<float*>(lds);
-    float* const ml = o + C::GROUPS * R * DP;
+    float2* const ml = reinterpret_cast<float2*>(o + G * R * DP);
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < R; ++r) {
 #pragma unroll
-        for (int c = 0; c < NC; ++c) *reinterpret_cast<f32x4*>(o + (slot * R + r) * DP + (c * 8 + p) * 4) = O[r][c];
-        if (p == 0) {
-            ml[(slot * R + r) * 2] = m[r];
-            ml[(slot * R + r) * 2 + 1] = l[r];
-        }
+        for (int c = 0; c < NC; ++c)
+            if ((c * LANES + p) * 4 < DP) *reinterpret_cast<f32x4*>(o + (slot * R + r) * DP + (c * LANES + p) * 4) = O[r][c];
+        if (p == 0) ml[r * G + slot] = make_float2(m[r], l[r]);
     }
     __syncthreads();
-    for (int i = tid; i < R * (DP / 4); i += kThreads) {
-        const int r = i / (DP / 4), d = i % (DP / 4) * 4;
+    static_assert(R == kThreads / kWave, "");
+    {
+        const int r = tid / kWave, g = tid % G;
+        const float2 part = ml[r * G + g];
+        float top = part.x, sum;
+#pragma unroll
+        for (int d = 1; d < G; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+        const float f = part.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(part.x - top);
+        sum = part.y == 0.f ? 0.f : f * part.y;
+#pragma unroll
+        for (int d = 1; d < G; d *= 2) sum += __shfl_xor(sum, d);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // (the wavefront's own row)
+        ml[r * G + g] = make_float2(part.y == 0.f ? -1.f : f, sum);
         const long long row = job.row(r);
-        if (row < 0) continue;
-        float top = -INFINITY, sum = 0.f;
-        for (int g = 0; g < C::GROUPS; ++g) top = fmaxf(top, ml[(g * R + r) * 2]);
+        if (row >= 0 && tid % kWave == 0) job.store_sums(row, r, top, sum);
+    }
+    __syncthreads();
+    for (int i = tid / 2; i < R * (DP / 4); i += kThreads / 2) {
+        const int r = i / (DP / 4), d = i % (DP / 4) * 4, g0 = tid % 2 * (G / 2);
         f32x4 all = {0.f, 0.f, 0.f, 0.f};
-        for (int g = 0; g < C::GROUPS; ++g) {
-            const float part = ml[(g * R + r) * 2 + 1];
-            if (part == 0.f) continue;          // (no key)
-            const float f = __builtin_amdgcn_exp2f(ml[(g * R + r) * 2] - top);
-            sum += f * part;
-            all += f * *reinterpret_cast<const f32x4*>(o + (g * R + r) * DP + d);
+#pragma unroll
+        for (int g = 0; g < G / 2; ++g) {
+            const float f = ml[r * G + g0 + g].x;
+            const f32x4 part = *reinterpret_cast<const f32x4*>(o + ((g0 + g) * R + r) * DP + d);
+            if (f != -1.f) all += f * part;          // (of no key there is no sum)
         }
-        job.store(job.place(row, r), d, all, sum);
-        if (d == 0) job.store_sums(row, r, top, sum);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) all[e] += __shfl_xor(all[e], 1);
+        const long long row = job.row(r);
+        if (row >= 0 && tid % 2 == 0) job.store(job.place(row, r), d, all, ml[r * G].y);
     }
 }
 

@@ -72,10 +72,10 @@ Plan plan(long long T, int B, int Hq, int Hk, int D, int line, int elem, long lo
         return p;
     }
     p.own_splits = prefix ? 0 : 1;         // (without any keys rows are zero)
-    // Parts of a request's keys: so many that requests of unequal length, which the host does not know, keep the device busy to the end (24 requests of up to
-    // 1500 float keys, 20 heads: 512, 1024 and 2048 workgroups 129, 129 and 122 us; 64 of up to 2048 bfloat16 keys, 8 heads: 98, 100 and 105)
+    // Parts of a request's keys: so many that requests of unequal length, which the host does not know, keep the device busy to the end (512, 1024 and 2048
+    // workgroups: 4 requests of up to 131072 bfloat16 keys, 8 heads, 303, 295 and 293 us; 64 of up to 2048, 98, 100 and 105; 24 of up to 1500 float keys, 20 heads, 97, 97 and 100)
     if (capacity) {
-        long long s = (elem == 4 ? 2048 : 1024) / (own_tiles * Hk);
+        long long s = 1024 / (own_tiles * Hk);
         if (s > up(capacity, 256)) s = up(capacity, 256);
         p.own_splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
     }
