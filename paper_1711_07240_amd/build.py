@@ -47,7 +47,8 @@ NO_SCRATCH = ["-Xarch_device", "-Wframe-larger-than=0", "-Xarch_device", "-Werro
 def _units(obj_dir):
     """(object file, source, extra flags) of every translation unit."""
     OBJ = obj_dir
-    units = [(os.path.join(OBJ, name + ".o"), os.path.join(CSRC, name + ".hip"), []) for name in ("cgbn", "cgbn_linear", "cgbn_head_norm", "cgbn_rotate", "cgbn_pages", "cgbn_attention")]
+    units = [(os.path.join(OBJ, name + ".o"), os.path.join(CSRC, name + ".hip"), [])
+             for name in ("cgbn", "cgbn_linear", "cgbn_head_norm", "cgbn_rotate", "cgbn_pages", "cgbn_attention")]
     for tname, t in (("f32", "float"), ("bf16", "bf16_t")):
         units.append((os.path.join(OBJ, f"attention_{tname}.o"), os.path.join(CSRC, "cgbn_attention_inst.hip"), [f"-DCGBN_INST_T={t}"]))
     for tname, t in (("f32", "float"), ("bf16", "bf16_t")):

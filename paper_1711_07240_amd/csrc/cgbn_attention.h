@@ -379,7 +379,7 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
         const int v_line = grp * 4 + (C::EB == 2 ? col >> 2 : 0), v_chunk = C::EB == 2 ? (col >> 1) & 1 : col >> 2;
         const int v_from = 2 * C::HALF + (k0 + v_line) * C::LINE + ((v_chunk ^ line_key<C::LINE>(v_line)) << 4) + (C::EB == 2 ? (col & 1) * 8 : (col & 3) * 4);
         // fragment i of a tile's keys (16 of them, 64 bytes of each), of its values (the keys of a weights' register by 16 of D)
-        constexpr int K_STEPS = C::KS * C::NT, V_STEPS = C::NP * C::ND, AHEAD = K_STEPS < 4 ? K_STEPS : 4;
+        constexpr int K_STEPS = C::KS * C::NT, V_STEPS = C::NP * C::ND, AHEAD = K_STEPS < 4 ? K_STEPS : C::EB == 2 ? 4 : 3;
         auto key_fragment = [&](int stage, int i) {
             return *(const lds_u32x4*)(base + ((k_from + stage * C::HALF) ^ (i / C::NT << 6)) + i % C::NT * 16 * C::LINE);
         };

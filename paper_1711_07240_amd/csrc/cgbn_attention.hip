@@ -33,7 +33,7 @@ Plan plan(long long T, int B, int Hq, int Hk, int D, int line, int elem, long lo
     const long long g = Hq / Hk, rows = T * g, each = several ? up(rows, B) : g;
     // tiles of rows: no more of them empty than has to be
     auto kind_of = [&](long long n) {
-        if (n <= kStreamRows && may_stream(D, elem)) return (int)STREAM;
+        if (n <= kStreamRows && may_stream(D, elem) && (rows / kStreamRows + B) * Hk < (1 << 22)) return (int)STREAM;          // (fewer than 2^32 threads)
         int kind = n <= rows_of(FEW, line, elem) ? FEW : n <= rows_of(SOME, line, elem) ? SOME : MANY;
         // float products take so much longer than what they are of that keys may as well be read again, if fewer empty rows are multiplied
         auto work = [&](int k) { return up(n, rows_of(k, line, elem)) * qt_of(k, line, elem) * (4 / wk_of(k, line)); };
