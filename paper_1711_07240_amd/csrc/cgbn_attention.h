@@ -433,15 +433,18 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
                 }
                 largest(S, top);
             }
+            bool grows = false;
 #pragma unroll
-            for (int t = 0; t < QT; ++t)
-                if (__any(top[t] * scale > m[t] + 8.f)) {
-                    const float most = fmaxf(m[t], row_max(top[t] * scale)), down = __builtin_amdgcn_exp2f(m[t] - (most == -INFINITY ? 0.f : most));
-                    m[t] = most;
-                    l[t] *= down;
+            for (int t = 0; t < QT; ++t) grows = grows || top[t] * scale > m[t] + 8.f;
+            if (!__any(grows)) return;
 #pragma unroll
-                    for (int d = 0; d < C::ND; ++d) O[t][d] *= down;
-                }
+            for (int t = 0; t < QT; ++t) {
+                const float most = fmaxf(m[t], row_max(top[t] * scale)), down = __builtin_amdgcn_exp2f(m[t] - (most == -INFINITY ? 0.f : most));
+                m[t] = most;
+                l[t] *= down;
+#pragma unroll
+                for (int d = 0; d < C::ND; ++d) O[t][d] *= down;
+            }
         };
 
         // Keys are one tile ahead of values: while a tile's weights are formed, on the vector unit, and its values multiplied, the next one's scores are.
