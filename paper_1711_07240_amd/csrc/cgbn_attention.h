@@ -4,7 +4,7 @@
 //
 // The prefix's keys are the same for every row, so its products are formed with all requests' rows side by side: a workgroup takes a tile of rows (a
 // row is one head of one token; the Hq / Hk heads that share keys lie side by side) and a range of keys, which it reads once for all of them.  A request's own keys are
-// met by its own rows alone.  Both are split over ranges of keys where there are few rows; the parts carry their largest score m, the sum l of
+// met by its own rows alone.  Both are split over ranges of keys where there are few rows; the parts carry a score m near their largest, the sum l of
 // exp(score - m) and the products o, all in 32 bits, and are joined in a fixed order.
 //
 // One pass over the keys: scores of a tile, their largest, exponentials, and the products with v are formed before the next tile is read; o and l
@@ -12,6 +12,16 @@
 // neighbouring keys of each 16: rounded to bfloat16 they are, as they are, the second operand of V^T P^T, if the keys of two such
 // tiles are dealt to the reduction in the order that the lanes hold them; V is read from LDS in the same order (bfloat16: by the reads that
 // transpose 4 x 16 blocks).  No score crosses lanes but for its row's maximum and sum.
+//
+// Keys and values go from memory to LDS directly, the next tile's while one is multiplied; scores are one tile ahead of values, so that the vector unit
+// forms a tile's weights while the matrix cores form the next one's scores.  Without that order 2919 us for what takes 555 (16 requests of up to 512 new tokens
+// behind 8191, 32 heads of 128 on 8, bfloat16).
+//
+// What bounds it: few rows the read of the keys (4 requests of up to 131072, 1.67 GB, 295 us, 5.7 TB/s, more than a copy's rate); many rows
+// the products and the weights' arithmetic together, 960 TF of the 1030 that the library's large product reaches on the same card: the matrix cores are busy 41 %
+// of the time, the vector unit about as long, at 1.9 to 2.1 GHz, and no single part of the loop taken out gains more than a fifth.  64 rows of
+// each key head behind 32768 keys with up to 2048 of their own are both, 100 us for 72 of reading.  Float with few rows reading too (stream(), below); with more the float
+// products, a fifth of the matrix cores' bfloat16 rate at best.  Small calls the launch and five trips to memory one after the other, 8 us.
 #pragma once
 
 #include "cgbn_gemm.h"

@@ -4,10 +4,11 @@
 // its length then takes beyond those it holds, which give its place in the free list.  After that every row is on its own: its request by bisection
 // of the rows' starts, its key's page from the table or, if the request did not hold it before, from the free list; the row
 // whose key is a page's first writes the new entry (a page that is new has its first key in this step).  So nothing is read that another row writes.
-// Bound by latency: a launch, two dependent reads, two sums.  Up to 1024 requests are one launch, whose workgroups all form the sums (16 requests 4 us;
-// 1024 with 131072 rows, 1.1 MB, 5.9, in two launches 9.1); of more the rows are a second one's.
+// Bound by latency: a launch, two dependent reads, two sums.  Up to 1024 requests are one launch, whose workgroups all form the sums (16 requests 4.2 us;
+// 1024 with 131072 rows, 1.1 MB, 6.2, in two launches 10.4); of more the rows are a second one's.
 //
-// page_store.  Bound by memory: one read and one write of the rows, 16 bytes a lane.  Pages hold a head's keys side by side ([page][head][key][D]), so
+// page_store.  Bound by memory: one read and one write of the rows, 16 bytes a lane (20011 tokens, 20 heads of 80 float, 502 MB, 104 us, 4.8 TB/s; 64 tokens of 8
+// heads of 128 bfloat16 4.4 us, a launch).  Pages hold a head's keys side by side ([page][head][key][D]), so
 // that attention, which reads one head at a time, finds whole pages of it in one run; a row is written in runs of D.
 #include "cgbn.h"
 #include "cgbn_grid.h"
