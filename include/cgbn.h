@@ -396,6 +396,7 @@ size_t cgbn_prefix_attention_workspace_bytes(long long T, int B, int Hq, int Hk,
  * A row that sees no key is zero.  lse[T][Hq], if not NULL: the logarithm of the sum of the exponentials of a row's scores, -infinity where there is no key.
  *   Keys beyond lengths[b], in pages that are not there, or later than a row's own are not looked at, whatever their places hold.  max_pages = 0: no own tokens,
  *   table and lengths are not read.  Weights are rounded to bfloat16 for the products of bfloat16 tensors, their sum is not.
+ * Weights times values are summed before they are divided: values above about 1e33 over the number of keys may overflow.
  *   D a multiple of 8 up to 256; rows of q and out on 16 bytes; T * Hq < 2^26 - 3, B * Hk <= 2^22. */
 cgbn_status cgbn_prefix_attention(const void* q, long long ldq, long long T, int B, const int* rows, const int* lengths, int Hq, int Hk,
                                   int D, float scale, const void* k_pages, const void* v_pages, int pages, int page,

@@ -20,7 +20,7 @@
 // What bounds it: few rows the read of the keys (4 requests of up to 131072, 1.67 GB, 295 us, 5.7 TB/s, more than a copy's rate); many rows
 // the products and the weights' arithmetic together, 960 TF of the 1030 that the library's large product reaches on the same card: the matrix cores are busy 41 %
 // of the time, the vector unit about as long, at 1.9 to 2.1 GHz, and no single part of the loop taken out gains more than a fifth.  64 rows of
-// each key head behind 32768 keys with up to 2048 of their own are both, 100 us for 72 of reading.  Float with few rows reading too (stream(), below); with more the float
+// each key head behind 32768 keys with up to 2048 of their own are both, 97.5 us for 72 of reading.  Float with few rows reading too (stream(), below); with more the float
 // products, a fifth of the matrix cores' bfloat16 rate at best.  Small calls the launch and five trips to memory one after the other, 8 us.
 #pragma once
 
@@ -37,7 +37,10 @@ struct AttendArgs {
     const int *rows, *lengths, *prefix_table, *table;
     long long ldq, ldo, T;             // elements from row to row
     int B, Hq, Hk, g, D, pages, page_bits, prefix, max_pages;
-    int prefix_splits, prefix_per, own_splits;
+    int prefix_splits, prefix_per;
+    int own_splits, own_least;         // parts of a request's own keys at most, and keys of a part at least
+    int own_groups;                    // workgroups for them
+    float* dense;                      // workspace: parts to a key, as the lengths have it, see deal()
     int prefix_tiles, own_tiles;       // tiles of rows
     int prefix_jobs, jobs;             // workgroups, those of the prefix first
     int whole;                         // a workgroup takes the prefix and then its request's own keys
@@ -171,30 +174,127 @@ struct RowsOf {
         w.length = A.max_pages ? (int)min((long long)max(A.lengths[w.b], 0), (long long)A.max_pages << A.page_bits) : 0;
         return w;
     }
+    __device__ __forceinline__ bool none() const { return r0 < 0 || r0 >= count; }
+    // own keys that row `at` of the tile sees, and that all of them do together
+    __device__ __forceinline__ int sees(const AttendArgs& A, int at) const
+    {
+        const int r = r0 + at;
+        return r < count ? min(max(length - fresh + r / A.g + 1, 0), length) : 0;
+    }
+    __device__ __forceinline__ int end(const AttendArgs& A, int rows_of_a_tile) const { return sees(A, min(rows_of_a_tile, count - r0) - 1); }
 };
+
+// Parts of a request's `length` own keys, if there are to be `dense` of them to a key; keys of one: they are equal
+__device__ __forceinline__ int parts_of(const AttendArgs& A, int length, float dense) { return length ? min((int)((float)length * dense) + 1, A.own_splits) : 0; }
+__device__ __forceinline__ int keys_of_part(int length, int parts) { return ((length + parts - 1) / parts + 127) / 128 * 128; }
+
+// A request of the batch, as a lane sees it
+struct Request {
+    int token0, fresh, length, tiles;
+    __device__ __forceinline__ Request(const AttendArgs& A, int b, int rows_of_a_tile)
+    {
+        token0 = b;
+        fresh = 1;
+        if (A.rows) {
+            token0 = (int)min(max((long long)A.rows[b], 0ll), A.T);
+            fresh = max((int)min((long long)A.rows[b + 1], A.T) - token0, 0);
+        }
+        length = A.max_pages ? (int)min((long long)max(A.lengths[b], 0), (long long)A.max_pages << A.page_bits) : 0;
+        tiles = (fresh * A.g + rows_of_a_tile - 1) / rows_of_a_tile;
+    }
+};
+
+// Requests' own keys in parts.  The host does not know the lengths, so it starts own_groups workgroups, and each finds the part that is its own: of `tiles` tiles of
+// rows (with their heads) and K keys for all of them, (own_groups - tiles) / K parts to a key and one to a tile for what is left are no more than there are workgroups.
+// One long request among short ones is in as many parts as its keys are worth (64 requests of about 100 bfloat16 keys, one of 65536, 8 heads: 71 us, with equally many parts
+// to each 528), and there are few workgroups without any (tables for 65536 keys, all requests short: 30 and 35 us).
+// A wavefront looks at 256 requests at a time, four neighbours to a lane.  Rows are left at none if there is no part for workgroup `id`.
+template <int N> __device__ __forceinline__ void deal(const AttendArgs& A, int id, int rows_of_a_tile, RowsOf* rows, int* head, int* split, int* parts, int* per)
+{
+    const int lane = (int)threadIdx.x % kWave;
+    float keys = 0.f;
+    for (int b0 = lane * N; b0 < A.B; b0 += kWave * N)
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const Request q(A, min(b0 + k, A.B - 1), rows_of_a_tile);
+            keys += b0 + k < A.B ? (float)q.tiles * (float)q.length : 0.f;
+        }
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) keys += __shfl_xor(keys, d);
+    // (below the quotient by more than all roundings together, since the sum is over 1024 requests at most, 22 additions deep, so that the parts do not outgrow
+    // the workgroups)
+    const float dense = fminf((float)(A.own_groups - A.own_tiles * A.Hk) / (keys * (float)A.Hk), 1.f / (float)A.own_least) * (1.f - 0x1p-16f);
+    if (id == 0 && threadIdx.x == 0) *A.dense = dense;
+    int before = 0;          // (no more than `id`)
+    for (int b0 = 0; b0 < A.B; b0 += kWave * N) {
+        int jobs[N], all = 0;          // (rows make up own_tiles tiles or fewer, of 64 parts at most, so that a wavefront's sum has room)
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const Request q(A, min(b0 + lane * N + k, A.B - 1), rows_of_a_tile);
+            jobs[k] = b0 + lane * N + k < A.B ? q.tiles * parts_of(A, q.length, dense) * A.Hk : 0;
+            all += jobs[k];
+        }
+        int upto = all;
+#pragma unroll
+        for (int d = 1; d < kWave; d *= 2) {
+            const int o = __shfl_up(upto, d);
+            if (lane >= d) upto += o;
+        }
+        const unsigned long long in = __ballot(before + upto > id);
+        if (in) {
+            const int at = __ffsll((long long)in) - 1;
+            int j = __builtin_amdgcn_readfirstlane(id - before - __shfl(upto - all, at)), b = b0 + at * N;
+#pragma unroll
+            for (int k = 0; k < N - 1; ++k) {
+                const int n = __builtin_amdgcn_readfirstlane(__shfl(jobs[k], at));
+                if (b != b0 + at * N + k || j < n) continue;
+                j -= n;
+                ++b;
+            }
+            const Request q(A, b, rows_of_a_tile);
+            *parts = parts_of(A, q.length, dense);
+            *per = keys_of_part(q.length, *parts);
+            *head = j % A.Hk;
+            *split = j / A.Hk % *parts;
+            *rows = {j / A.Hk / *parts * rows_of_a_tile, q.fresh * A.g, q.token0, q.length, q.fresh, b};
+            return;
+        }
+        before += __builtin_amdgcn_readfirstlane(__shfl(upto, kWave - 1));
+    }
+}
 
 // What a workgroup has to do: its rows, its keys, and where its results go.  ROWS: of a tile
 template <typename T, int ROWS> struct Job {
     const AttendArgs& A;
-    int id, split, parts, head;        // parts: of its keys, if those are a request's
+    int id, split, parts, head, per;   // parts: of its keys, if those are a request's; keys of one
     bool prefix, direct;
     RowsOf rows;
 
-    __device__ __forceinline__ Job(const AttendArgs& args, int id_, bool prefix_job) : A(args), id(id_), parts(args.own_splits), prefix(prefix_job)
+    __device__ __forceinline__ Job(const AttendArgs& args, int id_, bool prefix_job) : A(args), id(id_), split(0), parts(args.own_splits), head(0), per(0), prefix(prefix_job)
     {
-        int tile_and_head = id;
-        split = prefix ? id / A.Hk / A.prefix_tiles : A.whole ? 0 : id / A.Hk % A.own_splits;
-        if (A.whole && id >= A.cut) {
-            tile_and_head = A.cut + (id - A.cut) / A.tail_splits;
-            split = (id - A.cut) % A.tail_splits;
-            parts = A.tail_splits;
+        if (!prefix && !A.whole && A.own_splits > 1) {
+            rows = {0, 0, 0, 0, 0, 0};
+            if (A.B <= kWave) deal<1>(A, id, ROWS, &rows, &head, &split, &parts, &per);
+            else deal<4>(A, id, ROWS, &rows, &head, &split, &parts, &per);
+            parts = __builtin_amdgcn_readfirstlane(parts);
+            direct = A.prefix_splits == 0 && parts == 1;
+        } else {
+            int tile_and_head = id;
+            split = prefix ? id / A.Hk / A.prefix_tiles : 0;
+            if (A.whole && id >= A.cut) {
+                tile_and_head = A.cut + (id - A.cut) / A.tail_splits;
+                split = (id - A.cut) % A.tail_splits;
+                parts = A.tail_splits;
+            }
+            direct = A.direct && parts == 1;
+            head = tile_and_head % A.Hk;
+            const int tile = tile_and_head / A.Hk;
+            rows = prefix ? RowsOf::of_prefix(A, tile % A.prefix_tiles * ROWS) : RowsOf::of_tile(A, tile, ROWS);
         }
-        direct = A.direct && parts == 1;
-        head = tile_and_head % A.Hk;
-        const int tile = tile_and_head / A.Hk;
-        rows = prefix ? RowsOf::of_prefix(A, tile % A.prefix_tiles * ROWS) : RowsOf::of_tile(A, A.whole ? tile : tile / A.own_splits, ROWS);
+        // (scalars, also where lanes have found them together)
+        for (int* v : {&split, &head, &per, &rows.r0, &rows.count, &rows.token0, &rows.length, &rows.fresh, &rows.b}) *v = __builtin_amdgcn_readfirstlane(*v);
     }
-    __device__ __forceinline__ bool none() const { return rows.r0 < 0 || rows.r0 >= rows.count; }
+    __device__ __forceinline__ bool none() const { return rows.none(); }
     // of [T][Hq]; own keys that it sees
     __device__ __forceinline__ long long row(int at) const
     {
@@ -203,22 +303,22 @@ template <typename T, int ROWS> struct Job {
     }
     __device__ __forceinline__ int sees(int at) const
     {
-        const int r = rows.r0 + at;
-        return r < rows.count ? min(max(rows.length - rows.fresh + r / A.g + 1, 0), rows.length) : 0;
+        return rows.sees(A, at);
     }
     // Its keys, the prefix's or the request's own; those below `least` are seen by all of its rows
     __device__ __forceinline__ void keys(int own, int* begin, int* end, int* least) const
     {
-        const int own_end = sees(min(ROWS, rows.count - rows.r0) - 1);
+        const int own_end = rows.end(A, ROWS);
         *begin = 0;
         *end = own ? own_end : A.prefix;
         if (prefix) {
             *begin = split * A.prefix_per;
             *end = min(*begin + A.prefix_per, A.prefix);
         } else if (parts > 1) {
-            // equal parts of its own keys, or of those behind the prefix's (below 2^31 together)
-            const int before = A.whole ? A.prefix : 0, all = before + own_end, per = (int)(((unsigned)all + parts - 1) / parts + 127) / 128 * 128;
-            const int from = (int)min((long long)split * per, (long long)all) - (own ? before : 0), to = (int)min((long long)split * per + per, (long long)all) - (own ? before : 0);
+            // parts of its own keys, or equal ones of those behind the prefix's (below 2^31 together)
+            const int before = A.whole ? A.prefix : 0, all = before + own_end;
+            const int n = A.whole ? (int)(((unsigned)all + parts - 1) / parts + 127) / 128 * 128 : per;
+            const int from = (int)min((long long)split * n, (long long)all) - (own ? before : 0), to = (int)min((long long)split * n + n, (long long)all) - (own ? before : 0);
             *begin = max(from, 0);
             *end = min(to, *end);
         }
@@ -864,6 +964,26 @@ template <typename T, int DP, int PREFIX, int OWN> __global__ __launch_bounds__(
 
 constexpr int kMaxParts = 128;
 
+// Parts of a token's own keys that there are
+__device__ __forceinline__ int own_parts(const AttendArgs& A, int token)
+{
+    if (A.own_splits <= 1) return A.own_splits;
+    int b = token;
+    if (A.rows) {          // the last request that starts at this token or before it; 64 are looked at in each step
+        int lo = 0, hi = A.B;
+        const int lane = (int)threadIdx.x % kWave;
+        while (hi - lo > 1) {
+            const int step = (hi - lo + kWave - 1) / kWave, c = lo + lane * step, n = __popcll(__ballot(c < hi && A.rows[c] <= token));
+            const int at = lo + (n ? n - 1 : 0) * step;
+            hi = min(hi, at + step);
+            lo = at;
+        }
+        b = lo;
+    }
+    const int length = (int)min((long long)max(A.lengths[b], 0), (long long)A.max_pages << A.page_bits);
+    return parts_of(A, length, *A.dense);
+}
+
 // Joins a row's parts: WAVES wavefronts to a row, lanes in groups of D / 4 (up to a power of two) that take every so manieth part; added part by part
 // within a group, then over the groups and the wavefronts in a fixed tree.  All of the parts' sums are fetched at once, and the products of four at a time.
 template <typename T, int LANES, int WAVES> __global__ __launch_bounds__(kThreads) void attend_join(const AttendArgs A)
@@ -871,11 +991,13 @@ template <typename T, int LANES, int WAVES> __global__ __launch_bounds__(kThread
     constexpr int GROUPS = kWave / LANES, STEP = GROUPS * WAVES, AHEAD = 4;
     __shared__ float weights[4][kMaxParts];
     __shared__ f32x4 joined[WAVES == 1 ? 1 : 4][LANES];
-    const int w = (int)threadIdx.x / kWave, lane = (int)threadIdx.x % kWave, parts = A.prefix_splits + A.own_splits;
+    const int w = (int)threadIdx.x / kWave, lane = (int)threadIdx.x % kWave;
     const long long r = (long long)blockIdx.x * (4 / WAVES) + (WAVES == 1 ? w : 0);
     const int token = (int)((unsigned)r / (unsigned)A.Hq);          // (rows are fewer than 2^26)
     const long long end = A.rows ? min(max((long long)A.rows[A.B], 0ll), A.T) : A.T, all = A.T * A.Hq;
     if (token >= end) return;                                       // (with several wavefronts to a row, all of the workgroup)
+    const int parts = A.prefix_splits + own_parts(A, token);
+    if (parts == 1 && A.prefix_splits == 0) return;                 // (stored already)
     float top = -INFINITY;
     float2 ml[kMaxParts / kWave];
 #pragma unroll

@@ -11,7 +11,7 @@ constexpr int kMaxHeads = 1 << 10, kMaxRequests = 1 << 20, kMaxPage = 1024, kMax
 constexpr long long kMaxKeys = 1ll << 30, kMaxRows = 1ll << 26;          // rows: heads of tokens
 
 struct Plan {
-    int prefix_kind, own_kind, prefix_splits, prefix_per, own_splits, prefix_tiles, own_tiles, whole, tail_splits;
+    int prefix_kind, own_kind, prefix_splits, prefix_per, own_splits, own_least, own_groups, prefix_tiles, own_tiles, whole, tail_splits;
     long long prefix_jobs, jobs, cut;
     int parts() const { return prefix_splits + own_splits; }
 };
@@ -21,6 +21,8 @@ bool sizes_fit(long long T, int B, int Hq, int Hk, int D, long long prefix, long
     if (T < 0 || B < 0 || B > kMaxRequests || Hk < 1 || Hq < Hk || Hq > kMaxHeads || Hq % Hk != 0 || D < 8 || D > 256 || D % 8 != 0) return false;
     return T <= (kMaxRows - 4) / Hq && (long long)B * Hk <= (1 << 22) && prefix >= 0 && prefix < kMaxKeys && capacity >= 0 && capacity < kMaxKeys;
 }
+
+constexpr size_t kDense = 256;          // bytes of workspace for AttendArgs::dense
 
 long long up(long long a, long long b) { return (a + b - 1) / b; }
 
@@ -72,13 +74,19 @@ Plan plan(long long T, int B, int Hq, int Hk, int D, int line, int elem, long lo
         return p;
     }
     p.own_splits = prefix ? 0 : 1;         // (without any keys rows are zero)
-    // Parts of a request's keys: so many that requests of unequal length, which the host does not know, keep the device busy to the end (512, 1024 and 2048
-    // workgroups: 4 requests of up to 131072 bfloat16 keys, 8 heads, 303, 295 and 293 us; 64 of up to 2048, 98, 100 and 105; 24 of up to 1500 float keys, 20 heads, 97, 97 and 100)
+    // Parts of a request's keys, whose number goes by the lengths, which the host does not know (see deal()): two rounds of the 512 workgroups that the device holds
+    // at a time, or 512 more than there are tiles (768 workgroups in all: 24 drafts of up to 1500 float keys, 20 heads, 98 us, 1024: 90; 64 requests of 100
+    // bfloat16 keys of which one has 65536, 81 and 73).  With many tiles one part to each is quicker where requests are alike, and no one's end is waited for where
+    // they are not (256 requests of 8 heads, one part and several: 2000 keys each 357 and 369 us, 200 keys 52 and 68, one of 32768 among those 532 and 95; with 2000
+    // requests of one head 188 and 251, 51 and 123, 376 and 125), so it is both up to 2048 tiles and 1024 requests.  A part has 128 keys or more where tiles are few,
+    // 512 where they are many.
+    const long long tiles = own_tiles * Hk;
+    p.own_least = tiles <= 64 ? 128 : tiles <= 128 ? 256 : 512;
     if (capacity) {
-        long long s = 1024 / (own_tiles * Hk);
-        if (s > up(capacity, 256)) s = up(capacity, 256);
-        p.own_splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+        const long long s = up(capacity, p.own_least);
+        p.own_splits = (int)(tiles > 2048 || B > 1024 ? 1 : s > 64 ? 64 : s);
     }
+    p.own_groups = (int)(p.own_splits > 1 ? (tiles <= 512 ? 512 : tiles) + 512 : tiles * p.own_splits);
     // Parts of the prefix: a workgroup for each compute unit, which leaves room for one that reads beside it (64 rows, 32768 bfloat16 keys of 8 heads, 128, 256, 512 and
     // 1024 workgroups: 112, 98, 105 and 130 us); with few rows reading is all there is to do, as above
     if (prefix) {
@@ -89,7 +97,7 @@ Plan plan(long long T, int B, int Hq, int Hk, int D, int line, int elem, long lo
         p.prefix_splits = (int)up(prefix, p.prefix_per);
     }
     p.prefix_jobs = (long long)p.prefix_tiles * p.prefix_splits * Hk;
-    p.jobs = p.prefix_jobs + own_tiles * p.own_splits * Hk;
+    p.jobs = p.prefix_jobs + p.own_groups;
     return p;
 }
 
@@ -97,7 +105,7 @@ Plan plan(long long T, int B, int Hq, int Hk, int D, int line, int elem, long lo
 size_t scratch(const Plan& p, long long T, int Hq, int D, int line, int elem)
 {
     const long long rows = p.whole ? (p.jobs - p.cut) * rows_of(p.own_kind, line, elem) : p.parts() <= 1 ? 0 : p.parts() * T * Hq;
-    return (size_t)rows * (D + 2) * sizeof(float);
+    return (size_t)rows * (D + 2) * sizeof(float) + (p.own_splits > 1 ? kDense : 0);
 }
 
 }  // namespace
@@ -152,12 +160,14 @@ cgbn_status cgbn_prefix_attention(const void* q, long long ldq, long long T, int
     const size_t need = scratch(p, T, Hq, D, line, elem);
     if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need)) return CGBN_ERR_WORKSPACE;
     A.part_o = static_cast<float*>(workspace);
-    A.part_ml = reinterpret_cast<float2*>(A.part_o + need / sizeof(float) / (D + 2) * D);
+    const size_t part_rows = (p.own_splits > 1 ? need - kDense : need) / sizeof(float) / (D + 2);
+    A.part_ml = reinterpret_cast<float2*>(A.part_o + part_rows * D);
+    A.dense = reinterpret_cast<float*>(A.part_ml + part_rows);
     A.q = static_cast<const char*>(q); A.k_pages = static_cast<const char*>(k_pages); A.v_pages = static_cast<const char*>(v_pages);
     A.out = static_cast<char*>(out); A.lse = lse; A.rows = rows; A.lengths = lengths; A.prefix_table = prefix_table; A.table = table;
     A.ldq = ldq; A.ldo = ldo; A.T = T; A.B = B; A.Hq = Hq; A.Hk = Hk; A.g = Hq / Hk; A.D = D; A.pages = pages; A.prefix = prefix; A.max_pages = max_pages;
     while ((1 << A.page_bits) < page) ++A.page_bits;
-    A.prefix_splits = p.prefix_splits; A.prefix_per = p.prefix_per; A.own_splits = p.own_splits; A.prefix_tiles = p.prefix_tiles; A.own_tiles = p.own_tiles;
+    A.prefix_splits = p.prefix_splits; A.prefix_per = p.prefix_per; A.own_splits = p.own_splits; A.own_least = p.own_least; A.own_groups = p.own_groups; A.prefix_tiles = p.prefix_tiles; A.own_tiles = p.own_tiles;
     A.prefix_jobs = (int)p.prefix_jobs; A.jobs = (int)p.jobs; A.whole = p.whole; A.cut = (int)p.cut; A.tail_splits = p.tail_splits; A.direct = p.parts() <= 1; A.scale = scale * 1.4426950408889634f;
     hipStream_t st = static_cast<hipStream_t>(stream);
     return dtype == CGBN_F32 ? launch_attend<float>(A, p.prefix_kind, p.own_kind, st) : launch_attend<bf16_t>(A, p.prefix_kind, p.own_kind, st);

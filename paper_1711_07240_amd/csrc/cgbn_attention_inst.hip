@@ -24,11 +24,11 @@ template <typename T, int DP> static void launch_width(const AttendArgs& A, int 
 #undef CGBN_CASE
 }
 
-// a workgroup to a row where it has many parts
+// a workgroup to a row where it may have many parts, and rows are few enough for that
 template <typename T, int LANES> static void launch_join(const AttendArgs& A, hipStream_t st)
 {
     const long long rows = A.T * A.Hq;
-    if (A.prefix_splits + A.own_splits > 8 && rows < (1 << 20)) hipLaunchKernelGGL((attend_join<T, LANES, 4>), dim3((unsigned)rows), dim3(kThreads), 0, st, A);
+    if (A.prefix_splits + A.own_splits > 8 && rows < (1 << 14)) hipLaunchKernelGGL((attend_join<T, LANES, 4>), dim3((unsigned)rows), dim3(kThreads), 0, st, A);
     else hipLaunchKernelGGL((attend_join<T, LANES, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(kThreads), 0, st, A);
 }
 

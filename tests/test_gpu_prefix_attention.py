@@ -99,6 +99,39 @@ def test_long_keys_in_many_parts(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("prefix", [0, 300])
+@pytest.mark.parametrize("B,most", [(3, 30000), (64, 9000), (65, 9000), (300, 6001), (1024, 5000), (1025, 3000)])
+def test_one_request_much_longer_than_the_others(B, most, prefix, dtype):
+    """Keys are dealt to workgroups by the lengths, which only the device knows; among the others are requests without keys and without new tokens."""
+    rng = np.random.default_rng(B)
+    lengths = [int(n) for n in rng.integers(0, 90, B)]
+    lengths[B // 3] = most
+    a = Attention(dtype, [1] * B, lengths, prefix, 16, 4, 2, 32)
+    got = a.call(single=True)
+    a.check(*got)
+    assert all(torch.equal(x, y) for x, y in zip(got, a.call(single=True)))
+    fresh = [int(n) for n in rng.integers(0, 4, B)]
+    fresh[B // 3] = 3
+    a = Attention(dtype, fresh, [n + m for n, m in zip(fresh, lengths)], prefix, 16, 4, 2, 32, pad=2)
+    a.check(*a.call())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("fresh", [[7, 0, 90, 1], [300, 2, 1, 33]])
+def test_a_long_request_with_many_new_tokens(fresh, dtype):
+    a = Attention(dtype, fresh, [fresh[0] + 5000, 40, fresh[2], 700], 600, 16, 4, 2, 40, pad=1)
+    a.check(*a.call(), rows=[0, 1, 6, 15, 16, 31, 32, 63, 64, 89, 127, 128, 255, 299])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lengths", [[128] * 64, [129] * 64, [512, 513, 1, 0] * 16, [2048] * 16, [16, 32, 48, 640] * 32])
+def test_lengths_at_the_ends_of_parts(lengths, dtype):
+    """In tables with room for far more; a request of one part is stored without a join."""
+    a = Attention(dtype, [1] * len(lengths), lengths, 0, 16, 8, 4, 32, extra=3000)
+    a.check(*a.call(single=True))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_many_requests(dtype):
     rng = np.random.default_rng(5)
     fresh = [int(n) for n in rng.integers(0, 4, 150)]
