@@ -32,15 +32,16 @@ struct AttendArgs {
     const char *q, *k_pages, *v_pages;
     char* out;
     float* lse;                        // may be null
-    float* part_o;                     // [parts][T][Hq][D], not divided by l
-    float2* part_ml;                   // [parts][T][Hq]
+    float* part_o;                     // [parts][T][Hq][D], not divided by l; where own keys are dealt theirs are behind the prefix's, [workgroup][row of a tile][D]
+    float2* part_ml;                   // the same of two
     const int *rows, *lengths, *prefix_table, *table;
     long long ldq, ldo, T;             // elements from row to row
     int B, Hq, Hk, g, D, pages, page_bits, prefix, max_pages;
     int prefix_splits, prefix_per;
     int own_splits, own_least;         // parts of a request's own keys at most, and keys of a part at least
     int own_groups;                    // workgroups for them
-    float* dense;                      // workspace: parts to a key, as the lengths have it, see deal()
+    float* dense;                      // workspace: parts to a key, as the lengths have it, see deal(); [B]: a request's first workgroup
+    int* own_first;
     int prefix_tiles, own_tiles;       // tiles of rows
     int prefix_jobs, jobs;             // workgroups, those of the prefix first
     int whole;                         // a workgroup takes the prefix and then its request's own keys
@@ -251,6 +252,7 @@ template <int N> __device__ __forceinline__ void deal(const AttendArgs& A, int i
                 j -= n;
                 ++b;
             }
+            if (j == 0 && threadIdx.x == 0) A.own_first[b] = id;
             const Request q(A, b, rows_of_a_tile);
             *parts = parts_of(A, q.length, dense);
             *per = keys_of_part(q.length, *parts);
@@ -330,7 +332,8 @@ template <typename T, int ROWS> struct Job {
     __device__ __forceinline__ long long part_row(long long r, int at) const
     {
         if (A.whole) return (long long)(id - A.cut) * ROWS + at;
-        return (long long)(prefix ? split : A.prefix_splits + split) * A.T * A.Hq + r;
+        if (!prefix && A.own_splits > 1) return (long long)A.prefix_splits * A.T * A.Hq + (long long)id * ROWS + at;
+        return (long long)(prefix ? split : A.prefix_splits) * A.T * A.Hq + r;
     }
     __device__ __forceinline__ char* place(long long r, int at) const
     {
@@ -964,29 +967,46 @@ template <typename T, int DP, int PREFIX, int OWN> __global__ __launch_bounds__(
 
 constexpr int kMaxParts = 128;
 
-// Parts of a token's own keys that there are
-__device__ __forceinline__ int own_parts(const AttendArgs& A, int token)
-{
-    if (A.own_splits <= 1) return A.own_splits;
-    int b = token;
-    if (A.rows) {          // the last request that starts at this token or before it; 64 are looked at in each step
-        int lo = 0, hi = A.B;
-        const int lane = (int)threadIdx.x % kWave;
-        while (hi - lo > 1) {
-            const int step = (hi - lo + kWave - 1) / kWave, c = lo + lane * step, n = __popcll(__ballot(c < hi && A.rows[c] <= token));
-            const int at = lo + (n ? n - 1 : 0) * step;
-            hi = min(hi, at + step);
-            lo = at;
+// A row's parts: the prefix's, and those of own keys that there are
+struct PartsOf {
+    int prefix, all, step;             // parts; rows from one of own keys to the next
+    long long first, next, row;        // rows: of the first part of own keys; from one of the prefix to the next; in the prefix's
+    __device__ __forceinline__ PartsOf(const AttendArgs& A, long long r, int token, int rows_of_a_tile)
+    {
+        next = A.T * A.Hq;
+        row = r;
+        prefix = A.prefix_splits;
+        first = prefix * next + r;
+        step = 0;
+        all = prefix + A.own_splits;
+        if (A.own_splits <= 1) return;
+        int b = token, token0 = token;
+        if (A.rows) {          // the last request that starts at this token or before it; 64 are looked at in each step
+            int lo = 0, hi = A.B;
+            const int lane = (int)threadIdx.x % kWave;
+            while (hi - lo > 1) {
+                const int step = (hi - lo + kWave - 1) / kWave, c = lo + lane * step, n = __popcll(__ballot(c < hi && A.rows[c] <= token));
+                const int at = lo + (n ? n - 1 : 0) * step;
+                hi = min(hi, at + step);
+                lo = at;
+            }
+            b = lo;
+            token0 = min(max(A.rows[b], 0), token);
         }
-        b = lo;
+        const int length = (int)min((long long)max(A.lengths[b], 0), (long long)A.max_pages << A.page_bits), parts = parts_of(A, length, *A.dense);
+        const int h = (int)(r - (long long)token * A.Hq), head = h / A.g, i = (token - token0) * A.g + h - head * A.g, tile = i / rows_of_a_tile;
+        all = prefix + parts;
+        // (no workgroup behind the last one, whatever `rows` are)
+        const int job = parts ? min(max(A.own_first[b] + tile * parts * A.Hk + head, 0), max(A.own_groups - (parts - 1) * A.Hk - 1, 0)) : 0;
+        first = prefix * next + (long long)job * rows_of_a_tile + (i - tile * rows_of_a_tile);
+        step = A.Hk * rows_of_a_tile;
     }
-    const int length = (int)min((long long)max(A.lengths[b], 0), (long long)A.max_pages << A.page_bits);
-    return parts_of(A, length, *A.dense);
-}
+    __device__ __forceinline__ long long at(int p) const { return p < prefix ? p * next + row : first + (long long)(p - prefix) * step; }
+};
 
 // Joins a row's parts: WAVES wavefronts to a row, lanes in groups of D / 4 (up to a power of two) that take every so manieth part; added part by part
 // within a group, then over the groups and the wavefronts in a fixed tree.  All of the parts' sums are fetched at once, and the products of four at a time.
-template <typename T, int LANES, int WAVES> __global__ __launch_bounds__(kThreads) void attend_join(const AttendArgs A)
+template <typename T, int LANES, int WAVES> __global__ __launch_bounds__(kThreads) void attend_join(const AttendArgs A, int rows_of_a_tile)
 {
     constexpr int GROUPS = kWave / LANES, STEP = GROUPS * WAVES, AHEAD = 4;
     __shared__ float weights[4][kMaxParts];
@@ -994,16 +1014,17 @@ template <typename T, int LANES, int WAVES> __global__ __launch_bounds__(kThread
     const int w = (int)threadIdx.x / kWave, lane = (int)threadIdx.x % kWave;
     const long long r = (long long)blockIdx.x * (4 / WAVES) + (WAVES == 1 ? w : 0);
     const int token = (int)((unsigned)r / (unsigned)A.Hq);          // (rows are fewer than 2^26)
-    const long long end = A.rows ? min(max((long long)A.rows[A.B], 0ll), A.T) : A.T, all = A.T * A.Hq;
+    const long long end = A.rows ? min(max((long long)A.rows[A.B], 0ll), A.T) : A.T;
     if (token >= end) return;                                       // (with several wavefronts to a row, all of the workgroup)
-    const int parts = A.prefix_splits + own_parts(A, token);
+    const PartsOf of(A, r, token, rows_of_a_tile);
+    const int parts = of.all;
     if (parts == 1 && A.prefix_splits == 0) return;                 // (stored already)
     float top = -INFINITY;
     float2 ml[kMaxParts / kWave];
 #pragma unroll
     for (int k = 0; k < kMaxParts / kWave; ++k) {
         ml[k] = make_float2(-INFINITY, 0.f);
-        if (k * kWave + lane < parts) ml[k] = A.part_ml[(k * kWave + lane) * all + r];
+        if (k * kWave + lane < parts) ml[k] = A.part_ml[of.at(k * kWave + lane)];
         if (ml[k].y != 0.f) top = fmaxf(top, ml[k].x);
     }
     top = row_max(top);
@@ -1030,7 +1051,7 @@ template <typename T, int LANES, int WAVES> __global__ __launch_bounds__(kThread
         for (int k = 0; k < AHEAD; ++k) {
             const int p = p0 + k * STEP;
             f[k] = p < parts ? weights[w][p] : -1.f;
-            if (f[k] != -1.f && d < A.D) v[k] = *reinterpret_cast<const f32x4*>(A.part_o + (p * all + r) * A.D + d);
+            if (f[k] != -1.f && d < A.D) v[k] = *reinterpret_cast<const f32x4*>(A.part_o + of.at(p) * A.D + d);
             else v[k] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
 #pragma unroll

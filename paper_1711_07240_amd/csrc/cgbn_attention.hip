@@ -22,8 +22,6 @@ bool sizes_fit(long long T, int B, int Hq, int Hk, int D, long long prefix, long
     return T <= (kMaxRows - 4) / Hq && (long long)B * Hk <= (1 << 22) && prefix >= 0 && prefix < kMaxKeys && capacity >= 0 && capacity < kMaxKeys;
 }
 
-constexpr size_t kDense = 256;          // bytes of workspace for AttendArgs::dense
-
 long long up(long long a, long long b) { return (a + b - 1) / b; }
 
 // What the device has to know of the lengths stays there: ranges of a request's own keys are cut by its length where they are read, `own_splits` of
@@ -101,11 +99,16 @@ Plan plan(long long T, int B, int Hq, int Hk, int D, int line, int elem, long lo
     return p;
 }
 
-// bytes of the parts
-size_t scratch(const Plan& p, long long T, int Hq, int D, int line, int elem)
+// Rows of the parts: where own keys are dealt, a tile for each workgroup, as most requests have far fewer parts than there may be (256 requests of 64 heads in
+// tables for 65536 keys: 21 MB, with room for 64 parts of each 545 MB); bytes
+long long part_rows(const Plan& p, long long T, int Hq, int line, int elem)
 {
-    const long long rows = p.whole ? (p.jobs - p.cut) * rows_of(p.own_kind, line, elem) : p.parts() <= 1 ? 0 : p.parts() * T * Hq;
-    return (size_t)rows * (D + 2) * sizeof(float) + (p.own_splits > 1 ? kDense : 0);
+    const int tile = rows_of(p.own_kind, line, elem);
+    return p.whole ? (p.jobs - p.cut) * tile : p.own_splits > 1 ? p.prefix_splits * T * Hq + (long long)p.own_groups * tile : p.parts() <= 1 ? 0 : p.parts() * T * Hq;
+}
+size_t scratch(const Plan& p, long long T, int B, int Hq, int D, int line, int elem)
+{
+    return (size_t)part_rows(p, T, Hq, line, elem) * (D + 2) * sizeof(float) + (p.own_splits > 1 ? (1 + (size_t)B) * sizeof(int) : 0);
 }
 
 }  // namespace
@@ -121,9 +124,9 @@ size_t cgbn_prefix_attention_workspace_bytes(long long T, int B, int Hq, int Hk,
     if (T == 0 || B == 0) return 256;
     const int elem = dtype == CGBN_F32 ? 4 : 2, line = line_of(width_of(D), elem);
     // requests of one row each go in other tiles when it is said that they are
-    size_t most = scratch(plan(T, B, Hq, Hk, D, line, elem, prefix, capacity, true), T, Hq, D, line, elem);
+    size_t most = scratch(plan(T, B, Hq, Hk, D, line, elem, prefix, capacity, true), T, B, Hq, D, line, elem);
     if (T == B) {
-        const size_t single = scratch(plan(T, B, Hq, Hk, D, line, elem, prefix, capacity, false), T, Hq, D, line, elem);
+        const size_t single = scratch(plan(T, B, Hq, Hk, D, line, elem, prefix, capacity, false), T, B, Hq, D, line, elem);
         if (single > most) most = single;
     }
     const size_t bytes = (most + 255) / 256 * 256;
@@ -157,12 +160,13 @@ cgbn_status cgbn_prefix_attention(const void* q, long long ldq, long long T, int
     if (p.jobs >= (1ll << 24)) return CGBN_ERR_SHAPE;           // 2^32 threads
     AttendArgs A;
     std::memset(&A, 0, sizeof(A));
-    const size_t need = scratch(p, T, Hq, D, line, elem);
+    const size_t need = scratch(p, T, B, Hq, D, line, elem);
     if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need)) return CGBN_ERR_WORKSPACE;
     A.part_o = static_cast<float*>(workspace);
-    const size_t part_rows = (p.own_splits > 1 ? need - kDense : need) / sizeof(float) / (D + 2);
-    A.part_ml = reinterpret_cast<float2*>(A.part_o + part_rows * D);
-    A.dense = reinterpret_cast<float*>(A.part_ml + part_rows);
+    const long long of_parts = part_rows(p, T, Hq, line, elem);
+    A.part_ml = reinterpret_cast<float2*>(A.part_o + of_parts * D);
+    A.dense = reinterpret_cast<float*>(A.part_ml + of_parts);
+    A.own_first = reinterpret_cast<int*>(A.dense + 1);
     A.q = static_cast<const char*>(q); A.k_pages = static_cast<const char*>(k_pages); A.v_pages = static_cast<const char*>(v_pages);
     A.out = static_cast<char*>(out); A.lse = lse; A.rows = rows; A.lengths = lengths; A.prefix_table = prefix_table; A.table = table;
     A.ldq = ldq; A.ldo = ldo; A.T = T; A.B = B; A.Hq = Hq; A.Hk = Hk; A.g = Hq / Hk; A.D = D; A.pages = pages; A.prefix = prefix; A.max_pages = max_pages;

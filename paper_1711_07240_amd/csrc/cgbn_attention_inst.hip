@@ -25,11 +25,11 @@ template <typename T, int DP> static void launch_width(const AttendArgs& A, int 
 }
 
 // a workgroup to a row where it may have many parts, and rows are few enough for that
-template <typename T, int LANES> static void launch_join(const AttendArgs& A, hipStream_t st)
+template <typename T, int LANES> static void launch_join(const AttendArgs& A, int tile, hipStream_t st)
 {
     const long long rows = A.T * A.Hq;
-    if (A.prefix_splits + A.own_splits > 8 && rows < (1 << 14)) hipLaunchKernelGGL((attend_join<T, LANES, 4>), dim3((unsigned)rows), dim3(kThreads), 0, st, A);
-    else hipLaunchKernelGGL((attend_join<T, LANES, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(kThreads), 0, st, A);
+    if (A.prefix_splits + A.own_splits > 8 && rows < (1 << 14)) hipLaunchKernelGGL((attend_join<T, LANES, 4>), dim3((unsigned)rows), dim3(kThreads), 0, st, A, tile);
+    else hipLaunchKernelGGL((attend_join<T, LANES, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(kThreads), 0, st, A, tile);
 }
 
 template <> cgbn_status launch_attend<CGBN_INST_T>(const AttendArgs& A, int prefix, int own, hipStream_t st)
@@ -44,17 +44,17 @@ template <> cgbn_status launch_attend<CGBN_INST_T>(const AttendArgs& A, int pref
     default: launch_width<T, 256>(A, prefix, own, st);
     }
     if (hipGetLastError() != hipSuccess) return CGBN_ERR_HIP;
+    const int tile = rows_of(own, line_of(width_of(A.D), sizeof(T)), sizeof(T));
     if (A.whole && A.tail_splits > 1) {
-        const int rows = rows_of(own, line_of(width_of(A.D), sizeof(T)), sizeof(T));
         const int tiles = (A.jobs - A.cut) / A.tail_splits;
-        hipLaunchKernelGGL(attend_join_tail<T>, dim3((unsigned)(tiles * (rows / kTailRows))), dim3(kThreads), 0, st, A, rows);
+        hipLaunchKernelGGL(attend_join_tail<T>, dim3((unsigned)(tiles * (tile / kTailRows))), dim3(kThreads), 0, st, A, tile);
         if (hipGetLastError() != hipSuccess) return CGBN_ERR_HIP;
     }
     if (!A.direct) {
-        if (A.D <= 32) launch_join<T, 8>(A, st);
-        else if (A.D <= 64) launch_join<T, 16>(A, st);
-        else if (A.D <= 128) launch_join<T, 32>(A, st);
-        else launch_join<T, 64>(A, st);
+        if (A.D <= 32) launch_join<T, 8>(A, tile, st);
+        else if (A.D <= 64) launch_join<T, 16>(A, tile, st);
+        else if (A.D <= 128) launch_join<T, 32>(A, tile, st);
+        else launch_join<T, 64>(A, tile, st);
         if (hipGetLastError() != hipSuccess) return CGBN_ERR_HIP;
     }
     return CGBN_OK;

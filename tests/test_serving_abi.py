@@ -116,6 +116,9 @@ def test_workspace_sizes():
     assert L.cgbn_prefix_attention_workspace_bytes(1, 1, 8, 8, 64, 0, 0, 7) == 0
     assert L.cgbn_page_plan_workspace_bytes(16, 16) == 256 and L.cgbn_page_plan_workspace_bytes(5000, 16) == 20224
     assert L.cgbn_page_plan_workspace_bytes(1, 1 << 20) == 512 and L.cgbn_page_plan_workspace_bytes(-1, 0) == 0
+    # many requests in tables for far more keys than most have: by the workgroups, not by the parts that each may have
+    for B, Hq, Hk in ((256, 64, 8), (1024, 64, 2), (64, 32, 8)):
+        assert L.cgbn_prefix_attention_workspace_bytes(B, B, Hq, Hk, 128, 0, 65536, "bf16") < 100 << 20
     # of one request after the other, with the workspace asked for: refused for something that is looked at later, never for it
     for T, B, rows in ((64, 64, None), (64, 64, 11 * P), (70, 9, 11 * P), (5000, 3, 11 * P)):
         n = L.cgbn_prefix_attention_workspace_bytes(T, B, 4, 2, 64, 700, 640, 1)
