@@ -151,9 +151,10 @@ __device__ __forceinline__ int request_of_tile(const AttendArgs& A, int i, int r
 // The rows of a workgroup, from r0 on of `count`: of request b, of whose `fresh` tokens token0 is the first, or of all requests (prefix)
 struct RowsOf {
     int r0, count, token0, length, fresh, b;
-    static __device__ __forceinline__ RowsOf of_prefix(const AttendArgs& A, int r0)
+    static __host__ __device__ __forceinline__ RowsOf of_prefix(const AttendArgs& A, int r0)
     {
-        const int fresh = A.rows ? (int)min(max((long long)A.rows[A.B], 0ll), A.T) : (int)A.T;
+        const long long last = A.rows ? A.rows[A.B] : A.T;
+        const int fresh = (int)(last < 0 ? 0 : last < A.T ? last : A.T);
         return {r0, fresh * A.g, 0, 0, fresh, 0};          // (T * Hq stays below 2^26)
     }
     static __device__ __forceinline__ RowsOf of_tile(const AttendArgs& A, int i, int rows_of_a_tile)
@@ -265,21 +266,40 @@ template <int N> __device__ __forceinline__ void deal(const AttendArgs& A, int i
     }
 }
 
-// What a workgroup has to do: its rows, its keys, and where its results go.  ROWS: of a tile
-template <typename T, int ROWS> struct Job {
-    const AttendArgs& A;
-    int id, split, parts, head, per;   // parts: of its keys, if those are a request's; keys of one
+// Where a workgroup's results go: they are the call's (direct), or a part.
+struct Place {
+    int id, split;
     bool prefix, direct;
+
+    // Parts of its own keys, before the lengths are looked at.  (A prefix's workgroup has none; what there are of the prefix is in A.direct.)
+    static __host__ __device__ __forceinline__ int first_parts(const AttendArgs& A, bool prefix) { return prefix ? 1 : A.own_splits; }
+    static __host__ __device__ __forceinline__ bool is_direct(const AttendArgs& A, bool prefix, int parts)
+    {
+        if (!prefix && !A.whole && A.own_splits > 1) return A.prefix_splits == 0 && parts == 1;
+        return A.direct && parts == 1;
+    }
+    // Row r of [T][Hq], `at` of this workgroup's tile: which row of the parts it is
+    __host__ __device__ __forceinline__ long long part_row(const AttendArgs& A, int rows_of_a_tile, long long r, int at) const
+    {
+        if (A.whole) return (long long)(id - A.cut) * rows_of_a_tile + at;
+        if (!prefix && A.own_splits > 1) return (long long)A.prefix_splits * A.T * A.Hq + (long long)id * rows_of_a_tile + at;
+        return (long long)(prefix ? split : A.prefix_splits) * A.T * A.Hq + r;
+    }
+};
+
+// What a workgroup has to do: its rows, its keys, and where its results go.  ROWS: of a tile
+template <typename T, int ROWS> struct Job : Place {
+    const AttendArgs& A;
+    int parts, head, per;              // parts: of its keys, if those are a request's; keys of one
     RowsOf rows;
 
-    __device__ __forceinline__ Job(const AttendArgs& args, int id_, bool prefix_job) : A(args), id(id_), split(0), parts(args.own_splits), head(0), per(0), prefix(prefix_job)
+    __device__ __forceinline__ Job(const AttendArgs& args, int id_, bool prefix_job) : Place{id_, 0, prefix_job, false}, A(args), parts(first_parts(args, prefix_job)), head(0), per(0)
     {
         if (!prefix && !A.whole && A.own_splits > 1) {
             rows = {0, 0, 0, 0, 0, 0};
             if (A.B <= kWave) deal<1>(A, id, ROWS, &rows, &head, &split, &parts, &per);
             else deal<4>(A, id, ROWS, &rows, &head, &split, &parts, &per);
             parts = __builtin_amdgcn_readfirstlane(parts);
-            direct = A.prefix_splits == 0 && parts == 1;
         } else {
             int tile_and_head = id;
             split = prefix ? id / A.Hk / A.prefix_tiles : 0;
@@ -288,11 +308,11 @@ template <typename T, int ROWS> struct Job {
                 split = (id - A.cut) % A.tail_splits;
                 parts = A.tail_splits;
             }
-            direct = A.direct && parts == 1;
             head = tile_and_head % A.Hk;
             const int tile = tile_and_head / A.Hk;
             rows = prefix ? RowsOf::of_prefix(A, tile % A.prefix_tiles * ROWS) : RowsOf::of_tile(A, tile, ROWS);
         }
+        direct = is_direct(A, prefix, parts);
         // (scalars, also where lanes have found them together)
         for (int* v : {&split, &head, &per, &rows.r0, &rows.count, &rows.token0, &rows.length, &rows.fresh, &rows.b}) *v = __builtin_amdgcn_readfirstlane(*v);
     }
@@ -329,20 +349,14 @@ template <typename T, int ROWS> struct Job {
     __device__ __forceinline__ const int* table(int own) const { return own ? A.table + (long long)rows.b * A.max_pages : A.prefix_table; }
 
     // Where row r of [T][Hq], `at` of this workgroup, goes: to the result or to this part's place; its sums
-    __device__ __forceinline__ long long part_row(long long r, int at) const
-    {
-        if (A.whole) return (long long)(id - A.cut) * ROWS + at;
-        if (!prefix && A.own_splits > 1) return (long long)A.prefix_splits * A.T * A.Hq + (long long)id * ROWS + at;
-        return (long long)(prefix ? split : A.prefix_splits) * A.T * A.Hq + r;
-    }
     __device__ __forceinline__ char* place(long long r, int at) const
     {
         const int token = (int)((unsigned)r / (unsigned)A.Hq), h = (int)r - token * A.Hq;
-        return direct ? A.out + (token * A.ldo + h * A.D) * (long long)sizeof(T) : reinterpret_cast<char*>(A.part_o + part_row(r, at) * A.D);
+        return direct ? A.out + (token * A.ldo + h * A.D) * (long long)sizeof(T) : reinterpret_cast<char*>(A.part_o + part_row(A, ROWS, r, at) * A.D);
     }
     __device__ __forceinline__ void store_sums(long long r, int at, float m, float l) const
     {
-        if (!direct) A.part_ml[part_row(r, at)] = make_float2(m, l);
+        if (!direct) A.part_ml[part_row(A, ROWS, r, at)] = make_float2(m, l);
         else if (A.lse) A.lse[r] = l == 0.f ? -INFINITY : 0.6931471805599453f * (m + __builtin_amdgcn_logf(l));
     }
     // four values from d on
