@@ -394,7 +394,8 @@ size_t cgbn_prefix_attention_workspace_bytes(long long T, int B, int Hq, int Hk,
  * Request b's queries are rows rows[b] ... rows[b + 1] - 1 (rows[0] = 0, ascending), its last tokens: the j-th of n sees the prefix and its request's tokens up to
  * itself, the first lengths[b] - n + j + 1.  rows may be NULL: one row each, T = B.  Rows behind rows[B] are left as they were.
  * A row that sees no key is zero.  lse[T][Hq], if not NULL: the logarithm of the sum of the exponentials of a row's scores, -infinity where there is no key.
- *   Keys beyond lengths[b], in pages that are not there, or later than a row's own are not looked at, whatever their places hold.  max_pages = 0: no own tokens,
+ *   Keys beyond lengths[b], in pages that are not there, or later than a row's own are not looked at, whatever their places hold. lengths[b] may be more than
+ *   max_pages * page, as a plan's are: tokens that the table has no room for are not there, and count where a row's own token is.  max_pages = 0: no own tokens,
  *   table and lengths are not read.  Weights are rounded to bfloat16 for the products of bfloat16 tensors, their sum is not.
  * Weights times values are summed before they are divided: values above about 1e33 over the number of keys may overflow.
  *   D a multiple of 8 up to 256; rows of q and out on 16 bytes; T * Hq < 2^26 - 3, B * Hk <= 2^22. */

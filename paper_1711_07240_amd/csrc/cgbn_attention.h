@@ -148,52 +148,14 @@ __device__ __forceinline__ int request_of_tile(const AttendArgs& A, int i, int r
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// The rows of a workgroup, from r0 on of `count`: of request b, of whose `fresh` tokens token0 is the first, or of all requests (prefix)
-struct RowsOf {
-    int r0, count, token0, length, fresh, b;
-    static __host__ __device__ __forceinline__ RowsOf of_prefix(const AttendArgs& A, int r0)
-    {
-        const long long last = A.rows ? A.rows[A.B] : A.T;
-        const int fresh = (int)(last < 0 ? 0 : last < A.T ? last : A.T);
-        return {r0, fresh * A.g, 0, 0, fresh, 0};          // (T * Hq stays below 2^26)
-    }
-    static __device__ __forceinline__ RowsOf of_tile(const AttendArgs& A, int i, int rows_of_a_tile)
-    {
-        RowsOf w;
-        if (A.rows) {
-            w.b = request_of_tile(A, i, rows_of_a_tile);
-            w.token0 = (int)min(max((long long)A.rows[w.b], 0ll), A.T);
-            w.fresh = max((int)min((long long)A.rows[w.b + 1], A.T) - w.token0, 0);
-            w.r0 = (i - (int)tiles_before(A, w.b, rows_of_a_tile)) * rows_of_a_tile;
-        } else {
-            const int per = (A.g + rows_of_a_tile - 1) / rows_of_a_tile;
-            w.b = i / per;
-            w.token0 = w.b;
-            w.fresh = 1;
-            w.r0 = (i - w.b * per) * rows_of_a_tile;
-        }
-        w.count = w.fresh * A.g;
-        w.length = A.max_pages ? (int)min((long long)max(A.lengths[w.b], 0), (long long)A.max_pages << A.page_bits) : 0;
-        return w;
-    }
-    __device__ __forceinline__ bool none() const { return r0 < 0 || r0 >= count; }
-    // own keys that row `at` of the tile sees, and that all of them do together
-    __device__ __forceinline__ int sees(const AttendArgs& A, int at) const
-    {
-        const int r = r0 + at;
-        return r < count ? min(max(length - fresh + r / A.g + 1, 0), length) : 0;
-    }
-    __device__ __forceinline__ int end(const AttendArgs& A, int rows_of_a_tile) const { return sees(A, min(rows_of_a_tile, count - r0) - 1); }
-};
+// Tokens of request b's own that have a place in its row of the table: no other keys are looked at
+__host__ __device__ __forceinline__ int tokens_of(const AttendArgs& A, int b) { return A.max_pages ? max(A.lengths[b], 0) : 0; }
+__host__ __device__ __forceinline__ int keys_of_request(const AttendArgs& A, int b) { return min(tokens_of(A, b), A.max_pages << A.page_bits); }          // (below 2^30)
 
-// Parts of a request's `length` own keys, if there are to be `dense` of them to a key; keys of one: they are equal
-__device__ __forceinline__ int parts_of(const AttendArgs& A, int length, float dense) { return length ? min((int)((float)length * dense) + 1, A.own_splits) : 0; }
-__device__ __forceinline__ int keys_of_part(int length, int parts) { return ((length + parts - 1) / parts + 127) / 128 * 128; }
-
-// A request of the batch, as a lane sees it
+// A request of the batch: the first of its `fresh` new tokens, its tokens in all, of which the table may hold fewer (keys), tiles of its rows
 struct Request {
-    int token0, fresh, length, tiles;
-    __device__ __forceinline__ Request(const AttendArgs& A, int b, int rows_of_a_tile)
+    int token0, fresh, tokens, keys, tiles;
+    __host__ __device__ __forceinline__ Request(const AttendArgs& A, int b, int rows_of_a_tile)
     {
         token0 = b;
         fresh = 1;
@@ -201,10 +163,48 @@ struct Request {
             token0 = (int)min(max((long long)A.rows[b], 0ll), A.T);
             fresh = max((int)min((long long)A.rows[b + 1], A.T) - token0, 0);
         }
-        length = A.max_pages ? (int)min((long long)max(A.lengths[b], 0), (long long)A.max_pages << A.page_bits) : 0;
+        tokens = tokens_of(A, b);
+        keys = keys_of_request(A, b);
         tiles = (fresh * A.g + rows_of_a_tile - 1) / rows_of_a_tile;
     }
 };
+
+// The rows of a workgroup, from r0 on of `count`: of request b, of whose new tokens token0 is the first and comes behind `before` others, or of all requests (prefix)
+struct RowsOf {
+    int r0, count, token0, before, keys, b;
+    static __host__ __device__ __forceinline__ RowsOf of_prefix(const AttendArgs& A, int r0)
+    {
+        const int fresh = A.rows ? (int)min(max((long long)A.rows[A.B], 0ll), A.T) : (int)A.T;
+        return {r0, fresh * A.g, 0, 0, 0, 0};          // (T * Hq stays below 2^26)
+    }
+    static __host__ __device__ __forceinline__ RowsOf of_request(const AttendArgs& A, const Request& q, int b, int r0) { return {r0, q.fresh * A.g, q.token0, q.tokens - q.fresh, q.keys, b}; }
+    static __device__ __forceinline__ RowsOf of_tile(const AttendArgs& A, int i, int rows_of_a_tile)
+    {
+        int b, r0;
+        if (A.rows) {
+            b = request_of_tile(A, i, rows_of_a_tile);
+            r0 = (i - (int)tiles_before(A, b, rows_of_a_tile)) * rows_of_a_tile;
+        } else {
+            const int per = (A.g + rows_of_a_tile - 1) / rows_of_a_tile;
+            b = i / per;
+            r0 = (i - b * per) * rows_of_a_tile;
+        }
+        return of_request(A, Request(A, b, rows_of_a_tile), b, r0);
+    }
+    __host__ __device__ __forceinline__ bool none() const { return r0 < 0 || r0 >= count; }
+    // Own keys that row `at` of the tile sees, those that are there of its request's first ones up to itself, and that all rows do together.  (Which is its own goes by
+    // the tokens, also by those that the table has no room for: they are the request's last ones.)
+    __host__ __device__ __forceinline__ int sees(const AttendArgs& A, int at) const
+    {
+        const int r = r0 + at;
+        return r < count ? min(max(before + r / A.g + 1, 0), keys) : 0;
+    }
+    __host__ __device__ __forceinline__ int end(const AttendArgs& A, int rows_of_a_tile) const { return sees(A, min(rows_of_a_tile, count - r0) - 1); }
+};
+
+// Parts of a request's `length` own keys, if there are to be `dense` of them to a key; keys of one: they are equal
+__device__ __forceinline__ int parts_of(const AttendArgs& A, int length, float dense) { return length ? min((int)((float)length * dense) + 1, A.own_splits) : 0; }
+__device__ __forceinline__ int keys_of_part(int length, int parts) { return ((length + parts - 1) / parts + 127) / 128 * 128; }
 
 // Requests' own keys in parts.  The host does not know the lengths, so it starts own_groups workgroups, and each finds the part that is its own: of `tiles` tiles of
 // rows (with their heads) and K keys for all of them, (own_groups - tiles) / K parts to a key and one to a tile for what is left are no more than there are workgroups.
@@ -219,7 +219,7 @@ template <int N> __device__ __forceinline__ void deal(const AttendArgs& A, int i
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const Request q(A, min(b0 + k, A.B - 1), rows_of_a_tile);
-            keys += b0 + k < A.B ? (float)q.tiles * (float)q.length : 0.f;
+            keys += b0 + k < A.B ? (float)q.tiles * (float)q.keys : 0.f;
         }
 #pragma unroll
     for (int d = 1; d < kWave; d *= 2) keys += __shfl_xor(keys, d);
@@ -233,7 +233,7 @@ template <int N> __device__ __forceinline__ void deal(const AttendArgs& A, int i
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const Request q(A, min(b0 + lane * N + k, A.B - 1), rows_of_a_tile);
-            jobs[k] = b0 + lane * N + k < A.B ? q.tiles * parts_of(A, q.length, dense) * A.Hk : 0;
+            jobs[k] = b0 + lane * N + k < A.B ? q.tiles * parts_of(A, q.keys, dense) * A.Hk : 0;
             all += jobs[k];
         }
         int upto = all;
@@ -255,11 +255,11 @@ template <int N> __device__ __forceinline__ void deal(const AttendArgs& A, int i
             }
             if (j == 0 && threadIdx.x == 0) A.own_first[b] = id;
             const Request q(A, b, rows_of_a_tile);
-            *parts = parts_of(A, q.length, dense);
-            *per = keys_of_part(q.length, *parts);
+            *parts = parts_of(A, q.keys, dense);
+            *per = keys_of_part(q.keys, *parts);
             *head = j % A.Hk;
             *split = j / A.Hk % *parts;
-            *rows = {j / A.Hk / *parts * rows_of_a_tile, q.fresh * A.g, q.token0, q.length, q.fresh, b};
+            *rows = RowsOf::of_request(A, q, b, j / A.Hk / *parts * rows_of_a_tile);
             return;
         }
         before += __builtin_amdgcn_readfirstlane(__shfl(upto, kWave - 1));
@@ -314,7 +314,7 @@ template <typename T, int ROWS> struct Job : Place {
         }
         direct = is_direct(A, prefix, parts);
         // (scalars, also where lanes have found them together)
-        for (int* v : {&split, &head, &per, &rows.r0, &rows.count, &rows.token0, &rows.length, &rows.fresh, &rows.b}) *v = __builtin_amdgcn_readfirstlane(*v);
+        for (int* v : {&split, &head, &per, &rows.r0, &rows.count, &rows.token0, &rows.before, &rows.keys, &rows.b}) *v = __builtin_amdgcn_readfirstlane(*v);
     }
     __device__ __forceinline__ bool none() const { return rows.none(); }
     // of [T][Hq]; own keys that it sees
@@ -1007,7 +1007,7 @@ struct PartsOf {
             b = lo;
             token0 = min(max(A.rows[b], 0), token);
         }
-        const int length = (int)min((long long)max(A.lengths[b], 0), (long long)A.max_pages << A.page_bits), parts = parts_of(A, length, *A.dense);
+        const int parts = parts_of(A, keys_of_request(A, b), *A.dense);
         const int h = (int)(r - (long long)token * A.Hq), head = h / A.g, i = (token - token0) * A.g + h - head * A.g, tile = i / rows_of_a_tile;
         all = prefix + parts;
         // (no workgroup behind the last one, whatever `rows` are)

@@ -1,10 +1,12 @@
 // What the attention's workgroups do with the arguments that a call gives them, followed on the host: the entry point is the library's, in the place of
 // the launch stands a function that looks where every workgroup would store.  Reads calls from stdin, one a line:
 //   elem T B single Hq Hk D prefix max_pages page fresh...           (fresh: new tokens of each request, none if single)
-// and answers with a line each: "ok", what it found wrong, or the status if the call is refused.
+// and answers with a line each: "ok", what it found wrong, or the status if the call is refused.  Or a request's rows, which it answers with the keys that each sees:
+//   sees fresh tokens max_pages page g
 #include "cgbn.h"
 #include "cgbn_attention.h"
 
+#include <algorithm>
 #include <cstdio>
 #include <iostream>
 #include <sstream>
@@ -87,11 +89,32 @@ template <> cgbn_status launch_attend<bf16_t>(const AttendArgs& A, int prefix, i
 
 #include "cgbn_attention.hip"
 
+static void sees(std::istringstream& in)
+{
+    std::string word;
+    int fresh, tokens, max_pages, page, g;
+    in >> word >> fresh >> tokens >> max_pages >> page >> g;
+    AttendArgs A;
+    std::memset(&A, 0, sizeof(A));
+    const int rows[2] = {0, fresh};
+    A.rows = rows; A.lengths = &tokens; A.T = fresh; A.B = 1; A.Hk = 1; A.Hq = A.g = g; A.max_pages = max_pages; A.page_bits = __builtin_ctz(page);
+    for (int r0 = 0; r0 < fresh * g; r0 += 16) {
+        const RowsOf w = RowsOf::of_request(A, Request(A, 0, 16), 0, r0);
+        for (int at = 0; at < 16 && r0 + at < fresh * g; ++at) std::printf("%d ", w.sees(A, at));
+        if (w.sees(A, std::min(16, fresh * g - r0) - 1) != w.end(A, 16) || w.sees(A, 16 + fresh * g)) std::printf("wrong end of %d ", r0);
+    }
+    std::printf("\n");
+}
+
 int main()
 {
     std::string text;
     while (std::getline(std::cin, text)) {
         std::istringstream in(text);
+        if (text.compare(0, 4, "sees") == 0) {
+            sees(in);
+            continue;
+        }
         int elem, B, single, Hq, Hk, D, prefix, max_pages, page, n;
         long long T;
         in >> elem >> T >> B >> single >> Hq >> Hk >> D >> prefix >> max_pages >> page;

@@ -1,5 +1,5 @@
 """Where the attention's workgroups store, followed on the host (attention_jobs.hip): for thousands of calls every row of the parts lies in the workspace
-that the call asked for and is stored once, and what is stored in parts is joined."""
+that the call asked for and is stored once, and what is stored in parts is joined; and which of its request's keys a row sees."""
 
 import os
 import random
@@ -22,7 +22,7 @@ def jobs(tmp_path_factory):
                    capture_output=True)
 
     def ask(calls):
-        lines = [" ".join(str(int(n)) for n in c) for c in calls]
+        lines = [" ".join(n if isinstance(n, str) else str(int(n)) for n in c) for c in calls]
         done = subprocess.run([str(program)], input="\n".join(lines) + "\n", capture_output=True, text=True, check=True, timeout=300)
         return list(zip(lines, done.stdout.splitlines(), strict=True))
 
@@ -62,3 +62,14 @@ def test_calls_of_all_sizes(jobs):
     # (more than 1024 heads are refused)
     wrong = [(line, answer) for call, (line, answer) in zip(calls, jobs(calls)) if answer != ("status 2" if call[4] > 1024 else "ok")]
     assert not wrong, (len(wrong), wrong[:3])
+
+
+@pytest.mark.parametrize("g", [1, 3, 17])
+def test_keys_that_rows_see(jobs, g):
+    """The j-th of n new tokens its request's first tokens - n + j + 1, whether the table has room for all of them or not; of those the ones that it has room for."""
+    sizes = [(1, 64, 4, 16), (2, 65, 4, 16), (4, 18, 1, 16), (100, 100, 4, 16), (36, 100, 4, 16), (5, 2, 4, 16), (3, 0, 4, 16), (3, -7, 4, 16), (9, 700, 0, 16),
+             (2, (1 << 31) - 1, 65536, 1024), (40, 1000, 7, 1), (6, 6, 1, 1)]
+    for (n, tokens, most, page), (line, answer) in zip(sizes, jobs([("sees", *size, g) for size in sizes])):
+        tokens = max(tokens, 0) if most else 0
+        want = [min(max(tokens - n + j + 1, 0), most * page) for j in range(n) for _ in range(g)]
+        assert [int(x) for x in answer.split()] == want, line
