@@ -374,7 +374,8 @@ size_t cgbn_page_plan_workspace_bytes(int B, long long T);
  *                   from the taken[0]-th on, first request first; where the list or the row of the table is at its end there are none (-1 in the table)
  *   slots[T], positions[T]   each row's place in the cache (-1: it has none) and its position, `before` (the prefix's length) + its index
  *                   in its request; rows behind the last token: -1 and 0
- *   counts[2]       pages of the list that are taken now; new tokens that got no place or no row (at most 2^31 - 1).  counts may be exactly taken.
+ *   counts[2]       pages of the list that are taken now; new tokens that got no place (slot -1, also in a page that is not there, of the list or of
+ *                   the table, as behind the end of the list in later steps) or no row (at most 2^31 - 1).  counts may be exactly taken.
  * have[b] is cut to max_pages * page.  0 <= before <= 2^30, B <= 2^20, T <= 2^29, 1 <= max_pages <= 2^16. */
 cgbn_status cgbn_page_plan(const int* have, const int* fresh, int B, int before, const int* free_pages, int free_count, const int* taken,
                            int* counts, int* table, int max_pages, int pages, int page, long long T, int* rows, int* lengths, int* slots,

@@ -61,22 +61,15 @@ def plan(have, fresh, before, free_pages, taken, table, max_pages, pages, page, 
                 more = j
                 break
             positions[row] = before + key
-            if at >= max_pages:
-                left_out += 1
-                continue
-            there = True
-            if at >= held:
-                if key % page == 0:
-                    there = taken < len(free_pages)
-                    table[b, at] = -1
-                    if there:
-                        table[b, at] = free_pages[taken] if 0 <= free_pages[taken] < pages else -1
-                        taken += 1
-                    ran_out = not there
-                there = not ran_out
-            left_out += not there
-            if there and 0 <= table[b, at] < pages:
+            if at >= held and at < max_pages and key % page == 0:
+                table[b, at] = -1
+                if taken < len(free_pages):
+                    table[b, at] = free_pages[taken] if 0 <= free_pages[taken] < pages else -1
+                    taken += 1
+            if at < max_pages and 0 <= table[b, at] < pages:
                 slots[row] = int(table[b, at]) * page + key % page
+            else:
+                left_out += 1
         rows.append(rows[-1] + more)
         lengths.append(had + more)
     return rows, lengths, table, slots, positions, [taken, min(left_out, 2 ** 31 - 1)]

@@ -5,7 +5,7 @@
 // of the rows' starts, its key's page from the table or, if the request did not hold it before, from the free list; the row
 // whose key is a page's first writes the new entry (a page that is new has its first key in this step).  So nothing is read that another row writes.
 // Bound by latency: a launch, two dependent reads, two sums.  Up to 1024 requests are one launch, whose workgroups all form the sums (16 requests 4.2 us;
-// 1024 with 131072 rows, 1.1 MB, 6.2, in two launches 10.4); of more the rows are a second one's.
+// 1024 with 131072 rows, 1.1 MB, 6.5, in two launches 10.4); of more the rows are a second one's.
 //
 // page_store.  Bound by memory: one read and one write of the rows, 16 bytes a lane (20011 tokens, 20 heads of 80 float, 502 MB, 104 us, 4.8 TB/s; 64 tokens of 8
 // heads of 128 bfloat16 4.4 us, a launch).  Pages hold a head's keys side by side ([page][head][key][D]), so
@@ -25,6 +25,7 @@ struct PlanArgs {
     int* first;                    // [B]: place in the free list of a request's first new page
     long long T;
     int B, before, free_count, max_pages, pages, page_bits;
+    int count_later;               // the first launch counts only the tokens without a row, a second one those without a place
 };
 
 constexpr int kPlanThreads = 1024;
@@ -58,8 +59,10 @@ __device__ __forceinline__ int scan_before(int v, int most, int* lds, int* total
 __device__ __forceinline__ int held_by(const PlanArgs& A, int b) { return min(max(A.have[b], 0), A.max_pages << A.page_bits); }
 __device__ __forceinline__ int pages_of(const PlanArgs& A, int keys) { return min((keys + (1 << A.page_bits) - 1) >> A.page_bits, A.max_pages); }
 
-// One row.  start: the request's first row; first: its place in the free list; have: the tokens that it holds
-__device__ __forceinline__ void fill_row(const PlanArgs& A, int t, int b, int start, int first, int have)
+__device__ __forceinline__ bool there(const PlanArgs& A, int id) { return id >= 0 && id < A.pages; }
+
+// One row.  start: the request's first row; first: its place in the free list; have: the tokens that it holds.  -> whether the token has a place
+__device__ __forceinline__ bool fill_row(const PlanArgs& A, int t, int b, int start, int first, int have)
 {
     const int key = have + (t - start), at = key >> A.page_bits, held = pages_of(A, have);
     int id = -1;
@@ -71,11 +74,12 @@ __device__ __forceinline__ void fill_row(const PlanArgs& A, int t, int b, int st
             const int from = first + (at - held);
             if (from < A.free_count) id = A.free_pages[from];
         }
-        if (id < 0 || id >= A.pages) id = -1;
+        if (!there(A, id)) id = -1;
         if (at >= held && (key & ((1 << A.page_bits) - 1)) == 0) *entry = id;
     }
     A.slots[t] = id < 0 ? -1 : (id << A.page_bits) + (key & ((1 << A.page_bits) - 1));
     A.positions[t] = A.before + key;
+    return id >= 0;
 }
 
 // The last request that starts at row t or before it: the one whose row it is, if it is any's
@@ -92,66 +96,109 @@ __device__ __forceinline__ int request_of(const int* starts, int B, int t)
 
 // What a request takes of the step.  row: its first row; first: its place in the free list
 struct Share {
-    int next, length, want, left_out;          // the next request's first row; tokens and new pages; tokens without a place or a row
+    int next, length, want, cut;          // the next request's first row; tokens and new pages; tokens without a row
     __device__ __forceinline__ Share(const PlanArgs& A, int have, int fresh, int row)
     {
         next = min(add_most(row, min(fresh, kMost), kMost), (int)A.T);
         length = have + (next - row);
         want = max(pages_of(A, length) - pages_of(A, have), 0);
-        left_out = fresh;
+        cut = fresh - (next - row);
     }
-    __device__ __forceinline__ void place(const PlanArgs& A, int have, int first)
+    // Tokens with a row and without a place, but for those in pages that the list has given: the last held page is not there (`entry`, looked at if it takes new
+    // tokens), the list is at its end, the row of the table is
+    __device__ __forceinline__ int without_place(const PlanArgs& A, int have, int entry, int first) const
     {
-        const int given = min(want, max(A.free_count - first, 0));
-        left_out -= max(min((pages_of(A, have) + given) << A.page_bits, length) - have, 0);
+        const int held = pages_of(A, have), given = min(want, max(A.free_count - first, 0)), room = (held + given) << A.page_bits;
+        return max(length - max(room, have), 0) + (length > have && have < held << A.page_bits && !there(A, entry) ? min(length, held << A.page_bits) - have : 0);
     }
 };
 
+// Adds to counts[1], which stops at 2^31 - 1.  (Whole numbers: in any order the same; the sum is below 2^31 + 2^29 at any time, and who takes it over the border puts it back.)
+__device__ __forceinline__ void count_more(const PlanArgs& A, unsigned n)
+{
+    unsigned* const to = reinterpret_cast<unsigned*>(A.counts + 1);
+    if (n && atomicAdd(to, n) + n > 0x7fffffffu) atomicMin(to, 0x7fffffffu);
+}
+
 // Up to kPlanThreads requests: a thread to each, and every row.  Each workgroup forms the sums for itself and fills rows of its own; the first one
-// stores what is not a row's.
+// stores what is not a row's and, where there are others, has no rows: it counts the tokens without a place meanwhile, from what decides it (1024 requests
+// with 131072 rows 6.5 us, 6.2 without the count, 8.2 with a launch of its own for it).
 __global__ __launch_bounds__(kPlanThreads) void plan_few(const PlanArgs A)
 {
     __shared__ int lds[kPlanThreads / kWave], starts[kPlanThreads + 1], firsts[kPlanThreads], haves[kPlanThreads];
     __shared__ unsigned long long left_out;
-    const int T = (int)A.T, b = (int)threadIdx.x;
-    const bool in = b < A.B;
+    const int T = (int)A.T, b = (int)threadIdx.x, others = (int)gridDim.x - 1;
+    const bool in = b < A.B, main = blockIdx.x == 0, counts = main && others && !A.count_later;
     const int have = in ? held_by(A, b) : 0, fresh = in ? max(A.fresh[b], 0) : 0, taken = min(max(A.taken[0], 0), A.free_count);
+    const int entry = counts && in && fresh && have & ((1 << A.page_bits) - 1) ? A.table[(long long)b * A.max_pages + (have >> A.page_bits)] : 0;
     if (b == 0) left_out = 0;
     int total;
     const int row = min(scan_before(min(fresh, kMost), kMost, lds, &total), T);
-    Share share(A, have, fresh, row);
+    const Share share(A, have, fresh, row);
     const int first = add_most(taken, scan_before(share.want, kMost, lds, &total), kMost);
-    share.place(A, have, first);
     starts[b] = row;
     firsts[b] = first;
     haves[b] = have;
     if (b == A.B - 1 || (A.B == 0 && b == 0)) starts[A.B] = in ? share.next : 0;
-    if (blockIdx.x == 0) {
+    unsigned long long without = 0;
+    if (main) {
         if (in) {
             A.rows[b] = row;
             A.lengths[b] = share.length;
-            if (share.left_out) atomicAdd(&left_out, (unsigned long long)share.left_out);          // (whole numbers: in any order the same)
+            without = (unsigned long long)share.cut + (counts ? share.without_place(A, have, entry, first) : 0);
         }
         if (b == A.B - 1 || (A.B == 0 && b == 0)) A.rows[A.B] = in ? share.next : 0;
     }
     __syncthreads();
-    if (blockIdx.x == 0 && b == 0) {
-        A.counts[0] = min(add_most(taken, total, kMost), A.free_count);
-        A.counts[1] = (int)min(left_out, 0x7fffffffull);
-    }
-    const int end = starts[A.B];
-    for (int t = (int)(blockIdx.x * kPlanThreads + threadIdx.x); t < T; t += (int)gridDim.x * kPlanThreads) {
-        if (t >= end) {
-            A.slots[t] = -1;
-            A.positions[t] = 0;
-            continue;
+    const int end = starts[A.B], stop = min(add_most(taken, total, kMost), A.free_count);
+    if (counts) {
+        // pages that the list has given and that are not there
+        constexpr int AHEAD = 8;
+        for (int i0 = taken + b; i0 < stop; i0 += AHEAD * kPlanThreads) {
+            int id[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) id[k] = A.free_pages[min(i0 + k * kPlanThreads, stop - 1)];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int i = i0 + k * kPlanThreads;
+                if (there(A, id[k]) || i >= stop) continue;
+                const int of = request_of(firsts, A.B, i), page = pages_of(A, haves[of]) + (i - firsts[of]);
+                without += max(min(haves[of] + (starts[of + 1] - starts[of]), (page + 1) << A.page_bits) - (page << A.page_bits), 0);
+            }
         }
-        const int of = request_of(starts, A.B, t);
-        fill_row(A, t, of, starts[of], firsts[of], haves[of]);
+    }
+    if (!main || !others) {
+        const int workers = others ? others : 1;
+        for (int t = ((int)blockIdx.x - (others ? 1 : 0)) * kPlanThreads + b; t < T; t += workers * kPlanThreads) {
+            if (t >= end) {
+                A.slots[t] = -1;
+                A.positions[t] = 0;
+                continue;
+            }
+            const int of = request_of(starts, A.B, t);
+            without += !fill_row(A, t, of, starts[of], firsts[of], haves[of]);
+        }
+    }
+    if (!main) return;
+    if (without) atomicAdd(&left_out, without);          // (whole numbers: in any order the same)
+    __syncthreads();
+    if (b == 0) {
+        A.counts[0] = stop;
+        A.counts[1] = (int)min(left_out, 0x7fffffffull);
     }
 }
 
-// Any number of requests, a run of them to a thread: the sums, by one workgroup.
+// ... of so many rows that a launch of their own counts those without a place
+__global__ __launch_bounds__(kThreads) void count_rows(const PlanArgs A)
+{
+    const int T = A.rows[A.B];
+    unsigned n = 0;
+    for (int t = (int)(blockIdx.x * kThreads + threadIdx.x); t < T; t += (int)gridDim.x * kThreads) n += A.slots[t] < 0;
+    for (int d = 1; d < kWave; d *= 2) n += __shfl_xor(n, d);
+    if (threadIdx.x % kWave == 0) count_more(A, n);
+}
+
+// Any number of requests, a run of them to a thread: the sums, by one workgroup.  counts[1] is the tokens without a row; the rows' launch adds those without a place.
 __global__ __launch_bounds__(kPlanThreads) void plan_sums(const PlanArgs A)
 {
     __shared__ int lds[kPlanThreads / kWave];
@@ -173,10 +220,8 @@ __global__ __launch_bounds__(kPlanThreads) void plan_sums(const PlanArgs A)
     row = row0;
     unsigned long long out = 0;
     for (int b = b0; b < b1; ++b) {
-        const int have = held_by(A, b);
-        Share share(A, have, max(A.fresh[b], 0), row);
-        share.place(A, have, first);
-        out += share.left_out;
+        const Share share(A, held_by(A, b), max(A.fresh[b], 0), row);
+        out += share.cut;
         A.rows[b] = row;
         A.lengths[b] = share.length;
         A.first[b] = first;
@@ -195,14 +240,16 @@ __global__ __launch_bounds__(kPlanThreads) void plan_sums(const PlanArgs A)
 __global__ __launch_bounds__(kThreads) void plan_rows(const PlanArgs A)
 {
     const int t = (int)(blockIdx.x * kThreads + threadIdx.x);
-    if (t >= A.T) return;
-    if (t >= A.rows[A.B]) {
+    bool without = false;
+    if (t < A.rows[A.B]) {
+        const int b = request_of(A.rows, A.B, t);
+        without = !fill_row(A, t, b, A.rows[b], A.first[b], held_by(A, b));
+    } else if (t < A.T) {
         A.slots[t] = -1;
         A.positions[t] = 0;
-        return;
     }
-    const int b = request_of(A.rows, A.B, t);
-    fill_row(A, t, b, A.rows[b], A.first[b], held_by(A, b));
+    const unsigned n = __popcll(__ballot(without));
+    if (threadIdx.x % kWave == 0) count_more(A, n);
 }
 
 struct StoreArgs {
@@ -253,6 +300,9 @@ cgbn_status launched() { return hipGetLastError() == hipSuccess ? CGBN_OK : CGBN
 
 constexpr int kMaxRequests = 1 << 20, kMaxPage = 1024, kMaxTable = 1 << 16, kMaxRows = 1 << 29;
 constexpr int kAlone = 4096;       // rows that one workgroup fills
+// Pages of the list that one workgroup looks at beside the others' rows, where they are of fewer than 16 tokens: with more of them a launch that reads the slots is
+// the shorter way (64 requests, pages of one token, 32768 of them 6.8 and 8.5 us, 65536 9.1 and 8.2, 131072 14.4 and 8.7; of 16 tokens, 65536 10.2 and 13.9, 262144 27 and 34)
+constexpr int kListed = 3 << 14;
 
 bool page_fits(int page, int pages) { return page >= 1 && page <= kMaxPage && (page & (page - 1)) == 0 && pages >= 0 && (long long)pages * page < (1ll << 31); }
 // One launch: with several workgroups none may store the pages taken over what the others still read.
@@ -310,8 +360,11 @@ cgbn_status cgbn_page_plan(const int* have, const int* fresh, int B, int before,
     A.max_pages = max_pages; A.pages = pages; A.page_bits = bits_of(page);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (one) {
-        const long long groups = T <= kAlone ? 1 : (T + kPlanThreads - 1) / kPlanThreads;
+        const long long groups = T <= kAlone ? 1 : 1 + (T + kPlanThreads - 1) / kPlanThreads;
+        A.count_later = groups > 1 && page < 16 && T >> A.page_bits > kListed;
         hipLaunchKernelGGL(plan_few, dim3((unsigned)(groups < 256 ? groups : 256)), dim3(kPlanThreads), 0, st, A);
+        if (launched() != CGBN_OK) return CGBN_ERR_HIP;
+        if (A.count_later) hipLaunchKernelGGL(count_rows, dim3(512), dim3(kThreads), 0, st, A);
         return launched();
     }
     hipLaunchKernelGGL(plan_sums, dim3(1), dim3(kPlanThreads), 0, st, A);

@@ -1,12 +1,16 @@
-"""The serving operators where calls that the header allows are out of the ordinary: a prefix alone, tokens that a table has no room for."""
+"""The serving operators where calls that the header allows are out of the ordinary: a prefix alone, tokens that a table has no room for, tokens
+that get no place in the cache."""
 
+import numpy as np
 import pytest
 import torch
 
-from layers_harness import DEV
+from layers_harness import DEV, workspace
 from paper_1711_07240_amd import block as B
-from serving_harness import Attention
+from paper_1711_07240_amd import cgbn as L
+from serving_harness import Attention, ints
 from test_gpu_block import _off
+from test_gpu_pages import _plan, _requests
 
 pytestmark = pytest.mark.gpu
 TYPES = ["f32", "bf16"]
@@ -59,3 +63,82 @@ def test_a_request_outgrows_its_table(dtype, tol):
     second = pages.step(x[5:])
     assert pages.slots.tolist()[3:] == [-1, -1] and pages.taken.tolist() == [4, 2]
     assert _off(second[:3], want[5:8]) <= tol
+
+
+# ---- the plan, where tokens get no place ----
+
+
+def _holes(seed, B, page, most, prompts, longest, holes):
+    """Requests as a server has them, with `holes` of their pages and of the list's not there."""
+    rng = np.random.default_rng(seed)
+    have, fresh, table, free, pages = _requests(rng, B, page, most, prompts, longest)
+    table[rng.random(table.shape) < holes] = pages
+    free = np.where(rng.random(len(free)) < holes, rng.choice([-1, -(1 << 31), pages, (1 << 31) - 1], len(free)), free)
+    return have, fresh, table, free, pages, int(fresh.sum())
+
+
+# one workgroup; several, whose first one counts; the same with pages of one and two tokens, which are counted by a launch of their own; more requests than threads
+@pytest.mark.parametrize("holes", [0.0, 0.15, 1.0])
+@pytest.mark.parametrize("B,page,most,prompts,longest", [(7, 4, 9, 0.5, 30), (300, 8, 64, 0.3, 60), (300, 8, 64, 0.9, 90), (1, 16, 2000, 1.0, 19999), (1024, 16, 40, 0.5, 100),
+                                                         (1000, 1, 200, 0.9, 190), (3, 2, 50000, 1.0, 60000), (1025, 16, 8, 0.2, 30), (2500, 64, 5, 0.2, 100)])
+def test_tokens_without_a_place_are_counted(B, page, most, prompts, longest, holes):
+    have, fresh, table, free, pages, total = _holes(B, B, page, most, prompts, longest, holes)
+    for rows in (total + 5, max(total - total // 9, 0)):
+        for part in (len(free), len(free) // 2):
+            for in_place in (False, True):
+                want = _plan(have, fresh, 0, free[:part], min(3, part), table, pages, page, rows, in_place)
+                assert want[5][1] == total - sum(s >= 0 for s in want[3])
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("B,T,page", [(3, 40, 16), (5, 5000, 16), (4, 50000, 1), (1030, 1100, 16)])
+def test_counts_stop_at_the_largest_number(B, T, page, in_place):
+    """More tokens than 2^31 - 1 are asked for, one fewer, one more; none of them has a place."""
+    for total in ((1 << 31) - 2, (1 << 31) - 1, 1 << 31, (1 << 32) + 7):
+        first = min(total // 2, (1 << 31) - 1)
+        second = min(total - first, (1 << 31) - 1)
+        fresh = [first, second, total - first - second] + [0] * (B - 3)
+        dev, taken, table = ints(fresh), ints([0, 0]), ints([[-1]] * B)
+        counts = taken if in_place else ints([3, 3])
+        rows, lengths, slots, positions = (torch.zeros(n, dtype=torch.int32, device=DEV) for n in (B + 1, B, T, T))
+        nb = L.cgbn_page_plan_workspace_bytes(B, T)
+        L.cgbn_page_plan(ints([0] * B), dev, B, 0, ints([0]), 0, taken, counts, table, 1, 4, page, T, rows, lengths, slots, positions, workspace(nb), nb)
+        torch.cuda.synchronize()
+        assert counts.tolist() == [0, min(total, (1 << 31) - 1)] and bool((slots == -1).all())
+
+
+def test_steps_after_the_pages_have_ended():
+    """A server's steps in a graph: every token that gets no place is counted in its step."""
+    B, page, most, pages, T = 4, 4, 9, 6, 8
+    have, fresh, taken, table, free = ints([0] * B), ints([0] * B), ints([0, 0]), ints([[-1] * most] * B), ints(range(pages))
+    rows, lengths, slots, positions = (torch.zeros(n, dtype=torch.int32, device=DEV) for n in (B + 1, B, T, T))
+
+    def step():
+        L.cgbn_page_plan(have, fresh, B, 0, free, pages, taken, taken, table, most, pages, page, T, rows, lengths, slots, positions)
+        have.copy_(lengths)
+
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    lost = []
+    for more in ([2, 1, 2, 3], [2, 2, 2, 2], [2, 2, 1, 3], [1, 1, 1, 1], [1, 1, 1, 1], [2, 2, 2, 2], [5, 5, 0, 0]):
+        fresh.copy_(ints(more))
+        graph.replay()
+        torch.cuda.synchronize()
+        given = slots.tolist()
+        assert taken.tolist()[1] == sum(more) - sum(s >= 0 for s in given)
+        lost.append(taken.tolist()[1])
+    assert lost[0] == 0 and all(lost[-3:])
+
+
+def test_a_full_cache_goes_on_counting():
+    blk = B.Block(channels=64, heads=2, head_size=32, width=96, positions=128, dtype="f32")
+    pages = B.Pages(blk, requests=2, rows=4, pages=2, page=2, most=9)
+    x = torch.randn(4, 64, device=DEV)
+    pages.fresh.fill_(2)
+    pages.step(x)
+    for n in range(1, 5):
+        pages.fresh.copy_(torch.tensor([1, n % 2]))
+        pages.step(x)
+        assert pages.taken.tolist() == [2, 1 + n % 2]
