@@ -213,6 +213,11 @@ class Pages:
         cgbn.cgbn_page_plan(have, fresh, requests, self.prefix, self.free, self.pages, self.taken, self.taken, table, table.shape[1], self.pages, self.page,
                             slots.shape[0], rows, lengths, slots, positions, self.plan_room)
 
+    def _check(self, x, rows):
+        """The kernels go by the sizes that they are given: of other rows they would read or store what is not theirs."""
+        if x.shape != (rows, self.block.C) or x.dtype != self.block.dt or not x.is_contiguous():
+            raise ValueError(f"rows side by side, {rows} x {self.block.C} of {self.block.dt}, and not {tuple(x.shape)} of {x.dtype}")
+
     def _answer(self, x, table, requests, rows, lengths, slots, positions):
         b, m, inner = self.block, x.shape[0], self.block.H * self.block.D
         qkv = b._linear(b._frozen(x), b.p["qkv"], b.p["bias"])
@@ -232,6 +237,7 @@ class Pages:
     def share(self, x):
         """x [S, C]: the prefix of all requests, before the first step.  -> the block's output for it"""
         s = x.shape[0]
+        self._check(x, s)
         table = self._ints(1, -(-s // self.page))
         have, fresh, rows, lengths = self._ints(1), self._ints(1) + s, self._ints(2), self._ints(1)
         slots, positions = self._ints(s), self._ints(s)
@@ -245,6 +251,7 @@ class Pages:
 
     def step(self, x):
         """x [rows, C]: the new tokens, request by request, `fresh` says how many of each; rows behind them are padding.  -> output, row by row"""
+        self._check(x, self.T)
         self._plan(self.table, self.have, self.fresh, self.B, self.rows, self.lengths, self.slots, self.positions)
         out = self._answer(x, self.table, self.B, self.rows, self.lengths, self.slots, self.positions)
         self.have.copy_(self.lengths)

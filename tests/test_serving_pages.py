@@ -1,0 +1,41 @@
+"""The block's cache in pages without a GPU: the library's calls are written down instead of made."""
+
+import pytest
+import torch
+
+from paper_1711_07240_amd import block as B
+from paper_1711_07240_amd import cgbn as L
+
+LAUNCH = ["frozen_forward", "linear_forward", "gated_forward", "head_norm_forward", "rotate_forward", "page_plan", "page_store", "prefix_attention"]
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    made = []
+    for name in LAUNCH:
+        monkeypatch.setattr(L, "cgbn_" + name, lambda *args, _name=name: made.append((_name, args)))
+    return made
+
+
+def _pages(dtype="f32", rows=6, pages=30):
+    blk = B.Block(channels=64, heads=2, head_size=32, width=96, positions=128, dtype=dtype, device="cpu")
+    return blk, B.Pages(blk, requests=3, rows=rows, pages=pages, page=4, most=6)
+
+
+def _rows(n, blk, channels=64):
+    return torch.ones(n, channels, dtype=blk.dt)
+
+
+def test_rows_of_another_size_or_type_are_refused(calls):
+    """More rows than the plan has slots for would be stored by what lies behind them; values of half the size would be read past their end."""
+    blk, pages = _pages()
+    for x in (_rows(7, blk), _rows(5, blk), _rows(6, blk, 63), _rows(6, blk).bfloat16(), _rows(12, blk)[::2], _rows(6, blk).flatten()):
+        with pytest.raises(ValueError):
+            pages.step(x)
+    for x in (_rows(9, blk, 65), _rows(9, blk).bfloat16(), _rows(18, blk)[::2], _rows(9, blk).flatten()):
+        with pytest.raises(ValueError):
+            pages.share(x)
+    assert not calls
+    pages.share(_rows(9, blk))
+    pages.step(_rows(6, blk))
+    assert [name for name, _ in calls].count("prefix_attention") == 2
