@@ -204,7 +204,7 @@ class Pages:
         self.slots, self.positions = self._ints(rows), self._ints(rows)
         plan = cgbn.cgbn_page_plan_workspace_bytes(requests, rows)
         self.plan_room = torch.empty(plan, device=block.device, dtype=torch.uint8)
-        self.room = None
+        self.room, self.stepped = None, False
 
     def _ints(self, *shape):
         return torch.zeros(*shape, device=self.block.device, dtype=torch.int32)
@@ -235,9 +235,15 @@ class Pages:
         return b._linear(h, b.p["down"], residual=x1)
 
     def share(self, x):
-        """x [S, C]: the prefix of all requests, before the first step.  -> the block's output for it"""
+        """x [S, C]: the prefix of all requests, once and before the first step.  -> the block's output for it"""
         s = x.shape[0]
         self._check(x, s)
+        if s == 0:
+            return torch.empty_like(x)
+        if self.prefix or self.stepped:
+            raise ValueError("a prefix is shared once, before the first step")
+        if s > self.pages * self.page:
+            raise ValueError(f"{s} tokens, and room for {self.pages * self.page}")
         table = self._ints(1, -(-s // self.page))
         have, fresh, rows, lengths = self._ints(1), self._ints(1) + s, self._ints(2), self._ints(1)
         slots, positions = self._ints(s), self._ints(s)
@@ -252,6 +258,7 @@ class Pages:
     def step(self, x):
         """x [rows, C]: the new tokens, request by request, `fresh` says how many of each; rows behind them are padding.  -> output, row by row"""
         self._check(x, self.T)
+        self.stepped = True
         self._plan(self.table, self.have, self.fresh, self.B, self.rows, self.lengths, self.slots, self.positions)
         out = self._answer(x, self.table, self.B, self.rows, self.lengths, self.slots, self.positions)
         self.have.copy_(self.lengths)

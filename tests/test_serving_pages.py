@@ -39,3 +39,21 @@ def test_rows_of_another_size_or_type_are_refused(calls):
     pages.share(_rows(9, blk))
     pages.step(_rows(6, blk))
     assert [name for name, _ in calls].count("prefix_attention") == 2
+
+
+def test_the_prefix_is_shared_once_and_first(calls):
+    """A second one would take the first one's place, with positions behind it; after a step requests' tokens stand where it belongs."""
+    blk, pages = _pages()
+    with pytest.raises(ValueError):
+        pages.share(_rows(121, blk))                    # one token more than there are pages for
+    assert pages.share(_rows(0, blk)).shape == (0, 64) and not calls and pages.prefix == 0
+    pages.share(_rows(120, blk))
+    with pytest.raises(ValueError):
+        pages.share(_rows(4, blk))
+    assert pages.prefix == 120 and pages.prefix_table.numel() == 30
+    blk, pages = _pages()
+    pages.step(_rows(6, blk))
+    made = len(calls)
+    with pytest.raises(ValueError):
+        pages.share(_rows(4, blk))
+    assert len(calls) == made
