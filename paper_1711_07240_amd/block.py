@@ -75,10 +75,11 @@ class Block:
         cgbn.cgbn_frozen_backward(dy, dy.shape[0], self.C, 1, 1, "NHWC", self.dtype, self.norm["var"], self.norm["gamma"], EPS, dx)
         return dx
 
-    def _linear(self, x, w, bias=None, residual=None):
+    def _linear(self, x, w, bias=None, residual=None, room=None):
+        """room: in the place of _room(), if the workspace is another's"""
         m, n, k = x.shape[0], *w.shape
         y = self._empty(m, n)
-        ws = self._room(cgbn.cgbn_linear_workspace_bytes(m, n, k, self.dtype, False))
+        ws = (room or self._room)(cgbn.cgbn_linear_workspace_bytes(m, n, k, self.dtype, False))
         cgbn.cgbn_linear_forward(x, w, bias, residual, m, n, k, "none", y, None, self.dtype, ws)
         return y
 
@@ -100,11 +101,11 @@ class Block:
                                     self.cos.shape[0], self.p["wq"], self.p["wk"], EPS, out, out.shape[1], out[:, inner:], out.shape[1],
                                     self.dtype)
 
-    def _gated(self, y, save):
+    def _gated(self, y, save, room=None):
         m = y.shape[0]
         h = self._empty(m, self.F)
         gate, up = (torch.empty_like(h), torch.empty_like(h)) if save else (None, None)
-        ws = self._room(cgbn.cgbn_gated_workspace_bytes(m, self.F, self.C, self.dtype, False))
+        ws = (room or self._room)(cgbn.cgbn_gated_workspace_bytes(m, self.F, self.C, self.dtype, False))
         cgbn.cgbn_gated_forward(y, self.p["gate"], self.p["up"], m, self.F, self.C, "silu", h, gate, up, self.dtype, ws)
         return h, gate, up
 
@@ -204,7 +205,7 @@ class Pages:
         self.slots, self.positions = self._ints(rows), self._ints(rows)
         plan = cgbn.cgbn_page_plan_workspace_bytes(requests, rows)
         self.plan_room = torch.empty(plan, device=block.device, dtype=torch.uint8)
-        self.room, self.stepped = None, False
+        self.room, self.layers, self.stepped = None, None, False
 
     def _ints(self, *shape):
         return torch.zeros(*shape, device=self.block.device, dtype=torch.int32)
@@ -213,6 +214,12 @@ class Pages:
         cgbn.cgbn_page_plan(have, fresh, requests, self.prefix, self.free, self.pages, self.taken, self.taken, table, table.shape[1], self.pages, self.page,
                             slots.shape[0], rows, lengths, slots, positions, self.plan_room)
 
+    def _layers(self, nbytes):
+        """The layers' workspace.  Not the block's, which another call may replace by a larger one while a captured step still uses it, or use at the same time."""
+        if self.layers is None or self.layers.numel() < nbytes:
+            self.layers = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.block.device)
+        return self.layers
+
     def _check(self, x, rows):
         """The kernels go by the sizes that they are given: of other rows they would read or store what is not theirs."""
         if x.shape != (rows, self.block.C) or x.dtype != self.block.dt or not x.is_contiguous():
@@ -220,7 +227,7 @@ class Pages:
 
     def _answer(self, x, table, requests, rows, lengths, slots, positions):
         b, m, inner = self.block, x.shape[0], self.block.H * self.block.D
-        qkv = b._linear(b._frozen(x), b.p["qkv"], b.p["bias"])
+        qkv = b._linear(b._frozen(x), b.p["qkv"], b.p["bias"], room=self._layers)
         b._rotate(qkv, positions, qkv)
         row = 3 * inner
         cgbn.cgbn_page_store(qkv[:, inner:], row, qkv[:, 2 * inner:], row, m, b.H, b.D, slots, self.k, self.v, self.pages, self.page, b.dtype)
@@ -230,9 +237,9 @@ class Pages:
             self.room = torch.empty(need, device=b.device, dtype=torch.uint8)
         cgbn.cgbn_prefix_attention(qkv, row, m, requests, rows, lengths, b.H, b.H, b.D, b.D ** -0.5, self.k, self.v, self.pages, self.page, self.prefix_table,
                                    self.prefix, table, table.shape[1], a, inner, None, b.dtype, self.room)
-        x1 = b._linear(a, b.p["o"], residual=x)
-        h, _, _ = b._gated(b._frozen(x1), False)
-        return b._linear(h, b.p["down"], residual=x1)
+        x1 = b._linear(a, b.p["o"], residual=x, room=self._layers)
+        h, _, _ = b._gated(b._frozen(x1), False, self._layers)
+        return b._linear(h, b.p["down"], residual=x1, room=self._layers)
 
     def share(self, x):
         """x [S, C]: the prefix of all requests, once and before the first step.  -> the block's output for it"""

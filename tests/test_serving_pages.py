@@ -57,3 +57,30 @@ def test_the_prefix_is_shared_once_and_first(calls):
     with pytest.raises(ValueError):
         pages.share(_rows(4, blk))
     assert len(calls) == made
+
+
+def _workspaces(made):
+    at = {"linear_forward": 11, "gated_forward": 11}
+    return [(name, args[at[name]].data_ptr(), args[at[name]].numel()) for name, args in made if name in at]
+
+
+def test_a_step_keeps_its_workspaces(calls):
+    """A captured step goes on using them, so what the block does beside it must not take them or put others in their place."""
+    blk, pages = _pages("bf16", rows=300, pages=90)
+    pages.share(_rows(33, blk))
+    del calls[:]
+    pages.step(_rows(300, blk))
+    first = _workspaces(calls)
+    del calls[:]
+    blk._linear(_rows(40000, blk), blk.p["o"])
+    blk._linear(_rows(1, blk), blk.p["o"])
+    blk._gated(_rows(300, blk), False)
+    theirs = {at for _, at, _ in _workspaces(calls)}
+    del calls[:]
+    pages.step(_rows(300, blk))
+    assert _workspaces(calls) == first and len(first) == 4
+    assert not theirs & {at for _, at, _ in first}
+    other = B.Pages(blk, requests=3, rows=300, pages=90, page=4, most=6)
+    del calls[:]
+    other.step(_rows(300, blk))
+    assert not {at for _, at, _ in _workspaces(calls)} & {at for _, at, _ in first}
