@@ -353,8 +353,8 @@ cgbn_status cgbn_rotary_frequencies(int R, double base, cgbn_scaling scaling, do
 
 /* The first R values of every head of D are turned by the token's position (a, b) -> magnitude (a cos t - b sin t, b cos t + a sin t) with t = p freq[i],
  * p = positions[token] (any int; the token's own index if positions is NULL), freq[R/2] a DEVICE vector of doubles; the others are copied.  Rows, heads, strides and
- * `style` as in cgbn_head_norm_forward; Hk may be 0; yq may be exactly q (with its stride), yk exactly k.  Turns are counted in 64 bits: angles are as exact
- * at position 2^31 as at 0, up to the product's own rounding. */
+ * `style` as in cgbn_head_norm_forward; Hk may be 0; yq may be exactly q (with its stride), yk exactly k.  Turns are counted in 64 bits: an angle is off by
+ * less than 1.3 * 2^-52 of itself (2^-20 radians at position 2^31 of the fastest pair), its cosine and sine by 2^-23 beside that.  Up to 2^14 heads, T <= 2^30, T (Hq + Hk) <= 2^33. */
 cgbn_status cgbn_rotate_forward(const void* q, long long ldq, const void* k, long long ldk, long long T, int Hq, int Hk, int D, int R,
                                 cgbn_rotation style, const int* positions, const double* freq, float magnitude, void* yq, long long ldyq,
                                 void* yk, long long ldyk, cgbn_dtype dtype, void* stream);
@@ -376,14 +376,14 @@ size_t cgbn_page_plan_workspace_bytes(int B, long long T);
  *                   in its request; rows behind the last token: -1 and 0
  *   counts[2]       pages of the list that are taken now; new tokens that got no place (slot -1, also in a page that is not there, of the list or of
  *                   the table, as behind the end of the list in later steps) or no row (at most 2^31 - 1).  counts may be exactly taken.
- * have[b] is cut to max_pages * page.  0 <= before <= 2^30, B <= 2^20, T <= 2^29, 1 <= max_pages <= 2^16. */
+ * have[b] is cut to max_pages * page.  0 <= before <= 2^30, B <= 2^20, T <= 2^29, 1 <= max_pages <= 2^16, free_count < 2^30. */
 cgbn_status cgbn_page_plan(const int* have, const int* fresh, int B, int before, const int* free_pages, int free_count, const int* taken,
                            int* counts, int* table, int max_pages, int pages, int page, long long T, int* rows, int* lengths, int* slots,
                            int* positions, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Puts T tokens' keys and values (Hk heads of D values side by side, row to row ldk and ldv elements, rows on 16 bytes) to their places in
  * the pages; tokens whose slot is outside the pools are left out.  Two tokens of one call have different slots (of equal ones either may stay, in parts).
- * D a multiple of 8 up to 256. */
+ * D a multiple of 8 up to 256, Hk <= 1024, T <= 2^30. */
 cgbn_status cgbn_page_store(const void* k, long long ldk, const void* v, long long ldv, long long T, int Hk, int D, const int* slots,
                             void* k_pages, void* v_pages, int pages, int page, cgbn_dtype dtype, void* stream);
 
@@ -399,7 +399,9 @@ size_t cgbn_prefix_attention_workspace_bytes(long long T, int B, int Hq, int Hk,
  *   max_pages * page, as a plan's are: tokens that the table has no room for are not there, and count where a row's own token is.  max_pages = 0: no own tokens,
  *   table and lengths are not read.  Weights are rounded to bfloat16 for the products of bfloat16 tensors, their sum is not.
  * Weights times values are summed before they are divided: values above about 1e33 over the number of keys may overflow.
- *   D a multiple of 8 up to 256; rows of q and out on 16 bytes; T * Hq < 2^26 - 3, B * Hk <= 2^22. */
+ * A row whose scores are all -infinity (of infinite queries or keys) is zero, as one without keys.
+ *   D a multiple of 8 up to 256; Hq <= 1024; rows of q and out on 16 bytes; T * Hq < 2^26 - 3, B <= 2^20, B * Hk <= 2^22; max_pages <= 2^20, prefix and
+ *   max_pages * page < 2^30. */
 cgbn_status cgbn_prefix_attention(const void* q, long long ldq, long long T, int B, const int* rows, const int* lengths, int Hq, int Hk,
                                   int D, float scale, const void* k_pages, const void* v_pages, int pages, int page,
                                   const int* prefix_table, int prefix, const int* table, int max_pages, void* out, long long ldo,

@@ -192,7 +192,9 @@ class Block:
 class Pages:
     """Requests that a block answers, behind a prefix that they share: a cache in `pages` pages of `page` tokens, up to `rows` new tokens a step.
 
-    `step` can be captured into a graph and replayed: x, `fresh` (how many tokens each request gets) and the cache change in place."""
+    `step` can be captured into a graph and replayed: x, `fresh` (how many tokens each request gets) and the cache change in place.
+    `taken` has the pages that are taken and how many of the step's tokens got no place or row: those are answered without what they would have left in the
+    cache.  Requests do not end here and give no pages back: for others a program makes another cache."""
 
     def __init__(self, block, requests, rows, pages, page=16, most=64):
         self.block, self.B, self.T, self.pages, self.page, self.most, self.prefix = block, requests, rows, pages, page, most, 0

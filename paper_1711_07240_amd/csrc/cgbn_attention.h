@@ -14,13 +14,13 @@
 // transpose 4 x 16 blocks).  No score crosses lanes but for its row's maximum and sum.
 //
 // Keys and values go from memory to LDS directly, the next tile's while one is multiplied; scores are one tile ahead of values, so that the vector unit
-// forms a tile's weights while the matrix cores form the next one's scores.  Without that order 2919 us for what takes 555 (16 requests of up to 512 new tokens
+// forms a tile's weights while the matrix cores form the next one's scores.  Without that order 2919 us for what takes 552 (16 requests of up to 512 new tokens
 // behind 8191, 32 heads of 128 on 8, bfloat16).
 //
 // What bounds it: few rows the read of the keys (4 requests of up to 131072, 1.67 GB, 295 us, 5.7 TB/s, more than a copy's rate); many rows
-// the products and the weights' arithmetic together, 960 TF of the 1030 that the library's large product reaches on the same card: the matrix cores are busy 41 %
+// the products and the weights' arithmetic together, 960 TF, two thirds of the 1450 that the library's large product reaches on the same card: the matrix cores are busy 41 %
 // of the time, the vector unit about as long, at 1.9 to 2.1 GHz, and no single part of the loop taken out gains more than a fifth.  64 rows of
-// each key head behind 32768 keys with up to 2048 of their own are both, 97.5 us for 72 of reading.  Float with few rows reading too (stream(), below); with more the float
+// each key head behind 32768 keys with up to 2048 of their own are both, 99 us for 68 of reading.  Float with few rows reading too (stream(), below); with more the float
 // products, a fifth of the matrix cores' bfloat16 rate at best.  Small calls the launch and five trips to memory one after the other, 8 us.
 #pragma once
 
@@ -418,6 +418,7 @@ template <typename T, int DP, int KIND> __device__ __forceinline__ void attend(c
 
     // this thread's part of a tile's loads: key r0 + pass * PASS, chunk `chunk` of its line, which goes to place tid of the pass.  A load writes its
     // wavefront's lanes side by side, so the chunks of a line change places (xor a number of the key) instead of leaving gaps, for the reads below.
+    // Reads of keys meet no bank twice so; those that transpose values do, two lanes to a bank, half of the cycles that they take (bfloat16, 128 wide).
     const int load_row = tid / C::CH, line = A.D * C::EB;
     auto chunk = [&](int pass) { return ((tid % C::CH) ^ line_key<C::LINE>(pass * C::PASS + load_row)) * 16; };
     if (A.D < DP || DP * C::EB < C::LINE) {                       // places that no load reaches

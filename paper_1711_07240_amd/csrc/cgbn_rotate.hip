@@ -36,7 +36,8 @@ struct RotateArgs {
 
 constexpr int kMaxHalf = 512;      // angles of a token
 
-// cos and sin of a quarter turn times x, |x| <= 1/2, by their Taylor polynomials: off by less than 2^-24 with the rounding of what they are given
+// cos and sin of a quarter turn times x, |x| <= 1/2, by their Taylor polynomials: off by less than 1.75 units of 2^-24 (1.5 the sine), with the rounding of x to float:
+// the largest over 6e7 angles
 __device__ __forceinline__ void quarter(float x, float* c, float* s)
 {
     const float t = x * 1.5707963267948966f, u = t * t;
@@ -44,7 +45,7 @@ __device__ __forceinline__ void quarter(float x, float* c, float* s)
     *c = fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, -2.7557319e-7f, 2.4801587e-5f), -1.3888889e-3f), 4.1666667e-2f), -0.5f), 1.f);
 }
 
-// cos and sin of t radians: whole and quarter turns taken off in 64 bits, exactly
+// cos and sin of t radians: whole and quarter turns taken off in 64 bits, exactly, once they are counted (t, the constant and their product: off by less than 1.3 * 2^-52 of t)
 __device__ __forceinline__ void cos_sin(double t, float* c, float* s)
 {
     double turns = t * 0.15915494309189535;
