@@ -207,7 +207,7 @@ class Pages:
         self.slots, self.positions = self._ints(rows), self._ints(rows)
         plan = cgbn.cgbn_page_plan_workspace_bytes(requests, rows)
         self.plan_room = torch.empty(plan, device=block.device, dtype=torch.uint8)
-        self.room, self.layers, self.stepped = None, None, False
+        self.room, self.layers, self.kept, self.stepped = None, None, [], False
 
     def _ints(self, *shape):
         return torch.zeros(*shape, device=self.block.device, dtype=torch.int32)
@@ -218,9 +218,15 @@ class Pages:
 
     def _layers(self, nbytes):
         """The layers' workspace.  Not the block's, which another call may replace by a larger one while a captured step still uses it, or use at the same time."""
-        if self.layers is None or self.layers.numel() < nbytes:
-            self.layers = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.block.device)
+        self.layers = self._at_least(self.layers, nbytes)
         return self.layers
+
+    def _at_least(self, room, nbytes):
+        if room is not None and room.numel() >= nbytes:
+            return room
+        if room is not None:
+            self.kept.append(room)          # (a captured step of fewer rows may still use it)
+        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.block.device)
 
     def _check(self, x, rows):
         """The kernels go by the sizes that they are given: of other rows they would read or store what is not theirs."""
@@ -235,8 +241,7 @@ class Pages:
         cgbn.cgbn_page_store(qkv[:, inner:], row, qkv[:, 2 * inner:], row, m, b.H, b.D, slots, self.k, self.v, self.pages, self.page, b.dtype)
         a = torch.zeros(m, inner, device=b.device, dtype=b.dt)          # rows behind the last token stay zero
         need = cgbn.cgbn_prefix_attention_workspace_bytes(m, requests, b.H, b.H, b.D, self.prefix, table.shape[1] * self.page, b.dtype)
-        if self.room is None or self.room.numel() < need:
-            self.room = torch.empty(need, device=b.device, dtype=torch.uint8)
+        self.room = self._at_least(self.room, need)
         cgbn.cgbn_prefix_attention(qkv, row, m, requests, rows, lengths, b.H, b.H, b.D, b.D ** -0.5, self.k, self.v, self.pages, self.page, self.prefix_table,
                                    self.prefix, table, table.shape[1], a, inner, None, b.dtype, self.room)
         x1 = b._linear(a, b.p["o"], residual=x, room=self._layers)
@@ -265,11 +270,13 @@ class Pages:
         return out
 
     def step(self, x):
-        """x [rows, C]: the new tokens, request by request, `fresh` says how many of each; rows behind them are padding.  -> output, row by row"""
-        self._check(x, self.T)
+        """x [rows, C], or fewer rows: the new tokens, request by request, `fresh` says how many of each; rows behind them are padding.  -> output, row by row"""
+        m = x.shape[0]
+        self._check(x, min(max(m, 1), self.T))
         self.stepped = True
-        self._plan(self.table, self.have, self.fresh, self.B, self.rows, self.lengths, self.slots, self.positions)
-        out = self._answer(x, self.table, self.B, self.rows, self.lengths, self.slots, self.positions)
+        slots, positions = self.slots[:m], self.positions[:m]
+        self._plan(self.table, self.have, self.fresh, self.B, self.rows, self.lengths, slots, positions)
+        out = self._answer(x, self.table, self.B, self.rows, self.lengths, slots, positions)
         self.have.copy_(self.lengths)
         return out
 

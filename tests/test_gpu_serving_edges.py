@@ -142,3 +142,37 @@ def test_a_full_cache_goes_on_counting():
         pages.fresh.copy_(torch.tensor([1, n % 2]))
         pages.step(x)
         assert pages.taken.tolist() == [2, 1 + n % 2]
+
+
+def test_steps_of_fewer_rows():
+    """Of as many as there are tokens, and of fewer: what is cut off is counted; a captured one goes on beside eager ones of more rows."""
+    blk = B.Block(channels=64, heads=2, head_size=32, width=96, positions=512, dtype="bf16")
+    x = torch.randn(300, 64, device=DEV, generator=torch.Generator(device=DEV).manual_seed(5)).to(blk.dt)
+    eager, captured = (B.Pages(blk, requests=3, rows=300, pages=600, page=4, most=200) for _ in range(2))
+    one = x[:3].clone()
+    captured.fresh.zero_()
+    captured.step(one)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = captured.step(one)
+    for n, fresh in enumerate([[1, 1, 1], [100, 50, 150], [1, 1, 1], [1, 0, 1], [290, 1, 3], [1, 1, 1], [2, 2, 2]]):
+        for p in (eager, captured):
+            p.fresh.copy_(torch.tensor(fresh))
+        if sum(fresh) > 6:
+            want, got = eager.step(x), captured.step(x)
+            blk._linear(x.repeat(40, 1), blk.p["o"])          # (what a workspace was before would be taken by others)
+        else:
+            one.copy_(x[n:n + 3])
+            want, got = eager.step(one), out
+            graph.replay()
+        torch.cuda.synchronize()
+        rows = min(sum(fresh), len(want))
+        assert torch.equal(got[:rows], want[:rows]) and torch.equal(captured.table, eager.table) and torch.equal(captured.k, eager.k), n
+        assert eager.taken.tolist()[1] == captured.taken.tolist()[1] == sum(fresh) - rows
+    # the same rows with padding behind them and without, by other tiles
+    results = []
+    for rows in (x[:3], x):
+        pages = B.Pages(blk, requests=3, rows=300, pages=600, page=4, most=200)
+        pages.fresh.fill_(1)
+        results.append(pages.step(rows)[:3])
+    assert _off(results[0], results[1].cpu()) <= 3e-2

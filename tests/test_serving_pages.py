@@ -29,7 +29,7 @@ def _rows(n, blk, channels=64):
 def test_rows_of_another_size_or_type_are_refused(calls):
     """More rows than the plan has slots for would be stored by what lies behind them; values of half the size would be read past their end."""
     blk, pages = _pages()
-    for x in (_rows(7, blk), _rows(5, blk), _rows(6, blk, 63), _rows(6, blk).bfloat16(), _rows(12, blk)[::2], _rows(6, blk).flatten()):
+    for x in (_rows(7, blk), _rows(0, blk), _rows(6, blk, 63), _rows(6, blk).bfloat16(), _rows(12, blk)[::2], _rows(6, blk).flatten()):
         with pytest.raises(ValueError):
             pages.step(x)
     for x in (_rows(9, blk, 65), _rows(9, blk).bfloat16(), _rows(18, blk)[::2], _rows(9, blk).flatten()):
@@ -84,3 +84,15 @@ def test_a_step_keeps_its_workspaces(calls):
     del calls[:]
     other.step(_rows(300, blk))
     assert not {at for _, at, _ in _workspaces(calls)} & {at for _, at, _ in first}
+
+
+def test_a_step_of_fewer_rows(calls):
+    """The plan cuts tokens at the rows that there are; a captured step's workspaces stay when one of more rows needs larger ones."""
+    blk, pages = _pages("bf16", rows=300, pages=90)
+    pages.step(_rows(2, blk))
+    first, room = _workspaces(calls), pages.room.data_ptr()
+    plan, store, attend = (next(args for name, args in calls if name == n) for n in ("page_plan", "page_store", "prefix_attention"))
+    assert plan[12] == 2 and plan[15].numel() == plan[16].numel() == 2 and store[4] == 2 and store[7].numel() == 2 and attend[2] == 2
+    assert pages.step(_rows(300, blk)).shape == (300, 64)
+    kept = {t.data_ptr() for t in (pages.room, pages.layers, *pages.kept)}
+    assert {at for _, at, _ in first} | {room} <= kept
